@@ -365,6 +365,99 @@ int omc_compress_var_static(const float *values, uint64_t numel, omc_format_t fm
  */
 int omc_static_status(void *stream, uint32_t *host_status);
 
+/* ----------------------------------------------------------------------------------------------
+ * One layer's training step.  The paper trains with the parameters held by the store and leaves the
+ * precision of the layer arithmetic open (Sec. 2.1: full precision, or a format the hardware
+ * supports); the calls below are this library's own: products at four bits on the tensor cores, and
+ * the layer norm of the paper's Conformer blocks, each with its backward pass.  They take no plan.
+ *
+ * Element types of activations, gradients and results.  Sums are FP32 throughout, a result is
+ * rounded once (to nearest, ties to even).  A matrix is rows x cols with cols contiguous and `ld`
+ * (>= cols) elements from row to row; any ld and any element-aligned address are accepted, rows
+ * on 16-byte boundaries are read and written faster. */
+enum { OMC_TYPE_F32 = 0, OMC_TYPE_F16 = 1, OMC_TYPE_BF16 = 2 };
+
+/*
+ * The 4-bit microscaled format (OCP MXFP4): blocks of 32 consecutive values share one scale.
+ *   code   E2M1, 4 bits: sign, exponent, mantissa; magnitudes 0, 0.5, 1, 1.5, 2, 3, 4, 6.
+ *   scale  E8M0, 8 bits: 2^(byte - 127); 255 is NaN and makes the whole block NaN.
+ * Encoding: the scale is 2^(floor(log2(largest magnitude of the block)) - 2), at least 2^-127; each
+ * value divided by it is rounded to the nearest E2M1 value, ties to even, and saturates at +-6.  A
+ * block that holds an Inf or a NaN gets the NaN scale and codes 0.
+ * Layout of a quantised rows x cols matrix (sizes: omc_mx_sizes):
+ *   codes   row r at byte r * 16 * ceil(cols / 32), two codes a byte, the even column in the low four
+ *           bits; the codes between cols and the next multiple of 32 are 0.
+ *   scales  row r, block j (columns 32 j ...) at byte
+ *             ((r / 128) * ceil(cols / 256) + j / 8) * 1024 + (j % 8) / 4 * 512 + r % 32 * 16 + r % 128 / 32 * 4 + j % 4
+ *           (the order in which the tensor cores take them).  In rows < rows the bytes behind the last
+ *           block are 0; the bytes of rows >= rows may hold anything.
+ * omc_mx_sizes: host only; 1 <= rows, cols < 2^31.  Either output pointer may be NULL.
+ */
+int omc_mx_sizes(uint64_t rows, uint64_t cols, uint64_t *codes_bytes, uint64_t *scales_bytes);
+
+/*
+ * omc_mx_quantise -- x (rows x cols) to four bits along its rows (codes, scales), and/or along its
+ * columns (codes_t, scales_t: the quantised cols x rows transpose, blocks of 32 rows of x), reading x
+ * once.  A training step needs both: the product of the forward pass sums along one axis, the
+ * products of the backward pass along the other.  One of the two pairs may be NULL, NULL.
+ *   x  device, read only.    codes, scales, codes_t, scales_t  device, 16-byte aligned, written.
+ */
+int omc_mx_quantise(const void *x, int type, uint64_t rows, uint64_t cols, uint64_t ld, uint8_t *codes, uint8_t *scales,
+                    uint8_t *codes_t, uint8_t *scales_t, void *stream);
+
+/*
+ * omc_mx_dequantise -- the values of a quantised rows x cols matrix, rounded to `type` (FP32 and BF16
+ * hold every value of the format but BF16's and FP32's own underflow; FP16 saturates to Inf).
+ */
+int omc_mx_dequantise(const uint8_t *codes, const uint8_t *scales, uint64_t rows, uint64_t cols, void *out, int type,
+                      uint64_t ld, void *stream);
+
+/*
+ * omc_mx_matmul -- Y = X W^T of two quantised matrices, X M x K and W N x K, on the tensor cores at four
+ * bits with FP32 sums: forward Y = X W^T; backward dX = dY W (W quantised along N: the transposed pair
+ * of omc_mx_quantise) and dW = dY^T X (both quantised along the rows of the batch).
+ *   y       device, M x N of `type`, written; any ldy >= N, element-aligned.
+ *   status  device, one 32-bit word of the caller's, cleared by the caller: set non-zero by a kernel
+ *           that gave up waiting for one of its own copies (y is then incomplete; the context stays
+ *           usable).  Not expected to happen; the bounded wait exists so that a fault cannot hang the GPU.
+ * A NaN block of X or W makes the rows or columns of Y that it enters NaN.  M <= 128 * 65535.
+ */
+int omc_mx_matmul(const uint8_t *x_codes, const uint8_t *x_scales, uint64_t M, const uint8_t *w_codes, const uint8_t *w_scales,
+                  uint64_t N, uint64_t K, void *y, int type, uint64_t ldy, uint32_t *status, void *stream);
+
+/*
+ * omc_mx_linear -- the forward product from activations that are not quantised yet: exactly
+ * omc_mx_quantise of x along its rows followed by omc_mx_matmul with W.
+ *   workspace  device, 16-byte aligned, codes_bytes + scales_bytes of omc_mx_sizes(M, K); contents
+ *              undefined afterwards.
+ */
+int omc_mx_linear(const void *x, int type, uint64_t M, uint64_t K, uint64_t ldx, const uint8_t *w_codes, const uint8_t *w_scales,
+                  uint64_t N, void *y, int y_type, uint64_t ldy, uint8_t *workspace, uint32_t *status, void *stream);
+
+/*
+ * omc_layer_norm -- y = (x - mean) * rstd * gamma + beta per row, rstd = 1 / sqrt(variance + eps), the
+ * variance taken around the mean (two passes over the row, which stays on the chip).
+ *   gamma, beta  device, cols floats, 16-byte aligned (a norm variable of the store's arenas).
+ *   mean, rstd   device, rows floats each, written; either may be NULL.
+ *   rows = 0 is allowed and does nothing.  x and y may be the same matrix.
+ */
+int omc_layer_norm(const void *x, int type, uint64_t rows, uint64_t cols, uint64_t ld, const float *gamma, const float *beta,
+                   float eps, void *y, uint64_t ldy, float *mean, float *rstd, void *stream);
+
+/*
+ * omc_layer_norm_backward -- from dy and what the forward call read and left behind: with
+ * xhat = (x - mean) * rstd and g = dy * gamma,
+ *   dx = rstd * (g - mean(g) - xhat * mean(g * xhat)),   dgamma = sum over rows of dy * xhat,   dbeta = sum over rows of dy.
+ *   dgamma, dbeta  device, cols floats, 16-byte aligned, written (zeros for rows = 0); a place in a
+ *                  gradient arena will do.  The order of the additions is fixed: same input, same bits.
+ *   workspace      device, 16-byte aligned, omc_layer_norm_workspace(rows, cols) bytes, undefined afterwards.
+ *   dx may be the same matrix as dy or x.
+ */
+int omc_layer_norm_workspace(uint64_t rows, uint64_t cols, uint64_t *bytes);
+int omc_layer_norm_backward(const void *dy, uint64_t ld_dy, const void *x, uint64_t ld_x, int type, uint64_t rows, uint64_t cols,
+                            const float *gamma, const float *mean, const float *rstd, void *dx, uint64_t ld_dx, float *dgamma,
+                            float *dbeta, void *workspace, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -18,11 +18,13 @@ KIND_WEIGHT_MATRIX, KIND_BIAS, KIND_NORM, KIND_OTHER = 0, 1, 2, 3
 PLAN_PVT, PLAN_WEIGHTS_ONLY = 1, 2
 PLAN_DEFAULT = PLAN_PVT | PLAN_WEIGHTS_ONLY
 FORMAT_FIXED_POINT = 1
+F32, F16, BF16 = 0, 1, 2       # OMC_TYPE_*
 
 EXPORTS = ["omc_strerror", "omc_last_cuda_error", "omc_plan", "omc_plan_destroy", "omc_plan_seed", "omc_plan_sizes",
            "omc_plan_var", "omc_plan_division", "omc_plan_prepare", "omc_plan_status", "omc_plan_inject_wait_timeout", "omc_compress", "omc_decompress",
            "omc_update_recompress", "omc_update_recompress_host", "omc_transition", "omc_aggregate", "omc_aggregate_sum", "omc_aggregate_add", "omc_divide", "omc_matmul",
-           "omc_compress_var_static", "omc_static_status"]
+           "omc_compress_var_static", "omc_static_status", "omc_mx_sizes", "omc_mx_quantise", "omc_mx_dequantise", "omc_mx_matmul",
+           "omc_mx_linear", "omc_layer_norm", "omc_layer_norm_workspace", "omc_layer_norm_backward"]
 STATIC_MAX_NUMEL = 1 << 28
 
 
@@ -82,6 +84,15 @@ def lib():
         L.omc_divide.argtypes = [vp, vp, C.c_uint32, vp]
         L.omc_compress_var_static.argtypes = [vp, C.c_uint64, Format, C.c_uint32, vp, vp, vp]
         L.omc_static_status.argtypes = [vp, u32p]
+        u64, i32 = C.c_uint64, C.c_int
+        L.omc_mx_sizes.argtypes = [u64, u64, u64p, u64p]
+        L.omc_mx_quantise.argtypes = [vp, i32, u64, u64, u64, vp, vp, vp, vp, vp]
+        L.omc_mx_dequantise.argtypes = [vp, vp, u64, u64, vp, i32, u64, vp]
+        L.omc_mx_matmul.argtypes = [vp, vp, u64, vp, vp, u64, u64, vp, i32, u64, vp, vp]
+        L.omc_mx_linear.argtypes = [vp, i32, u64, u64, u64, vp, vp, u64, vp, i32, u64, vp, vp, vp]
+        L.omc_layer_norm.argtypes = [vp, i32, u64, u64, u64, vp, vp, C.c_float, vp, u64, vp, vp, vp]
+        L.omc_layer_norm_workspace.argtypes = [u64, u64, u64p]
+        L.omc_layer_norm_backward.argtypes = [vp, u64, vp, u64, i32, u64, u64, vp, vp, vp, vp, u64, vp, vp, vp, vp]
         _lib = L
     return _lib
 
@@ -248,3 +259,50 @@ def static_status(stream=0) -> int:
     st = C.c_uint32(0)
     _check(lib().omc_static_status(stream, C.byref(st)), "omc_static_status")
     return st.value
+
+
+# ---- one layer's training step (no plan; addresses are ints, types are F32 / F16 / BF16) --------
+
+def mx_sizes(rows: int, cols: int):
+    """omc_mx_sizes: (bytes of the codes, bytes of the scales) of a quantised rows x cols matrix."""
+    a, b = C.c_uint64(), C.c_uint64()
+    _check(lib().omc_mx_sizes(int(rows), int(cols), C.byref(a), C.byref(b)), "omc_mx_sizes")
+    return a.value, b.value
+
+
+def mx_quantise(x, type_, rows, cols, ld, codes=0, scales=0, codes_t=0, scales_t=0, stream=0):
+    """omc_mx_quantise: x to four bits along its rows and/or (the _t pair) along its columns."""
+    _check(lib().omc_mx_quantise(x, type_, rows, cols, ld, codes, scales, codes_t, scales_t, stream), "omc_mx_quantise")
+
+
+def mx_dequantise(codes, scales, rows, cols, out, type_, ld, stream=0):
+    """omc_mx_dequantise: the values of a quantised matrix."""
+    _check(lib().omc_mx_dequantise(codes, scales, rows, cols, out, type_, ld, stream), "omc_mx_dequantise")
+
+
+def mx_matmul(x_codes, x_scales, M, w_codes, w_scales, N, K, y, type_, ldy, status, stream=0):
+    """omc_mx_matmul: Y = X W^T of two quantised matrices."""
+    _check(lib().omc_mx_matmul(x_codes, x_scales, M, w_codes, w_scales, N, K, y, type_, ldy, status, stream), "omc_mx_matmul")
+
+
+def mx_linear(x, type_, M, K, ldx, w_codes, w_scales, N, y, y_type, ldy, workspace, status, stream=0):
+    """omc_mx_linear: Y = X W^T with X quantised on the way (workspace: sum(mx_sizes(M, K)) bytes)."""
+    _check(lib().omc_mx_linear(x, type_, M, K, ldx, w_codes, w_scales, N, y, y_type, ldy, workspace, status, stream), "omc_mx_linear")
+
+
+def layer_norm(x, type_, rows, cols, ld, gamma, beta, eps, y, ldy, mean=0, rstd=0, stream=0):
+    """omc_layer_norm: normalisation over the last dimension; mean and rstd may be 0 (not wanted)."""
+    _check(lib().omc_layer_norm(x, type_, rows, cols, ld, gamma, beta, eps, y, ldy, mean, rstd, stream), "omc_layer_norm")
+
+
+def layer_norm_workspace_bytes(rows: int, cols: int) -> int:
+    """omc_layer_norm_workspace: workspace of layer_norm_backward."""
+    n = C.c_uint64()
+    _check(lib().omc_layer_norm_workspace(int(rows), int(cols), C.byref(n)), "omc_layer_norm_workspace")
+    return n.value
+
+
+def layer_norm_backward(dy, ld_dy, x, ld_x, type_, rows, cols, gamma, mean, rstd, dx, ld_dx, dgamma, dbeta, workspace, stream=0):
+    """omc_layer_norm_backward: dx, and the gradients of gain and bias."""
+    _check(lib().omc_layer_norm_backward(dy, ld_dy, x, ld_x, type_, rows, cols, gamma, mean, rstd, dx, ld_dx, dgamma, dbeta, workspace,
+                                         stream), "omc_layer_norm_backward")

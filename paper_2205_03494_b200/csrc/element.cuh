@@ -1,0 +1,91 @@
+// Element types of the layer operators (omc_type): loads, stores and conversions.
+#pragma once
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+#include "../../include/omc.h"
+
+namespace omc {
+namespace el {
+
+__device__ __forceinline__ float to_float(float v) { return v; }
+__device__ __forceinline__ float to_float(__half v) { return __half2float(v); }
+__device__ __forceinline__ float to_float(__nv_bfloat16 v) { return __bfloat162float(v); }
+template <typename T> __device__ __forceinline__ T from_float(float v);
+template <> __device__ __forceinline__ float from_float<float>(float v) { return v; }
+template <> __device__ __forceinline__ __half from_float<__half>(float v) { return __float2half_rn(v); }
+template <> __device__ __forceinline__ __nv_bfloat16 from_float<__nv_bfloat16>(float v) { return __float2bfloat16_rn(v); }
+
+// A 32-bit word of T as FP32 values (one or two), and back.
+template <typename T> struct Word;
+template <> struct Word<float> {
+    static constexpr int N = 1;
+    static __device__ __forceinline__ void unpack(uint32_t w, float *v) { v[0] = __uint_as_float(w); }
+    static __device__ __forceinline__ uint32_t pack(const float *v) { return __float_as_uint(v[0]); }
+};
+template <> struct Word<__half> {
+    static constexpr int N = 2;
+    static __device__ __forceinline__ void unpack(uint32_t w, float *v)
+    {
+        const float2 f = __half22float2(*reinterpret_cast<const __half2 *>(&w));
+        v[0] = f.x;
+        v[1] = f.y;
+    }
+    static __device__ __forceinline__ uint32_t pack(const float *v)
+    {
+        const __half2 h = __floats2half2_rn(v[0], v[1]);
+        return *reinterpret_cast<const uint32_t *>(&h);
+    }
+};
+template <> struct Word<__nv_bfloat16> {
+    static constexpr int N = 2;
+    static __device__ __forceinline__ void unpack(uint32_t w, float *v)
+    {
+        v[0] = __uint_as_float(w << 16);
+        v[1] = __uint_as_float(w & 0xFFFF0000u);
+    }
+    static __device__ __forceinline__ uint32_t pack(const float *v)
+    {
+        const __nv_bfloat162 h = __floats2bfloat162_rn(v[0], v[1]);
+        return *reinterpret_cast<const uint32_t *>(&h);
+    }
+};
+
+// Every kernel of the layer operators lets its successor start early and waits for the kernel before it here,
+// in every CTA and before any global access: a CTA that left without waiting could let the successor's wait end
+// while that earlier kernel still runs.
+__device__ __forceinline__ void enter_stream_order()
+{
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+}
+
+inline size_t size_of(int type) { return type == OMC_TYPE_F32 ? 4 : 2; }
+inline bool type_ok(int type) { return type == OMC_TYPE_F32 || type == OMC_TYPE_F16 || type == OMC_TYPE_BF16; }
+inline bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+
+// Launch as the programmatic dependent of the kernel before it on the stream.
+template <typename... P, typename... A>
+cudaError_t launch(void (*kernel)(P...), dim3 grid, uint32_t threads, uint32_t smem, uint32_t cluster, void *stream, A... args)
+{
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = grid;
+    cfg.blockDim = dim3(threads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = static_cast<cudaStream_t>(stream);
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = cluster;
+    attr[1].val.clusterDim.y = 1;
+    attr[1].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = cluster > 1 ? 2 : 1;
+    return cudaLaunchKernelEx(&cfg, kernel, static_cast<P>(args)...);
+}
+
+}  // namespace el
+}  // namespace omc
