@@ -5,6 +5,8 @@
 //     dx = rstd (g - mean(g) - xhat mean(g xhat)),  g = dy gamma;   dgamma = sum_rows dy xhat,  dbeta = sum_rows dy
 #include <cuda_runtime.h>
 
+#include <type_traits>
+
 #include "element.cuh"
 #include "omc_internal.h"
 
@@ -103,38 +105,307 @@ norm_columns_kernel(const T *__restrict__ dy, uint64_t ld_dy, const T *__restric
     part[(uint64_t)blockIdx.y * 2 * cols + cols + c] = sb;
 }
 
+// ---- rows that fit in registers ------------------------------------------------------------------
+// A row is held by a group of `warps` warps, E values a thread; a CTA has several groups, each of which walks
+// over rows of its own and loads the next row while it works on this one.
+//   VECTOR: rows start on 16-byte boundaries and whole 16-byte pieces cover them; piece i of thread t is piece i G + t of the
+//   row (G threads in the group).  Otherwise value i of thread t is value i G + t.
+template <typename T, bool VECTOR, int E>
+struct Row {
+    static constexpr int PER = VECTOR ? 16 / (int)sizeof(T) : 1;      // values of one load
+    static constexpr int NV = E / PER;
+    using Piece = typename std::conditional<VECTOR, uint4, T>::type;
+    Piece raw[NV];
+
+    __device__ __forceinline__ void load(const T *row, uint32_t cols, uint32_t t, uint32_t G)
+    {
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const uint32_t c = (i * G + t) * PER;
+            if (c < cols) raw[i] = *reinterpret_cast<const Piece *>(row + c);
+        }
+    }
+    __device__ __forceinline__ void values(float *v) const
+    {
+        if constexpr (VECTOR) {
+            constexpr int N = el::Word<T>::N;
+#pragma unroll
+            for (int i = 0; i < NV; ++i) {
+                el::Word<T>::unpack(raw[i].x, v + i * PER);
+                el::Word<T>::unpack(raw[i].y, v + i * PER + N);
+                el::Word<T>::unpack(raw[i].z, v + i * PER + 2 * N);
+                el::Word<T>::unpack(raw[i].w, v + i * PER + 3 * N);
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < NV; ++i) v[i] = el::to_float(raw[i]);
+        }
+    }
+    static __device__ __forceinline__ void store(T *row, uint32_t cols, uint32_t t, uint32_t G, const float *v)
+    {
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const uint32_t c = (i * G + t) * PER;
+            if (c >= cols) continue;
+            if constexpr (VECTOR) {
+                constexpr int N = el::Word<T>::N;
+                const float *p = v + i * PER;
+                *reinterpret_cast<uint4 *>(row + c) = make_uint4(el::Word<T>::pack(p), el::Word<T>::pack(p + N), el::Word<T>::pack(p + 2 * N),
+                                                                 el::Word<T>::pack(p + 3 * N));
+            } else {
+                row[c] = el::from_float<T>(v[i]);
+            }
+        }
+    }
+    // Calls f(index of the value in v, column) for the values inside the row.
+    template <typename F>
+    static __device__ __forceinline__ void each(uint32_t cols, uint32_t t, uint32_t G, F f)
+    {
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const uint32_t c = (i * G + t) * PER;
+            if (c < cols) {
+#pragma unroll
+                for (int j = 0; j < PER; ++j) f(i * PER + j, c + j);
+            }
+        }
+    }
+};
+
+// Sums over a group, known to all its threads.  Consecutive calls use the two halves of `room` in turn, so that
+// one barrier per call is enough: who writes a half again has passed the barrier of the call between.
+struct Group {
+    uint32_t warps, index, thread;
+    float2 *room;       // [2][16] of this group
+    uint32_t turn;
+
+    __device__ __forceinline__ float2 sum(float2 v)
+    {
+#pragma unroll
+        for (int d = 16; d >= 1; d >>= 1) {
+            v.x += __shfl_xor_sync(0xFFFFFFFFu, v.x, d);
+            v.y += __shfl_xor_sync(0xFFFFFFFFu, v.y, d);
+        }
+        if (warps > 1) {
+            float2 *half = room + 16 * (turn & 1);
+            ++turn;
+            const uint32_t lane = threadIdx.x & 31;
+            if (lane == 0) half[thread >> 5] = v;
+            asm volatile("bar.sync %0, %1;" ::"r"(index + 1), "r"(warps * 32) : "memory");
+            v = lane < warps ? half[lane] : make_float2(0.f, 0.f);
+#pragma unroll
+            for (int d = 8; d >= 1; d >>= 1) {
+                v.x += __shfl_xor_sync(0xFFFFFFFFu, v.x, d);
+                v.y += __shfl_xor_sync(0xFFFFFFFFu, v.y, d);
+            }
+            v.x = __shfl_sync(0xFFFFFFFFu, v.x, 0);
+            v.y = __shfl_sync(0xFFFFFFFFu, v.y, 0);
+        }
+        return v;
+    }
+};
+
+constexpr int MAX_GROUPS = 15;      // named barriers 1 .. 15
+
+__device__ __forceinline__ Group make_group(uint32_t warps, float2 *room)
+{
+    Group g;
+    g.warps = warps;
+    g.index = threadIdx.x / (warps * 32);
+    g.thread = threadIdx.x - g.index * warps * 32;
+    g.room = room + g.index * 32;
+    g.turn = 0;
+    return g;
+}
+
+template <typename T, bool VECTOR, int E>
+__global__ void __launch_bounds__(512, VECTOR && E == 8 ? 2 : 1)
+norm_kernel(const T *x, uint32_t rows, uint32_t cols, uint64_t ld, const float *__restrict__ gamma, const float *__restrict__ beta, float eps,
+            T *y, uint64_t ldy, float *__restrict__ mean_out, float *__restrict__ rstd_out, uint32_t warps)
+{
+    using R = Row<T, VECTOR, E>;
+    __shared__ float2 room[MAX_GROUPS * 32];
+    Group g = make_group(warps, room);
+    const uint32_t G = warps * 32, groups = blockDim.x / G, t = g.thread;
+    const float inv = 1.f / (float)cols;
+    el::enter_stream_order();
+    float ga[E], be[E];
+    R::each(cols, t, G, [&](int i, uint32_t c) { ga[i] = gamma[c]; be[i] = beta[c]; });
+    const uint32_t step = gridDim.x * groups;
+    uint32_t row = blockIdx.x * groups + g.index;
+    R next;
+    if (row < rows) next.load(x + row * ld, cols, t, G);
+    for (; row < rows; row += step) {
+        float v[E];
+        next.values(v);
+        if (row + step < rows) next.load(x + (row + step) * ld, cols, t, G);
+        float s = 0.f;
+        R::each(cols, t, G, [&](int i, uint32_t) { s += v[i]; });
+        const float mean = g.sum(make_float2(s, 0.f)).x * inv;
+        s = 0.f;
+        R::each(cols, t, G, [&](int i, uint32_t) { v[i] -= mean; s = __fmaf_rn(v[i], v[i], s); });
+        const float rstd = 1.f / sqrtf(g.sum(make_float2(s, 0.f)).x * inv + eps);
+        R::each(cols, t, G, [&](int i, uint32_t) { v[i] = __fmaf_rn(v[i] * rstd, ga[i], be[i]); });
+        R::store(y + row * ldy, cols, t, G, v);
+        if (t == 0) {
+            if (mean_out) mean_out[row] = mean;
+            if (rstd_out) rstd_out[row] = rstd;
+        }
+    }
+}
+
+// dx, and this CTA's part of the column sums: each thread adds up its own columns over its group's rows in registers.
+template <typename T, bool VECTOR, int E>
+__global__ void __launch_bounds__(512, VECTOR && E == 8 ? 2 : 1)
+norm_backward_kernel(const T *dy, uint64_t ld_dy, const T *x, uint64_t ld_x, uint32_t rows, uint32_t cols, const float *__restrict__ gamma,
+                     const float *__restrict__ mean_in, const float *__restrict__ rstd_in, T *dx, uint64_t ld_dx, float *__restrict__ part,
+                     uint32_t warps)
+{
+    using R = Row<T, VECTOR, E>;
+    __shared__ float2 room[MAX_GROUPS * 32];
+    extern __shared__ float columns[];                     // 2 x cols: the groups' sums joined
+    Group g = make_group(warps, room);
+    const uint32_t G = warps * 32, groups = blockDim.x / G, t = g.thread;
+    const float inv = 1.f / (float)cols;
+    el::enter_stream_order();
+    float sg[E], sb[E];
+#pragma unroll
+    for (int i = 0; i < E; ++i) sg[i] = sb[i] = 0.f;
+    const uint32_t step = gridDim.x * groups;
+    uint32_t row = blockIdx.x * groups + g.index;
+    R next_x, next_d;
+    float mean = 0.f, rstd = 0.f;
+    if (row < rows) {
+        next_x.load(x + row * ld_x, cols, t, G);
+        next_d.load(dy + row * ld_dy, cols, t, G);
+        mean = mean_in[row];
+        rstd = rstd_in[row];
+    }
+    for (; row < rows; row += step) {
+        float h[E], d[E];
+        next_x.values(h);
+        next_d.values(d);
+        const float mu = mean, rs = rstd;
+        if (row + step < rows) {
+            next_x.load(x + (row + step) * ld_x, cols, t, G);
+            next_d.load(dy + (row + step) * ld_dy, cols, t, G);
+            mean = mean_in[row + step];
+            rstd = rstd_in[row + step];
+        }
+        float2 s = make_float2(0.f, 0.f);
+        R::each(cols, t, G, [&](int i, uint32_t c) {        // (gamma from L1: in registers it would cost a CTA per SM)
+            h[i] = (h[i] - mu) * rs;
+            sg[i] = __fmaf_rn(d[i], h[i], sg[i]);
+            sb[i] += d[i];
+            d[i] *= __ldg(gamma + c);
+            s.x += d[i];
+            s.y = __fmaf_rn(d[i], h[i], s.y);
+        });
+        s = g.sum(s);
+        const float m1 = s.x * inv, m2 = s.y * inv;
+        R::each(cols, t, G, [&](int i, uint32_t) { d[i] = (d[i] - m1 - h[i] * m2) * rs; });
+        R::store(dx + row * ld_dx, cols, t, G, d);
+    }
+    for (uint32_t k = 0; k < groups; ++k) {
+        if (g.index == k)
+            R::each(cols, t, G, [&](int i, uint32_t c) {
+                columns[c] = k ? columns[c] + sg[i] : sg[i];
+                columns[cols + c] = k ? columns[cols + c] + sb[i] : sb[i];
+            });
+        __syncthreads();
+    }
+    float *out = part + (uint64_t)blockIdx.x * 2 * cols;
+    for (uint32_t c = threadIdx.x; c < 2 * cols; c += blockDim.x) out[c] = columns[c];
+}
+
+// Sums of the parts: 32 columns per CTA, eight threads to a column.
 __global__ void __launch_bounds__(THREADS)
 norm_finish_kernel(const float *__restrict__ part, uint32_t parts, uint32_t cols, float *__restrict__ dgamma, float *__restrict__ dbeta)
 {
     el::enter_stream_order();
-    const uint32_t c = blockIdx.x * THREADS + threadIdx.x;
-    if (c >= 2 * cols) return;
+    __shared__ float room[THREADS];
+    const uint32_t c = blockIdx.x * 32 + (threadIdx.x & 31);
     float s = 0.f;
-    for (uint32_t p = 0; p < parts; ++p) s += part[(uint64_t)p * 2 * cols + c];
-    if (c < cols) dgamma[c] = s;
-    else dbeta[c - cols] = s;
+    if (c < 2 * cols)
+        for (uint32_t p = threadIdx.x >> 5; p < parts; p += THREADS / 32) s += part[(uint64_t)p * 2 * cols + c];
+    room[threadIdx.x] = s;
+    __syncthreads();
+    if (threadIdx.x < 32 && c < 2 * cols) {
+        for (int k = 1; k < THREADS / 32; ++k) s += room[threadIdx.x + 32 * k];
+        if (c < cols) dgamma[c] = s;
+        else dbeta[c - cols] = s;
+    }
 }
 
-// Partial column sums: one per SM of the device the kernels are laid out for.
-uint32_t parts_of(uint64_t rows) { return (uint32_t)(rows < DEFAULT_SMS ? rows : DEFAULT_SMS); }
+// Parts of the column sums: two CTAs on each of the 148 SMs that the kernels are laid out for.  (Not taken from the device:
+// the order of the additions follows from the shape alone.)
+constexpr uint32_t MAX_PARTS = 2 * DEFAULT_SMS;
+uint32_t parts_of(uint64_t rows) { return (uint32_t)(rows < MAX_PARTS ? rows : MAX_PARTS); }
 
 bool shape_ok(uint64_t rows, uint64_t cols) { return cols >= 1 && rows < (1ull << 31) && cols < (1ull << 30); }
+
+// Whether 16-byte loads cover every row.
+template <typename T>
+bool vector_rows(const void *p, uint64_t ld, uint64_t cols)
+{
+    return el::aligned16(p) && ld * sizeof(T) % 16 == 0 && cols * sizeof(T) % 16 == 0;
+}
+
+constexpr uint32_t REGISTER_COLS = 8192;      // 16 warps of 16 values a thread
+
+template <typename T, bool VECTOR, int E>
+int forward_rows(const void *x, uint32_t rows, uint32_t cols, uint64_t ld, const float *gamma, const float *beta, float eps, void *y,
+                 uint64_t ldy, float *mean, float *rstd, void *stream)
+{
+    const uint32_t warps = (cols + 32 * E - 1) / (32 * E), groups = warps >= 8 ? 1 : 8 / warps;
+    const uint32_t ctas = (rows + groups - 1) / groups, most = DEFAULT_SMS * 4;
+    return note_cuda(el::launch(norm_kernel<T, VECTOR, E>, dim3(ctas < most ? ctas : most), warps * groups * 32, 0, 1, stream,
+                                static_cast<const T *>(x), rows, cols, ld, gamma, beta, eps, static_cast<T *>(y), ldy, mean, rstd, warps));
+}
 
 template <typename T>
 int forward(const void *x, uint64_t rows, uint64_t cols, uint64_t ld, const float *gamma, const float *beta, float eps, void *y,
             uint64_t ldy, float *mean, float *rstd, void *stream)
 {
-    return note_cuda(el::launch(norm_wide_kernel<T>, dim3((uint32_t)rows), THREADS, 0, 1, stream, static_cast<const T *>(x), (uint32_t)cols,
-                                ld, gamma, beta, eps, static_cast<T *>(y), ldy, mean, rstd));
+    if (cols > REGISTER_COLS)
+        return note_cuda(el::launch(norm_wide_kernel<T>, dim3((uint32_t)rows), THREADS, 0, 1, stream, static_cast<const T *>(x),
+                                    (uint32_t)cols, ld, gamma, beta, eps, static_cast<T *>(y), ldy, mean, rstd));
+    const bool vec = vector_rows<T>(x, ld, cols) && vector_rows<T>(y, ldy, cols);
+    auto f = vec ? (cols <= 256 ? forward_rows<T, true, 8> : forward_rows<T, true, 16>)
+                 : (cols <= 256 ? forward_rows<T, false, 8> : forward_rows<T, false, 16>);
+    return f(x, (uint32_t)rows, (uint32_t)cols, ld, gamma, beta, eps, y, ldy, mean, rstd, stream);
+}
+
+template <typename T, bool VECTOR, int E>
+int backward_rows(const void *dy, uint64_t ld_dy, const void *x, uint64_t ld_x, uint32_t rows, uint32_t cols, const float *gamma,
+                  const float *mean, const float *rstd, void *dx, uint64_t ld_dx, float *part, uint32_t *parts, void *stream)
+{
+    const uint32_t warps = (cols + 32 * E - 1) / (32 * E);
+    const uint32_t groups = warps >= 16 ? 1 : (16 / warps < MAX_GROUPS ? 16 / warps : MAX_GROUPS);
+    const uint32_t ctas = (rows + groups - 1) / groups, smem = 8 * cols;
+    *parts = ctas < MAX_PARTS ? ctas : MAX_PARTS;
+    auto kernel = norm_backward_kernel<T, VECTOR, E>;
+    if (smem > 40 * 1024) {
+        const int rc = note_cuda(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 8 * (int)REGISTER_COLS));
+        if (rc) return rc;
+    }
+    return note_cuda(el::launch(kernel, dim3(*parts), warps * groups * 32, smem, 1, stream, static_cast<const T *>(dy), ld_dy,
+                                static_cast<const T *>(x), ld_x, rows, cols, gamma, mean, rstd, static_cast<T *>(dx), ld_dx, part, warps));
 }
 
 template <typename T>
 int backward(const void *dy, uint64_t ld_dy, const void *x, uint64_t ld_x, uint64_t rows, uint64_t cols, const float *gamma,
              const float *mean, const float *rstd, void *dx, uint64_t ld_dx, float *dgamma, float *dbeta, float *part, void *stream)
 {
-    const uint32_t c = (uint32_t)cols, parts = parts_of(rows);
+    const uint32_t c = (uint32_t)cols;
+    uint32_t parts = parts_of(rows);
     int rc = 0;
-    if (rows) {
+    if (rows && cols <= REGISTER_COLS) {
+        const bool vec = vector_rows<T>(dy, ld_dy, cols) && vector_rows<T>(x, ld_x, cols) && vector_rows<T>(dx, ld_dx, cols);
+        auto f = vec ? (cols <= REGISTER_COLS / 2 ? backward_rows<T, true, 8> : backward_rows<T, true, 16>)
+                     : (cols <= REGISTER_COLS / 2 ? backward_rows<T, false, 8> : backward_rows<T, false, 16>);
+        rc = f(dy, ld_dy, x, ld_x, (uint32_t)rows, c, gamma, mean, rstd, dx, ld_dx, part, &parts, stream);
+    } else if (rows) {
         // the column sums first: dx may overwrite dy or x
         rc = note_cuda(el::launch(norm_columns_kernel<T>, dim3((c + THREADS - 1) / THREADS, parts), THREADS, 0, 1, stream,
                                   static_cast<const T *>(dy), ld_dy, static_cast<const T *>(x), ld_x, (uint32_t)rows, c, mean, rstd, part));
@@ -143,8 +414,8 @@ int backward(const void *dy, uint64_t ld_dy, const void *x, uint64_t ld_x, uint6
                                       ld_dy, static_cast<const T *>(x), ld_x, c, gamma, mean, rstd, static_cast<T *>(dx), ld_dx));
     }
     if (!rc)
-        rc = note_cuda(el::launch(norm_finish_kernel, dim3((2 * c + THREADS - 1) / THREADS), THREADS, 0, 1, stream,
-                                  static_cast<const float *>(part), parts, c, dgamma, dbeta));
+        rc = note_cuda(el::launch(norm_finish_kernel, dim3((2 * c + 31) / 32), THREADS, 0, 1, stream, static_cast<const float *>(part), parts, c,
+                                  dgamma, dbeta));
     return rc;
 }
 
