@@ -106,71 +106,107 @@ norm_columns_kernel(const T *__restrict__ dy, uint64_t ld_dy, const T *__restric
 }
 
 // ---- rows that fit in registers ------------------------------------------------------------------
-// A row is held by a group of `warps` warps, E values a thread; a CTA has several groups, each of which walks
-// over rows of its own and loads the next row while it works on this one.
-//   VECTOR: rows start on 16-byte boundaries and whole 16-byte pieces cover them; piece i of thread t is piece i G + t of the
-//   row (G threads in the group).  Otherwise value i of thread t is value i G + t.
+// A row is held by a group of `warps` warps, E values a thread; a CTA has several groups, each of which walks over
+// rows of its own.  The rows ahead are on their way into a ring of row images in shared memory (cp.async), so
+// that what is in flight takes no registers.
+//   VECTOR: rows start on 16-byte boundaries and are whole 16-byte chunks; chunk i G + t belongs to thread t (of G), which
+//   copies and reads it itself: no barrier.  Otherwise the image starts at the boundary below the row (never
+//   below the matrix), value i G + t belongs to thread t, and the group meets between copying and reading.
 template <typename T, bool VECTOR, int E>
 struct Row {
-    static constexpr int PER = VECTOR ? 16 / (int)sizeof(T) : 1;      // values of one load
-    static constexpr int NV = E / PER;
-    using Piece = typename std::conditional<VECTOR, uint4, T>::type;
-    Piece raw[NV];
+    static constexpr uint32_t SIZE = sizeof(T), PER = 16 / SIZE;      // values of one chunk
+    static constexpr int CHUNKS = E / PER;                            // of a thread
 
-    __device__ __forceinline__ void load(const T *row, uint32_t cols, uint32_t t, uint32_t G)
+    static __host__ __device__ constexpr uint32_t image_bytes(uint32_t G) { return G * E * SIZE + (VECTOR ? 0 : 16); }
+
+    static __device__ __forceinline__ void copy16(uint32_t dst, const void *src, uint32_t bytes)      // the rest of the 16 becomes 0
     {
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
+    }
+    static __device__ __forceinline__ void fetch(uint8_t *image, const T *row, bool first_row, uint32_t cols, uint32_t t, uint32_t G)
+    {
+        const uint32_t dst = (uint32_t)__cvta_generic_to_shared(image);
+        if constexpr (VECTOR) {
 #pragma unroll
-        for (int i = 0; i < NV; ++i) {
-            const uint32_t c = (i * G + t) * PER;
-            if (c < cols) raw[i] = *reinterpret_cast<const Piece *>(row + c);
+            for (int i = 0; i < CHUNKS; ++i) {
+                const uint32_t k = i * G + t;
+                if (k * PER < cols) copy16(dst + k * 16, row + k * PER, 16);
+            }
+        } else {
+            const uint32_t skip = (uint32_t)(reinterpret_cast<uintptr_t>(row) & 15u), total = skip + cols * SIZE;
+            const uint8_t *src = reinterpret_cast<const uint8_t *>(row) - skip;
+#pragma unroll
+            for (int i = 0; i <= CHUNKS; ++i) {
+                const uint32_t k = i * G + t;
+                if (k * 16 >= total) break;
+                if (k == 0 && skip && first_row) {          // nothing before the matrix is read
+                    for (uint32_t j = skip; j < 16 && j < total; j += SIZE)
+                        *reinterpret_cast<T *>(image + j) = *reinterpret_cast<const T *>(src + j);
+                } else {
+                    copy16(dst + k * 16, src + k * 16, min(16u, total - k * 16));
+                }
+            }
         }
     }
-    __device__ __forceinline__ void values(float *v) const
+    static __device__ __forceinline__ void values(const uint8_t *image, const T *row, uint32_t cols, uint32_t t, uint32_t G, float *v)
     {
         if constexpr (VECTOR) {
             constexpr int N = el::Word<T>::N;
 #pragma unroll
-            for (int i = 0; i < NV; ++i) {
-                el::Word<T>::unpack(raw[i].x, v + i * PER);
-                el::Word<T>::unpack(raw[i].y, v + i * PER + N);
-                el::Word<T>::unpack(raw[i].z, v + i * PER + 2 * N);
-                el::Word<T>::unpack(raw[i].w, v + i * PER + 3 * N);
+            for (int i = 0; i < CHUNKS; ++i) {
+                const uint4 w = *reinterpret_cast<const uint4 *>(image + (i * G + t) * 16);
+                el::Word<T>::unpack(w.x, v + i * PER);
+                el::Word<T>::unpack(w.y, v + i * PER + N);
+                el::Word<T>::unpack(w.z, v + i * PER + 2 * N);
+                el::Word<T>::unpack(w.w, v + i * PER + 3 * N);
             }
         } else {
+            const T *p = reinterpret_cast<const T *>(image + (reinterpret_cast<uintptr_t>(row) & 15u));
 #pragma unroll
-            for (int i = 0; i < NV; ++i) v[i] = el::to_float(raw[i]);
+            for (int i = 0; i < E; ++i) v[i] = el::to_float(p[i * G + t]);       // (behind the row: never used)
         }
     }
     static __device__ __forceinline__ void store(T *row, uint32_t cols, uint32_t t, uint32_t G, const float *v)
     {
+        if constexpr (VECTOR) {
+            constexpr int N = el::Word<T>::N;
 #pragma unroll
-        for (int i = 0; i < NV; ++i) {
-            const uint32_t c = (i * G + t) * PER;
-            if (c >= cols) continue;
-            if constexpr (VECTOR) {
-                constexpr int N = el::Word<T>::N;
+            for (int i = 0; i < CHUNKS; ++i) {
+                const uint32_t k = i * G + t;
                 const float *p = v + i * PER;
-                *reinterpret_cast<uint4 *>(row + c) = make_uint4(el::Word<T>::pack(p), el::Word<T>::pack(p + N), el::Word<T>::pack(p + 2 * N),
-                                                                 el::Word<T>::pack(p + 3 * N));
-            } else {
-                row[c] = el::from_float<T>(v[i]);
+                if (k * PER < cols)
+                    *reinterpret_cast<uint4 *>(row + k * PER) = make_uint4(el::Word<T>::pack(p), el::Word<T>::pack(p + N),
+                                                                           el::Word<T>::pack(p + 2 * N), el::Word<T>::pack(p + 3 * N));
             }
+        } else {
+#pragma unroll
+            for (int i = 0; i < E; ++i)
+                if (i * G + t < cols) row[i * G + t] = el::from_float<T>(v[i]);
         }
     }
     // Calls f(index of the value in v, column) for the values inside the row.
     template <typename F>
     static __device__ __forceinline__ void each(uint32_t cols, uint32_t t, uint32_t G, F f)
     {
+        if constexpr (VECTOR) {
 #pragma unroll
-        for (int i = 0; i < NV; ++i) {
-            const uint32_t c = (i * G + t) * PER;
-            if (c < cols) {
+            for (int i = 0; i < CHUNKS; ++i) {
+                const uint32_t c = (i * G + t) * PER;
+                if (c < cols) {
 #pragma unroll
-                for (int j = 0; j < PER; ++j) f(i * PER + j, c + j);
+                    for (uint32_t j = 0; j < PER; ++j) f(i * PER + j, c + j);
+                }
             }
+        } else {
+#pragma unroll
+            for (int i = 0; i < E; ++i)
+                if (i * G + t < cols) f(i, i * G + t);
         }
     }
 };
+__device__ __forceinline__ void commit_copies() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int LEFT>
+__device__ __forceinline__ void wait_copies() { asm volatile("cp.async.wait_group %0;" ::"n"(LEFT) : "memory"); }
 
 // Sums over a group, known to all its threads.  Consecutive calls use the two halves of `room` in turn, so that
 // one barrier per call is enough: who writes a half again has passed the barrier of the call between.
@@ -179,6 +215,11 @@ struct Group {
     float2 *room;       // [2][16] of this group
     uint32_t turn;
 
+    __device__ __forceinline__ void meet()
+    {
+        if (warps > 1) asm volatile("bar.sync %0, %1;" ::"r"(index + 1), "r"(warps * 32) : "memory");
+        else __syncwarp();
+    }
     __device__ __forceinline__ float2 sum(float2 v)
     {
 #pragma unroll
@@ -191,7 +232,7 @@ struct Group {
             ++turn;
             const uint32_t lane = threadIdx.x & 31;
             if (lane == 0) half[thread >> 5] = v;
-            asm volatile("bar.sync %0, %1;" ::"r"(index + 1), "r"(warps * 32) : "memory");
+            meet();
             v = lane < warps ? half[lane] : make_float2(0.f, 0.f);
 #pragma unroll
             for (int d = 8; d >= 1; d >>= 1) {
@@ -218,27 +259,42 @@ __device__ __forceinline__ Group make_group(uint32_t warps, float2 *room)
     return g;
 }
 
+// Row images of a group: three (two ahead of the one in work), or two where a row is long.
+template <int E> constexpr int stages_of = E == 8 ? 3 : 2;
+constexpr int FORWARD_STAGES = 3;
+
 template <typename T, bool VECTOR, int E>
-__global__ void __launch_bounds__(512, VECTOR && E == 8 ? 2 : 1)
+__global__ void __launch_bounds__(512, E == 8 ? 2 : 1)
 norm_kernel(const T *x, uint32_t rows, uint32_t cols, uint64_t ld, const float *__restrict__ gamma, const float *__restrict__ beta, float eps,
             T *y, uint64_t ldy, float *__restrict__ mean_out, float *__restrict__ rstd_out, uint32_t warps)
 {
     using R = Row<T, VECTOR, E>;
+    constexpr int S = FORWARD_STAGES;
     __shared__ float2 room[MAX_GROUPS * 32];
+    extern __shared__ __align__(16) uint8_t images[];
     Group g = make_group(warps, room);
-    const uint32_t G = warps * 32, groups = blockDim.x / G, t = g.thread;
+    const uint32_t G = warps * 32, groups = blockDim.x / G, t = g.thread, bytes = R::image_bytes(G);
+    uint8_t *ring = images + g.index * S * bytes;
     const float inv = 1.f / (float)cols;
     el::enter_stream_order();
+    const uint32_t step = gridDim.x * groups, first = blockIdx.x * groups + g.index;
+    auto fetch = [&](uint64_t row, uint32_t s) {
+        if (row < rows) R::fetch(ring + s * bytes, x + row * ld, row == 0, cols, t, G);
+        commit_copies();
+    };
+#pragma unroll
+    for (int s = 0; s < S - 1; ++s) fetch(first + (uint64_t)s * step, s);
     float ga[E], be[E];
     R::each(cols, t, G, [&](int i, uint32_t c) { ga[i] = gamma[c]; be[i] = beta[c]; });
-    const uint32_t step = gridDim.x * groups;
-    uint32_t row = blockIdx.x * groups + g.index;
-    R next;
-    if (row < rows) next.load(x + row * ld, cols, t, G);
-    for (; row < rows; row += step) {
+    uint32_t now = 0, ahead = S - 1;
+    for (uint64_t row = first; row < rows; row += step) {
+        fetch(row + (uint64_t)(S - 1) * step, ahead);      // where the row before was: its group has met since
+        wait_copies<S - 1>();
+        if (!VECTOR) g.meet();
         float v[E];
-        next.values(v);
-        if (row + step < rows) next.load(x + (row + step) * ld, cols, t, G);
+        R::values(ring + now * bytes, x + row * ld, cols, t, G, v);
+        now = now + 1 == S ? 0 : now + 1;
+        ahead = ahead + 1 == S ? 0 : ahead + 1;
         float s = 0.f;
         R::each(cols, t, G, [&](int i, uint32_t) { s += v[i]; });
         const float mean = g.sum(make_float2(s, 0.f)).x * inv;
@@ -256,42 +312,53 @@ norm_kernel(const T *x, uint32_t rows, uint32_t cols, uint64_t ld, const float *
 
 // dx, and this CTA's part of the column sums: each thread adds up its own columns over its group's rows in registers.
 template <typename T, bool VECTOR, int E>
-__global__ void __launch_bounds__(512, VECTOR && E == 8 ? 2 : 1)
+__global__ void __launch_bounds__(512, E == 8 ? 2 : 1)
 norm_backward_kernel(const T *dy, uint64_t ld_dy, const T *x, uint64_t ld_x, uint32_t rows, uint32_t cols, const float *__restrict__ gamma,
                      const float *__restrict__ mean_in, const float *__restrict__ rstd_in, T *dx, uint64_t ld_dx, float *__restrict__ part,
                      uint32_t warps)
 {
     using R = Row<T, VECTOR, E>;
+    constexpr int S = stages_of<E>;
     __shared__ float2 room[MAX_GROUPS * 32];
-    extern __shared__ float columns[];                     // 2 x cols: the groups' sums joined
+    extern __shared__ __align__(16) uint8_t images[];
     Group g = make_group(warps, room);
-    const uint32_t G = warps * 32, groups = blockDim.x / G, t = g.thread;
+    const uint32_t G = warps * 32, groups = blockDim.x / G, t = g.thread, bytes = R::image_bytes(G);
+    uint8_t *ring = images + g.index * S * 2 * bytes;      // x and dy
     const float inv = 1.f / (float)cols;
     el::enter_stream_order();
+    const uint32_t step = gridDim.x * groups, first = blockIdx.x * groups + g.index;
+    auto fetch = [&](uint64_t row, uint32_t s) {
+        if (row < rows) {
+            R::fetch(ring + s * 2 * bytes, x + row * ld_x, row == 0, cols, t, G);
+            R::fetch(ring + s * 2 * bytes + bytes, dy + row * ld_dy, row == 0, cols, t, G);
+        }
+        commit_copies();
+    };
+#pragma unroll
+    for (int s = 0; s < S - 1; ++s) fetch(first + (uint64_t)s * step, s);
     float sg[E], sb[E];
 #pragma unroll
     for (int i = 0; i < E; ++i) sg[i] = sb[i] = 0.f;
-    const uint32_t step = gridDim.x * groups;
-    uint32_t row = blockIdx.x * groups + g.index;
-    R next_x, next_d;
     float mean = 0.f, rstd = 0.f;
-    if (row < rows) {
-        next_x.load(x + row * ld_x, cols, t, G);
-        next_d.load(dy + row * ld_dy, cols, t, G);
-        mean = mean_in[row];
-        rstd = rstd_in[row];
+    if (first < rows) {
+        mean = mean_in[first];
+        rstd = rstd_in[first];
     }
-    for (; row < rows; row += step) {
-        float h[E], d[E];
-        next_x.values(h);
-        next_d.values(d);
+    uint32_t now = 0, ahead = S - 1;
+    for (uint64_t row = first; row < rows; row += step) {
+        fetch(row + (uint64_t)(S - 1) * step, ahead);      // where the row before was: its group has met since
         const float mu = mean, rs = rstd;
         if (row + step < rows) {
-            next_x.load(x + (row + step) * ld_x, cols, t, G);
-            next_d.load(dy + (row + step) * ld_dy, cols, t, G);
             mean = mean_in[row + step];
             rstd = rstd_in[row + step];
         }
+        wait_copies<S - 1>();
+        if (!VECTOR) g.meet();
+        float h[E], d[E];
+        R::values(ring + now * 2 * bytes, x + row * ld_x, cols, t, G, h);
+        R::values(ring + now * 2 * bytes + bytes, dy + row * ld_dy, cols, t, G, d);
+        now = now + 1 == S ? 0 : now + 1;
+        ahead = ahead + 1 == S ? 0 : ahead + 1;
         float2 s = make_float2(0.f, 0.f);
         R::each(cols, t, G, [&](int i, uint32_t c) {        // (gamma from L1: in registers it would cost a CTA per SM)
             h[i] = (h[i] - mu) * rs;
@@ -306,6 +373,8 @@ norm_backward_kernel(const T *dy, uint64_t ld_dy, const T *x, uint64_t ld_x, uin
         R::each(cols, t, G, [&](int i, uint32_t) { d[i] = (d[i] - m1 - h[i] * m2) * rs; });
         R::store(dx + row * ld_dx, cols, t, G, d);
     }
+    __syncthreads();
+    float *columns = reinterpret_cast<float *>(images);    // 2 x cols: the groups' sums joined, in their order
     for (uint32_t k = 0; k < groups; ++k) {
         if (g.index == k)
             R::each(cols, t, G, [&](int i, uint32_t c) {
@@ -353,13 +422,26 @@ bool vector_rows(const void *p, uint64_t ld, uint64_t cols)
 
 constexpr uint32_t REGISTER_COLS = 8192;      // 16 warps of 16 values a thread
 
+// More dynamic shared memory than a kernel has by default.
+template <typename K>
+int allow_smem(K kernel, uint32_t smem)
+{
+    return smem <= 40 * 1024 ? 0 : note_cuda(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+}
+
 template <typename T, bool VECTOR, int E>
 int forward_rows(const void *x, uint32_t rows, uint32_t cols, uint64_t ld, const float *gamma, const float *beta, float eps, void *y,
                  uint64_t ldy, float *mean, float *rstd, void *stream)
 {
     const uint32_t warps = (cols + 32 * E - 1) / (32 * E), groups = warps >= 8 ? 1 : 8 / warps;
-    const uint32_t ctas = (rows + groups - 1) / groups, most = DEFAULT_SMS * 4;
-    return note_cuda(el::launch(norm_kernel<T, VECTOR, E>, dim3(ctas < most ? ctas : most), warps * groups * 32, 0, 1, stream,
+    const uint32_t ctas = (rows + groups - 1) / groups, threads = warps * groups * 32;
+    const uint32_t smem = groups * FORWARD_STAGES * Row<T, VECTOR, E>::image_bytes(warps * 32);
+    // as many CTAs as are resident: by registers (64, 84 or 128 a thread) and by shared memory
+    const uint32_t by_regs = 65536 / (threads * (E == 8 ? 64 : VECTOR ? 84 : 128)), by_smem = 220 * 1024 / (smem + 5 * 1024);
+    const uint32_t most = DEFAULT_SMS * (by_regs < by_smem ? by_regs : by_smem);
+    auto kernel = norm_kernel<T, VECTOR, E>;
+    if (const int rc = allow_smem(kernel, smem)) return rc;
+    return note_cuda(el::launch(kernel, dim3(ctas < most ? ctas : most), threads, smem, 1, stream,
                                 static_cast<const T *>(x), rows, cols, ld, gamma, beta, eps, static_cast<T *>(y), ldy, mean, rstd, warps));
 }
 
@@ -382,13 +464,13 @@ int backward_rows(const void *dy, uint64_t ld_dy, const void *x, uint64_t ld_x, 
 {
     const uint32_t warps = (cols + 32 * E - 1) / (32 * E);
     const uint32_t groups = warps >= 16 ? 1 : (16 / warps < MAX_GROUPS ? 16 / warps : MAX_GROUPS);
-    const uint32_t ctas = (rows + groups - 1) / groups, smem = 8 * cols;
-    *parts = ctas < MAX_PARTS ? ctas : MAX_PARTS;
+    const uint32_t ctas = (rows + groups - 1) / groups;
+    const uint32_t ring = groups * stages_of<E> * 2 * Row<T, VECTOR, E>::image_bytes(warps * 32);
+    const uint32_t smem = ring > 8 * cols ? ring : 8 * cols;
+    const uint32_t most = E == 8 ? MAX_PARTS : MAX_PARTS / 2;      // two CTAs on an SM, or one of long rows
+    *parts = ctas < most ? ctas : most;
     auto kernel = norm_backward_kernel<T, VECTOR, E>;
-    if (smem > 40 * 1024) {
-        const int rc = note_cuda(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 8 * (int)REGISTER_COLS));
-        if (rc) return rc;
-    }
+    if (const int rc = allow_smem(kernel, smem)) return rc;
     return note_cuda(el::launch(kernel, dim3(*parts), warps * groups * 32, smem, 1, stream, static_cast<const T *>(dy), ld_dy,
                                 static_cast<const T *>(x), ld_x, rows, cols, gamma, mean, rstd, static_cast<T *>(dx), ld_dx, part, warps));
 }
