@@ -184,6 +184,43 @@ struct Row {
                 if (i * G + t < cols) row[i * G + t] = el::from_float<T>(v[i]);
         }
     }
+    // The thread's values of an FP32 vector of the row's length; 0 behind its end.
+    static __device__ __forceinline__ void vector(const float *p, uint32_t cols, uint32_t t, uint32_t G, float *v)
+    {
+        if constexpr (VECTOR) {
+#pragma unroll
+            for (int i = 0; i < CHUNKS; ++i) {
+                const uint32_t c = (i * G + t) * PER;
+#pragma unroll
+                for (uint32_t j = 0; j < PER; j += 4) {
+                    const float4 f = c < cols ? __ldg(reinterpret_cast<const float4 *>(p + c + j)) : make_float4(0.f, 0.f, 0.f, 0.f);
+                    v[i * PER + j] = f.x;
+                    v[i * PER + j + 1] = f.y;
+                    v[i * PER + j + 2] = f.z;
+                    v[i * PER + j + 3] = f.w;
+                }
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < E; ++i) v[i] = i * G + t < cols ? __ldg(p + i * G + t) : 0.f;
+        }
+    }
+    // Sets the values behind the row's end.
+    static __device__ __forceinline__ void fill(uint32_t cols, uint32_t t, uint32_t G, float *v, float to)
+    {
+        if constexpr (VECTOR) {
+#pragma unroll
+            for (int i = 0; i < CHUNKS; ++i)
+                if ((i * G + t) * PER >= cols) {
+#pragma unroll
+                    for (uint32_t j = 0; j < PER; ++j) v[i * PER + j] = to;
+                }
+        } else {
+#pragma unroll
+            for (int i = 0; i < E; ++i)
+                if (i * G + t >= cols) v[i] = to;
+        }
+    }
     // Calls f(index of the value in v, column) for the values inside the row.
     template <typename F>
     static __device__ __forceinline__ void each(uint32_t cols, uint32_t t, uint32_t G, F f)
@@ -212,7 +249,7 @@ __device__ __forceinline__ void wait_copies() { asm volatile("cp.async.wait_grou
 // one barrier per call is enough: who writes a half again has passed the barrier of the call between.
 struct Group {
     uint32_t warps, index, thread;
-    float2 *room;       // [2][16] of this group
+    float *room;        // [2][32] of this group
     uint32_t turn;
 
     __device__ __forceinline__ void meet()
@@ -220,57 +257,92 @@ struct Group {
         if (warps > 1) asm volatile("bar.sync %0, %1;" ::"r"(index + 1), "r"(warps * 32) : "memory");
         else __syncwarp();
     }
-    __device__ __forceinline__ float2 sum(float2 v)
+    // One value: every lane ends with the total.
+    __device__ __forceinline__ float sum(float v)
     {
 #pragma unroll
-        for (int d = 16; d >= 1; d >>= 1) {
-            v.x += __shfl_xor_sync(0xFFFFFFFFu, v.x, d);
-            v.y += __shfl_xor_sync(0xFFFFFFFFu, v.y, d);
-        }
+        for (int d = 16; d >= 1; d >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, d);
         if (warps > 1) {
-            float2 *half = room + 16 * (turn & 1);
+            float *half = room + 32 * (turn & 1);
             ++turn;
             const uint32_t lane = threadIdx.x & 31;
             if (lane == 0) half[thread >> 5] = v;
             meet();
-            v = lane < warps ? half[lane] : make_float2(0.f, 0.f);
+            v = (lane & 15) < warps ? half[lane & 15] : 0.f;
 #pragma unroll
-            for (int d = 8; d >= 1; d >>= 1) {
-                v.x += __shfl_xor_sync(0xFFFFFFFFu, v.x, d);
-                v.y += __shfl_xor_sync(0xFFFFFFFFu, v.y, d);
-            }
-            v.x = __shfl_sync(0xFFFFFFFFu, v.x, 0);
-            v.y = __shfl_sync(0xFFFFFFFFu, v.y, 0);
+            for (int d = 8; d >= 1; d >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, d);
         }
         return v;
+    }
+    // Two values: the lower sixteen lanes add up the first, the upper sixteen the second.
+    __device__ __forceinline__ float2 sum2(float a, float b)
+    {
+        const uint32_t lane = threadIdx.x & 31;
+        const bool upper = lane >= 16;
+        float v = (upper ? b : a) + __shfl_xor_sync(0xFFFFFFFFu, upper ? a : b, 16);
+#pragma unroll
+        for (int d = 8; d >= 1; d >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, d);
+        if (warps > 1) {
+            float *half = room + 32 * (turn & 1);
+            ++turn;
+            if ((lane & 15) == 0) half[(thread >> 5) + (upper ? 16 : 0)] = v;
+            meet();
+            v = (lane & 15) < warps ? half[lane] : 0.f;
+#pragma unroll
+            for (int d = 8; d >= 1; d >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, d);
+        }
+        return make_float2(__shfl_sync(0xFFFFFFFFu, v, 0), __shfl_sync(0xFFFFFFFFu, v, 16));
     }
 };
 
 constexpr int MAX_GROUPS = 15;      // named barriers 1 .. 15
 
-__device__ __forceinline__ Group make_group(uint32_t warps, float2 *room)
+__device__ __forceinline__ Group make_group(uint32_t warps, float *room)
 {
     Group g;
     g.warps = warps;
     g.index = threadIdx.x / (warps * 32);
     g.thread = threadIdx.x - g.index * warps * 32;
-    g.room = room + g.index * 32;
+    g.room = room + g.index * 64;
     g.turn = 0;
     return g;
 }
 
-// Row images of a group: three (two ahead of the one in work), or two where a row is long.
-template <int E> constexpr int stages_of = E == 8 ? 3 : 2;
-constexpr int FORWARD_STAGES = 3;
+// Two FP32 values in one instruction each.
+__device__ __forceinline__ float2 add2(float2 a, float2 b)
+{
+    uint64_t r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(*reinterpret_cast<uint64_t *>(&a)), "l"(*reinterpret_cast<uint64_t *>(&b)));
+    return *reinterpret_cast<float2 *>(&r);
+}
+__device__ __forceinline__ float2 mul2(float2 a, float2 b)
+{
+    uint64_t r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(*reinterpret_cast<uint64_t *>(&a)), "l"(*reinterpret_cast<uint64_t *>(&b)));
+    return *reinterpret_cast<float2 *>(&r);
+}
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c)
+{
+    uint64_t r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;"
+        : "=l"(r) : "l"(*reinterpret_cast<uint64_t *>(&a)), "l"(*reinterpret_cast<uint64_t *>(&b)), "l"(*reinterpret_cast<uint64_t *>(&c)));
+    return *reinterpret_cast<float2 *>(&r);
+}
+__device__ __forceinline__ float2 twice(float v) { return make_float2(v, v); }
+
+constexpr int STAGES = 3;      // row images of a group: two ahead of the one in work
+
+// Registers a thread of the forward kernel gets: what lets 1024, 768 or 512 threads share an SM.
+template <bool VECTOR, int E> constexpr int forward_registers = E == 8 ? 64 : VECTOR ? 80 : 128;
 
 template <typename T, bool VECTOR, int E>
-__global__ void __launch_bounds__(512, E == 8 ? 2 : 1)
+__global__ void __maxnreg__((forward_registers<VECTOR, E>))
 norm_kernel(const T *x, uint32_t rows, uint32_t cols, uint64_t ld, const float *__restrict__ gamma, const float *__restrict__ beta, float eps,
             T *y, uint64_t ldy, float *__restrict__ mean_out, float *__restrict__ rstd_out, uint32_t warps)
 {
     using R = Row<T, VECTOR, E>;
-    constexpr int S = FORWARD_STAGES;
-    __shared__ float2 room[MAX_GROUPS * 32];
+    constexpr int S = STAGES;
+    __shared__ float room[MAX_GROUPS * 64];
     extern __shared__ __align__(16) uint8_t images[];
     Group g = make_group(warps, room);
     const uint32_t G = warps * 32, groups = blockDim.x / G, t = g.thread, bytes = R::image_bytes(G);
@@ -278,35 +350,54 @@ norm_kernel(const T *x, uint32_t rows, uint32_t cols, uint64_t ld, const float *
     const float inv = 1.f / (float)cols;
     el::enter_stream_order();
     const uint32_t step = gridDim.x * groups, first = blockIdx.x * groups + g.index;
-    auto fetch = [&](uint64_t row, uint32_t s) {
-        if (row < rows) R::fetch(ring + s * bytes, x + row * ld, row == 0, cols, t, G);
+    const bool whole = cols == G * E;                      // no thread holds anything behind a row's end
+    const T *src = x + (uint64_t)first * ld, *row_x = src;
+    T *row_y = y + (uint64_t)first * ldy;
+    uint32_t coming = first;                               // the row to fetch next (no overflow: rows < 2^31, step < 2^14)
+    auto fetch = [&](uint32_t s) {
+        if (coming < rows) R::fetch(ring + s * bytes, src, coming == 0, cols, t, G);
         commit_copies();
+        coming += step;
+        src += step * ld;
     };
 #pragma unroll
-    for (int s = 0; s < S - 1; ++s) fetch(first + (uint64_t)s * step, s);
+    for (int s = 0; s < S - 1; ++s) fetch(s);
     float ga[E], be[E];
-    R::each(cols, t, G, [&](int i, uint32_t c) { ga[i] = gamma[c]; be[i] = beta[c]; });
+    R::vector(gamma, cols, t, G, ga);
+    R::vector(beta, cols, t, G, be);
     uint32_t now = 0, ahead = S - 1;
-    for (uint64_t row = first; row < rows; row += step) {
-        fetch(row + (uint64_t)(S - 1) * step, ahead);      // where the row before was: its group has met since
+    for (uint32_t row = first; row < rows; row += step) {
+        fetch(ahead);                                      // where the row before was: its group has met since
         wait_copies<S - 1>();
         if (!VECTOR) g.meet();
         float v[E];
-        R::values(ring + now * bytes, x + row * ld, cols, t, G, v);
+        R::values(ring + now * bytes, row_x, cols, t, G, v);
         now = now + 1 == S ? 0 : now + 1;
         ahead = ahead + 1 == S ? 0 : ahead + 1;
-        float s = 0.f;
-        R::each(cols, t, G, [&](int i, uint32_t) { s += v[i]; });
-        const float mean = g.sum(make_float2(s, 0.f)).x * inv;
-        s = 0.f;
-        R::each(cols, t, G, [&](int i, uint32_t) { v[i] -= mean; s = __fmaf_rn(v[i], v[i], s); });
-        const float rstd = 1.f / sqrtf(g.sum(make_float2(s, 0.f)).x * inv + eps);
-        R::each(cols, t, G, [&](int i, uint32_t) { v[i] = __fmaf_rn(v[i] * rstd, ga[i], be[i]); });
-        R::store(y + row * ldy, cols, t, G, v);
+        if (!whole) R::fill(cols, t, G, v, 0.f);
+        float2 *p = reinterpret_cast<float2 *>(v);
+        float2 s = twice(0.f);
+#pragma unroll
+        for (int i = 0; i < E / 2; ++i) s = add2(s, p[i]);
+        const float mean = g.sum(s.x + s.y) * inv;
+        if (!whole) R::fill(cols, t, G, v, mean);
+        s = twice(0.f);
+#pragma unroll
+        for (int i = 0; i < E / 2; ++i) {
+            p[i] = add2(p[i], twice(-mean));
+            s = fma2(p[i], p[i], s);
+        }
+        const float rstd = __frsqrt_rn(g.sum(s.x + s.y) * inv + eps);
+#pragma unroll
+        for (int i = 0; i < E / 2; ++i)
+            p[i] = fma2(mul2(p[i], twice(rstd)), make_float2(ga[2 * i], ga[2 * i + 1]), make_float2(be[2 * i], be[2 * i + 1]));
+        R::store(row_y, cols, t, G, v);
         if (t == 0) {
             if (mean_out) mean_out[row] = mean;
             if (rstd_out) rstd_out[row] = rstd;
         }
+        if (!VECTOR) row_x += step * ld;
+        row_y += step * ldy;
     }
 }
 
@@ -318,8 +409,8 @@ norm_backward_kernel(const T *dy, uint64_t ld_dy, const T *x, uint64_t ld_x, uin
                      uint32_t warps)
 {
     using R = Row<T, VECTOR, E>;
-    constexpr int S = stages_of<E>;
-    __shared__ float2 room[MAX_GROUPS * 32];
+    constexpr int S = STAGES;
+    __shared__ float room[MAX_GROUPS * 64];
     extern __shared__ __align__(16) uint8_t images[];
     Group g = make_group(warps, room);
     const uint32_t G = warps * 32, groups = blockDim.x / G, t = g.thread, bytes = R::image_bytes(G);
@@ -327,26 +418,33 @@ norm_backward_kernel(const T *dy, uint64_t ld_dy, const T *x, uint64_t ld_x, uin
     const float inv = 1.f / (float)cols;
     el::enter_stream_order();
     const uint32_t step = gridDim.x * groups, first = blockIdx.x * groups + g.index;
-    auto fetch = [&](uint64_t row, uint32_t s) {
-        if (row < rows) {
-            R::fetch(ring + s * 2 * bytes, x + row * ld_x, row == 0, cols, t, G);
-            R::fetch(ring + s * 2 * bytes + bytes, dy + row * ld_dy, row == 0, cols, t, G);
+    const bool whole = cols == G * E;                      // no thread holds anything behind a row's end
+    const T *src_x = x + (uint64_t)first * ld_x, *src_d = dy + (uint64_t)first * ld_dy, *row_x = src_x, *row_d = src_d;
+    T *row_dx = dx + (uint64_t)first * ld_dx;
+    uint32_t coming = first;                               // the row to fetch next (no overflow: rows < 2^31, step < 2^14)
+    auto fetch = [&](uint32_t s) {
+        if (coming < rows) {
+            R::fetch(ring + s * 2 * bytes, src_x, coming == 0, cols, t, G);
+            R::fetch(ring + s * 2 * bytes + bytes, src_d, coming == 0, cols, t, G);
         }
         commit_copies();
+        coming += step;
+        src_x += step * ld_x;
+        src_d += step * ld_dy;
     };
 #pragma unroll
-    for (int s = 0; s < S - 1; ++s) fetch(first + (uint64_t)s * step, s);
-    float sg[E], sb[E];
+    for (int s = 0; s < S - 1; ++s) fetch(s);
+    float2 sg[E / 2], sb[E / 2];
 #pragma unroll
-    for (int i = 0; i < E; ++i) sg[i] = sb[i] = 0.f;
+    for (int i = 0; i < E / 2; ++i) sg[i] = sb[i] = twice(0.f);
     float mean = 0.f, rstd = 0.f;
     if (first < rows) {
         mean = mean_in[first];
         rstd = rstd_in[first];
     }
     uint32_t now = 0, ahead = S - 1;
-    for (uint64_t row = first; row < rows; row += step) {
-        fetch(row + (uint64_t)(S - 1) * step, ahead);      // where the row before was: its group has met since
+    for (uint32_t row = first; row < rows; row += step) {
+        fetch(ahead);                                      // where the row before was: its group has met since
         const float mu = mean, rs = rstd;
         if (row + step < rows) {
             mean = mean_in[row + step];
@@ -355,31 +453,46 @@ norm_backward_kernel(const T *dy, uint64_t ld_dy, const T *x, uint64_t ld_x, uin
         wait_copies<S - 1>();
         if (!VECTOR) g.meet();
         float h[E], d[E];
-        R::values(ring + now * 2 * bytes, x + row * ld_x, cols, t, G, h);
-        R::values(ring + now * 2 * bytes + bytes, dy + row * ld_dy, cols, t, G, d);
+        R::values(ring + now * 2 * bytes, row_x, cols, t, G, h);
+        R::values(ring + now * 2 * bytes + bytes, row_d, cols, t, G, d);
         now = now + 1 == S ? 0 : now + 1;
         ahead = ahead + 1 == S ? 0 : ahead + 1;
-        float2 s = make_float2(0.f, 0.f);
-        R::each(cols, t, G, [&](int i, uint32_t c) {        // (gamma from L1: in registers it would cost a CTA per SM)
-            h[i] = (h[i] - mu) * rs;
-            sg[i] = __fmaf_rn(d[i], h[i], sg[i]);
-            sb[i] += d[i];
-            d[i] *= __ldg(gamma + c);
-            s.x += d[i];
-            s.y = __fmaf_rn(d[i], h[i], s.y);
-        });
-        s = g.sum(s);
-        const float m1 = s.x * inv, m2 = s.y * inv;
-        R::each(cols, t, G, [&](int i, uint32_t) { d[i] = (d[i] - m1 - h[i] * m2) * rs; });
-        R::store(dx + row * ld_dx, cols, t, G, d);
+        if (!whole) {
+            R::fill(cols, t, G, h, mu);
+            R::fill(cols, t, G, d, 0.f);
+        }
+        float ga[E];                                       // from L1 each time: registers are short here
+        R::vector(gamma, cols, t, G, ga);
+        float2 *ph = reinterpret_cast<float2 *>(h), *pd = reinterpret_cast<float2 *>(d);
+        float2 s1 = twice(0.f), s2 = twice(0.f);
+#pragma unroll
+        for (int i = 0; i < E / 2; ++i) {
+            ph[i] = mul2(add2(ph[i], twice(-mu)), twice(rs));
+            sg[i] = fma2(pd[i], ph[i], sg[i]);
+            sb[i] = add2(sb[i], pd[i]);
+            pd[i] = mul2(pd[i], make_float2(ga[2 * i], ga[2 * i + 1]));
+            s1 = add2(s1, pd[i]);
+            s2 = fma2(pd[i], ph[i], s2);
+        }
+        const float2 m = g.sum2(s1.x + s1.y, s2.x + s2.y);
+        const float2 m1 = twice(-(m.x * inv)), m2 = twice(-(m.y * inv));
+#pragma unroll
+        for (int i = 0; i < E / 2; ++i) pd[i] = mul2(fma2(ph[i], m2, add2(pd[i], m1)), twice(rs));
+        R::store(row_dx, cols, t, G, d);
+        if (!VECTOR) {
+            row_x += step * ld_x;
+            row_d += step * ld_dy;
+        }
+        row_dx += step * ld_dx;
     }
     __syncthreads();
     float *columns = reinterpret_cast<float *>(images);    // 2 x cols: the groups' sums joined, in their order
     for (uint32_t k = 0; k < groups; ++k) {
         if (g.index == k)
             R::each(cols, t, G, [&](int i, uint32_t c) {
-                columns[c] = k ? columns[c] + sg[i] : sg[i];
-                columns[cols + c] = k ? columns[cols + c] + sb[i] : sb[i];
+                const float dg = i & 1 ? sg[i / 2].y : sg[i / 2].x, db = i & 1 ? sb[i / 2].y : sb[i / 2].x;
+                columns[c] = k ? columns[c] + dg : dg;
+                columns[cols + c] = k ? columns[cols + c] + db : db;
             });
         __syncthreads();
     }
@@ -435,9 +548,9 @@ int forward_rows(const void *x, uint32_t rows, uint32_t cols, uint64_t ld, const
 {
     const uint32_t warps = (cols + 32 * E - 1) / (32 * E), groups = warps >= 8 ? 1 : 8 / warps;
     const uint32_t ctas = (rows + groups - 1) / groups, threads = warps * groups * 32;
-    const uint32_t smem = groups * FORWARD_STAGES * Row<T, VECTOR, E>::image_bytes(warps * 32);
-    // as many CTAs as are resident: by registers (64, 84 or 128 a thread) and by shared memory
-    const uint32_t by_regs = 65536 / (threads * (E == 8 ? 64 : VECTOR ? 84 : 128)), by_smem = 220 * 1024 / (smem + 5 * 1024);
+    const uint32_t smem = groups * STAGES * Row<T, VECTOR, E>::image_bytes(warps * 32);
+    // as many CTAs as are resident
+    const uint32_t by_regs = 65536 / (threads * forward_registers<VECTOR, E>), by_smem = 220 * 1024 / (smem + 5 * 1024);
     const uint32_t most = DEFAULT_SMS * (by_regs < by_smem ? by_regs : by_smem);
     auto kernel = norm_kernel<T, VECTOR, E>;
     if (const int rc = allow_smem(kernel, smem)) return rc;
@@ -465,9 +578,9 @@ int backward_rows(const void *dy, uint64_t ld_dy, const void *x, uint64_t ld_x, 
     const uint32_t warps = (cols + 32 * E - 1) / (32 * E);
     const uint32_t groups = warps >= 16 ? 1 : (16 / warps < MAX_GROUPS ? 16 / warps : MAX_GROUPS);
     const uint32_t ctas = (rows + groups - 1) / groups;
-    const uint32_t ring = groups * stages_of<E> * 2 * Row<T, VECTOR, E>::image_bytes(warps * 32);
+    const uint32_t ring = groups * STAGES * 2 * Row<T, VECTOR, E>::image_bytes(warps * 32);
     const uint32_t smem = ring > 8 * cols ? ring : 8 * cols;
-    const uint32_t most = E == 8 ? MAX_PARTS : MAX_PARTS / 2;      // two CTAs on an SM, or one of long rows
+    const uint32_t most = E == 8 ? MAX_PARTS : MAX_PARTS / 2;      // as many CTAs as are resident
     *parts = ctas < most ? ctas : most;
     auto kernel = norm_backward_kernel<T, VECTOR, E>;
     if (const int rc = allow_smem(kernel, smem)) return rc;
@@ -484,8 +597,8 @@ int backward(const void *dy, uint64_t ld_dy, const void *x, uint64_t ld_x, uint6
     int rc = 0;
     if (rows && cols <= REGISTER_COLS) {
         const bool vec = vector_rows<T>(dy, ld_dy, cols) && vector_rows<T>(x, ld_x, cols) && vector_rows<T>(dx, ld_dx, cols);
-        auto f = vec ? (cols <= REGISTER_COLS / 2 ? backward_rows<T, true, 8> : backward_rows<T, true, 16>)
-                     : (cols <= REGISTER_COLS / 2 ? backward_rows<T, false, 8> : backward_rows<T, false, 16>);
+        auto f = vec ? (cols <= 256 ? backward_rows<T, true, 8> : backward_rows<T, true, 16>)
+                     : (cols <= 256 ? backward_rows<T, false, 8> : backward_rows<T, false, 16>);
         rc = f(dy, ld_dy, x, ld_x, (uint32_t)rows, c, gamma, mean, rstd, dx, ld_dx, part, &parts, stream);
     } else if (rows) {
         // the column sums first: dx may overwrite dy or x
