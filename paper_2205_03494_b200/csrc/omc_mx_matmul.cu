@@ -218,6 +218,179 @@ mx_matmul_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constan
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"((uint32_t)TMEM_COLS) : "memory");
 }
 
+// ---- large products: one persistent CTA per SM, tiles of 128 x 256 -----------------------------------
+// 48 KB of codes per K step for twice the products of a 128 x 128 tile's 32 KB: what bounds the smaller tile is the
+// traffic from L2 to shared memory.
+//   warp 0   copies (one thread); warp 1   scales to tensor memory and products (one thread)
+//   warps 4-11   epilogue: a quarter of the lanes and half of the columns each
+// Tensor memory (512 columns): the two accumulators would fill it, and the scales need 2 x 24 columns, so
+// accumulator 1 starts 48 columns early, inside accumulator 0.  The epilogue reads the shared columns
+// first and releases them; the products of the next tile start then, under the rest of the epilogue.
+// The scales of K steps it and it + 1 have columns of their own; those of step it - 2 are free once its products are
+// through, which the issuing thread sees from the stage's own barrier.
+// The kernel does not let its successor start early: it would only take room on SMs that are busy to the end.
+struct Wide {
+    static constexpr int NT = 256;
+    static constexpr int TILE_X_BYTES = NT * BK / 2;
+    static constexpr int STAGE = TILE_W_BYTES + TILE_X_BYTES + 3 * SCALE_BYTES;
+    static constexpr int NSTAGES = 4;
+    static constexpr int SMEM = NSTAGES * STAGE + 1024 + 256;
+    static constexpr int THREADS = 384, EPILOGUE_THREADS = 256;
+    static constexpr int SLOT_COLS = 3 * SCALE_COLS, SHARED_COLS = 2 * SLOT_COLS;
+    static constexpr int ACC1 = 256 - SHARED_COLS, SCALES = 512 - SHARED_COLS;
+    static_assert(STAGE % 1024 == 0 && SMEM <= 227 * 1024 && 8 * (2 * NSTAGES + 7) <= 256, "");
+};
+
+// Tiles in the order in which the CTAs take them: bands of sixteen tiles of W's rows, so that the tiles in work
+// at a time form a block of about sixteen by nine and share their operands in L2.
+__device__ __forceinline__ void tile_of(uint32_t t, uint32_t tiles_n, uint32_t tiles_m, uint32_t &tn, uint32_t &tm)
+{
+    const uint32_t per_band = 16 * tiles_m, band = t / per_band, in_band = t - band * per_band;
+    const uint32_t width = min(16u, tiles_n - band * 16);
+    tm = in_band / width;
+    tn = band * 16 + in_band - tm * width;
+}
+
+template <typename T>
+__global__ void __launch_bounds__(Wide::THREADS, 1)
+mx_matmul_wide_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_x,
+                      const uint8_t *__restrict__ w_scales, const uint8_t *__restrict__ x_scales, T *__restrict__ y, uint64_t ldy,
+                      uint32_t M, uint32_t N, uint32_t K, uint32_t *status)
+{
+    using C = Wide;
+    constexpr int NS = C::NSTAGES;
+    extern __shared__ uint8_t smem_raw[];
+    const uint32_t base = (saddr(smem_raw) + 1023u) & ~1023u;
+    const uint32_t bars = base + NS * C::STAGE;      // full[NS], empty[NS], acc_full[2], acc_shared[2], acc_empty[2], tmem slot
+    auto full = [&](int s) { return bars + 8u * s; };
+    auto empty = [&](int s) { return bars + 8u * (NS + s); };
+    auto acc_full = [&](int b) { return bars + 8u * (2 * NS + b); };
+    auto acc_shared = [&](int b) { return bars + 8u * (2 * NS + 2 + b); };      // the shared columns have been read
+    auto acc_empty = [&](int b) { return bars + 8u * (2 * NS + 4 + b); };       // all have
+    const uint32_t tmem_slot = bars + 8u * (2 * NS + 6);
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const uint32_t ksteps = (K + BK - 1) / BK;
+    const uint32_t tiles_n = (N + BM - 1) / BM, tiles_m = (M + C::NT - 1) / C::NT, ntiles = tiles_n * tiles_m;
+
+    if (tid == 0) {
+        for (int s = 0; s < NS; ++s) { mbar_init(full(s), 1); mbar_init(empty(s), 1); }
+        for (int b = 0; b < 2; ++b) {
+            mbar_init(acc_full(b), 1);
+            mbar_init(acc_shared(b), C::EPILOGUE_THREADS);
+            mbar_init(acc_empty(b), C::EPILOGUE_THREADS);
+        }
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    if (warp == 1) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(tmem_slot), "r"(512u) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+    __syncthreads();
+    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+    uint32_t tmem_base;
+    asm volatile("ld.shared.u32 %0, [%1];" : "=r"(tmem_base) : "r"(tmem_slot));
+
+    bool ok = true;
+    if (tid == 0) {
+        const uint32_t x_blocks = (M + 127) / 128;
+        uint32_t it = 0;
+        for (uint32_t t = blockIdx.x; t < ntiles && ok; t += gridDim.x) {
+            uint32_t tn, tm;
+            tile_of(t, tiles_n, tiles_m, tn, tm);
+            const uint8_t *ws = w_scales + (uint64_t)tn * ksteps * SCALE_BYTES;
+            const uint8_t *xs0 = x_scales + (uint64_t)(2 * tm) * ksteps * SCALE_BYTES;
+            const uint8_t *xs1 = x_scales + (uint64_t)min(2 * tm + 1, x_blocks - 1) * ksteps * SCALE_BYTES;      // (no such rows: any scales)
+            for (uint32_t k = 0; k < ksteps; ++k, ++it) {
+                const int s = it % NS;
+                if (it >= (uint32_t)NS) ok = mbar_wait(empty(s), ((it / NS) - 1) & 1u, WAIT_LIMIT);
+                if (!ok) break;
+                const uint32_t a = base + s * C::STAGE, sc = a + TILE_W_BYTES + C::TILE_X_BYTES;
+                mbar_expect_tx(full(s), C::STAGE);
+                tma_load_2d(a, &map_w, (int)(k * (BK / 2)), (int)(tn * BM), full(s));
+                tma_load_2d(a + TILE_W_BYTES, &map_x, (int)(k * (BK / 2)), (int)(tm * C::NT), full(s));
+                bulk_load(sc, ws + (uint64_t)k * SCALE_BYTES, SCALE_BYTES, full(s));
+                bulk_load(sc + SCALE_BYTES, xs0 + (uint64_t)k * SCALE_BYTES, SCALE_BYTES, full(s));
+                bulk_load(sc + 2 * SCALE_BYTES, xs1 + (uint64_t)k * SCALE_BYTES, SCALE_BYTES, full(s));
+            }
+        }
+    } else if (tid == 32) {
+        uint32_t it = 0, lt = 0;
+        for (uint32_t t = blockIdx.x; t < ntiles && ok; t += gridDim.x, ++lt) {
+            const uint32_t buf = lt & 1u;
+            if (lt >= 1) ok = mbar_wait(acc_shared(buf ^ 1u), ((lt - 1) >> 1) & 1u, WAIT_LIMIT);     // of the tile before
+            if (ok && lt >= 2) ok = mbar_wait(acc_empty(buf), ((lt >> 1) - 1) & 1u, WAIT_LIMIT);     // of the one before that
+            if (!ok) break;
+            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+            const uint32_t d = tmem_base + buf * C::ACC1;
+            for (uint32_t k = 0; k < ksteps; ++k, ++it) {
+                const int s = it % NS;
+                ok = mbar_wait(full(s), (it / NS) & 1u, WAIT_LIMIT);
+                if (ok && it >= 2) ok = mbar_wait(empty((it - 2) % NS), ((it - 2) / NS) & 1u, WAIT_LIMIT);      // its scale columns are free
+                if (!ok) break;
+                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                const uint32_t a = base + s * C::STAGE, b = a + TILE_W_BYTES, sc = b + C::TILE_X_BYTES;
+                const uint32_t ta = tmem_base + C::SCALES + (it & 1u) * C::SLOT_COLS, tb = ta + SCALE_COLS;
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    copy_scales(ta + 4 * h, sc + 512 * h);
+                    copy_scales(tb + 8 * h, sc + SCALE_BYTES + 512 * h);                     // X's rows 0 .. 127
+                    copy_scales(tb + 8 * h + 4, sc + 2 * SCALE_BYTES + 512 * h);             // 128 .. 255
+                }
+#pragma unroll
+                for (int i = 0; i < BK / INSTR_K; ++i)
+                    mma_mx(d, umma_desc(a + i * INSTR_K / 2), umma_desc(b + i * INSTR_K / 2), instr_desc(BM, C::NT, i & 1),
+                           ta + 4 * (i >> 1), tb + 8 * (i >> 1), (k | (uint32_t)i) != 0);
+                umma_commit(empty(s));
+            }
+            if (ok) umma_commit(acc_full(buf));
+        }
+    } else if (warp >= 4) {
+        const int q = warp & 3, half = (warp - 4) >> 2;
+        uint32_t lt = 0;
+        for (uint32_t t = blockIdx.x; t < ntiles; t += gridDim.x, ++lt) {
+            const uint32_t buf = lt & 1u;
+            uint32_t tn, tm;
+            tile_of(t, tiles_n, tiles_m, tn, tm);
+            ok = mbar_wait(acc_full(buf), (lt >> 1) & 1u, WAIT_LIMIT);
+            ok = __all_sync(0xFFFFFFFFu, ok);
+            if (!ok) break;
+            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+            const uint32_t n = tn * BM + q * 32 + lane, m0 = tm * C::NT;
+            const uint32_t acc = tmem_base + buf * C::ACC1 + ((uint32_t)(q * 32) << 16);
+            T *out = y + (uint64_t)m0 * ldy + n;
+            // shared columns: the last 48 of accumulator 0 (upper half), the first 48 of accumulator 1 (lower half)
+            const bool mine = (half == 1) == (buf == 0);
+            if (!mine) mbar_arrive(acc_shared(buf));
+#pragma unroll 1
+            for (int i = 0; i < 8; ++i) {
+                const int c = half * 128 + (half == 1 && buf == 0 ? 7 - i : i) * 16;
+                uint32_t v[16];
+                tmem_load16(acc + c, v);
+                if (mine && i == C::SHARED_COLS / 16 - 1) {
+                    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+                    mbar_arrive(acc_shared(buf));
+                }
+                if (n < N) {
+                    T *p = out + (uint64_t)c * ldy;
+#pragma unroll
+                    for (int j = 0; j < 16; ++j, p += ldy)
+                        if (m0 + c + j < M) *p = el::from_float<T>(__uint_as_float(v[j]));
+                }
+            }
+            asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+            mbar_arrive(acc_empty(buf));
+        }
+    }
+    if (!ok) atomicExch(status, 1u);
+    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+    __syncwarp();
+    __syncthreads();
+    if (warp == 1)
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(512u) : "memory");
+}
+
 // The codes as bytes: boxes of box_rows rows x 128 bytes, 128-byte swizzle, zeros outside.
 bool make_codes_map(CUtensorMap *m, const void *ptr, uint64_t rows, uint64_t cols, uint32_t box_rows)
 {
@@ -262,6 +435,19 @@ int launch(const Product &p)
                                 p.w_scales, p.x_scales, static_cast<T *>(p.y), p.ldy, p.M, p.N, p.K, splits, p.status));
 }
 
+template <typename T>
+int launch_wide(const Product &p)
+{
+    CUtensorMap map_w, map_x;
+    if (!make_codes_map(&map_w, p.w_codes, p.N, p.K, BM) || !make_codes_map(&map_x, p.x_codes, p.M, p.K, Wide::NT)) return OMC_ERR_CUDA;
+    const int rc = note_cuda(cudaFuncSetAttribute(mx_matmul_wide_kernel<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, Wide::SMEM));
+    if (rc) return rc;
+    const uint64_t ntiles = (uint64_t)((p.N + BM - 1) / BM) * ((p.M + Wide::NT - 1) / Wide::NT);
+    const uint32_t sms = (uint32_t)sm_count();
+    return note_cuda(el::launch(mx_matmul_wide_kernel<T>, dim3(ntiles < sms ? (uint32_t)ntiles : sms), Wide::THREADS, Wide::SMEM, 1, p.stream,
+                                map_w, map_x, p.w_scales, p.x_scales, static_cast<T *>(p.y), p.ldy, p.M, p.N, p.K, p.status));
+}
+
 // Few rows of X: the narrowest tile that holds them all (their scales start at a multiple of 128 rows).
 template <typename T>
 int launch_any(const Product &p)
@@ -269,6 +455,7 @@ int launch_any(const Product &p)
     if (p.M <= 16) return launch<16, T>(p);
     if (p.M <= 32) return launch<32, T>(p);
     if (p.M <= 64) return launch<64, T>(p);
+    if ((uint64_t)((p.N + 127) / 128) * ((p.M + 255) / 256) >= 96) return launch_wide<T>(p);
     return launch<128, T>(p);
 }
 
