@@ -63,6 +63,18 @@ __device__ __forceinline__ void copy_scales(uint32_t tmem, uint32_t smem)
     const uint64_t desc = (uint64_t)((smem >> 4) & 0x3FFFu) | (1ull << 16) | (8ull << 32) | (1ull << 46);
     asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(tmem), "l"(desc) : "memory");
 }
+// Eight columns of tensor memory of this warp's quarter of the lanes, a word each from every lane's registers.
+__device__ __forceinline__ void tmem_store8(uint32_t taddr, uint4 a, uint4 b)
+{
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
+                 ::"r"(taddr), "r"(a.x), "r"(a.y), "r"(a.z), "r"(a.w), "r"(b.x), "r"(b.y), "r"(b.z), "r"(b.w) : "memory");
+}
+__device__ __forceinline__ uint4 shared16(uint32_t addr)
+{
+    uint4 v;
+    asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(addr) : "memory");
+    return v;
+}
 __device__ __forceinline__ void bulk_load(uint32_t dst, const void *src, uint32_t bytes, uint32_t bar)
 {
     asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
@@ -223,11 +235,13 @@ mx_matmul_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constan
 // traffic from L2 to shared memory.
 //   warp 0   copies (one thread); warp 1   scales to tensor memory and products (one thread)
 //   warps 4-11   epilogue: a quarter of the lanes and half of the columns each
-// Tensor memory (512 columns): the two accumulators would fill it, and the scales need 2 x 24 columns, so
-// accumulator 1 starts 48 columns early, inside accumulator 0.  The epilogue reads the shared columns
+//   warps 12-15  scales from shared to tensor memory, a copy in each quarter of the lanes.  (tcgen05.cp does the same in
+//   one instruction per 512 bytes, but in the tensor pipe, between the products: measured 30 us of 142 at 16384 x 2048 x 8192.)
+// Tensor memory (512 columns): the two accumulators would fill it, and the scales need 3 x 24 columns, so
+// accumulator 1 starts 80 columns early, inside accumulator 0.  The epilogue reads the shared columns
 // first and releases them; the products of the next tile start then, under the rest of the epilogue.
-// The scales of K steps it and it + 1 have columns of their own; those of step it - 2 are free once its products are
-// through, which the issuing thread sees from the stage's own barrier.
+// The scales of three K steps have columns of their own; those of step it - 3 are free once its products are through,
+// which the stage's own barrier tells.
 // The kernel does not let its successor start early: it would only take room on SMs that are busy to the end.
 struct Wide {
     static constexpr int NT = 256;
@@ -235,10 +249,10 @@ struct Wide {
     static constexpr int STAGE = TILE_W_BYTES + TILE_X_BYTES + 3 * SCALE_BYTES;
     static constexpr int NSTAGES = 4;
     static constexpr int SMEM = NSTAGES * STAGE + 1024 + 256;
-    static constexpr int THREADS = 384, EPILOGUE_THREADS = 256;
-    static constexpr int SLOT_COLS = 3 * SCALE_COLS, SHARED_COLS = 2 * SLOT_COLS;
+    static constexpr int THREADS = 512, EPILOGUE_THREADS = 256, SCALE_THREADS = 128;
+    static constexpr int SLOTS = 3, SLOT_COLS = 3 * SCALE_COLS, SHARED_COLS = 80;      // (3 x 24, in whole loads of 16)
     static constexpr int ACC1 = 256 - SHARED_COLS, SCALES = 512 - SHARED_COLS;
-    static_assert(STAGE % 1024 == 0 && SMEM <= 227 * 1024 && 8 * (2 * NSTAGES + 7) <= 256, "");
+    static_assert(STAGE % 1024 == 0 && SMEM <= 227 * 1024 && 8 * (2 * NSTAGES + 7 + SLOTS) <= 256, "");
 };
 
 // Tiles in the order in which the CTAs take them: bands of sixteen tiles of W's rows, so that the tiles in work
@@ -261,19 +275,21 @@ mx_matmul_wide_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_co
     constexpr int NS = C::NSTAGES;
     extern __shared__ uint8_t smem_raw[];
     const uint32_t base = (saddr(smem_raw) + 1023u) & ~1023u;
-    const uint32_t bars = base + NS * C::STAGE;      // full[NS], empty[NS], acc_full[2], acc_shared[2], acc_empty[2], tmem slot
+    const uint32_t bars = base + NS * C::STAGE;      // full[NS], empty[NS], acc_full[2], acc_shared[2], acc_empty[2], scaled[SLOTS], tmem slot
     auto full = [&](int s) { return bars + 8u * s; };
     auto empty = [&](int s) { return bars + 8u * (NS + s); };
     auto acc_full = [&](int b) { return bars + 8u * (2 * NS + b); };
     auto acc_shared = [&](int b) { return bars + 8u * (2 * NS + 2 + b); };      // the shared columns have been read
     auto acc_empty = [&](int b) { return bars + 8u * (2 * NS + 4 + b); };       // all have
-    const uint32_t tmem_slot = bars + 8u * (2 * NS + 6);
+    auto scaled = [&](int s) { return bars + 8u * (2 * NS + 6 + s); };          // a step's scales are in tensor memory
+    const uint32_t tmem_slot = bars + 8u * (2 * NS + 6 + C::SLOTS);
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const uint32_t ksteps = (K + BK - 1) / BK;
     const uint32_t tiles_n = (N + BM - 1) / BM, tiles_m = (M + C::NT - 1) / C::NT, ntiles = tiles_n * tiles_m;
 
     if (tid == 0) {
         for (int s = 0; s < NS; ++s) { mbar_init(full(s), 1); mbar_init(empty(s), 1); }
+        for (int s = 0; s < C::SLOTS; ++s) mbar_init(scaled(s), C::SCALE_THREADS);
         for (int b = 0; b < 2; ++b) {
             mbar_init(acc_full(b), 1);
             mbar_init(acc_shared(b), C::EPILOGUE_THREADS);
@@ -327,17 +343,11 @@ mx_matmul_wide_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_co
             for (uint32_t k = 0; k < ksteps; ++k, ++it) {
                 const int s = it % NS;
                 ok = mbar_wait(full(s), (it / NS) & 1u, WAIT_LIMIT);
-                if (ok && it >= 2) ok = mbar_wait(empty((it - 2) % NS), ((it - 2) / NS) & 1u, WAIT_LIMIT);      // its scale columns are free
+                if (ok) ok = mbar_wait(scaled(it % C::SLOTS), (it / C::SLOTS) & 1u, WAIT_LIMIT);
                 if (!ok) break;
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                const uint32_t a = base + s * C::STAGE, b = a + TILE_W_BYTES, sc = b + C::TILE_X_BYTES;
-                const uint32_t ta = tmem_base + C::SCALES + (it & 1u) * C::SLOT_COLS, tb = ta + SCALE_COLS;
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    copy_scales(ta + 4 * h, sc + 512 * h);
-                    copy_scales(tb + 8 * h, sc + SCALE_BYTES + 512 * h);                     // X's rows 0 .. 127
-                    copy_scales(tb + 8 * h + 4, sc + 2 * SCALE_BYTES + 512 * h);             // 128 .. 255
-                }
+                const uint32_t a = base + s * C::STAGE, b = a + TILE_W_BYTES;
+                const uint32_t ta = tmem_base + C::SCALES + it % C::SLOTS * C::SLOT_COLS, tb = ta + SCALE_COLS;
 #pragma unroll
                 for (int i = 0; i < BK / INSTR_K; ++i)
                     mma_mx(d, umma_desc(a + i * INSTR_K / 2), umma_desc(b + i * INSTR_K / 2), instr_desc(BM, C::NT, i & 1),
@@ -345,6 +355,25 @@ mx_matmul_wide_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_co
                 umma_commit(empty(s));
             }
             if (ok) umma_commit(acc_full(buf));
+        }
+    } else if (warp >= 12) {
+        const uint32_t quarter = (uint32_t)((warp & 3) * 32) << 16;
+        const uint32_t steps = (ntiles - blockIdx.x + gridDim.x - 1) / gridDim.x * ksteps;
+        for (uint32_t it = 0; it < steps; ++it) {
+            const int s = it % NS;
+            if (it >= (uint32_t)C::SLOTS) ok = mbar_wait(empty((it - C::SLOTS) % NS), ((it - C::SLOTS) / NS) & 1u, WAIT_LIMIT);      // columns are free
+            ok = ok && mbar_wait(full(s), (it / NS) & 1u, WAIT_LIMIT);
+            ok = __all_sync(0xFFFFFFFFu, ok);
+            if (!ok) break;
+            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+            const uint32_t sc = base + s * C::STAGE + TILE_W_BYTES + C::TILE_X_BYTES + lane * 16;
+            const uint32_t ta = tmem_base + C::SCALES + it % C::SLOTS * C::SLOT_COLS + quarter, tb = ta + SCALE_COLS;
+            tmem_store8(ta, shared16(sc), shared16(sc + 512));
+            tmem_store8(tb, shared16(sc + SCALE_BYTES), shared16(sc + 2 * SCALE_BYTES));                    // columns 0 .. 127: X's rows 0 .. 127, 128 .. 255
+            tmem_store8(tb + 8, shared16(sc + SCALE_BYTES + 512), shared16(sc + 2 * SCALE_BYTES + 512));    // columns 128 .. 255
+            asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
+            asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+            mbar_arrive(scaled(it % C::SLOTS));
         }
     } else if (warp >= 4) {
         const int q = warp & 3, half = (warp - 4) >> 2;
@@ -360,7 +389,7 @@ mx_matmul_wide_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_co
             const uint32_t n = tn * BM + q * 32 + lane, m0 = tm * C::NT;
             const uint32_t acc = tmem_base + buf * C::ACC1 + ((uint32_t)(q * 32) << 16);
             T *out = y + (uint64_t)m0 * ldy + n;
-            // shared columns: the last 48 of accumulator 0 (upper half), the first 48 of accumulator 1 (lower half)
+            // shared columns: the last 80 of accumulator 0 (upper half), the first 80 of accumulator 1 (lower half)
             const bool mine = (half == 1) == (buf == 0);
             if (!mine) mbar_arrive(acc_shared(buf));
 #pragma unroll 1
