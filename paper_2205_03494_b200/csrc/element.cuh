@@ -5,9 +5,13 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
-#include "../../include/omc.h"
+#include <atomic>
+
+#include "omc_internal.h"
 
 namespace omc {
+int note_cuda(cudaError_t e);
+
 namespace el {
 
 __device__ __forceinline__ float to_float(float v) { return v; }
@@ -65,6 +69,35 @@ __device__ __forceinline__ void enter_stream_order()
 inline size_t size_of(int type) { return type == OMC_TYPE_F32 ? 4 : 2; }
 inline bool type_ok(int type) { return type == OMC_TYPE_F32 || type == OMC_TYPE_F16 || type == OMC_TYPE_BF16; }
 inline bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+
+constexpr int MAX_DEVICES = 64;
+
+// SMs of the current device, asked for once per device.
+inline uint32_t sm_count()
+{
+    static std::atomic<int> known[MAX_DEVICES];
+    int dev = 0, n = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess) return DEFAULT_SMS;
+    if (dev < MAX_DEVICES && (n = known[dev].load(std::memory_order_relaxed)) > 0) return (uint32_t)n;
+    if (cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || n < 1) return DEFAULT_SMS;
+    if (dev < MAX_DEVICES) known[dev].store(n, std::memory_order_relaxed);
+    return (uint32_t)n;
+}
+
+// More dynamic shared memory than a kernel has by default: the runtime is told once per kernel and device, always the same.
+constexpr uint32_t MOST_SMEM = 220 * 1024;
+template <auto KERNEL>
+int allow_smem(uint32_t bytes)
+{
+    static std::atomic<bool> told[MAX_DEVICES];
+    if (bytes <= 40 * 1024) return OMC_OK;
+    int dev = 0;
+    if (const int rc = note_cuda(cudaGetDevice(&dev))) return rc;
+    if (dev < MAX_DEVICES && told[dev].load(std::memory_order_acquire)) return OMC_OK;
+    if (const int rc = note_cuda(cudaFuncSetAttribute(KERNEL, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)MOST_SMEM))) return rc;
+    if (dev < MAX_DEVICES) told[dev].store(true, std::memory_order_release);
+    return OMC_OK;
+}
 
 // Launch as the programmatic dependent of the kernel before it on the stream.
 template <typename... P, typename... A>

@@ -10,10 +10,6 @@
 #include "mx_format.cuh"
 #include "omc_internal.h"
 
-namespace omc {
-int note_cuda(cudaError_t e);
-}
-
 namespace {
 
 using namespace omc;
@@ -66,28 +62,42 @@ __device__ __forceinline__ uint32_t gather_scales(uint32_t scale, int lane)
     return w;
 }
 
-// Along the rows only: a warp takes 256 columns of one row.
-template <typename T, bool VECTOR>
+// Along the rows only: a warp takes PIECES times 256 columns, one piece after the other through the matrix, and asks for all
+// of them before it works on the first.
+template <typename T, bool VECTOR, int PIECES>
 __global__ void __launch_bounds__(32 * WARPS)
 quantise_rows_kernel(const T *__restrict__ x, uint32_t rows, uint32_t cols, uint64_t ld, uint8_t *__restrict__ codes,
                      uint8_t *__restrict__ scales)
 {
     el::enter_stream_order();
     const uint32_t ksteps = (cols + 255) / 256;
-    const uint32_t item = blockIdx.x * WARPS + (threadIdx.x >> 5);
-    const uint32_t row = item / ksteps, k = item % ksteps;
-    if (row >= rows) return;
+    const uint32_t first = (blockIdx.x * WARPS + (threadIdx.x >> 5)) * PIECES;
     const int lane = threadIdx.x & 31;
-    const uint32_t col = k * 256 + lane * 8;
-    float v[8];
-    load8<T, VECTOR>(x + row * ld, col, cols, v);
-    uint32_t scale;
-    const uint32_t c = encode_block(v, scale);
     const uint64_t rb = mx::row_bytes(cols);
-    if (col / 2 < rb) *reinterpret_cast<uint32_t *>(codes + row * rb + col / 2) = c;
-    const uint32_t w = gather_scales(scale, lane);
-    if ((lane & 15) == 0)
-        *reinterpret_cast<uint32_t *>(scales + mx::scale_offset(row, (uint64_t)k * 8 + (lane >> 2), ksteps)) = w;
+    uint32_t row = first / ksteps, k = first % ksteps;
+    uint32_t row_of[PIECES], k_of[PIECES];
+    float v[PIECES][8];
+#pragma unroll
+    for (int i = 0; i < PIECES; ++i) {
+        row_of[i] = row;
+        k_of[i] = k;
+        if (row < rows) load8<T, VECTOR>(x + row * ld, k * 256 + lane * 8, cols, v[i]);
+        if (++k == ksteps) {
+            k = 0;
+            ++row;
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < PIECES; ++i) {
+        if (row_of[i] >= rows) break;
+        const uint32_t col = k_of[i] * 256 + lane * 8;
+        uint32_t scale;
+        const uint32_t c = encode_block(v[i], scale);
+        if (col / 2 < rb) *reinterpret_cast<uint32_t *>(codes + row_of[i] * rb + col / 2) = c;
+        const uint32_t w = gather_scales(scale, lane);
+        if ((lane & 15) == 0)
+            *reinterpret_cast<uint32_t *>(scales + mx::scale_offset(row_of[i], (uint64_t)k_of[i] * 8 + (lane >> 2), ksteps)) = w;
+    }
 }
 
 // Along the columns, and along the rows too if ROWS: a CTA takes a tile of 128 x 128.
@@ -235,11 +245,16 @@ int quantise(const void *x, uint32_t rows, uint32_t cols, uint64_t ld, uint8_t *
     const T *src = static_cast<const T *>(x);
     if (!codes_t) {
         const uint64_t items = (uint64_t)rows * ((cols + 255) / 256);
-        return note_cuda(el::launch(quantise_rows_kernel<T, VECTOR>, dim3((uint32_t)((items + WARPS - 1) / WARPS)), 32 * WARPS, 0, 1,
-                                    stream, src, rows, cols, ld, codes, scales));
+        // few pieces: one a warp, so that more warps share them
+        if (items <= 148 * 64)
+            return note_cuda(el::launch(quantise_rows_kernel<T, VECTOR, 1>, dim3((uint32_t)((items + WARPS - 1) / WARPS)), 32 * WARPS, 0, 1,
+                                        stream, src, rows, cols, ld, codes, scales));
+        return note_cuda(el::launch(quantise_rows_kernel<T, VECTOR, 4>, dim3((uint32_t)((items + 4 * WARPS - 1) / (4 * WARPS))), 32 * WARPS,
+                                    0, 1, stream, src, rows, cols, ld, codes, scales));
     }
     auto kernel = codes ? quantise_tile_kernel<T, VECTOR, true> : quantise_tile_kernel<T, VECTOR, false>;
-    const int rc = note_cuda(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, tile_smem<T>()));
+    const int rc = codes ? el::allow_smem<quantise_tile_kernel<T, VECTOR, true>>(tile_smem<T>())
+                         : el::allow_smem<quantise_tile_kernel<T, VECTOR, false>>(tile_smem<T>());
     if (rc) return rc;
     const uint64_t tiles = (uint64_t)((rows + TILE - 1) / TILE) * ((cols + TILE - 1) / TILE);
     return note_cuda(el::launch(kernel, dim3((uint32_t)tiles), 256, tile_smem<T>(), 1, stream, src, rows, cols, ld, codes, scales,

@@ -20,7 +20,6 @@
 #include "tensor_core.cuh"
 
 namespace omc {
-int note_cuda(cudaError_t e);
 bool mx_shape_ok(uint64_t rows, uint64_t cols);
 }
 
@@ -80,14 +79,26 @@ __device__ __forceinline__ void bulk_load(uint32_t dst, const void *src, uint32_
     asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
                  ::"r"(dst), "l"(src), "r"(bytes), "r"(bar) : "memory");
 }
-__device__ __forceinline__ void tmem_load16(uint32_t taddr, uint32_t *v)
+__device__ __forceinline__ void tmem_load16_async(uint32_t taddr, uint32_t *v)
 {
     asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 "
                  "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
                  : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]),
                    "=r"(v[8]), "=r"(v[9]), "=r"(v[10]), "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15])
                  : "r"(taddr));
-    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+}
+__device__ __forceinline__ void tmem_load_wait() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+// After the wait: nothing computed from these registers may move above it.
+__device__ __forceinline__ void loaded16(uint32_t *v)
+{
+    asm volatile("" : "+r"(v[0]), "+r"(v[1]), "+r"(v[2]), "+r"(v[3]), "+r"(v[4]), "+r"(v[5]), "+r"(v[6]), "+r"(v[7]),
+                 "+r"(v[8]), "+r"(v[9]), "+r"(v[10]), "+r"(v[11]), "+r"(v[12]), "+r"(v[13]), "+r"(v[14]), "+r"(v[15]));
+}
+__device__ __forceinline__ void tmem_load16(uint32_t taddr, uint32_t *v)
+{
+    tmem_load16_async(taddr, v);
+    tmem_load_wait();
+    loaded16(v);
 }
 __device__ __forceinline__ float load_remote(uint32_t cluster_addr)
 {
@@ -391,22 +402,36 @@ mx_matmul_wide_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_co
             T *out = y + (uint64_t)m0 * ldy + n;
             // shared columns: the last 80 of accumulator 0 (upper half), the first 80 of accumulator 1 (lower half)
             const bool mine = (half == 1) == (buf == 0);
-            if (!mine) mbar_arrive(acc_shared(buf));
+            auto put = [&](int c, const uint32_t *v) {           // sixteen columns from c on
+                if (n >= N) return;
+                T *p = out + (uint64_t)c * ldy;
+#pragma unroll
+                for (int j = 0; j < 16; ++j, p += ldy)
+                    if (m0 + c + j < M) *p = el::from_float<T>(__uint_as_float(v[j]));
+            };
+            int c = half * 128, c_end = c + 128;
+            if (mine) {
+                const int first = buf == 0 ? 256 - C::SHARED_COLS : 0;
+                uint32_t v[C::SHARED_COLS];
+#pragma unroll
+                for (int i = 0; i < C::SHARED_COLS; i += 16) tmem_load16_async(acc + first + i, v + i);
+                tmem_load_wait();
+#pragma unroll
+                for (int i = 0; i < C::SHARED_COLS; i += 16) loaded16(v + i);
+                asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+                mbar_arrive(acc_shared(buf));
+#pragma unroll
+                for (int i = 0; i < C::SHARED_COLS; i += 16) put(first + i, v + i);
+                if (buf == 0) c_end = first;
+                else c = C::SHARED_COLS;
+            } else {
+                mbar_arrive(acc_shared(buf));
+            }
 #pragma unroll 1
-            for (int i = 0; i < 8; ++i) {
-                const int c = half * 128 + (half == 1 && buf == 0 ? 7 - i : i) * 16;
+            for (; c < c_end; c += 16) {
                 uint32_t v[16];
                 tmem_load16(acc + c, v);
-                if (mine && i == C::SHARED_COLS / 16 - 1) {
-                    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-                    mbar_arrive(acc_shared(buf));
-                }
-                if (n < N) {
-                    T *p = out + (uint64_t)c * ldy;
-#pragma unroll
-                    for (int j = 0; j < 16; ++j, p += ldy)
-                        if (m0 + c + j < M) *p = el::from_float<T>(__uint_as_float(v[j]));
-                }
+                put(c, v);
             }
             asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
             mbar_arrive(acc_empty(buf));
@@ -442,24 +467,17 @@ struct Product {
     void *stream;
 };
 
-int sm_count()
-{
-    int dev = 0, n = 0;
-    if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) return DEFAULT_SMS;
-    return n;
-}
-
 template <int NT, typename T>
 int launch(const Product &p)
 {
     CUtensorMap map_w, map_x;
     if (!make_codes_map(&map_w, p.w_codes, p.N, p.K, BM) || !make_codes_map(&map_x, p.x_codes, p.M, p.K, NT)) return OMC_ERR_CUDA;
-    const int rc = note_cuda(cudaFuncSetAttribute(mx_matmul_kernel<NT, T>, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM));
+    const int rc = el::allow_smem<mx_matmul_kernel<NT, T>>(SMEM);
     if (rc) return rc;
     const uint32_t tiles_n = (p.N + BM - 1) / BM, tiles_m = (p.M + NT - 1) / NT, ksteps = (p.K + BK - 1) / BK;
     // divide K while the CTAs still fit on the device at once and each keeps two steps
     uint32_t splits = 1;
-    while (splits < 8 && (uint64_t)tiles_n * tiles_m * splits * 2 <= 2u * (uint32_t)sm_count() && ksteps >= splits * 4) splits *= 2;
+    while (splits < 8 && (uint64_t)tiles_n * tiles_m * splits * 2 <= 2u * el::sm_count() && ksteps >= splits * 4) splits *= 2;
     return note_cuda(el::launch(mx_matmul_kernel<NT, T>, dim3(tiles_n * splits, tiles_m), THREADS, SMEM, splits, p.stream, map_w, map_x,
                                 p.w_scales, p.x_scales, static_cast<T *>(p.y), p.ldy, p.M, p.N, p.K, splits, p.status));
 }
@@ -469,10 +487,10 @@ int launch_wide(const Product &p)
 {
     CUtensorMap map_w, map_x;
     if (!make_codes_map(&map_w, p.w_codes, p.N, p.K, BM) || !make_codes_map(&map_x, p.x_codes, p.M, p.K, Wide::NT)) return OMC_ERR_CUDA;
-    const int rc = note_cuda(cudaFuncSetAttribute(mx_matmul_wide_kernel<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, Wide::SMEM));
+    const int rc = el::allow_smem<mx_matmul_wide_kernel<T>>(Wide::SMEM);
     if (rc) return rc;
     const uint64_t ntiles = (uint64_t)((p.N + BM - 1) / BM) * ((p.M + Wide::NT - 1) / Wide::NT);
-    const uint32_t sms = (uint32_t)sm_count();
+    const uint32_t sms = el::sm_count();
     return note_cuda(el::launch(mx_matmul_wide_kernel<T>, dim3(ntiles < sms ? (uint32_t)ntiles : sms), Wide::THREADS, Wide::SMEM, 1, p.stream,
                                 map_w, map_x, p.w_scales, p.x_scales, static_cast<T *>(p.y), p.ldy, p.M, p.N, p.K, p.status));
 }

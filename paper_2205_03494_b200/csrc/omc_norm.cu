@@ -10,10 +10,6 @@
 #include "element.cuh"
 #include "omc_internal.h"
 
-namespace omc {
-int note_cuda(cudaError_t e);
-}
-
 namespace {
 
 using namespace omc;
@@ -535,13 +531,6 @@ bool vector_rows(const void *p, uint64_t ld, uint64_t cols)
 
 constexpr uint32_t REGISTER_COLS = 8192;      // 16 warps of 16 values a thread
 
-// More dynamic shared memory than a kernel has by default.
-template <typename K>
-int allow_smem(K kernel, uint32_t smem)
-{
-    return smem <= 40 * 1024 ? 0 : note_cuda(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
-}
-
 template <typename T, bool VECTOR, int E>
 int forward_rows(const void *x, uint32_t rows, uint32_t cols, uint64_t ld, const float *gamma, const float *beta, float eps, void *y,
                  uint64_t ldy, float *mean, float *rstd, void *stream)
@@ -552,9 +541,8 @@ int forward_rows(const void *x, uint32_t rows, uint32_t cols, uint64_t ld, const
     // as many CTAs as are resident
     const uint32_t by_regs = 65536 / (threads * forward_registers<VECTOR, E>), by_smem = 220 * 1024 / (smem + 5 * 1024);
     const uint32_t most = DEFAULT_SMS * (by_regs < by_smem ? by_regs : by_smem);
-    auto kernel = norm_kernel<T, VECTOR, E>;
-    if (const int rc = allow_smem(kernel, smem)) return rc;
-    return note_cuda(el::launch(kernel, dim3(ctas < most ? ctas : most), threads, smem, 1, stream,
+    if (const int rc = el::allow_smem<norm_kernel<T, VECTOR, E>>(smem)) return rc;
+    return note_cuda(el::launch(norm_kernel<T, VECTOR, E>, dim3(ctas < most ? ctas : most), threads, smem, 1, stream,
                                 static_cast<const T *>(x), rows, cols, ld, gamma, beta, eps, static_cast<T *>(y), ldy, mean, rstd, warps));
 }
 
@@ -582,9 +570,8 @@ int backward_rows(const void *dy, uint64_t ld_dy, const void *x, uint64_t ld_x, 
     const uint32_t smem = ring > 8 * cols ? ring : 8 * cols;
     const uint32_t most = E == 8 ? MAX_PARTS : MAX_PARTS / 2;      // as many CTAs as are resident
     *parts = ctas < most ? ctas : most;
-    auto kernel = norm_backward_kernel<T, VECTOR, E>;
-    if (const int rc = allow_smem(kernel, smem)) return rc;
-    return note_cuda(el::launch(kernel, dim3(*parts), warps * groups * 32, smem, 1, stream, static_cast<const T *>(dy), ld_dy,
+    if (const int rc = el::allow_smem<norm_backward_kernel<T, VECTOR, E>>(smem)) return rc;
+    return note_cuda(el::launch(norm_backward_kernel<T, VECTOR, E>, dim3(*parts), warps * groups * 32, smem, 1, stream, static_cast<const T *>(dy), ld_dy,
                                 static_cast<const T *>(x), ld_x, rows, cols, gamma, mean, rstd, static_cast<T *>(dx), ld_dx, part, warps));
 }
 
