@@ -17,40 +17,73 @@ using el::Word;
 
 constexpr int WARPS = 8;
 
-// Eight consecutive values of a row as FP32, zeros behind the row's end.
+// Eight consecutive values as they are stored: four words of 16-bit types, eight of FP32.
+template <typename T> constexpr int WORDS8 = 8 / Word<T>::N;
+
 template <typename T, bool VECTOR>
-__device__ __forceinline__ void load8(const T *row, uint32_t col, uint32_t cols, float *v)
+__device__ __forceinline__ void load8(const T *row, uint32_t col, uint32_t cols, uint32_t *w)
 {
     if (VECTOR && col + 8 <= cols) {
-        constexpr int N = Word<T>::N;
 #pragma unroll
-        for (int i = 0; i < 2 / N; ++i) {
-            const uint4 w = *reinterpret_cast<const uint4 *>(row + col + 4 * N * i);
-            Word<T>::unpack(w.x, v + N * (4 * i));
-            Word<T>::unpack(w.y, v + N * (4 * i + 1));
-            Word<T>::unpack(w.z, v + N * (4 * i + 2));
-            Word<T>::unpack(w.w, v + N * (4 * i + 3));
+        for (int i = 0; i < WORDS8<T>; i += 4) {
+            const uint4 q = *reinterpret_cast<const uint4 *>(row + col + i * Word<T>::N);
+            w[i] = q.x;
+            w[i + 1] = q.y;
+            w[i + 2] = q.z;
+            w[i + 3] = q.w;
         }
-    } else {
+    } else {                       // zeros behind the row's end
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = col + i < cols ? el::to_float(row[col + i]) : 0.f;
+        for (int i = 0; i < WORDS8<T>; ++i) {
+            if constexpr (sizeof(T) == 4) {
+                w[i] = col + i < cols ? reinterpret_cast<const uint32_t *>(row)[col + i] : 0u;
+            } else {
+                const uint16_t *p = reinterpret_cast<const uint16_t *>(row) + col + 2 * i;
+                const uint32_t lo = col + 2 * i < cols ? p[0] : 0u, hi = col + 2 * i + 1 < cols ? p[1] : 0u;
+                w[i] = lo | (hi << 16);
+            }
+        }
     }
 }
 
+// Largest magnitude, two 16-bit values at a time: the order of the magnitudes is that of their bit patterns, Inf and
+// NaN on top.
+template <typename T>
+__device__ __forceinline__ uint32_t max_magnitude(uint32_t acc, uint32_t w)
+{
+    if constexpr (sizeof(T) == 4) return max(acc, w & 0x7FFFFFFFu);
+    uint32_t r;
+    asm("max.u16x2 %0, %1, %2;" : "=r"(r) : "r"(acc), "r"(w & 0x7FFF7FFFu));
+    return r;
+}
+// A magnitude of T as FP32 bits (T 16 bits wide: the lower half of m).
+template <typename T>
+__device__ __forceinline__ uint32_t fp32_bits(uint32_t m)
+{
+    if constexpr (sizeof(T) == 4) return m;
+    float f[2];
+    Word<T>::unpack(m, f);
+    return __float_as_uint(f[0]);
+}
+
 // Codes and scale of the block that four neighbouring lanes hold, eight values each.
-__device__ __forceinline__ uint32_t encode_block(const float *v, uint32_t &scale)
+template <typename T>
+__device__ __forceinline__ uint32_t encode_block(const uint32_t *w, uint32_t &scale)
 {
     uint32_t top = 0;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) top = max(top, mx::magnitude(v[i]));
+    for (int i = 0; i < WORDS8<T>; ++i) top = max_magnitude<T>(top, w[i]);
+    if constexpr (sizeof(T) == 2) top = max(top >> 16, top & 0xFFFFu);
     top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, 1));
     top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, 2));
-    scale = mx::scale_of(top);
-    const float f = mx::inverse_scale(scale);
-    float u[8];
+    scale = mx::scale_of(fp32_bits<T>(top));
+    const float2 f = el::twice(mx::inverse_scale(scale));
+    float v[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) u[i] = v[i] * f;
-    const uint32_t codes = mx::encode8(u);
+    for (int i = 0; i < WORDS8<T>; ++i) Word<T>::unpack(w[i], v + Word<T>::N * i);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) reinterpret_cast<float2 *>(v)[i] = el::mul2(reinterpret_cast<float2 *>(v)[i], f);
+    const uint32_t codes = mx::encode8(v);
     return scale == mx::NAN_SCALE ? 0u : codes;
 }
 // The scales of the four blocks that sixteen lanes hold, one byte each.
@@ -62,41 +95,56 @@ __device__ __forceinline__ uint32_t gather_scales(uint32_t scale, int lane)
     return w;
 }
 
-// Along the rows only: a warp takes PIECES times 256 columns, one piece after the other through the matrix, and asks for all
-// of them before it works on the first.
-template <typename T, bool VECTOR, int PIECES>
+// The pieces of a matrix (256 columns of a row) that a warp takes: every `stride`-th, counted along the rows, without a
+// division per piece.
+struct Walk {
+    uint32_t row, k, step_rows, step_k, ksteps;
+
+    __device__ __forceinline__ Walk(uint32_t first, uint32_t stride, uint32_t ksteps_)
+        : row(first / ksteps_), k(first % ksteps_), step_rows(stride / ksteps_), step_k(stride % ksteps_), ksteps(ksteps_) {}
+    __device__ __forceinline__ void next()
+    {
+        row += step_rows;
+        k += step_k;
+        if (k >= ksteps) {
+            k -= ksteps;
+            ++row;
+        }
+    }
+};
+
+// Along the rows only: a warp walks over pieces and asks for the next AHEAD while it works on one.
+constexpr int AHEAD = 4;
+
+template <typename T, bool VECTOR>
 __global__ void __launch_bounds__(32 * WARPS)
 quantise_rows_kernel(const T *__restrict__ x, uint32_t rows, uint32_t cols, uint64_t ld, uint8_t *__restrict__ codes,
                      uint8_t *__restrict__ scales)
 {
-    el::enter_stream_order();
     const uint32_t ksteps = (cols + 255) / 256;
-    const uint32_t first = (blockIdx.x * WARPS + (threadIdx.x >> 5)) * PIECES;
     const int lane = threadIdx.x & 31;
     const uint64_t rb = mx::row_bytes(cols);
-    uint32_t row = first / ksteps, k = first % ksteps;
-    uint32_t row_of[PIECES], k_of[PIECES];
-    float v[PIECES][8];
+    Walk at(blockIdx.x * WARPS + (threadIdx.x >> 5), gridDim.x * WARPS, ksteps), ask = at;
+    el::enter_stream_order();
+    uint32_t w[AHEAD][WORDS8<T>];
 #pragma unroll
-    for (int i = 0; i < PIECES; ++i) {
-        row_of[i] = row;
-        k_of[i] = k;
-        if (row < rows) load8<T, VECTOR>(x + row * ld, k * 256 + lane * 8, cols, v[i]);
-        if (++k == ksteps) {
-            k = 0;
-            ++row;
+    for (int i = 0; i < AHEAD; ++i, ask.next())
+        if (ask.row < rows) load8<T, VECTOR>(x + ask.row * ld, ask.k * 256 + lane * 8, cols, w[i]);
+    while (at.row < rows) {
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) {
+            if (at.row >= rows) break;
+            const uint32_t col = at.k * 256 + lane * 8;
+            uint32_t scale;
+            const uint32_t c = encode_block<T>(w[i], scale);
+            if (ask.row < rows) load8<T, VECTOR>(x + ask.row * ld, ask.k * 256 + lane * 8, cols, w[i]);
+            if (col / 2 < rb) *reinterpret_cast<uint32_t *>(codes + at.row * rb + col / 2) = c;
+            const uint32_t s = gather_scales(scale, lane);
+            if ((lane & 15) == 0)
+                *reinterpret_cast<uint32_t *>(scales + mx::scale_offset(at.row, (uint64_t)at.k * 8 + (lane >> 2), ksteps)) = s;
+            at.next();
+            ask.next();
         }
-    }
-#pragma unroll
-    for (int i = 0; i < PIECES; ++i) {
-        if (row_of[i] >= rows) break;
-        const uint32_t col = k_of[i] * 256 + lane * 8;
-        uint32_t scale;
-        const uint32_t c = encode_block(v[i], scale);
-        if (col / 2 < rb) *reinterpret_cast<uint32_t *>(codes + row_of[i] * rb + col / 2) = c;
-        const uint32_t w = gather_scales(scale, lane);
-        if ((lane & 15) == 0)
-            *reinterpret_cast<uint32_t *>(scales + mx::scale_offset(row_of[i], (uint64_t)k_of[i] * 8 + (lane >> 2), ksteps)) = w;
     }
 }
 
@@ -109,77 +157,88 @@ __global__ void __launch_bounds__(256)
 quantise_tile_kernel(const T *__restrict__ x, uint32_t rows, uint32_t cols, uint64_t ld, uint8_t *__restrict__ codes,
                      uint8_t *__restrict__ scales, uint8_t *__restrict__ codes_t, uint8_t *__restrict__ scales_t)
 {
-    el::enter_stream_order();
     extern __shared__ __align__(16) uint8_t smem[];
     T *tile = reinterpret_cast<T *>(smem);
     uint8_t *out = smem + TILE * TILE * sizeof(T);
     uint8_t *atom = out + TILE * COLUMN_PITCH, *atom_t = atom + 512;
     const int tid = threadIdx.x, lane = tid & 31;
     const uint32_t col_tiles = (cols + TILE - 1) / TILE, row_tiles = (rows + TILE - 1) / TILE;
-    const uint32_t tc = blockIdx.x % col_tiles, tr = blockIdx.x / col_tiles;
+    const uint32_t tr = blockIdx.x / col_tiles, tc = blockIdx.x - tr * col_tiles;
     const uint32_t r0 = tr * TILE, c0 = tc * TILE;
     const uint64_t rb = mx::row_bytes(cols), rb_t = mx::row_bytes(rows);
+    el::enter_stream_order();
 
-    // sixteen lanes take 128 columns of a row
-#pragma unroll 4
-    for (int i = 0; i < 8; ++i) {
-        const uint32_t r = i * 16 + (tid >> 4), col = c0 + (tid & 15) * 8;
-        float v[8];
-        if (r0 + r < rows) {
-            load8<T, VECTOR>(x + (uint64_t)(r0 + r) * ld, col, cols, v);
-        } else {
+    // sixteen lanes take 128 columns of a row; four rows are asked for at a time
+    constexpr int BATCH = sizeof(T) == 4 ? 4 : 8;
 #pragma unroll
-            for (int j = 0; j < 8; ++j) v[j] = 0.f;
-        }
-        if constexpr (ROWS) {
-            uint32_t scale;
-            const uint32_t c = encode_block(v, scale);
-            if (r0 + r < rows && col / 2 < rb) *reinterpret_cast<uint32_t *>(codes + (r0 + r) * rb + col / 2) = c;
-            const uint32_t w = gather_scales(scale, lane);
-            if ((lane & 15) == 0) *reinterpret_cast<uint32_t *>(atom + (r & 31) * 16 + (r >> 5) * 4) = w;
-        }
-        T *dst = tile + r * TILE + (tid & 15) * 8;
-        constexpr int N = Word<T>::N;
+    for (int i0 = 0; i0 < 8; i0 += BATCH) {
+        uint32_t w[BATCH][WORDS8<T>];
 #pragma unroll
-        for (int j = 0; j < 2 / N; ++j)
-            reinterpret_cast<uint4 *>(dst)[j] = make_uint4(Word<T>::pack(v + N * (4 * j)), Word<T>::pack(v + N * (4 * j + 1)),
-                                                           Word<T>::pack(v + N * (4 * j + 2)), Word<T>::pack(v + N * (4 * j + 3)));
+        for (int i = 0; i < BATCH; ++i) {
+            const uint32_t r = r0 + (i0 + i) * 16 + (tid >> 4);
+            if (r < rows) {
+                load8<T, VECTOR>(x + (uint64_t)r * ld, c0 + (tid & 15) * 8, cols, w[i]);
+            } else {
+#pragma unroll
+                for (int j = 0; j < WORDS8<T>; ++j) w[i][j] = 0u;
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < BATCH; ++i) {
+            const uint32_t r = (i0 + i) * 16 + (tid >> 4), col = c0 + (tid & 15) * 8;
+            uint4 *dst = reinterpret_cast<uint4 *>(tile + r * TILE + (tid & 15) * 8);
+#pragma unroll
+            for (int j = 0; j < WORDS8<T> / 4; ++j) dst[j] = make_uint4(w[i][4 * j], w[i][4 * j + 1], w[i][4 * j + 2], w[i][4 * j + 3]);
+            if constexpr (ROWS) {
+                uint32_t scale;
+                const uint32_t c = encode_block<T>(w[i], scale);
+                if (r0 + r < rows && col / 2 < rb) *reinterpret_cast<uint32_t *>(codes + (r0 + r) * rb + col / 2) = c;
+                const uint32_t s = gather_scales(scale, lane);
+                if ((lane & 15) == 0) *reinterpret_cast<uint32_t *>(atom + (r & 31) * 16 + (r >> 5) * 4) = s;
+            }
+        }
     }
     __syncthreads();
 
     // a thread takes one block of 32 rows of two neighbouring columns
     {
         const int block = tid >> 6, pair = tid & 63;
-        float a[32], b[32];
+        float2 v[32];
         uint32_t top_a = 0, top_b = 0;
 #pragma unroll
         for (int i = 0; i < 32; ++i) {
             const T *p = tile + (block * 32 + i) * TILE + pair * 2;
             if constexpr (sizeof(T) == 4) {
-                const float2 f = *reinterpret_cast<const float2 *>(p);
-                a[i] = f.x;
-                b[i] = f.y;
+                v[i] = *reinterpret_cast<const float2 *>(p);
+                top_a = max_magnitude<T>(top_a, __float_as_uint(v[i].x));
+                top_b = max_magnitude<T>(top_b, __float_as_uint(v[i].y));
             } else {
-                float f[2];
-                Word<T>::unpack(*reinterpret_cast<const uint32_t *>(p), f);
-                a[i] = f[0];
-                b[i] = f[1];
+                const uint32_t w = *reinterpret_cast<const uint32_t *>(p);
+                top_a = max_magnitude<T>(top_a, w);
+                Word<T>::unpack(w, reinterpret_cast<float *>(v + i));
             }
-            top_a = max(top_a, mx::magnitude(a[i]));
-            top_b = max(top_b, mx::magnitude(b[i]));
         }
+        if constexpr (sizeof(T) == 2) {
+            top_b = top_a >> 16;
+            top_a &= 0xFFFFu;
+        }
+        const uint32_t sa = mx::scale_of(fp32_bits<T>(top_a)), sb = mx::scale_of(fp32_bits<T>(top_b));
+        const float2 f = make_float2(mx::inverse_scale(sa), mx::inverse_scale(sb));
+#pragma unroll
+        for (int i = 0; i < 32; ++i) v[i] = el::mul2(v[i], f);
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-            float *v = h ? b : a;
-            const uint32_t scale = mx::scale_of(h ? top_b : top_a);
-            const float f = mx::inverse_scale(scale);
+            uint32_t c[4];
 #pragma unroll
-            for (int i = 0; i < 32; ++i) v[i] *= f;
-            uint4 c = make_uint4(mx::encode8(v), mx::encode8(v + 8), mx::encode8(v + 16), mx::encode8(v + 24));
-            if (scale == mx::NAN_SCALE) c = make_uint4(0u, 0u, 0u, 0u);
+            for (int i = 0; i < 4; ++i) {
+                float u[8];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) u[j] = h ? v[8 * i + j].y : v[8 * i + j].x;
+                c[i] = (h ? sb : sa) == mx::NAN_SCALE ? 0u : mx::encode8(u);
+            }
             const int col = pair * 2 + h;
-            *reinterpret_cast<uint4 *>(out + col * COLUMN_PITCH + block * 16) = c;
-            atom_t[(col & 31) * 16 + (col >> 5) * 4 + block] = (uint8_t)scale;
+            *reinterpret_cast<uint4 *>(out + col * COLUMN_PITCH + block * 16) = make_uint4(c[0], c[1], c[2], c[3]);
+            atom_t[(col & 31) * 16 + (col >> 5) * 4 + block] = (uint8_t)(h ? sb : sa);
         }
     }
     __syncthreads();
@@ -204,38 +263,90 @@ quantise_tile_kernel(const T *__restrict__ x, uint32_t rows, uint32_t cols, uint
     }
 }
 
-// A warp takes 256 columns of one row.
+// A warp walks over pieces.  Rows off the 16-byte boundaries are turned in shared memory, so that neighbouring lanes store
+// neighbouring values (16-bit types in pairs that lie on 4-byte boundaries).
 template <typename T, bool VECTOR>
 __global__ void __launch_bounds__(32 * WARPS)
 dequantise_kernel(const uint8_t *__restrict__ codes, const uint8_t *__restrict__ scales, uint32_t rows, uint32_t cols,
                   T *__restrict__ out, uint64_t ld)
 {
-    el::enter_stream_order();
+    __shared__ __align__(16) T turned[VECTOR ? 1 : WARPS][VECTOR ? 8 : 256 + 8];
     const uint32_t ksteps = (cols + 255) / 256;
-    const uint32_t item = blockIdx.x * WARPS + (threadIdx.x >> 5);
-    const uint32_t row = item / ksteps, k = item % ksteps;
-    if (row >= rows) return;
     const int lane = threadIdx.x & 31;
-    const uint32_t col = k * 256 + lane * 8;
-    if (col >= cols) return;
-    const uint32_t c = *reinterpret_cast<const uint32_t *>(codes + row * mx::row_bytes(cols) + col / 2);
-    const float s = mx::scale_value(scales[mx::scale_offset(row, (uint64_t)k * 8 + (lane >> 2), ksteps)]);
-    float v[8];
-    mx::decode8(c, v);
+    const uint64_t rb = mx::row_bytes(cols);
+    Walk at(blockIdx.x * WARPS + (threadIdx.x >> 5), gridDim.x * WARPS, ksteps), ask = at;
+    el::enter_stream_order();
+    uint32_t c[AHEAD], b[AHEAD];
+    auto fetch = [&](int i) {
+        const uint32_t col = ask.k * 256 + lane * 8;
+        if (ask.row < rows && col < cols) {
+            c[i] = *reinterpret_cast<const uint32_t *>(codes + ask.row * rb + col / 2);
+            b[i] = scales[mx::scale_offset(ask.row, (uint64_t)ask.k * 8 + (lane >> 2), ksteps)];
+        }
+        ask.next();
+    };
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] *= s;
-    T *dst = out + row * ld + col;
-    if (VECTOR && col + 8 <= cols) {
-        constexpr int N = Word<T>::N;
+    for (int i = 0; i < AHEAD; ++i) fetch(i);
+    while (at.row < rows) {
 #pragma unroll
-        for (int j = 0; j < 2 / N; ++j)
-            reinterpret_cast<uint4 *>(dst)[j] = make_uint4(Word<T>::pack(v + N * (4 * j)), Word<T>::pack(v + N * (4 * j + 1)),
-                                                           Word<T>::pack(v + N * (4 * j + 2)), Word<T>::pack(v + N * (4 * j + 3)));
-    } else {
+        for (int i = 0; i < AHEAD; ++i) {
+            if (at.row >= rows) break;
+            const uint32_t col = at.k * 256 + lane * 8;
+            float v[8];
+            mx::decode8(c[i], v);
+            const float2 s = el::twice(mx::scale_value(b[i] & 255u));
+            fetch(i);
+            uint32_t w[WORDS8<T>];
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
-            if (col + i < cols) dst[i] = el::from_float<T>(v[i]);
+            for (int j = 0; j < 4; ++j) reinterpret_cast<float2 *>(v)[j] = el::mul2(reinterpret_cast<float2 *>(v)[j], s);
+#pragma unroll
+            for (int j = 0; j < WORDS8<T>; ++j) w[j] = Word<T>::pack(v + Word<T>::N * j);
+            if (VECTOR) {
+                T *dst = out + at.row * ld + col;
+                if (col + 8 <= cols) {
+#pragma unroll
+                    for (int j = 0; j < WORDS8<T>; j += 4) *reinterpret_cast<uint4 *>(dst + j * Word<T>::N) = make_uint4(w[j], w[j + 1], w[j + 2], w[j + 3]);
+                } else {
+#pragma unroll
+                    for (int j = 0; j < 8; ++j)
+                        if (col + j < cols) dst[j] = el::from_float<T>(v[j]);
+                }
+            } else {
+                T *mine = turned[threadIdx.x >> 5];
+                T *dst = out + at.row * ld + at.k * 256;
+                const uint32_t n = min(256u, cols - at.k * 256);
+                const uint32_t odd = sizeof(T) == 2 ? (uint32_t)(reinterpret_cast<uintptr_t>(dst) >> 1) & 1u : 0u;      // values before the first boundary
+                __syncwarp();
+#pragma unroll
+                for (int j = 0; j < 8; ++j) mine[odd + lane * 8 + j] = el::from_float<T>(v[j]);      // value e at odd + e
+                __syncwarp();
+                if constexpr (sizeof(T) == 2) {
+                    // pair p: places 2 p and 2 p + 1, values 2 p - odd and 2 p + 1 - odd
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const uint32_t e = 2 * (j * 32 + lane);
+                        if (e >= odd && e + 1 < odd + n)
+                            *reinterpret_cast<uint32_t *>(dst + e - odd) = *reinterpret_cast<const uint32_t *>(mine + e);
+                    }
+                    // what has no partner: the first value before a boundary, the last one behind
+                    if (lane == 0 && odd) dst[0] = mine[1];
+                    if (lane == 1 && ((odd + n) & 1) && (n > 1 || !odd)) dst[n - 1] = mine[odd + n - 1];
+                } else {
+#pragma unroll
+                    for (int j = 0; j < 8; ++j)
+                        if (j * 32 + lane < n) dst[j * 32 + lane] = mine[j * 32 + lane];
+                }
+            }
+            at.next();
+        }
     }
+}
+
+// CTAs for a walk over so many pieces: what is resident (eight CTAs on an SM), or one piece a warp.
+uint32_t walk_ctas(uint64_t pieces)
+{
+    const uint64_t most = 8ull * DEFAULT_SMS, wanted = (pieces + WARPS - 1) / WARPS;
+    return (uint32_t)(wanted < most ? wanted : most);
 }
 
 template <typename T, bool VECTOR>
@@ -244,13 +355,8 @@ int quantise(const void *x, uint32_t rows, uint32_t cols, uint64_t ld, uint8_t *
 {
     const T *src = static_cast<const T *>(x);
     if (!codes_t) {
-        const uint64_t items = (uint64_t)rows * ((cols + 255) / 256);
-        // few pieces: one a warp, so that more warps share them
-        if (items <= 148 * 64)
-            return note_cuda(el::launch(quantise_rows_kernel<T, VECTOR, 1>, dim3((uint32_t)((items + WARPS - 1) / WARPS)), 32 * WARPS, 0, 1,
-                                        stream, src, rows, cols, ld, codes, scales));
-        return note_cuda(el::launch(quantise_rows_kernel<T, VECTOR, 4>, dim3((uint32_t)((items + 4 * WARPS - 1) / (4 * WARPS))), 32 * WARPS,
-                                    0, 1, stream, src, rows, cols, ld, codes, scales));
+        return note_cuda(el::launch(quantise_rows_kernel<T, VECTOR>, dim3(walk_ctas((uint64_t)rows * ((cols + 255) / 256))), 32 * WARPS, 0, 1,
+                                    stream, src, rows, cols, ld, codes, scales));
     }
     auto kernel = codes ? quantise_tile_kernel<T, VECTOR, true> : quantise_tile_kernel<T, VECTOR, false>;
     const int rc = codes ? el::allow_smem<quantise_tile_kernel<T, VECTOR, true>>(tile_smem<T>())
@@ -264,8 +370,7 @@ int quantise(const void *x, uint32_t rows, uint32_t cols, uint64_t ld, uint8_t *
 template <typename T, bool VECTOR>
 int dequantise(const uint8_t *codes, const uint8_t *scales, uint32_t rows, uint32_t cols, void *out, uint64_t ld, void *stream)
 {
-    const uint64_t items = (uint64_t)rows * ((cols + 255) / 256);
-    return note_cuda(el::launch(dequantise_kernel<T, VECTOR>, dim3((uint32_t)((items + WARPS - 1) / WARPS)), 32 * WARPS, 0, 1, stream,
+    return note_cuda(el::launch(dequantise_kernel<T, VECTOR>, dim3(walk_ctas((uint64_t)rows * ((cols + 255) / 256))), 32 * WARPS, 0, 1, stream,
                                 codes, scales, rows, cols, static_cast<T *>(out), ld));
 }
 

@@ -13,6 +13,10 @@
 namespace {
 
 using namespace omc;
+using el::add2;
+using el::fma2;
+using el::mul2;
+using el::twice;
 
 constexpr int THREADS = 256;
 
@@ -303,28 +307,6 @@ __device__ __forceinline__ Group make_group(uint32_t warps, float *room)
     g.turn = 0;
     return g;
 }
-
-// Two FP32 values in one instruction each.
-__device__ __forceinline__ float2 add2(float2 a, float2 b)
-{
-    uint64_t r;
-    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(*reinterpret_cast<uint64_t *>(&a)), "l"(*reinterpret_cast<uint64_t *>(&b)));
-    return *reinterpret_cast<float2 *>(&r);
-}
-__device__ __forceinline__ float2 mul2(float2 a, float2 b)
-{
-    uint64_t r;
-    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(*reinterpret_cast<uint64_t *>(&a)), "l"(*reinterpret_cast<uint64_t *>(&b)));
-    return *reinterpret_cast<float2 *>(&r);
-}
-__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c)
-{
-    uint64_t r;
-    asm("fma.rn.f32x2 %0, %1, %2, %3;"
-        : "=l"(r) : "l"(*reinterpret_cast<uint64_t *>(&a)), "l"(*reinterpret_cast<uint64_t *>(&b)), "l"(*reinterpret_cast<uint64_t *>(&c)));
-    return *reinterpret_cast<float2 *>(&r);
-}
-__device__ __forceinline__ float2 twice(float v) { return make_float2(v, v); }
 
 constexpr int STAGES = 3;      // row images of a group: two ahead of the one in work
 

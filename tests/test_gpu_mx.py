@@ -120,6 +120,22 @@ def test_dequantise_every_code_and_scale(ty):
         assert bool((out[:, cols:] == -7.0).all()) and bool((g.t[:offset] == -7.0).all())
 
 
+@pytest.mark.parametrize("ty", list(TYPES))
+@pytest.mark.parametrize("rows,cols", [(1, 1), (3, 255), (5, 257), (7, 1000), (33, 2049), (2, 9000), (2000, 513)])
+def test_dequantise_wide_rows(rows, cols, ty):
+    """Many pieces to a row, rows that begin on every kind of address, last pieces of one value and of 255."""
+    code, dtype = TYPES[ty]
+    rng = np.random.default_rng(rows + cols)
+    cd, sd, want = stored_matrix(rng.standard_normal((rows, cols)) * 2.0 ** rng.integers(-6, 6, (rows, 1)))
+    for ld, offset in ((cols, 0), (cols, 1), (cols + 1, 3), ((cols + 7) // 8 * 8, 0), ((cols + 7) // 8 * 8, 1)):
+        g = Guarded(offset + rows * ld, dtype, "cuda", fill=-7.0)
+        out = g.t[offset:offset + rows * ld].view(rows, ld)
+        omc.mx_dequantise(cd.data_ptr(), sd.data_ptr(), rows, cols, out.data_ptr(), code, ld, stream=stream())
+        torch.cuda.synchronize()
+        assert g.intact() and bool((out[:, cols:] == -7.0).all()) and bool((g.t[:offset] == -7.0).all())
+        assert torch.equal(out[:, :cols].cpu(), torch.from_numpy(want).float().to(dtype))
+
+
 def stored_matrix(x, fill=0):
     codes, scales = mx.encode(x)
     packed, s = mx.pack(codes, scales, x.shape[1], fill)
