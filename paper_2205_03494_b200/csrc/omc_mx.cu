@@ -17,16 +17,15 @@ using el::Word;
 
 constexpr int WARPS = 8;
 
-// Eight consecutive values as they are stored: four words of 16-bit types, eight of FP32.
-template <typename T> constexpr int WORDS8 = 8 / Word<T>::N;
-
-template <typename T, bool VECTOR>
-__device__ __forceinline__ void load8(const T *row, uint32_t col, uint32_t cols, uint32_t *w)
+// E consecutive values as they are stored, two to a word of 16-bit types.
+template <typename T, bool VECTOR, int E>
+__device__ __forceinline__ void load(const T *row, uint32_t col, uint32_t cols, uint32_t *w)
 {
-    if (VECTOR && col + 8 <= cols) {
+    constexpr int N = Word<T>::N, WORDS = E / N;
+    if (VECTOR && col + E <= cols) {
 #pragma unroll
-        for (int i = 0; i < WORDS8<T>; i += 4) {
-            const uint4 q = *reinterpret_cast<const uint4 *>(row + col + i * Word<T>::N);
+        for (int i = 0; i < WORDS; i += 4) {
+            const uint4 q = *reinterpret_cast<const uint4 *>(row + col + i * N);
             w[i] = q.x;
             w[i + 1] = q.y;
             w[i + 2] = q.z;
@@ -34,7 +33,7 @@ __device__ __forceinline__ void load8(const T *row, uint32_t col, uint32_t cols,
         }
     } else {                       // zeros behind the row's end
 #pragma unroll
-        for (int i = 0; i < WORDS8<T>; ++i) {
+        for (int i = 0; i < WORDS; ++i) {
             if constexpr (sizeof(T) == 4) {
                 w[i] = col + i < cols ? reinterpret_cast<const uint32_t *>(row)[col + i] : 0u;
             } else {
@@ -66,84 +65,157 @@ __device__ __forceinline__ uint32_t fp32_bits(uint32_t m)
     return __float_as_uint(f[0]);
 }
 
-// Codes and scale of the block that four neighbouring lanes hold, eight values each.
-template <typename T>
-__device__ __forceinline__ uint32_t encode_block(const uint32_t *w, uint32_t &scale)
+// Codes and scale of the block that 32 / E neighbouring lanes hold, E values each.
+template <typename T, int E>
+__device__ __forceinline__ void encode_block(const uint32_t *w, uint32_t *codes, uint32_t &scale)
 {
-    uint32_t top = 0;
+    constexpr int N = Word<T>::N, WORDS = E / N;
+    uint32_t top = w[0] & (sizeof(T) == 4 ? 0x7FFFFFFFu : 0x7FFF7FFFu);
 #pragma unroll
-    for (int i = 0; i < WORDS8<T>; ++i) top = max_magnitude<T>(top, w[i]);
+    for (int i = 1; i < WORDS; ++i) top = max_magnitude<T>(top, w[i]);
     if constexpr (sizeof(T) == 2) top = max(top >> 16, top & 0xFFFFu);
-    top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, 1));
-    top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, 2));
+#pragma unroll
+    for (int d = 1; d < 32 / E; d *= 2) top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, d));
     scale = mx::scale_of(fp32_bits<T>(top));
     const float2 f = el::twice(mx::inverse_scale(scale));
-    float v[8];
 #pragma unroll
-    for (int i = 0; i < WORDS8<T>; ++i) Word<T>::unpack(w[i], v + Word<T>::N * i);
+    for (int c = 0; c < E / 8; ++c) {
+        float v[8];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) reinterpret_cast<float2 *>(v)[i] = el::mul2(reinterpret_cast<float2 *>(v)[i], f);
-    const uint32_t codes = mx::encode8(v);
-    return scale == mx::NAN_SCALE ? 0u : codes;
+        for (int i = 0; i < 8 / N; ++i) Word<T>::unpack(w[c * (8 / N) + i], v + N * i);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) reinterpret_cast<float2 *>(v)[i] = el::mul2(reinterpret_cast<float2 *>(v)[i], f);
+        codes[c] = scale == mx::NAN_SCALE ? 0u : mx::encode8(v);
+    }
 }
-// The scales of the four blocks that sixteen lanes hold, one byte each.
+// The scales of the four blocks that 128 / E lanes hold, one byte each.
+template <int E>
 __device__ __forceinline__ uint32_t gather_scales(uint32_t scale, int lane)
 {
-    uint32_t w = scale << (8 * ((lane >> 2) & 3));
-    w |= __shfl_xor_sync(0xFFFFFFFFu, w, 4);
-    w |= __shfl_xor_sync(0xFFFFFFFFu, w, 8);
+    constexpr int LANES = 32 / E;                        // of one block
+    uint32_t w = scale << (8 * ((lane / LANES) & 3));
+    w |= __shfl_xor_sync(0xFFFFFFFFu, w, LANES);
+    w |= __shfl_xor_sync(0xFFFFFFFFu, w, 2 * LANES);
     return w;
 }
 
-// The pieces of a matrix (256 columns of a row) that a warp takes: every `stride`-th, counted along the rows, without a
-// division per piece.
-struct Walk {
-    uint32_t row, k, step_rows, step_k, ksteps;
+// A CTA of the row kernels takes a strip of columns, 32 bytes of values a lane (blockIdx.x), of eight rows at a time, a row a
+// warp, and walks down the matrix: from row to row a warp's addresses move by constants.  It asks for the next AHEAD
+// rows' pieces while it works on one.
+constexpr int AHEAD = 3;
+template <typename T> constexpr int LANE_VALUES = 32 / (int)sizeof(T);         // 8 or 16
+template <typename T> constexpr uint32_t STRIP = 32 * LANE_VALUES<T>;          // columns: 256 or 512
+// CTAs on an SM, as the registers of the pieces on their way allow.
+constexpr int ROWS_CTAS = 4;
 
-    __device__ __forceinline__ Walk(uint32_t first, uint32_t stride, uint32_t ksteps_)
-        : row(first / ksteps_), k(first % ksteps_), step_rows(stride / ksteps_), step_k(stride % ksteps_), ksteps(ksteps_) {}
-    __device__ __forceinline__ void next()
+// Row r's place in the scales of a K step (256 columns): bytes from the place of row 0.
+__device__ __forceinline__ uint64_t row_offset(uint32_t r, uint32_t ksteps)
+{
+    return (uint64_t)(r >> 7) * ksteps * 1024 + ((r & 31) * 16 + ((r >> 5) & 3) * 4);
+}
+
+// Rows off the 16-byte boundaries: a strip's words come in from boundary to boundary, neighbouring lanes neighbouring words,
+// and are turned in shared memory.  Value e of the strip has place odd + e, odd = 1 where a 16-bit strip begins
+// in the upper half of a word; word j of a lane holds the places of word 32 j + lane.  The halves of a word that is
+// only partly inside are fetched alone (lane 0 the first, lane 1 the last): nothing outside the row is read.
+template <typename T>
+struct Turned {
+    static constexpr int E = LANE_VALUES<T>, PLACES = 4 / (int)sizeof(T);      // places of a word
+    uint32_t w[8], edge;
+
+    static __device__ __forceinline__ uint32_t odd(const T *row) { return PLACES == 2 ? (uint32_t)(reinterpret_cast<uintptr_t>(row) >> 1) & 1u : 0u; }
+    __device__ __forceinline__ void load(const T *row, uint32_t n, int lane)
     {
-        row += step_rows;
-        k += step_k;
-        if (k >= ksteps) {
-            k -= ksteps;
-            ++row;
+        const uint32_t o = odd(row);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const uint32_t p = (32 * j + lane) * PLACES;
+            w[j] = p >= o && p + PLACES <= o + n ? *reinterpret_cast<const uint32_t *>(row + p - o) : 0u;
+        }
+        if constexpr (PLACES == 2) {
+            edge = 0u;
+            if (lane == 0 && o) edge = *reinterpret_cast<const uint16_t *>(row);
+            if (lane == 1 && ((o + n) & 1) && (n > 1 || !o)) edge = *reinterpret_cast<const uint16_t *>(row + n - 1);
+        }
+    }
+    // This lane's E values; room: 260 words of this warp.
+    __device__ __forceinline__ void turn(uint32_t *room, uint32_t o, uint32_t n, int lane, uint32_t *v) const
+    {
+        __syncwarp();
+#pragma unroll
+        for (int j = 0; j < 8; ++j) room[32 * j + lane] = w[j];
+        if constexpr (PLACES == 2) {
+            if (lane == 2) room[256] = 0u;
+            __syncwarp();
+            uint16_t *half = reinterpret_cast<uint16_t *>(room);
+            if (lane == 0 && o) half[1] = (uint16_t)edge;
+            if (lane == 1 && ((o + n) & 1) && (n > 1 || !o)) half[o + n - 1] = (uint16_t)edge;
+        }
+        __syncwarp();
+        const uint4 a = *reinterpret_cast<const uint4 *>(room + lane * 8), b = *reinterpret_cast<const uint4 *>(room + lane * 8 + 4);
+        v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w, v[4] = b.x, v[5] = b.y, v[6] = b.z, v[7] = b.w;
+        if (o) {
+            const uint32_t last = room[lane * 8 + 8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] = __byte_perm(v[j], j < 7 ? v[j < 7 ? j + 1 : 7] : last, 0x5432);
         }
     }
 };
 
-// Along the rows only: a warp walks over pieces and asks for the next AHEAD while it works on one.
-constexpr int AHEAD = 4;
-
+// Along the rows only.
 template <typename T, bool VECTOR>
-__global__ void __launch_bounds__(32 * WARPS)
+__global__ void __launch_bounds__(32 * WARPS, ROWS_CTAS)
 quantise_rows_kernel(const T *__restrict__ x, uint32_t rows, uint32_t cols, uint64_t ld, uint8_t *__restrict__ codes,
                      uint8_t *__restrict__ scales)
 {
+    constexpr int E = LANE_VALUES<T>;
+    __shared__ __align__(16) uint32_t room[VECTOR ? 1 : WARPS][VECTOR ? 4 : 260];
     const uint32_t ksteps = (cols + 255) / 256;
-    const int lane = threadIdx.x & 31;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const uint64_t rb = mx::row_bytes(cols);
-    Walk at(blockIdx.x * WARPS + (threadIdx.x >> 5), gridDim.x * WARPS, ksteps), ask = at;
+    const uint32_t step = gridDim.y * WARPS, col = blockIdx.x * STRIP<T> + lane * E;
+    uint32_t row = blockIdx.y * WARPS + warp, coming = row;
+    const T *src = x + coming * ld + blockIdx.x * STRIP<T>, *now = src;        // the strip's first column
+    const uint32_t n = min(STRIP<T>, cols - blockIdx.x * STRIP<T>);
+    uint8_t *dst = codes + row * rb + col / 2;
+    const uint64_t src_step = step * ld, dst_step = step * rb;
+    // the lane that stores the scales of four blocks (128 columns), and where
+    const uint32_t block = col / 32;
+    const bool inside = col / 2 < rb, stores = lane % (128 / E) == 0 && block / 8 < ksteps;
+    uint8_t *const strip = scales + (uint64_t)(block / 8) * 1024 + (block / 4 & 1) * 512;
     el::enter_stream_order();
-    uint32_t w[AHEAD][WORDS8<T>];
+    uint32_t w[AHEAD][8];
+    Turned<T> t[VECTOR ? 1 : AHEAD];
+    auto fetch = [&](int i) {
+        if (coming < rows) {
+            if constexpr (VECTOR) load<T, true, E>(src, lane * E, n, w[i]);
+            else t[i].load(src, n, lane);
+        }
+        coming += step;
+        src += src_step;
+    };
 #pragma unroll
-    for (int i = 0; i < AHEAD; ++i, ask.next())
-        if (ask.row < rows) load8<T, VECTOR>(x + ask.row * ld, ask.k * 256 + lane * 8, cols, w[i]);
-    while (at.row < rows) {
+    for (int i = 0; i < AHEAD; ++i) fetch(i);
+    while (row < rows) {
 #pragma unroll
         for (int i = 0; i < AHEAD; ++i) {
-            if (at.row >= rows) break;
-            const uint32_t col = at.k * 256 + lane * 8;
-            uint32_t scale;
-            const uint32_t c = encode_block<T>(w[i], scale);
-            if (ask.row < rows) load8<T, VECTOR>(x + ask.row * ld, ask.k * 256 + lane * 8, cols, w[i]);
-            if (col / 2 < rb) *reinterpret_cast<uint32_t *>(codes + at.row * rb + col / 2) = c;
-            const uint32_t s = gather_scales(scale, lane);
-            if ((lane & 15) == 0)
-                *reinterpret_cast<uint32_t *>(scales + mx::scale_offset(at.row, (uint64_t)at.k * 8 + (lane >> 2), ksteps)) = s;
-            at.next();
-            ask.next();
+            if (row >= rows) break;
+            uint32_t scale, c[E / 8];
+            if constexpr (!VECTOR) {
+                t[i].turn(room[warp], Turned<T>::odd(now), n, lane, w[0]);
+                now += src_step;
+            }
+            encode_block<T, E>(w[VECTOR ? i : 0], c, scale);
+            fetch(i);
+            if constexpr (E == 16) {
+                if (inside) *reinterpret_cast<uint2 *>(dst) = make_uint2(c[0], c[1]);
+            } else {
+                if (inside) *reinterpret_cast<uint32_t *>(dst) = c[0];
+            }
+            const uint32_t s = gather_scales<E>(scale, lane);
+            if (stores) *reinterpret_cast<uint32_t *>(strip + row_offset(row, ksteps)) = s;
+            row += step;
+            dst += dst_step;
         }
     }
 }
@@ -169,18 +241,18 @@ quantise_tile_kernel(const T *__restrict__ x, uint32_t rows, uint32_t cols, uint
     el::enter_stream_order();
 
     // sixteen lanes take 128 columns of a row; four rows are asked for at a time
-    constexpr int BATCH = sizeof(T) == 4 ? 4 : 8;
+    constexpr int BATCH = sizeof(T) == 4 ? 4 : 8, WORDS8 = 8 / Word<T>::N;
 #pragma unroll
     for (int i0 = 0; i0 < 8; i0 += BATCH) {
-        uint32_t w[BATCH][WORDS8<T>];
+        uint32_t w[BATCH][WORDS8];
 #pragma unroll
         for (int i = 0; i < BATCH; ++i) {
             const uint32_t r = r0 + (i0 + i) * 16 + (tid >> 4);
             if (r < rows) {
-                load8<T, VECTOR>(x + (uint64_t)r * ld, c0 + (tid & 15) * 8, cols, w[i]);
+                load<T, VECTOR, 8>(x + (uint64_t)r * ld, c0 + (tid & 15) * 8, cols, w[i]);
             } else {
 #pragma unroll
-                for (int j = 0; j < WORDS8<T>; ++j) w[i][j] = 0u;
+                for (int j = 0; j < WORDS8; ++j) w[i][j] = 0u;
             }
         }
 #pragma unroll
@@ -188,12 +260,12 @@ quantise_tile_kernel(const T *__restrict__ x, uint32_t rows, uint32_t cols, uint
             const uint32_t r = (i0 + i) * 16 + (tid >> 4), col = c0 + (tid & 15) * 8;
             uint4 *dst = reinterpret_cast<uint4 *>(tile + r * TILE + (tid & 15) * 8);
 #pragma unroll
-            for (int j = 0; j < WORDS8<T> / 4; ++j) dst[j] = make_uint4(w[i][4 * j], w[i][4 * j + 1], w[i][4 * j + 2], w[i][4 * j + 3]);
+            for (int j = 0; j < WORDS8 / 4; ++j) dst[j] = make_uint4(w[i][4 * j], w[i][4 * j + 1], w[i][4 * j + 2], w[i][4 * j + 3]);
             if constexpr (ROWS) {
-                uint32_t scale;
-                const uint32_t c = encode_block<T>(w[i], scale);
+                uint32_t scale, c;
+                encode_block<T, 8>(w[i], &c, scale);
                 if (r0 + r < rows && col / 2 < rb) *reinterpret_cast<uint32_t *>(codes + (r0 + r) * rb + col / 2) = c;
-                const uint32_t s = gather_scales(scale, lane);
+                const uint32_t s = gather_scales<8>(scale, lane);
                 if ((lane & 15) == 0) *reinterpret_cast<uint32_t *>(atom + (r & 31) * 16 + (r >> 5) * 4) = s;
             }
         }
@@ -263,90 +335,76 @@ quantise_tile_kernel(const T *__restrict__ x, uint32_t rows, uint32_t cols, uint
     }
 }
 
-// A warp walks over pieces.  Rows off the 16-byte boundaries are turned in shared memory, so that neighbouring lanes store
-// neighbouring values (16-bit types in pairs that lie on 4-byte boundaries).
+// A warp takes 256 columns of a row.  Rows off the 16-byte boundaries are turned in shared memory, so that neighbouring
+// lanes store neighbouring values (16-bit types in pairs that lie on 4-byte boundaries).
 template <typename T, bool VECTOR>
 __global__ void __launch_bounds__(32 * WARPS)
 dequantise_kernel(const uint8_t *__restrict__ codes, const uint8_t *__restrict__ scales, uint32_t rows, uint32_t cols,
                   T *__restrict__ out, uint64_t ld)
 {
+    constexpr int N = Word<T>::N;
     __shared__ __align__(16) T turned[VECTOR ? 1 : WARPS][VECTOR ? 8 : 256 + 8];
     const uint32_t ksteps = (cols + 255) / 256;
     const int lane = threadIdx.x & 31;
     const uint64_t rb = mx::row_bytes(cols);
-    Walk at(blockIdx.x * WARPS + (threadIdx.x >> 5), gridDim.x * WARPS, ksteps), ask = at;
+    const uint32_t col = blockIdx.x * 256 + lane * 8;
     el::enter_stream_order();
-    uint32_t c[AHEAD], b[AHEAD];
-    auto fetch = [&](int i) {
-        const uint32_t col = ask.k * 256 + lane * 8;
-        if (ask.row < rows && col < cols) {
-            c[i] = *reinterpret_cast<const uint32_t *>(codes + ask.row * rb + col / 2);
-            b[i] = scales[mx::scale_offset(ask.row, (uint64_t)ask.k * 8 + (lane >> 2), ksteps)];
-        }
-        ask.next();
-    };
-#pragma unroll
-    for (int i = 0; i < AHEAD; ++i) fetch(i);
-    while (at.row < rows) {
-#pragma unroll
-        for (int i = 0; i < AHEAD; ++i) {
-            if (at.row >= rows) break;
-            const uint32_t col = at.k * 256 + lane * 8;
-            float v[8];
-            mx::decode8(c[i], v);
-            const float2 s = el::twice(mx::scale_value(b[i] & 255u));
-            fetch(i);
-            uint32_t w[WORDS8<T>];
+    for (uint32_t row = blockIdx.y * WARPS + (threadIdx.x >> 5); row < rows; row += gridDim.y * WARPS) {
+        float v[8];
+        if (col < cols) {
+            mx::decode8(*reinterpret_cast<const uint32_t *>(codes + row * rb + col / 2), v);
+            const float2 s = el::twice(mx::scale_value(scales[mx::scale_offset(row, blockIdx.x * 8 + (lane >> 2), ksteps)]));
 #pragma unroll
             for (int j = 0; j < 4; ++j) reinterpret_cast<float2 *>(v)[j] = el::mul2(reinterpret_cast<float2 *>(v)[j], s);
+        }
+        T *to = out + row * ld + blockIdx.x * 256;
+        if (VECTOR) {
+            if (col + 8 <= cols) {
 #pragma unroll
-            for (int j = 0; j < WORDS8<T>; ++j) w[j] = Word<T>::pack(v + Word<T>::N * j);
-            if (VECTOR) {
-                T *dst = out + at.row * ld + col;
-                if (col + 8 <= cols) {
-#pragma unroll
-                    for (int j = 0; j < WORDS8<T>; j += 4) *reinterpret_cast<uint4 *>(dst + j * Word<T>::N) = make_uint4(w[j], w[j + 1], w[j + 2], w[j + 3]);
-                } else {
-#pragma unroll
-                    for (int j = 0; j < 8; ++j)
-                        if (col + j < cols) dst[j] = el::from_float<T>(v[j]);
-                }
+                for (int j = 0; j < 8; j += 4 * N)
+                    *reinterpret_cast<uint4 *>(to + lane * 8 + j) = make_uint4(Word<T>::pack(v + j), Word<T>::pack(v + j + N),
+                                                                               Word<T>::pack(v + j + 2 * N), Word<T>::pack(v + j + 3 * N));
             } else {
-                T *mine = turned[threadIdx.x >> 5];
-                T *dst = out + at.row * ld + at.k * 256;
-                const uint32_t n = min(256u, cols - at.k * 256);
-                const uint32_t odd = sizeof(T) == 2 ? (uint32_t)(reinterpret_cast<uintptr_t>(dst) >> 1) & 1u : 0u;      // values before the first boundary
-                __syncwarp();
 #pragma unroll
-                for (int j = 0; j < 8; ++j) mine[odd + lane * 8 + j] = el::from_float<T>(v[j]);      // value e at odd + e
-                __syncwarp();
-                if constexpr (sizeof(T) == 2) {
-                    // pair p: places 2 p and 2 p + 1, values 2 p - odd and 2 p + 1 - odd
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        const uint32_t e = 2 * (j * 32 + lane);
-                        if (e >= odd && e + 1 < odd + n)
-                            *reinterpret_cast<uint32_t *>(dst + e - odd) = *reinterpret_cast<const uint32_t *>(mine + e);
-                    }
-                    // what has no partner: the first value before a boundary, the last one behind
-                    if (lane == 0 && odd) dst[0] = mine[1];
-                    if (lane == 1 && ((odd + n) & 1) && (n > 1 || !odd)) dst[n - 1] = mine[odd + n - 1];
-                } else {
-#pragma unroll
-                    for (int j = 0; j < 8; ++j)
-                        if (j * 32 + lane < n) dst[j * 32 + lane] = mine[j * 32 + lane];
-                }
+                for (int j = 0; j < 8; ++j)
+                    if (col + j < cols) to[lane * 8 + j] = el::from_float<T>(v[j]);
             }
-            at.next();
+        } else {
+            T *mine = turned[threadIdx.x >> 5];
+            const uint32_t n = min(256u, cols - blockIdx.x * 256);
+            const uint32_t odd = sizeof(T) == 2 ? (uint32_t)(reinterpret_cast<uintptr_t>(to) >> 1) & 1u : 0u;      // values before the first boundary
+            __syncwarp();
+#pragma unroll
+            for (int j = 0; j < 8; ++j) mine[odd + lane * 8 + j] = el::from_float<T>(v[j]);      // value e at odd + e
+            __syncwarp();
+            if constexpr (sizeof(T) == 2) {
+                // pair p: places 2 p and 2 p + 1, values 2 p - odd and 2 p + 1 - odd
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const uint32_t e = 2 * (j * 32 + lane);
+                    if (e >= odd && e + 1 < odd + n)
+                        *reinterpret_cast<uint32_t *>(to + e - odd) = *reinterpret_cast<const uint32_t *>(mine + e);
+                }
+                // what has no partner: the first value before a boundary, the last one behind
+                if (lane == 0 && odd) to[0] = mine[1];
+                if (lane == 1 && ((odd + n) & 1) && (n > 1 || !odd)) to[n - 1] = mine[odd + n - 1];
+            } else {
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+                    if (j * 32 + lane < n) to[j * 32 + lane] = mine[j * 32 + lane];
+            }
         }
     }
 }
 
-// CTAs for a walk over so many pieces: what is resident (eight CTAs on an SM), or one piece a warp.
-uint32_t walk_ctas(uint64_t pieces)
+// As many CTAs to a strip of columns as are resident at once, or, with so many strips that this would come out
+// uneven, about four times as many as are resident.
+dim3 strips(uint32_t rows, uint32_t cols, uint32_t strip, int per_sm)
 {
-    const uint64_t most = 8ull * DEFAULT_SMS, wanted = (pieces + WARPS - 1) / WARPS;
-    return (uint32_t)(wanted < most ? wanted : most);
+    const uint32_t resident = per_sm * el::sm_count(), across = (cols + strip - 1) / strip, groups = (rows + WARPS - 1) / WARPS;
+    uint32_t down = resident / across;
+    if (down < 4) down = (4 * resident + across - 1) / across;
+    return dim3(across, groups < down ? groups : down);
 }
 
 template <typename T, bool VECTOR>
@@ -355,7 +413,7 @@ int quantise(const void *x, uint32_t rows, uint32_t cols, uint64_t ld, uint8_t *
 {
     const T *src = static_cast<const T *>(x);
     if (!codes_t) {
-        return note_cuda(el::launch(quantise_rows_kernel<T, VECTOR>, dim3(walk_ctas((uint64_t)rows * ((cols + 255) / 256))), 32 * WARPS, 0, 1,
+        return note_cuda(el::launch(quantise_rows_kernel<T, VECTOR>, strips(rows, cols, STRIP<T>, ROWS_CTAS), 32 * WARPS, 0, 1,
                                     stream, src, rows, cols, ld, codes, scales));
     }
     auto kernel = codes ? quantise_tile_kernel<T, VECTOR, true> : quantise_tile_kernel<T, VECTOR, false>;
@@ -370,7 +428,8 @@ int quantise(const void *x, uint32_t rows, uint32_t cols, uint64_t ld, uint8_t *
 template <typename T, bool VECTOR>
 int dequantise(const uint8_t *codes, const uint8_t *scales, uint32_t rows, uint32_t cols, void *out, uint64_t ld, void *stream)
 {
-    return note_cuda(el::launch(dequantise_kernel<T, VECTOR>, dim3(walk_ctas((uint64_t)rows * ((cols + 255) / 256))), 32 * WARPS, 0, 1, stream,
+    const uint32_t groups = (rows + WARPS - 1) / WARPS;
+    return note_cuda(el::launch(dequantise_kernel<T, VECTOR>, dim3((cols + 255) / 256, groups < 65535 ? groups : 65535), 32 * WARPS, 0, 1, stream,
                                 codes, scales, rows, cols, static_cast<T *>(out), ld));
 }
 
