@@ -240,33 +240,38 @@ quantise_tile_kernel(const T *__restrict__ x, uint32_t rows, uint32_t cols, uint
     const uint64_t rb = mx::row_bytes(cols), rb_t = mx::row_bytes(rows);
     el::enter_stream_order();
 
-    // sixteen lanes take 128 columns of a row; four rows are asked for at a time
-    constexpr int BATCH = sizeof(T) == 4 ? 4 : 8, WORDS8 = 8 / Word<T>::N;
+    // 8 or 16 lanes take 128 columns of a row, 32 bytes a lane; four rows are asked for at a time
+    constexpr int E = LANE_VALUES<T>, LANES = TILE / E, STEP = 256 / LANES, BATCH = 4;
+    const uint32_t lane_col = (tid % LANES) * E, col = c0 + lane_col;
 #pragma unroll
-    for (int i0 = 0; i0 < 8; i0 += BATCH) {
-        uint32_t w[BATCH][WORDS8];
+    for (int i0 = 0; i0 < TILE / STEP; i0 += BATCH) {
+        uint32_t w[BATCH][8];
 #pragma unroll
         for (int i = 0; i < BATCH; ++i) {
-            const uint32_t r = r0 + (i0 + i) * 16 + (tid >> 4);
+            const uint32_t r = r0 + (i0 + i) * STEP + tid / LANES;
             if (r < rows) {
-                load<T, VECTOR, 8>(x + (uint64_t)r * ld, c0 + (tid & 15) * 8, cols, w[i]);
+                load<T, VECTOR, E>(x + (uint64_t)r * ld, col, cols, w[i]);
             } else {
 #pragma unroll
-                for (int j = 0; j < WORDS8; ++j) w[i][j] = 0u;
+                for (int j = 0; j < 8; ++j) w[i][j] = 0u;
             }
         }
 #pragma unroll
         for (int i = 0; i < BATCH; ++i) {
-            const uint32_t r = (i0 + i) * 16 + (tid >> 4), col = c0 + (tid & 15) * 8;
-            uint4 *dst = reinterpret_cast<uint4 *>(tile + r * TILE + (tid & 15) * 8);
-#pragma unroll
-            for (int j = 0; j < WORDS8 / 4; ++j) dst[j] = make_uint4(w[i][4 * j], w[i][4 * j + 1], w[i][4 * j + 2], w[i][4 * j + 3]);
+            const uint32_t r = (i0 + i) * STEP + tid / LANES;
+            uint4 *dst = reinterpret_cast<uint4 *>(tile + r * TILE + lane_col);
+            dst[0] = make_uint4(w[i][0], w[i][1], w[i][2], w[i][3]);
+            dst[1] = make_uint4(w[i][4], w[i][5], w[i][6], w[i][7]);
             if constexpr (ROWS) {
-                uint32_t scale, c;
-                encode_block<T, 8>(w[i], &c, scale);
-                if (r0 + r < rows && col / 2 < rb) *reinterpret_cast<uint32_t *>(codes + (r0 + r) * rb + col / 2) = c;
-                const uint32_t s = gather_scales<8>(scale, lane);
-                if ((lane & 15) == 0) *reinterpret_cast<uint32_t *>(atom + (r & 31) * 16 + (r >> 5) * 4) = s;
+                uint32_t scale, c[E / 8];
+                encode_block<T, E>(w[i], c, scale);
+                if (r0 + r < rows && col / 2 < rb) {
+                    uint8_t *to = codes + (r0 + r) * rb + col / 2;
+                    if constexpr (E == 16) *reinterpret_cast<uint2 *>(to) = make_uint2(c[0], c[1]);
+                    else *reinterpret_cast<uint32_t *>(to) = c[0];
+                }
+                const uint32_t s = gather_scales<E>(scale, lane);
+                if (tid % LANES == 0) *reinterpret_cast<uint32_t *>(atom + (r & 31) * 16 + (r >> 5) * 4) = s;
             }
         }
     }
@@ -359,7 +364,11 @@ dequantise_kernel(const uint8_t *__restrict__ codes, const uint8_t *__restrict__
         }
         T *to = out + row * ld + blockIdx.x * 256;
         if (VECTOR) {
-            if (col + 8 <= cols) {
+            if (N == 1 && col + 8 <= cols && (reinterpret_cast<uintptr_t>(to) & 31u) == 0) {
+                // whole 32-byte sectors: two 16-byte stores would write every sector in two halves
+                asm volatile("st.global.v8.f32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
+                             ::"l"(to + lane * 8), "f"(v[0]), "f"(v[1]), "f"(v[2]), "f"(v[3]), "f"(v[4]), "f"(v[5]), "f"(v[6]), "f"(v[7]) : "memory");
+            } else if (col + 8 <= cols) {
 #pragma unroll
                 for (int j = 0; j < 8; j += 4 * N)
                     *reinterpret_cast<uint4 *>(to + lane * 8 + j) = make_uint4(Word<T>::pack(v + j), Word<T>::pack(v + j + N),
