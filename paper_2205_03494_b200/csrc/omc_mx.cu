@@ -22,7 +22,11 @@ template <typename T, bool VECTOR, int E>
 __device__ __forceinline__ void load(const T *row, uint32_t col, uint32_t cols, uint32_t *w)
 {
     constexpr int N = Word<T>::N, WORDS = E / N;
-    if (VECTOR && col + E <= cols) {
+    if (VECTOR && col + E <= cols && WORDS == 8 && (reinterpret_cast<uintptr_t>(row + col) & 31u) == 0) {
+        asm volatile("ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                     : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]), "=r"(w[4]), "=r"(w[5]), "=r"(w[6]), "=r"(w[7])
+                     : "l"(row + col) : "memory");
+    } else if (VECTOR && col + E <= cols) {
 #pragma unroll
         for (int i = 0; i < WORDS; i += 4) {
             const uint4 q = *reinterpret_cast<const uint4 *>(row + col + i * N);
@@ -221,8 +225,24 @@ quantise_rows_kernel(const T *__restrict__ x, uint32_t rows, uint32_t cols, uint
 }
 
 // Along the columns, and along the rows too if ROWS: a CTA takes a tile of 128 x 128.
-constexpr int TILE = 128, COLUMN_PITCH = 80;      // bytes between the staged code columns (64 and a skew against bank conflicts)
-template <typename T> constexpr int tile_smem() { return TILE * TILE * (int)sizeof(T) + TILE * COLUMN_PITCH + 2 * 512; }
+constexpr int TILE = 128;
+template <typename T> constexpr int tile_smem() { return TILE * TILE * (int)sizeof(T) + TILE * 64 + 2 * 512; }
+
+// Orders in shared memory without bank conflicts.  The tile: a lane brings 32 bytes of a row, whose first halves are
+// stored side by side, then the second halves; place p of a row holds column tile_column(p).
+template <typename T>
+__device__ __forceinline__ uint32_t tile_column(uint32_t place)
+{
+    constexpr uint32_t H = LANE_VALUES<T> / 2;           // values of a half
+    return (place % 64) / H * (2 * H) + place / 64 * H + place % H;
+}
+// The codes of the columns, 64 bytes each in four chunks of 16: the chunk's place.
+template <typename T>
+__device__ __forceinline__ uint32_t code_place(uint32_t col, uint32_t chunk)
+{
+    const uint32_t turn = sizeof(T) == 2 ? (col >> 2 & 1) | (col >> 3 & 2) : col >> 3 & 3;
+    return (col ^ (col >> 1 & 1)) * 64 + (chunk ^ turn) * 16;
+}
 
 template <typename T, bool VECTOR, bool ROWS>
 __global__ void __launch_bounds__(256)
@@ -232,7 +252,7 @@ quantise_tile_kernel(const T *__restrict__ x, uint32_t rows, uint32_t cols, uint
     extern __shared__ __align__(16) uint8_t smem[];
     T *tile = reinterpret_cast<T *>(smem);
     uint8_t *out = smem + TILE * TILE * sizeof(T);
-    uint8_t *atom = out + TILE * COLUMN_PITCH, *atom_t = atom + 512;
+    uint8_t *atom = out + TILE * 64, *atom_t = atom + 512;
     const int tid = threadIdx.x, lane = tid & 31;
     const uint32_t col_tiles = (cols + TILE - 1) / TILE, row_tiles = (rows + TILE - 1) / TILE;
     const uint32_t tr = blockIdx.x / col_tiles, tc = blockIdx.x - tr * col_tiles;
@@ -259,9 +279,9 @@ quantise_tile_kernel(const T *__restrict__ x, uint32_t rows, uint32_t cols, uint
 #pragma unroll
         for (int i = 0; i < BATCH; ++i) {
             const uint32_t r = (i0 + i) * STEP + tid / LANES;
-            uint4 *dst = reinterpret_cast<uint4 *>(tile + r * TILE + lane_col);
-            dst[0] = make_uint4(w[i][0], w[i][1], w[i][2], w[i][3]);
-            dst[1] = make_uint4(w[i][4], w[i][5], w[i][6], w[i][7]);
+            T *dst = tile + r * TILE + lane_col / 2;
+            *reinterpret_cast<uint4 *>(dst) = make_uint4(w[i][0], w[i][1], w[i][2], w[i][3]);
+            *reinterpret_cast<uint4 *>(dst + TILE / 2) = make_uint4(w[i][4], w[i][5], w[i][6], w[i][7]);
             if constexpr (ROWS) {
                 uint32_t scale, c[E / 8];
                 encode_block<T, E>(w[i], c, scale);
@@ -313,8 +333,8 @@ quantise_tile_kernel(const T *__restrict__ x, uint32_t rows, uint32_t cols, uint
                 for (int j = 0; j < 8; ++j) u[j] = h ? v[8 * i + j].y : v[8 * i + j].x;
                 c[i] = (h ? sb : sa) == mx::NAN_SCALE ? 0u : mx::encode8(u);
             }
-            const int col = pair * 2 + h;
-            *reinterpret_cast<uint4 *>(out + col * COLUMN_PITCH + block * 16) = make_uint4(c[0], c[1], c[2], c[3]);
+            const uint32_t col = tile_column<T>(pair * 2) + h;
+            *reinterpret_cast<uint4 *>(out + code_place<T>(col, block)) = make_uint4(c[0], c[1], c[2], c[3]);
             atom_t[(col & 31) * 16 + (col >> 5) * 4 + block] = (uint8_t)(h ? sb : sa);
         }
     }
@@ -325,7 +345,7 @@ quantise_tile_kernel(const T *__restrict__ x, uint32_t rows, uint32_t cols, uint
         const uint32_t col = i * 64 + (tid >> 2), chunk = tid & 3;
         const uint64_t at = r0 / 2 + chunk * 16;
         if (c0 + col < cols && at < rb_t)
-            *reinterpret_cast<uint4 *>(codes_t + (c0 + col) * rb_t + at) = *reinterpret_cast<const uint4 *>(out + col * COLUMN_PITCH + chunk * 16);
+            *reinterpret_cast<uint4 *>(codes_t + (c0 + col) * rb_t + at) = *reinterpret_cast<const uint4 *>(out + code_place<T>(col, chunk));
     }
     // 512 bytes of scales per direction; behind the last odd one its partner's zeros
     if (tid < 128) {
