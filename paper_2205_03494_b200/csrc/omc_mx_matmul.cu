@@ -10,7 +10,8 @@
 // and 8 scales a row, per stage), warp 1 (one thread) moves each stage's scales into tensor memory
 // (tcgen05.cp) and issues the products, warps 2-5 store the result.  Two CTAs share an SM, so that one's
 // epilogue runs under the other's products.  With fewer tiles than SMs the K steps of a tile are
-// divided among the CTAs of a cluster, which add up their parts through distributed shared memory in a fixed order.
+// divided among the CTAs of a cluster: each sends its part of every splits-th row of X to that row's CTA (stores to distributed
+// shared memory, which nobody waits for), which adds the parts up in a fixed order.
 #include <cuda.h>
 #include <cuda_runtime.h>
 
@@ -100,11 +101,18 @@ __device__ __forceinline__ void tmem_load16(uint32_t taddr, uint32_t *v)
     tmem_load_wait();
     loaded16(v);
 }
-__device__ __forceinline__ float load_remote(uint32_t cluster_addr)
+__device__ __forceinline__ void store_remote(uint32_t cluster_addr, float v)
 {
-    float v;
-    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(cluster_addr) : "memory");
-    return v;
+    asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(cluster_addr), "f"(v) : "memory");
+}
+// Four neighbouring values of a row of Y, as many of them as the row has.
+template <typename T>
+__device__ __forceinline__ void put4(T *p, uint32_t left, float4 v)
+{
+    if (left > 0) p[0] = el::from_float<T>(v.x);
+    if (left > 1) p[1] = el::from_float<T>(v.y);
+    if (left > 2) p[2] = el::from_float<T>(v.z);
+    if (left > 3) p[3] = el::from_float<T>(v.w);
 }
 
 template <int NT>
@@ -201,16 +209,23 @@ mx_matmul_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constan
         ok = mbar_wait(done, 0u, WAIT_LIMIT);
         ok = __all_sync(0xFFFFFFFFu, ok);
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+    }
+    // every CTA of the cluster is through with its stages: parts may be put there
+    if (splits > 1) cluster_barrier();
+    if (warp >= 2) {
         if (ok) {
-            float *part = reinterpret_cast<float *>(base_ptr) + q * 32 + lane;      // [row of X][128]
 #pragma unroll 1
             for (int c = 0; c < NT; c += 16) {
                 if (m0 + c >= M) break;
                 uint32_t v[16];
                 tmem_load16(tmem_base + ((uint32_t)(q * 32) << 16) + c, v);
                 if (splits > 1) {
+                    // row c + j of the tile belongs to CTA (c + j) mod splits, there place (c + j) / splits of part `rank`
 #pragma unroll
-                    for (int j = 0; j < 16; ++j) part[(c + j) * BM] = __uint_as_float(v[j]);
+                    for (int j = 0; j < 16; ++j) {
+                        const uint32_t r = c + j, place = rank * (NT / splits) + r / splits;
+                        store_remote(map_to_cta(base + (place * BM + q * 32 + lane) * 4, r % splits), __uint_as_float(v[j]));
+                    }
                 } else if (n < N) {
 #pragma unroll
                     for (int j = 0; j < 16; ++j)
@@ -223,19 +238,20 @@ mx_matmul_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constan
     if (!ok) atomicExch(status, 1u);
     __syncthreads();
     if (splits > 1) {
-        // ---- the cluster's parts, added in the order of their K ranges; CTA r stores every splits-th row of X
-        cluster_barrier();
-        for (uint32_t c = rank + splits * (tid >> 5); c < NT && m0 + c < M; c += splits * (THREADS / 32)) {
-#pragma unroll
-            for (int j = 0; j < BM / 32; ++j) {
-                const uint32_t at = base + (c * BM + j * 32 + lane) * 4;
-                float sum = 0.f;
-                for (uint32_t r = 0; r < splits; ++r) sum += load_remote(map_to_cta(at, r));
-                const uint32_t nn = tile_n * BM + j * 32 + lane;
-                if (nn < N) y[(uint64_t)(m0 + c) * ldy + nn] = el::from_float<T>(sum);
+        cluster_barrier();                                 // the parts of this CTA's rows have arrived
+        const float4 *parts = reinterpret_cast<const float4 *>(base_ptr) + lane;
+        const uint32_t mine = NT / splits, nn = tile_n * BM + lane * 4;
+        for (uint32_t i = warp; i < mine && m0 + i * splits + rank < M; i += THREADS / 32) {
+            float4 sum = parts[i * 32];
+            for (uint32_t r = 1; r < splits; ++r) {         // in the order of their K ranges
+                const float4 v = parts[(r * mine + i) * 32];
+                sum.x += v.x;
+                sum.y += v.y;
+                sum.z += v.z;
+                sum.w += v.w;
             }
+            if (nn < N) put4(y + (uint64_t)(m0 + i * splits + rank) * ldy + nn, N - nn, sum);
         }
-        cluster_barrier();                                 // nobody leaves while its part is read
     }
     if (warp == 1)
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"((uint32_t)TMEM_COLS) : "memory");
@@ -475,9 +491,9 @@ int launch(const Product &p)
     const int rc = el::allow_smem<mx_matmul_kernel<NT, T>>(SMEM);
     if (rc) return rc;
     const uint32_t tiles_n = (p.N + BM - 1) / BM, tiles_m = (p.M + NT - 1) / NT, ksteps = (p.K + BK - 1) / BK;
-    // divide K while the CTAs still fit on the device at once and each keeps two steps
+    // divide K while the CTAs still fit on the device at once
     uint32_t splits = 1;
-    while (splits < 8 && (uint64_t)tiles_n * tiles_m * splits * 2 <= 2u * el::sm_count() && ksteps >= splits * 4) splits *= 2;
+    while (splits < 8 && (uint64_t)tiles_n * tiles_m * splits <= el::sm_count() && ksteps >= splits * 2) splits *= 2;
     return note_cuda(el::launch(mx_matmul_kernel<NT, T>, dim3(tiles_n * splits, tiles_m), THREADS, SMEM, splits, p.stream, map_w, map_x,
                                 p.w_scales, p.x_scales, static_cast<T *>(p.y), p.ldy, p.M, p.N, p.K, splits, p.status));
 }
