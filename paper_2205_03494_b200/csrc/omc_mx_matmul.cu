@@ -6,12 +6,23 @@
 // N side, so that a product with few rows of X wastes no tensor work on a side that is 128 at least, and the
 // accumulator's lanes run along Y's contiguous dimension: a warp's store is 32 neighbouring values.
 //
-// A CTA computes 128 x NT of Y.  Warp 0 (one thread) runs the copies over K (256 values, 128 bytes of codes
-// and 8 scales a row, per stage), warp 1 (one thread) moves each stage's scales into tensor memory
-// (tcgen05.cp) and issues the products, warps 2-5 store the result.  Two CTAs share an SM, so that one's
-// epilogue runs under the other's products.  With fewer tiles than SMs the K steps of a tile are
-// divided among the CTAs of a cluster: each sends its part of every splits-th row of X to that row's CTA (stores to distributed
-// shared memory, which nobody waits for), which adds the parts up in a fixed order.
+// One persistent CTA per SM walks over tiles of 128 x NT of Y.
+//   warp 0       (one thread) copies: per K step of 256 values 128 bytes of codes and 8 scales of each row
+//   warp 1       (one thread) products, tcgen05.mma of 128 x NT x 64
+//   warps 4-11   results: a quarter of tensor memory's lanes and half of the columns each
+//   warps 12-15  scales from shared to tensor memory, a copy in each quarter of the lanes.  (tcgen05.cp does the same in
+//                one instruction per 512 bytes, but in the tensor pipe, between the products: measured 30 us of 142 at
+//                M = 16384, N = 2048, K = 8192.)
+// Tensor memory (512 columns) holds two accumulators, so that the results of one tile are stored under the products of
+// the next, and the scales of three or four K steps; a step's columns are free again when its products are through,
+// which the barrier of its stage tells.  With NT = 256 the accumulators alone would fill it: accumulator 1 starts 80
+// columns early, inside accumulator 0; the shared columns are read first and released, then the next products start.
+// The widest tile needs the fewest bytes per product (a 128 x 128 tile was bound by the traffic from L2 to shared memory);
+// narrower ones spread a small product over more SMs.  With fewer tiles than SMs the K steps of a tile are divided
+// among the CTAs of a cluster: each owns a share of X's rows and gets the others' parts of these (stores to distributed
+// shared memory, which nobody waits for), which it adds up in a fixed order.
+// Every wait is bounded; tensor memory is released on every path.  It is taken only after the kernel before on the
+// stream has finished: nothing waits for another kernel while it holds what others need.
 #include <cuda.h>
 #include <cuda_runtime.h>
 
@@ -33,12 +44,9 @@ constexpr int BM = 128, BK = 256;                     // W rows per CTA; K per s
 constexpr int INSTR_K = 64;                           // K of one tcgen05.mma with 4-bit inputs
 constexpr int TILE_W_BYTES = BM * BK / 2;
 constexpr int SCALE_BYTES = 1024;                     // scales of 128 rows x 256 columns
-constexpr int TMEM_COLS = 256;                        // half of an SM's: two CTAs fit
-constexpr int SCALE_COLS = 8;                         // tensor-memory columns of 128 rows x 256 columns' scales
-constexpr int THREADS = 192;
-// Every instantiation asks for this much, so that never more than two CTAs (2 x 256 columns of tensor
-// memory) share an SM: a third would wait for tensor memory while its cluster's other CTAs hold some.
-constexpr int SMEM = 112 * 1024;
+constexpr int SCALE_COLS = 8;                         // ... in tensor-memory columns
+constexpr int THREADS = 512, EPILOGUE_THREADS = 256, SCALE_THREADS = 128;
+constexpr int TMEM_COLS = 512;
 
 // Instruction descriptor: A and B are E2M1 (type 1 at bits 7 and 10), both K-major, N/8 at bit 17, E8M0 scales (bit 23),
 // M/128 at bit 27; which bytes of a scale column apply (0: the first two, 2: the last two) at bits 4 (B) and 29 (A).
@@ -115,171 +123,39 @@ __device__ __forceinline__ void put4(T *p, uint32_t left, float4 v)
     if (left > 3) p[3] = el::from_float<T>(v.w);
 }
 
-template <int NT>
-struct Cfg {
-    static constexpr int TILE_X_BYTES = NT * BK / 2;
-    static constexpr int STAGE = TILE_W_BYTES + TILE_X_BYTES + 2 * SCALE_BYTES;
-    static constexpr int FIT = (SMEM - 1024 - 256) / STAGE;
-    static constexpr int NSTAGES = FIT < 6 ? FIT : 6;
-    static constexpr int D_COLS = NT < 32 ? 32 : NT;      // accumulator columns; the scales' follow
-    static_assert(STAGE % 1024 == 0 && D_COLS + NSTAGES * 2 * SCALE_COLS <= TMEM_COLS, "");
-    static_assert(BM * NT * 4 <= NSTAGES * STAGE, "a partial result fits where the stages were");
-};
-
-// blockIdx.x: tile of W's rows x cluster size + rank in the cluster; blockIdx.y: tile of X's rows.
-template <int NT, typename T>
-__global__ void __launch_bounds__(THREADS)
-mx_matmul_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_x,
-                 const uint8_t *__restrict__ w_scales, const uint8_t *__restrict__ x_scales, T *__restrict__ y, uint64_t ldy,
-                 uint32_t M, uint32_t N, uint32_t K, uint32_t splits, uint32_t *status)
+// The sums of the parts of `mine` rows of Y from row m on, in the order of the parts' K ranges; part r, row i at [r][i][128].
+template <typename T>
+__device__ __forceinline__ void add_parts(const float4 *parts, uint32_t warp, uint32_t warps, uint32_t splits, uint32_t mine, uint32_t m, uint32_t M,
+                                          uint32_t n, uint32_t N, T *y, uint64_t ldy)
 {
-    using C = Cfg<NT>;
-    constexpr int NS = C::NSTAGES;
-    extern __shared__ uint8_t smem_raw[];
-    const uint32_t base = (saddr(smem_raw) + 1023u) & ~1023u;
-    uint8_t *const base_ptr = smem_raw + (base - saddr(smem_raw));
-    const uint32_t bars = base + NS * C::STAGE;           // full[NS], empty[NS], done, tmem slot
-    auto full = [&](int s) { return bars + 8u * s; };
-    auto empty = [&](int s) { return bars + 8u * (NS + s); };
-    const uint32_t done = bars + 8u * (2 * NS), tmem_slot = done + 8u;
-    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-    const uint32_t rank = splits > 1 ? cluster_cta_rank() : 0u;
-    const uint32_t tile_n = blockIdx.x / splits, tile_m = blockIdx.y;
-    const uint32_t ksteps = (K + BK - 1) / BK;
-    const uint32_t k_begin = (uint32_t)((uint64_t)ksteps * rank / splits), k_end = (uint32_t)((uint64_t)ksteps * (rank + 1) / splits);
-
-    if (tid == 0) {
-        for (int s = 0; s < NS; ++s) { mbar_init(full(s), 1); mbar_init(empty(s), 1); }
-        mbar_init(done, 1);
-        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-    }
-    if (warp == 1) {
-        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(tmem_slot), "r"((uint32_t)TMEM_COLS) : "memory");
-        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
-    }
-    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-    __syncthreads();
-    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-    uint32_t tmem_base;
-    asm volatile("ld.shared.u32 %0, [%1];" : "=r"(tmem_base) : "r"(tmem_slot));
-    el::enter_stream_order();
-
-    bool ok = true;
-    if (tid == 0) {
-        // ---- producer
-        const uint8_t *ws = w_scales + (uint64_t)tile_n * ksteps * SCALE_BYTES;
-        const uint8_t *xs = x_scales + (uint64_t)(tile_m * NT / 128) * ksteps * SCALE_BYTES;
-        for (uint32_t k = k_begin, it = 0; k < k_end; ++k, ++it) {
-            const int s = it % NS;
-            if (it >= (uint32_t)NS) ok = mbar_wait(empty(s), ((it / NS) - 1) & 1u, WAIT_LIMIT);
-            if (!ok) break;
-            const uint32_t a = base + s * C::STAGE;
-            mbar_expect_tx(full(s), C::STAGE);
-            tma_load_2d(a, &map_w, (int)(k * (BK / 2)), (int)(tile_n * BM), full(s));
-            tma_load_2d(a + TILE_W_BYTES, &map_x, (int)(k * (BK / 2)), (int)(tile_m * NT), full(s));
-            bulk_load(a + TILE_W_BYTES + C::TILE_X_BYTES, ws + (uint64_t)k * SCALE_BYTES, SCALE_BYTES, full(s));
-            bulk_load(a + TILE_W_BYTES + C::TILE_X_BYTES + SCALE_BYTES, xs + (uint64_t)k * SCALE_BYTES, SCALE_BYTES, full(s));
+    for (uint32_t i = warp; i < mine && m + i < M; i += warps) {
+        float4 sum = parts[i * 32];
+        for (uint32_t r = 1; r < splits; ++r) {
+            const float4 v = parts[(r * mine + i) * 32];
+            sum.x += v.x;
+            sum.y += v.y;
+            sum.z += v.z;
+            sum.w += v.w;
         }
-    } else if (tid == 32) {
-        // ---- products; a stage's scales have columns of their own, free again when the stage is
-        for (uint32_t k = k_begin, it = 0; k < k_end; ++k, ++it) {
-            const int s = it % NS;
-            ok = mbar_wait(full(s), (it / NS) & 1u, WAIT_LIMIT);
-            if (!ok) break;
-            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-            const uint32_t a = base + s * C::STAGE, b = a + TILE_W_BYTES, sc = b + C::TILE_X_BYTES;
-            const uint32_t ta = tmem_base + C::D_COLS + s * 2 * SCALE_COLS, tb = ta + SCALE_COLS;
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                copy_scales(ta + 4 * h, sc + 512 * h);
-                copy_scales(tb + 4 * h, sc + SCALE_BYTES + 512 * h);
-            }
-#pragma unroll
-            for (int i = 0; i < BK / INSTR_K; ++i)
-                mma_mx(tmem_base, umma_desc(a + i * INSTR_K / 2), umma_desc(b + i * INSTR_K / 2), instr_desc(BM, NT, i & 1),
-                       ta + 4 * (i >> 1), tb + 4 * (i >> 1), (it | (uint32_t)i) != 0);
-            umma_commit(empty(s));
-        }
-        if (ok) umma_commit(done);
+        if (n < N) put4(y + (uint64_t)(m + i) * ldy + n, N - n, sum);
     }
-    __syncwarp();
-    const int q = warp & 3;                               // quarter of the lanes a warp may read
-    const uint32_t n = tile_n * BM + q * 32 + lane, m0 = tile_m * NT;
-    if (warp >= 2) {
-        ok = mbar_wait(done, 0u, WAIT_LIMIT);
-        ok = __all_sync(0xFFFFFFFFu, ok);
-        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-    }
-    // every CTA of the cluster is through with its stages: parts may be put there
-    if (splits > 1) cluster_barrier();
-    if (warp >= 2) {
-        if (ok) {
-#pragma unroll 1
-            for (int c = 0; c < NT; c += 16) {
-                if (m0 + c >= M) break;
-                uint32_t v[16];
-                tmem_load16(tmem_base + ((uint32_t)(q * 32) << 16) + c, v);
-                if (splits > 1) {
-                    // row c + j of the tile belongs to CTA (c + j) mod splits, there place (c + j) / splits of part `rank`
-#pragma unroll
-                    for (int j = 0; j < 16; ++j) {
-                        const uint32_t r = c + j, place = rank * (NT / splits) + r / splits;
-                        store_remote(map_to_cta(base + (place * BM + q * 32 + lane) * 4, r % splits), __uint_as_float(v[j]));
-                    }
-                } else if (n < N) {
-#pragma unroll
-                    for (int j = 0; j < 16; ++j)
-                        if (m0 + c + j < M) y[(uint64_t)(m0 + c + j) * ldy + n] = el::from_float<T>(__uint_as_float(v[j]));
-                }
-            }
-        }
-        asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-    }
-    if (!ok) atomicExch(status, 1u);
-    __syncthreads();
-    if (splits > 1) {
-        cluster_barrier();                                 // the parts of this CTA's rows have arrived
-        const float4 *parts = reinterpret_cast<const float4 *>(base_ptr) + lane;
-        const uint32_t mine = NT / splits, nn = tile_n * BM + lane * 4;
-        for (uint32_t i = warp; i < mine && m0 + i * splits + rank < M; i += THREADS / 32) {
-            float4 sum = parts[i * 32];
-            for (uint32_t r = 1; r < splits; ++r) {         // in the order of their K ranges
-                const float4 v = parts[(r * mine + i) * 32];
-                sum.x += v.x;
-                sum.y += v.y;
-                sum.z += v.z;
-                sum.w += v.w;
-            }
-            if (nn < N) put4(y + (uint64_t)(m0 + i * splits + rank) * ldy + nn, N - nn, sum);
-        }
-    }
-    if (warp == 1)
-        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"((uint32_t)TMEM_COLS) : "memory");
 }
 
-// ---- large products: one persistent CTA per SM, tiles of 128 x 256 -----------------------------------
-// 48 KB of codes per K step for twice the products of a 128 x 128 tile's 32 KB: what bounds the smaller tile is the
-// traffic from L2 to shared memory.
-//   warp 0   copies (one thread); warp 1   scales to tensor memory and products (one thread)
-//   warps 4-11   epilogue: a quarter of the lanes and half of the columns each
-//   warps 12-15  scales from shared to tensor memory, a copy in each quarter of the lanes.  (tcgen05.cp does the same in
-//   one instruction per 512 bytes, but in the tensor pipe, between the products: measured 30 us of 142 at 16384 x 2048 x 8192.)
-// Tensor memory (512 columns): the two accumulators would fill it, and the scales need 3 x 24 columns, so
-// accumulator 1 starts 80 columns early, inside accumulator 0.  The epilogue reads the shared columns
-// first and releases them; the products of the next tile start then, under the rest of the epilogue.
-// The scales of three K steps have columns of their own; those of step it - 3 are free once its products are through,
-// which the stage's own barrier tells.
-// The kernel does not let its successor start early: it would only take room on SMs that are busy to the end.
-struct Wide {
-    static constexpr int NT = 256;
+template <int NT_>
+struct Cfg {
+    static constexpr int NT = NT_;
     static constexpr int TILE_X_BYTES = NT * BK / 2;
-    static constexpr int STAGE = TILE_W_BYTES + TILE_X_BYTES + 3 * SCALE_BYTES;
-    static constexpr int NSTAGES = 4;
+    static constexpr int X_BLOCKS = NT > 128 ? 2 : 1;                     // blocks of 128 rows that X's scales come in
+    static constexpr int STAGE = TILE_W_BYTES + TILE_X_BYTES + (1 + X_BLOCKS) * SCALE_BYTES;
+    static constexpr int NSTAGES = 208 * 1024 / STAGE;
+    static constexpr int SLOTS = NT == 256 ? 3 : 4, SLOT_COLS = (1 + X_BLOCKS) * SCALE_COLS;
+    static constexpr int D_COLS = NT;
+    static constexpr int SHARED_COLS = NT == 256 ? 80 : 0;                // (3 x 24, in whole loads of 16)
+    static constexpr int ACC1 = D_COLS - SHARED_COLS, SCALES = ACC1 + D_COLS;
+    static constexpr int BARRIERS = 2 * NSTAGES + 6 + SLOTS;
     static constexpr int SMEM = NSTAGES * STAGE + 1024 + 256;
-    static constexpr int THREADS = 512, EPILOGUE_THREADS = 256, SCALE_THREADS = 128;
-    static constexpr int SLOTS = 3, SLOT_COLS = 3 * SCALE_COLS, SHARED_COLS = 80;      // (3 x 24, in whole loads of 16)
-    static constexpr int ACC1 = 256 - SHARED_COLS, SCALES = 512 - SHARED_COLS;
-    static_assert(STAGE % 1024 == 0 && SMEM <= 227 * 1024 && 8 * (2 * NSTAGES + 7 + SLOTS) <= 256, "");
+    static_assert(STAGE % 1024 == 0 && SMEM <= 227 * 1024 && 8 * BARRIERS + 8 <= 256, "");
+    static_assert(SCALES + SLOTS * SLOT_COLS <= 512 && BM * NT * 4 <= NSTAGES * STAGE, "");
 };
 
 // Tiles in the order in which the CTAs take them: bands of sixteen tiles of W's rows, so that the tiles in work
@@ -292,41 +168,47 @@ __device__ __forceinline__ void tile_of(uint32_t t, uint32_t tiles_n, uint32_t t
     tn = band * 16 + in_band - tm * width;
 }
 
-template <typename T>
-__global__ void __launch_bounds__(Wide::THREADS, 1)
-mx_matmul_wide_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_x,
-                      const uint8_t *__restrict__ w_scales, const uint8_t *__restrict__ x_scales, T *__restrict__ y, uint64_t ldy,
-                      uint32_t M, uint32_t N, uint32_t K, uint32_t *status)
+template <int NT, typename T>
+__global__ void __launch_bounds__(THREADS, 1)
+mx_matmul_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_x,
+                 const uint8_t *__restrict__ w_scales, const uint8_t *__restrict__ x_scales, T *__restrict__ y, uint64_t ldy,
+                 uint32_t M, uint32_t N, uint32_t K, uint32_t splits, uint32_t *status)
 {
-    using C = Wide;
+    using C = Cfg<NT>;
     constexpr int NS = C::NSTAGES;
     extern __shared__ uint8_t smem_raw[];
     const uint32_t base = (saddr(smem_raw) + 1023u) & ~1023u;
-    const uint32_t bars = base + NS * C::STAGE;      // full[NS], empty[NS], acc_full[2], acc_shared[2], acc_empty[2], scaled[SLOTS], tmem slot
+    uint8_t *const base_ptr = smem_raw + (base - saddr(smem_raw));
+    const uint32_t bars = base + NS * C::STAGE;      // full[NS], empty[NS], acc_full[2], acc_shared[2], acc_empty[2], scaled[SLOTS]; tmem slot
     auto full = [&](int s) { return bars + 8u * s; };
     auto empty = [&](int s) { return bars + 8u * (NS + s); };
     auto acc_full = [&](int b) { return bars + 8u * (2 * NS + b); };
     auto acc_shared = [&](int b) { return bars + 8u * (2 * NS + 2 + b); };      // the shared columns have been read
     auto acc_empty = [&](int b) { return bars + 8u * (2 * NS + 4 + b); };       // all have
     auto scaled = [&](int s) { return bars + 8u * (2 * NS + 6 + s); };          // a step's scales are in tensor memory
-    const uint32_t tmem_slot = bars + 8u * (2 * NS + 6 + C::SLOTS);
+    const uint32_t tmem_slot = bars + 8u * C::BARRIERS;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    // with divided K a cluster has one tile, and a CTA of it a range of its K steps
+    const uint32_t rank = splits > 1 ? cluster_cta_rank() : 0u;
     const uint32_t ksteps = (K + BK - 1) / BK;
-    const uint32_t tiles_n = (N + BM - 1) / BM, tiles_m = (M + C::NT - 1) / C::NT, ntiles = tiles_n * tiles_m;
+    const uint32_t k_begin = (uint32_t)((uint64_t)ksteps * rank / splits), k_end = (uint32_t)((uint64_t)ksteps * (rank + 1) / splits);
+    const uint32_t tiles_n = (N + BM - 1) / BM, tiles_m = (M + NT - 1) / NT, ntiles = tiles_n * tiles_m;
+    const uint32_t first = blockIdx.x / splits, step = gridDim.x / splits;
+    const uint32_t steps = (ntiles - first + step - 1) / step * (k_end - k_begin);      // of this CTA
 
     if (tid == 0) {
         for (int s = 0; s < NS; ++s) { mbar_init(full(s), 1); mbar_init(empty(s), 1); }
-        for (int s = 0; s < C::SLOTS; ++s) mbar_init(scaled(s), C::SCALE_THREADS);
+        for (int s = 0; s < C::SLOTS; ++s) mbar_init(scaled(s), SCALE_THREADS);
         for (int b = 0; b < 2; ++b) {
             mbar_init(acc_full(b), 1);
-            mbar_init(acc_shared(b), C::EPILOGUE_THREADS);
-            mbar_init(acc_empty(b), C::EPILOGUE_THREADS);
+            mbar_init(acc_shared(b), EPILOGUE_THREADS);
+            mbar_init(acc_empty(b), EPILOGUE_THREADS);
         }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     asm volatile("griddepcontrol.wait;" ::: "memory");
     if (warp == 1) {
-        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(tmem_slot), "r"(512u) : "memory");
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(tmem_slot), "r"((uint32_t)TMEM_COLS) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
     }
     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
@@ -339,53 +221,52 @@ mx_matmul_wide_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_co
     if (tid == 0) {
         const uint32_t x_blocks = (M + 127) / 128;
         uint32_t it = 0;
-        for (uint32_t t = blockIdx.x; t < ntiles && ok; t += gridDim.x) {
+        for (uint32_t t = first; t < ntiles && ok; t += step) {
             uint32_t tn, tm;
             tile_of(t, tiles_n, tiles_m, tn, tm);
+            const uint32_t xb = tm * NT / 128;
             const uint8_t *ws = w_scales + (uint64_t)tn * ksteps * SCALE_BYTES;
-            const uint8_t *xs0 = x_scales + (uint64_t)(2 * tm) * ksteps * SCALE_BYTES;
-            const uint8_t *xs1 = x_scales + (uint64_t)min(2 * tm + 1, x_blocks - 1) * ksteps * SCALE_BYTES;      // (no such rows: any scales)
-            for (uint32_t k = 0; k < ksteps; ++k, ++it) {
+            const uint8_t *xs0 = x_scales + (uint64_t)xb * ksteps * SCALE_BYTES;
+            const uint8_t *xs1 = x_scales + (uint64_t)min(xb + 1, x_blocks - 1) * ksteps * SCALE_BYTES;      // (no such rows: any scales)
+            for (uint32_t k = k_begin; k < k_end; ++k, ++it) {
                 const int s = it % NS;
                 if (it >= (uint32_t)NS) ok = mbar_wait(empty(s), ((it / NS) - 1) & 1u, WAIT_LIMIT);
                 if (!ok) break;
                 const uint32_t a = base + s * C::STAGE, sc = a + TILE_W_BYTES + C::TILE_X_BYTES;
                 mbar_expect_tx(full(s), C::STAGE);
                 tma_load_2d(a, &map_w, (int)(k * (BK / 2)), (int)(tn * BM), full(s));
-                tma_load_2d(a + TILE_W_BYTES, &map_x, (int)(k * (BK / 2)), (int)(tm * C::NT), full(s));
+                tma_load_2d(a + TILE_W_BYTES, &map_x, (int)(k * (BK / 2)), (int)(tm * NT), full(s));
                 bulk_load(sc, ws + (uint64_t)k * SCALE_BYTES, SCALE_BYTES, full(s));
                 bulk_load(sc + SCALE_BYTES, xs0 + (uint64_t)k * SCALE_BYTES, SCALE_BYTES, full(s));
-                bulk_load(sc + 2 * SCALE_BYTES, xs1 + (uint64_t)k * SCALE_BYTES, SCALE_BYTES, full(s));
+                if (C::X_BLOCKS == 2) bulk_load(sc + 2 * SCALE_BYTES, xs1 + (uint64_t)k * SCALE_BYTES, SCALE_BYTES, full(s));
             }
         }
     } else if (tid == 32) {
         uint32_t it = 0, lt = 0;
-        for (uint32_t t = blockIdx.x; t < ntiles && ok; t += gridDim.x, ++lt) {
+        for (uint32_t t = first; t < ntiles && ok; t += step, ++lt) {
             const uint32_t buf = lt & 1u;
-            if (lt >= 1) ok = mbar_wait(acc_shared(buf ^ 1u), ((lt - 1) >> 1) & 1u, WAIT_LIMIT);     // of the tile before
-            if (ok && lt >= 2) ok = mbar_wait(acc_empty(buf), ((lt >> 1) - 1) & 1u, WAIT_LIMIT);     // of the one before that
+            if (C::SHARED_COLS && lt >= 1) ok = mbar_wait(acc_shared(buf ^ 1u), ((lt - 1) >> 1) & 1u, WAIT_LIMIT);     // of the tile before
+            if (ok && lt >= 2) ok = mbar_wait(acc_empty(buf), ((lt >> 1) - 1) & 1u, WAIT_LIMIT);                       // of the one before that
             if (!ok) break;
-            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
             const uint32_t d = tmem_base + buf * C::ACC1;
-            for (uint32_t k = 0; k < ksteps; ++k, ++it) {
+            for (uint32_t k = k_begin; k < k_end; ++k, ++it) {
                 const int s = it % NS;
                 ok = mbar_wait(full(s), (it / NS) & 1u, WAIT_LIMIT);
-                if (ok) ok = mbar_wait(scaled(it % C::SLOTS), (it / C::SLOTS) & 1u, WAIT_LIMIT);
+                ok = ok && mbar_wait(scaled(it % C::SLOTS), (it / C::SLOTS) & 1u, WAIT_LIMIT);
                 if (!ok) break;
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
                 const uint32_t a = base + s * C::STAGE, b = a + TILE_W_BYTES;
                 const uint32_t ta = tmem_base + C::SCALES + it % C::SLOTS * C::SLOT_COLS, tb = ta + SCALE_COLS;
 #pragma unroll
                 for (int i = 0; i < BK / INSTR_K; ++i)
-                    mma_mx(d, umma_desc(a + i * INSTR_K / 2), umma_desc(b + i * INSTR_K / 2), instr_desc(BM, C::NT, i & 1),
-                           ta + 4 * (i >> 1), tb + 8 * (i >> 1), (k | (uint32_t)i) != 0);
+                    mma_mx(d, umma_desc(a + i * INSTR_K / 2), umma_desc(b + i * INSTR_K / 2), instr_desc(BM, NT, i & 1),
+                           ta + 4 * (i >> 1), tb + 4 * C::X_BLOCKS * (i >> 1), k != k_begin || i != 0);
                 umma_commit(empty(s));
             }
             if (ok) umma_commit(acc_full(buf));
         }
     } else if (warp >= 12) {
         const uint32_t quarter = (uint32_t)((warp & 3) * 32) << 16;
-        const uint32_t steps = (ntiles - blockIdx.x + gridDim.x - 1) / gridDim.x * ksteps;
         for (uint32_t it = 0; it < steps; ++it) {
             const int s = it % NS;
             if (it >= (uint32_t)C::SLOTS) ok = mbar_wait(empty((it - C::SLOTS) % NS), ((it - C::SLOTS) / NS) & 1u, WAIT_LIMIT);      // columns are free
@@ -396,8 +277,12 @@ mx_matmul_wide_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_co
             const uint32_t sc = base + s * C::STAGE + TILE_W_BYTES + C::TILE_X_BYTES + lane * 16;
             const uint32_t ta = tmem_base + C::SCALES + it % C::SLOTS * C::SLOT_COLS + quarter, tb = ta + SCALE_COLS;
             tmem_store8(ta, shared16(sc), shared16(sc + 512));
-            tmem_store8(tb, shared16(sc + SCALE_BYTES), shared16(sc + 2 * SCALE_BYTES));                    // columns 0 .. 127: X's rows 0 .. 127, 128 .. 255
-            tmem_store8(tb + 8, shared16(sc + SCALE_BYTES + 512), shared16(sc + 2 * SCALE_BYTES + 512));    // columns 128 .. 255
+            if constexpr (C::X_BLOCKS == 2) {
+                tmem_store8(tb, shared16(sc + SCALE_BYTES), shared16(sc + 2 * SCALE_BYTES));                    // K's first half: X's rows 0 .. 127, 128 .. 255
+                tmem_store8(tb + 8, shared16(sc + SCALE_BYTES + 512), shared16(sc + 2 * SCALE_BYTES + 512));    // its second
+            } else {
+                tmem_store8(tb, shared16(sc + SCALE_BYTES), shared16(sc + SCALE_BYTES + 512));
+            }
             asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
             asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
             mbar_arrive(scaled(it % C::SLOTS));
@@ -405,19 +290,18 @@ mx_matmul_wide_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_co
     } else if (warp >= 4) {
         const int q = warp & 3, half = (warp - 4) >> 2;
         uint32_t lt = 0;
-        for (uint32_t t = blockIdx.x; t < ntiles; t += gridDim.x, ++lt) {
+        for (uint32_t t = first; t < ntiles; t += step, ++lt) {
             const uint32_t buf = lt & 1u;
             uint32_t tn, tm;
             tile_of(t, tiles_n, tiles_m, tn, tm);
             ok = mbar_wait(acc_full(buf), (lt >> 1) & 1u, WAIT_LIMIT);
             ok = __all_sync(0xFFFFFFFFu, ok);
-            if (!ok) break;
+            if (t + step >= ntiles) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+            if (!ok || splits > 1) break;
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-            const uint32_t n = tn * BM + q * 32 + lane, m0 = tm * C::NT;
+            const uint32_t n = tn * BM + q * 32 + lane, m0 = tm * NT;
             const uint32_t acc = tmem_base + buf * C::ACC1 + ((uint32_t)(q * 32) << 16);
             T *out = y + (uint64_t)m0 * ldy + n;
-            // shared columns: the last 80 of accumulator 0 (upper half), the first 80 of accumulator 1 (lower half)
-            const bool mine = (half == 1) == (buf == 0);
             auto put = [&](int c, const uint32_t *v) {           // sixteen columns from c on
                 if (n >= N) return;
                 T *p = out + (uint64_t)c * ldy;
@@ -425,26 +309,29 @@ mx_matmul_wide_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_co
                 for (int j = 0; j < 16; ++j, p += ldy)
                     if (m0 + c + j < M) *p = el::from_float<T>(__uint_as_float(v[j]));
             };
-            int c = half * 128, c_end = c + 128;
-            if (mine) {
-                const int first = buf == 0 ? 256 - C::SHARED_COLS : 0;
-                uint32_t v[C::SHARED_COLS];
+            int c = half * (NT / 2), c_end = c + NT / 2;
+            if constexpr (C::SHARED_COLS != 0) {
+                // the last 80 columns of accumulator 0 (upper half), the first 80 of accumulator 1 (lower half)
+                if ((half == 1) == (buf == 0)) {
+                    const int from = buf == 0 ? 256 - C::SHARED_COLS : 0;
+                    uint32_t v[C::SHARED_COLS];
 #pragma unroll
-                for (int i = 0; i < C::SHARED_COLS; i += 16) tmem_load16_async(acc + first + i, v + i);
-                tmem_load_wait();
+                    for (int i = 0; i < C::SHARED_COLS; i += 16) tmem_load16_async(acc + from + i, v + i);
+                    tmem_load_wait();
 #pragma unroll
-                for (int i = 0; i < C::SHARED_COLS; i += 16) loaded16(v + i);
-                asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-                mbar_arrive(acc_shared(buf));
+                    for (int i = 0; i < C::SHARED_COLS; i += 16) loaded16(v + i);
+                    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+                    mbar_arrive(acc_shared(buf));
 #pragma unroll
-                for (int i = 0; i < C::SHARED_COLS; i += 16) put(first + i, v + i);
-                if (buf == 0) c_end = first;
-                else c = C::SHARED_COLS;
-            } else {
-                mbar_arrive(acc_shared(buf));
+                    for (int i = 0; i < C::SHARED_COLS; i += 16) put(from + i, v + i);
+                    if (buf == 0) c_end = from;
+                    else c = C::SHARED_COLS;
+                } else {
+                    mbar_arrive(acc_shared(buf));
+                }
             }
 #pragma unroll 1
-            for (; c < c_end; c += 16) {
+            for (; c < c_end && m0 + c < M; c += 16) {
                 uint32_t v[16];
                 tmem_load16(acc + c, v);
                 put(c, v);
@@ -453,12 +340,178 @@ mx_matmul_wide_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_co
             mbar_arrive(acc_empty(buf));
         }
     }
+    if (splits > 1) {
+        uint32_t tn, tm;
+        tile_of(first, tiles_n, tiles_m, tn, tm);
+        const uint32_t m0 = tm * NT, mine = NT / splits;
+        __syncwarp();
+        cluster_barrier();                                 // every CTA of the cluster is through with its stages: parts may be put there
+        if (warp >= 4 && warp < 12 && ok) {
+            const int q = warp & 3, half = (warp - 4) >> 2;
+            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+#pragma unroll 1
+            for (int c = half * (NT / 2); c < (half + 1) * (NT / 2) && m0 + c < M; c += 16) {
+                uint32_t v[16];
+                tmem_load16(tmem_base + ((uint32_t)(q * 32) << 16) + c, v);
+                // row r of the tile belongs to CTA r / mine, there place r mod mine of part `rank`
+                const uint32_t here = base + (rank * mine * BM + q * 32 + lane) * 4;
+                const uint32_t to = map_to_cta(here + (c & (mine - 1)) * BM * 4, c / mine);      // (mine >= 32)
+#pragma unroll
+                for (int j = 0; j < 16; ++j)
+                    if (m0 + c + j < M) store_remote(to + j * BM * 4, __uint_as_float(v[j]));
+            }
+            asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+        }
+        __syncwarp();
+        cluster_barrier();                                 // the parts of this CTA's rows have arrived
+        add_parts(reinterpret_cast<const float4 *>(base_ptr) + lane, warp, THREADS / 32, splits, mine, m0 + rank * mine, M, tn * BM + lane * 4, N, y, ldy);
+    }
     if (!ok) atomicExch(status, 1u);
     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
     __syncwarp();
     __syncthreads();
     if (warp == 1)
-        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(512u) : "memory");
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"((uint32_t)TMEM_COLS) : "memory");
+}
+
+// ---- few rows of X (at most 64): the time is that of W's way from memory and of the start-up --------------
+// Two CTAs of six warps share an SM, one tile each; the issuing thread copies the scales itself (tcgen05.cp; a step's before
+// the products of the step before it, so that these do not wait for the copy), each stage with columns of its own.
+template <int NT>
+struct Narrow {
+    static constexpr int TILE_X_BYTES = NT * BK / 2;
+    static constexpr int STAGE = TILE_W_BYTES + TILE_X_BYTES + 2 * SCALE_BYTES;
+    // Every instantiation asks for this much, so that never more than two CTAs (2 x 256 columns of tensor memory) share an
+    // SM: a third would wait for tensor memory while its cluster's other CTAs hold some.
+    static constexpr int SMEM = 112 * 1024;
+    static constexpr int NSTAGES = (SMEM - 1024 - 256) / STAGE;
+    static constexpr int D_COLS = NT < 32 ? 32 : NT, TMEM_COLS = 256;
+    static constexpr int THREADS = 192;
+    static_assert(STAGE % 1024 == 0 && D_COLS + NSTAGES * 2 * SCALE_COLS <= TMEM_COLS && 8 * (2 * NSTAGES + 2) <= 256, "");
+    static_assert(BM * NT * 4 <= NSTAGES * STAGE, "a partial result fits where the stages were");
+};
+
+template <int NT, typename T>
+__global__ void __launch_bounds__(Narrow<NT>::THREADS)
+mx_matmul_narrow_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_x,
+                        const uint8_t *__restrict__ w_scales, const uint8_t *__restrict__ x_scales, T *__restrict__ y, uint64_t ldy,
+                        uint32_t M, uint32_t N, uint32_t K, uint32_t splits, uint32_t *status)
+{
+    using C = Narrow<NT>;
+    constexpr int NS = C::NSTAGES;
+    extern __shared__ uint8_t smem_raw[];
+    const uint32_t base = (saddr(smem_raw) + 1023u) & ~1023u;
+    uint8_t *const base_ptr = smem_raw + (base - saddr(smem_raw));
+    const uint32_t bars = base + NS * C::STAGE;           // full[NS], empty[NS], done, tmem slot
+    auto full = [&](int s) { return bars + 8u * s; };
+    auto empty = [&](int s) { return bars + 8u * (NS + s); };
+    const uint32_t done = bars + 8u * (2 * NS), tmem_slot = done + 8u;
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const uint32_t rank = splits > 1 ? cluster_cta_rank() : 0u;
+    const uint32_t tile_n = blockIdx.x / splits;
+    const uint32_t ksteps = (K + BK - 1) / BK;
+    const uint32_t k_begin = (uint32_t)((uint64_t)ksteps * rank / splits), k_end = (uint32_t)((uint64_t)ksteps * (rank + 1) / splits);
+
+    if (tid == 0) {
+        for (int s = 0; s < NS; ++s) { mbar_init(full(s), 1); mbar_init(empty(s), 1); }
+        mbar_init(done, 1);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == 1) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(tmem_slot), "r"((uint32_t)C::TMEM_COLS) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+    __syncthreads();
+    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+    uint32_t tmem_base;
+    asm volatile("ld.shared.u32 %0, [%1];" : "=r"(tmem_base) : "r"(tmem_slot));
+    el::enter_stream_order();
+
+    bool ok = true;
+    if (tid == 0) {
+        const uint8_t *ws = w_scales + (uint64_t)tile_n * ksteps * SCALE_BYTES;
+        for (uint32_t k = k_begin, it = 0; k < k_end; ++k, ++it) {
+            const int s = it % NS;
+            if (it >= (uint32_t)NS) ok = mbar_wait(empty(s), ((it / NS) - 1) & 1u, WAIT_LIMIT);
+            if (!ok) break;
+            const uint32_t a = base + s * C::STAGE;
+            mbar_expect_tx(full(s), C::STAGE);
+            tma_load_2d(a, &map_w, (int)(k * (BK / 2)), (int)(tile_n * BM), full(s));
+            tma_load_2d(a + TILE_W_BYTES, &map_x, (int)(k * (BK / 2)), 0, full(s));
+            bulk_load(a + TILE_W_BYTES + C::TILE_X_BYTES, ws + (uint64_t)k * SCALE_BYTES, SCALE_BYTES, full(s));
+            bulk_load(a + TILE_W_BYTES + C::TILE_X_BYTES + SCALE_BYTES, x_scales + (uint64_t)k * SCALE_BYTES, SCALE_BYTES, full(s));
+        }
+    } else if (tid == 32) {
+        const uint32_t steps = k_end - k_begin;
+        auto bring_scales = [&](uint32_t it) {            // its columns were last read NS steps ago, before the stage was refilled
+            const int s = it % NS;
+            if (!mbar_wait(full(s), (it / NS) & 1u, WAIT_LIMIT)) return false;
+            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+            const uint32_t sc = base + s * C::STAGE + TILE_W_BYTES + C::TILE_X_BYTES;
+            const uint32_t ta = tmem_base + C::D_COLS + s * 2 * SCALE_COLS, tb = ta + SCALE_COLS;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                copy_scales(ta + 4 * h, sc + 512 * h);
+                copy_scales(tb + 4 * h, sc + SCALE_BYTES + 512 * h);
+            }
+            return true;
+        };
+        ok = bring_scales(0);
+        for (uint32_t it = 0; it < steps && ok; ++it) {
+            const int s = it % NS;
+            if (it + 1 < steps) ok = bring_scales(it + 1);
+            if (!ok) break;
+            const uint32_t a = base + s * C::STAGE, b = a + TILE_W_BYTES;
+            const uint32_t ta = tmem_base + C::D_COLS + s * 2 * SCALE_COLS, tb = ta + SCALE_COLS;
+#pragma unroll
+            for (int i = 0; i < BK / INSTR_K; ++i)
+                mma_mx(tmem_base, umma_desc(a + i * INSTR_K / 2), umma_desc(b + i * INSTR_K / 2), instr_desc(BM, NT, i & 1),
+                       ta + 4 * (i >> 1), tb + 4 * (i >> 1), (it | (uint32_t)i) != 0);
+            umma_commit(empty(s));
+        }
+        if (ok) umma_commit(done);
+    }
+    __syncwarp();
+    const int q = warp & 3;                               // quarter of the lanes a warp may read
+    const uint32_t n = tile_n * BM + q * 32 + lane, mine = NT / splits;
+    if (warp >= 2) {
+        ok = mbar_wait(done, 0u, WAIT_LIMIT);
+        ok = __all_sync(0xFFFFFFFFu, ok);
+        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+    }
+    // every CTA of the cluster is through with its stages: parts may be put there
+    if (splits > 1) cluster_barrier();
+    if (warp >= 2) {
+        if (ok) {
+#pragma unroll 1
+            for (int c = 0; c < NT && c < (int)M; c += 16) {
+                uint32_t v[16];
+                tmem_load16(tmem_base + ((uint32_t)(q * 32) << 16) + c, v);
+                if (splits > 1) {
+                    // row r of the tile belongs to CTA r / mine, there place r mod mine of part `rank`
+                    const uint32_t here = base + (rank * mine * BM + q * 32 + lane) * 4;
+#pragma unroll
+                    for (int j = 0; j < 16; ++j)
+                        if (c + j < M) store_remote(map_to_cta(here + ((c + j) & (mine - 1)) * BM * 4, (c + j) / mine), __uint_as_float(v[j]));
+                } else if (n < N) {
+#pragma unroll
+                    for (int j = 0; j < 16; ++j)
+                        if (c + j < M) y[(uint64_t)(c + j) * ldy + n] = el::from_float<T>(__uint_as_float(v[j]));
+                }
+            }
+        }
+        asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+    }
+    if (!ok) atomicExch(status, 1u);
+    __syncwarp();
+    __syncthreads();
+    if (splits > 1) {
+        cluster_barrier();                                 // the parts of this CTA's rows have arrived
+        add_parts(reinterpret_cast<const float4 *>(base_ptr) + lane, warp, C::THREADS / 32, splits, mine, rank * mine, M, tile_n * BM + lane * 4, N, y, ldy);
+    }
+    if (warp == 1)
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"((uint32_t)C::TMEM_COLS) : "memory");
 }
 
 // The codes as bytes: boxes of box_rows rows x 128 bytes, 128-byte swizzle, zeros outside.
@@ -483,43 +536,55 @@ struct Product {
     void *stream;
 };
 
+uint32_t ksteps_of(const Product &p) { return (p.K + BK - 1) / BK; }
+template <int NT>
+uint64_t tiles_of(const Product &p) { return (uint64_t)((p.N + BM - 1) / BM) * ((p.M + NT - 1) / NT); }
+
 template <int NT, typename T>
 int launch(const Product &p)
 {
+    using C = Cfg<NT>;
     CUtensorMap map_w, map_x;
     if (!make_codes_map(&map_w, p.w_codes, p.N, p.K, BM) || !make_codes_map(&map_x, p.x_codes, p.M, p.K, NT)) return OMC_ERR_CUDA;
-    const int rc = el::allow_smem<mx_matmul_kernel<NT, T>>(SMEM);
-    if (rc) return rc;
-    const uint32_t tiles_n = (p.N + BM - 1) / BM, tiles_m = (p.M + NT - 1) / NT, ksteps = (p.K + BK - 1) / BK;
-    // divide K while the CTAs still fit on the device at once
+    if (const int rc = el::allow_smem<mx_matmul_kernel<NT, T>>(C::SMEM)) return rc;
+    const uint32_t sms = el::sm_count(), ksteps = ksteps_of(p);
+    const uint64_t tiles = tiles_of<NT>(p);
+    if (tiles >= (1ull << 31)) return OMC_ERR_INVALID_ARG;
+    // Divide K while the clusters still fit on the device at once.  Joining the parts takes about 2 us, a step 0.34 us
+    // (128 x 8192 x 8192: 15.0 us undivided, 11.7 us in two; 1999 x 512 x 2048: 6.4 us undivided, 7.5 us in two).
     uint32_t splits = 1;
-    while (splits < 8 && (uint64_t)tiles_n * tiles_m * splits <= el::sm_count() && ksteps >= splits * 2) splits *= 2;
-    return note_cuda(el::launch(mx_matmul_kernel<NT, T>, dim3(tiles_n * splits, tiles_m), THREADS, SMEM, splits, p.stream, map_w, map_x,
-                                p.w_scales, p.x_scales, static_cast<T *>(p.y), p.ldy, p.M, p.N, p.K, splits, p.status));
+    while (splits < 4 && tiles * splits * 2 <= sms && ksteps >= 16) splits *= 2;
+    const uint32_t grid = splits > 1 ? (uint32_t)tiles * splits : tiles < sms ? (uint32_t)tiles : sms;
+    return note_cuda(el::launch(mx_matmul_kernel<NT, T>, dim3(grid), THREADS, C::SMEM, splits, p.stream, map_w, map_x, p.w_scales, p.x_scales,
+                                static_cast<T *>(p.y), p.ldy, p.M, p.N, p.K, splits, p.status));
 }
 
-template <typename T>
-int launch_wide(const Product &p)
+template <int NT, typename T>
+int launch_narrow(const Product &p)
 {
+    using C = Narrow<NT>;
     CUtensorMap map_w, map_x;
-    if (!make_codes_map(&map_w, p.w_codes, p.N, p.K, BM) || !make_codes_map(&map_x, p.x_codes, p.M, p.K, Wide::NT)) return OMC_ERR_CUDA;
-    const int rc = el::allow_smem<mx_matmul_wide_kernel<T>>(Wide::SMEM);
-    if (rc) return rc;
-    const uint64_t ntiles = (uint64_t)((p.N + BM - 1) / BM) * ((p.M + Wide::NT - 1) / Wide::NT);
-    const uint32_t sms = el::sm_count();
-    return note_cuda(el::launch(mx_matmul_wide_kernel<T>, dim3(ntiles < sms ? (uint32_t)ntiles : sms), Wide::THREADS, Wide::SMEM, 1, p.stream,
-                                map_w, map_x, p.w_scales, p.x_scales, static_cast<T *>(p.y), p.ldy, p.M, p.N, p.K, p.status));
+    if (!make_codes_map(&map_w, p.w_codes, p.N, p.K, BM) || !make_codes_map(&map_x, p.x_codes, p.M, p.K, NT)) return OMC_ERR_CUDA;
+    if (const int rc = el::allow_smem<mx_matmul_narrow_kernel<NT, T>>(C::SMEM)) return rc;
+    const uint32_t tiles = (uint32_t)tiles_of<NT>(p), ksteps = ksteps_of(p);
+    // divide K while all CTAs are resident at once, two to an SM, and a CTA keeps two steps (joining takes 0.5 us, a step 0.4 us)
+    uint32_t splits = 1;
+    while (splits < 8 && (uint64_t)tiles * splits <= el::sm_count() && ksteps >= splits * 4) splits *= 2;
+    return note_cuda(el::launch(mx_matmul_narrow_kernel<NT, T>, dim3(tiles * splits), C::THREADS, C::SMEM, splits, p.stream, map_w, map_x, p.w_scales,
+                                p.x_scales, static_cast<T *>(p.y), p.ldy, p.M, p.N, p.K, splits, p.status));
 }
 
-// Few rows of X: the narrowest tile that holds them all (their scales start at a multiple of 128 rows).
+// Up to 64 rows of X: the narrowest tile that holds them all.  More: tiles of 128 or 256 rows, whichever takes less time by
+// its number of rounds over the SMs; measured, a round takes about 0.35 (K steps + 2) us with 128 rows, 0.36 (K steps + 5) us
+// with 256 (1024 x 2048 x 2048: 6.7 and 7.7 us; 3000 x 1000 x 1000: 7.1 and 6.6 us).
 template <typename T>
 int launch_any(const Product &p)
 {
-    if (p.M <= 16) return launch<16, T>(p);
-    if (p.M <= 32) return launch<32, T>(p);
-    if (p.M <= 64) return launch<64, T>(p);
-    if ((uint64_t)((p.N + 127) / 128) * ((p.M + 255) / 256) >= 96) return launch_wide<T>(p);
-    return launch<128, T>(p);
+    if (p.M <= 16) return launch_narrow<16, T>(p);
+    if (p.M <= 32) return launch_narrow<32, T>(p);
+    if (p.M <= 64) return launch_narrow<64, T>(p);
+    const uint64_t sms = el::sm_count(), rounds128 = (tiles_of<128>(p) + sms - 1) / sms, rounds256 = (tiles_of<256>(p) + sms - 1) / sms;
+    return rounds128 * (ksteps_of(p) + 2) <= rounds256 * (ksteps_of(p) + 5) ? launch<128, T>(p) : launch<256, T>(p);
 }
 
 int product(const Product &p, int type)
