@@ -355,7 +355,7 @@ mx_matmul_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constan
                 tmem_load16(tmem_base + ((uint32_t)(q * 32) << 16) + c, v);
                 // row r of the tile belongs to CTA r / mine, there place r mod mine of part `rank`
                 const uint32_t here = base + (rank * mine * BM + q * 32 + lane) * 4;
-                const uint32_t to = map_to_cta(here + (c & (mine - 1)) * BM * 4, c / mine);      // (mine >= 32)
+                const uint32_t to = map_to_cta(here + (c & (mine - 1)) * BM * 4, c >> (31 - __clz(mine)));      // (mine >= 32)
 #pragma unroll
                 for (int j = 0; j < 16; ++j)
                     if (m0 + c + j < M) store_remote(to + j * BM * 4, __uint_as_float(v[j]));
@@ -490,10 +490,10 @@ mx_matmul_narrow_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_
                 tmem_load16(tmem_base + ((uint32_t)(q * 32) << 16) + c, v);
                 if (splits > 1) {
                     // row r of the tile belongs to CTA r / mine, there place r mod mine of part `rank`
-                    const uint32_t here = base + (rank * mine * BM + q * 32 + lane) * 4;
+                    const uint32_t here = base + (rank * mine * BM + q * 32 + lane) * 4, shift = 31 - __clz(mine);
 #pragma unroll
                     for (int j = 0; j < 16; ++j)
-                        if (c + j < M) store_remote(map_to_cta(here + ((c + j) & (mine - 1)) * BM * 4, (c + j) / mine), __uint_as_float(v[j]));
+                        if (c + j < M) store_remote(map_to_cta(here + ((c + j) & (mine - 1)) * BM * 4, (c + j) >> shift), __uint_as_float(v[j]));
                 } else if (n < N) {
 #pragma unroll
                     for (int j = 0; j < 16; ++j)
