@@ -26,7 +26,10 @@
 #include <cuda.h>
 #include <cuda_runtime.h>
 
+#include <type_traits>
+
 #include "element.cuh"
+#include "mx_encode.cuh"
 #include "mx_format.cuh"
 #include "omc_internal.h"
 #include "tensor_core.cuh"
@@ -391,12 +394,29 @@ struct Narrow {
     static_assert(BM * NT * 4 <= NSTAGES * STAGE, "a partial result fits where the stages were");
 };
 
-template <int NT, typename T>
+// Rows of X that are not quantised yet.
+template <typename TX>
+struct Values {
+    const TX *x;
+    uint64_t ld;
+    uint32_t rows;        // M rounded up to a power of two
+    uint32_t vector;      // rows start on 16-byte boundaries
+    using Type = TX;
+    static constexpr int N = el::Word<TX>::N;
+};
+struct Nothing {};
+
+// X quantised already (SOURCE = Nothing: map_x, x_scales), or at most 16 rows of values of type TX (SOURCE = Values<TX>), which warps 2-5 of
+// every CTA quantise for themselves on the way into the operand tile: a thread a block, 8 `rows` threads a K step, the other threads
+// the steps after it.  Tile rows behind `rows` stay as they are: they only enter columns that nobody reads.
+template <int NT, typename T, typename SOURCE>
 __global__ void __launch_bounds__(Narrow<NT>::THREADS)
 mx_matmul_narrow_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_x,
-                        const uint8_t *__restrict__ w_scales, const uint8_t *__restrict__ x_scales, T *__restrict__ y, uint64_t ldy,
+                        const uint8_t *__restrict__ w_scales, const uint8_t *__restrict__ x_scales, SOURCE source, T *__restrict__ y, uint64_t ldy,
                         uint32_t M, uint32_t N, uint32_t K, uint32_t splits, uint32_t *status)
 {
+    constexpr bool VALUES = !std::is_same<SOURCE, Nothing>::value;
+    static_assert(!VALUES || NT == 16, "sixteen rows of eight blocks are a thread each");
     using C = Narrow<NT>;
     constexpr int NS = C::NSTAGES;
     extern __shared__ uint8_t smem_raw[];
@@ -413,7 +433,9 @@ mx_matmul_narrow_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_
     const uint32_t k_begin = (uint32_t)((uint64_t)ksteps * rank / splits), k_end = (uint32_t)((uint64_t)ksteps * (rank + 1) / splits);
 
     if (tid == 0) {
-        for (int s = 0; s < NS; ++s) { mbar_init(full(s), 1); mbar_init(empty(s), 1); }
+        uint32_t arrivals = 1;
+        if constexpr (VALUES) arrivals += 8 * source.rows;
+        for (int s = 0; s < NS; ++s) { mbar_init(full(s), arrivals); mbar_init(empty(s), 1); }
         mbar_init(done, 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
@@ -436,11 +458,13 @@ mx_matmul_narrow_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_
             if (it >= (uint32_t)NS) ok = mbar_wait(empty(s), ((it / NS) - 1) & 1u, WAIT_LIMIT);
             if (!ok) break;
             const uint32_t a = base + s * C::STAGE;
-            mbar_expect_tx(full(s), C::STAGE);
+            mbar_expect_tx(full(s), VALUES ? TILE_W_BYTES + SCALE_BYTES : C::STAGE);
             tma_load_2d(a, &map_w, (int)(k * (BK / 2)), (int)(tile_n * BM), full(s));
-            tma_load_2d(a + TILE_W_BYTES, &map_x, (int)(k * (BK / 2)), 0, full(s));
             bulk_load(a + TILE_W_BYTES + C::TILE_X_BYTES, ws + (uint64_t)k * SCALE_BYTES, SCALE_BYTES, full(s));
-            bulk_load(a + TILE_W_BYTES + C::TILE_X_BYTES + SCALE_BYTES, x_scales + (uint64_t)k * SCALE_BYTES, SCALE_BYTES, full(s));
+            if constexpr (!VALUES) {
+                tma_load_2d(a + TILE_W_BYTES, &map_x, (int)(k * (BK / 2)), 0, full(s));
+                bulk_load(a + TILE_W_BYTES + C::TILE_X_BYTES + SCALE_BYTES, x_scales + (uint64_t)k * SCALE_BYTES, SCALE_BYTES, full(s));
+            }
         }
     } else if (tid == 32) {
         const uint32_t steps = k_end - k_begin;
@@ -471,12 +495,38 @@ mx_matmul_narrow_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_
             umma_commit(empty(s));
         }
         if (ok) umma_commit(done);
+    } else if (VALUES && warp >= 2) {
+        if constexpr (VALUES) {
+            const uint32_t t = tid - 64, team = 8 * source.rows, r = t % team / 8, block = t % 8;
+            for (uint32_t it = t / team; it < k_end - k_begin; it += 128 / team) {
+                const int s = it % NS;
+                const uint32_t col = (k_begin + it) * BK + block * 32;
+                uint32_t w[32 / SOURCE::N], codes[4], scale;
+                if (r >= M || col >= K) {
+#pragma unroll
+                    for (int i = 0; i < 32 / SOURCE::N; ++i) w[i] = 0u;
+                } else if (source.vector) {
+                    mx::load<typename SOURCE::Type, true, 32>(source.x + r * source.ld, col, K, w);
+                } else {
+                    mx::load<typename SOURCE::Type, false, 32>(source.x + r * source.ld, col, K, w);
+                }
+                mx::encode_block<typename SOURCE::Type, 32>(w, codes, scale);
+                if (it >= (uint32_t)NS) ok = mbar_wait(empty(s), ((it / NS) - 1) & 1u, WAIT_LIMIT);
+                if (!ok) break;
+                uint8_t *tile = base_ptr + s * C::STAGE + TILE_W_BYTES;
+                // 128-byte swizzle: 16-byte chunk c of row r sits at chunk c ^ (r mod 8)
+                *reinterpret_cast<uint4 *>(tile + r * 128 + ((block ^ (r & 7)) << 4)) = make_uint4(codes[0], codes[1], codes[2], codes[3]);
+                tile[C::TILE_X_BYTES + SCALE_BYTES + (block >> 2) * 512 + r * 16 + (block & 3)] = (uint8_t)scale;
+                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");    // visible to the tensor cores
+                mbar_arrive(full(s));
+            }
+        }
     }
     __syncwarp();
     const int q = warp & 3;                               // quarter of the lanes a warp may read
     const uint32_t n = tile_n * BM + q * 32 + lane, mine = NT / splits;
     if (warp >= 2) {
-        ok = mbar_wait(done, 0u, WAIT_LIMIT);
+        ok = mbar_wait(done, 0u, WAIT_LIMIT) && ok;
         ok = __all_sync(0xFFFFFFFFu, ok);
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
     }
@@ -559,19 +609,24 @@ int launch(const Product &p)
                                 static_cast<T *>(p.y), p.ldy, p.M, p.N, p.K, splits, p.status));
 }
 
-template <int NT, typename T>
-int launch_narrow(const Product &p)
+template <int NT, typename T, typename SOURCE>
+int launch_narrow(const Product &p, SOURCE source)
 {
     using C = Narrow<NT>;
     CUtensorMap map_w, map_x;
-    if (!make_codes_map(&map_w, p.w_codes, p.N, p.K, BM) || !make_codes_map(&map_x, p.x_codes, p.M, p.K, NT)) return OMC_ERR_CUDA;
-    if (const int rc = el::allow_smem<mx_matmul_narrow_kernel<NT, T>>(C::SMEM)) return rc;
+    if (!make_codes_map(&map_w, p.w_codes, p.N, p.K, BM)) return OMC_ERR_CUDA;
+    if (std::is_same<SOURCE, Nothing>::value) {
+        if (!make_codes_map(&map_x, p.x_codes, p.M, p.K, NT)) return OMC_ERR_CUDA;
+    } else {
+        map_x = map_w;      // not used
+    }
+    if (const int rc = el::allow_smem<mx_matmul_narrow_kernel<NT, T, SOURCE>>(C::SMEM)) return rc;
     const uint32_t tiles = (uint32_t)tiles_of<NT>(p), ksteps = ksteps_of(p);
     // divide K while all CTAs are resident at once, two to an SM, and a CTA keeps two steps (joining takes 0.5 us, a step 0.4 us)
     uint32_t splits = 1;
     while (splits < 8 && (uint64_t)tiles * splits <= el::sm_count() && ksteps >= splits * 4) splits *= 2;
-    return note_cuda(el::launch(mx_matmul_narrow_kernel<NT, T>, dim3(tiles * splits), C::THREADS, C::SMEM, splits, p.stream, map_w, map_x, p.w_scales,
-                                p.x_scales, static_cast<T *>(p.y), p.ldy, p.M, p.N, p.K, splits, p.status));
+    return note_cuda(el::launch(mx_matmul_narrow_kernel<NT, T, SOURCE>, dim3(tiles * splits), C::THREADS, C::SMEM, splits, p.stream, map_w, map_x,
+                                p.w_scales, p.x_scales, source, static_cast<T *>(p.y), p.ldy, p.M, p.N, p.K, splits, p.status));
 }
 
 // Up to 64 rows of X: the narrowest tile that holds them all.  More: tiles of 128 or 256 rows, whichever takes less time by
@@ -580,11 +635,23 @@ int launch_narrow(const Product &p)
 template <typename T>
 int launch_any(const Product &p)
 {
-    if (p.M <= 16) return launch_narrow<16, T>(p);
-    if (p.M <= 32) return launch_narrow<32, T>(p);
-    if (p.M <= 64) return launch_narrow<64, T>(p);
+    if (p.M <= 16) return launch_narrow<16, T>(p, Nothing());
+    if (p.M <= 32) return launch_narrow<32, T>(p, Nothing());
+    if (p.M <= 64) return launch_narrow<64, T>(p, Nothing());
     const uint64_t sms = el::sm_count(), rounds128 = (tiles_of<128>(p) + sms - 1) / sms, rounds256 = (tiles_of<256>(p) + sms - 1) / sms;
     return rounds128 * (ksteps_of(p) + 2) <= rounds256 * (ksteps_of(p) + 5) ? launch<128, T>(p) : launch<256, T>(p);
+}
+
+// At most this many rows of values are quantised inside the product.
+constexpr uint64_t VALUE_ROWS = 16;
+
+template <typename TX>
+int product_of_values(const Product &p, const void *x, uint64_t ld, int type)
+{
+    uint32_t rows = 1;
+    while (rows < p.M) rows *= 2;
+    const Values<TX> v = {static_cast<const TX *>(x), ld, rows, el::aligned16(x) && ld * sizeof(TX) % 16 == 0};
+    return type == OMC_TYPE_F32 ? launch_narrow<16, float>(p, v) : type == OMC_TYPE_F16 ? launch_narrow<16, __half>(p, v) : launch_narrow<16, __nv_bfloat16>(p, v);
 }
 
 int product(const Product &p, int type)
@@ -622,6 +689,11 @@ extern "C" int omc_mx_linear(const void *x, int type, uint64_t M, uint64_t K, ui
     if (reinterpret_cast<uintptr_t>(x) % el::size_of(type) || !el::aligned16(w_codes) || !el::aligned16(w_scales) ||
         !el::aligned16(workspace) || reinterpret_cast<uintptr_t>(y) % el::size_of(y_type) || reinterpret_cast<uintptr_t>(status) % 4)
         return OMC_ERR_MISALIGNED;
+    if (M <= VALUE_ROWS) {
+        const Product p = {nullptr, nullptr, w_codes, w_scales, (uint32_t)M, (uint32_t)N, (uint32_t)K, y, ldy, status, stream};
+        return type == OMC_TYPE_F32 ? product_of_values<float>(p, x, ldx, y_type)
+               : type == OMC_TYPE_F16 ? product_of_values<__half>(p, x, ldx, y_type) : product_of_values<__nv_bfloat16>(p, x, ldx, y_type);
+    }
     uint8_t *scales = workspace + mx::codes_bytes(M, K);
     const int rc = omc_mx_quantise(x, type, M, K, ldx, workspace, scales, nullptr, nullptr, stream);
     if (rc) return rc;
