@@ -9,6 +9,7 @@ raises.
 from __future__ import annotations
 
 import ctypes as C
+import importlib
 import os
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
@@ -263,6 +264,17 @@ def static_status(stream=0) -> int:
 
 # ---- one layer's training step (no plan; addresses are ints, types are F32 / F16 / BF16) --------
 
+_calls = None
+
+
+def _load_calls():
+    """The compiled entry points of these calls (built with the library, csrc/binding.c; no fallback exists)."""
+    global _calls
+    lib()
+    _calls = importlib.import_module("._calls", __name__)
+    return _calls
+
+
 def mx_sizes(rows: int, cols: int):
     """omc_mx_sizes: (bytes of the codes, bytes of the scales) of a quantised rows x cols matrix."""
     a, b = C.c_uint64(), C.c_uint64()
@@ -272,27 +284,37 @@ def mx_sizes(rows: int, cols: int):
 
 def mx_quantise(x, type_, rows, cols, ld, codes=0, scales=0, codes_t=0, scales_t=0, stream=0):
     """omc_mx_quantise: x to four bits along its rows and/or (the _t pair) along its columns."""
-    _check(lib().omc_mx_quantise(x, type_, rows, cols, ld, codes, scales, codes_t, scales_t, stream), "omc_mx_quantise")
+    rc = (_calls or _load_calls()).mx_quantise(x, type_, rows, cols, ld, codes, scales, codes_t, scales_t, stream)
+    if rc:
+        _check(rc, "omc_mx_quantise")
 
 
 def mx_dequantise(codes, scales, rows, cols, out, type_, ld, stream=0):
     """omc_mx_dequantise: the values of a quantised matrix."""
-    _check(lib().omc_mx_dequantise(codes, scales, rows, cols, out, type_, ld, stream), "omc_mx_dequantise")
+    rc = (_calls or _load_calls()).mx_dequantise(codes, scales, rows, cols, out, type_, ld, stream)
+    if rc:
+        _check(rc, "omc_mx_dequantise")
 
 
 def mx_matmul(x_codes, x_scales, M, w_codes, w_scales, N, K, y, type_, ldy, status, stream=0):
     """omc_mx_matmul: Y = X W^T of two quantised matrices."""
-    _check(lib().omc_mx_matmul(x_codes, x_scales, M, w_codes, w_scales, N, K, y, type_, ldy, status, stream), "omc_mx_matmul")
+    rc = (_calls or _load_calls()).mx_matmul(x_codes, x_scales, M, w_codes, w_scales, N, K, y, type_, ldy, status, stream)
+    if rc:
+        _check(rc, "omc_mx_matmul")
 
 
 def mx_linear(x, type_, M, K, ldx, w_codes, w_scales, N, y, y_type, ldy, workspace, status, stream=0):
     """omc_mx_linear: Y = X W^T with X quantised on the way (workspace: sum(mx_sizes(M, K)) bytes)."""
-    _check(lib().omc_mx_linear(x, type_, M, K, ldx, w_codes, w_scales, N, y, y_type, ldy, workspace, status, stream), "omc_mx_linear")
+    rc = (_calls or _load_calls()).mx_linear(x, type_, M, K, ldx, w_codes, w_scales, N, y, y_type, ldy, workspace, status, stream)
+    if rc:
+        _check(rc, "omc_mx_linear")
 
 
 def layer_norm(x, type_, rows, cols, ld, gamma, beta, eps, y, ldy, mean=0, rstd=0, stream=0):
     """omc_layer_norm: normalisation over the last dimension; mean and rstd may be 0 (not wanted)."""
-    _check(lib().omc_layer_norm(x, type_, rows, cols, ld, gamma, beta, eps, y, ldy, mean, rstd, stream), "omc_layer_norm")
+    rc = (_calls or _load_calls()).layer_norm(x, type_, rows, cols, ld, gamma, beta, eps, y, ldy, mean, rstd, stream)
+    if rc:
+        _check(rc, "omc_layer_norm")
 
 
 def layer_norm_workspace_bytes(rows: int, cols: int) -> int:
@@ -304,5 +326,6 @@ def layer_norm_workspace_bytes(rows: int, cols: int) -> int:
 
 def layer_norm_backward(dy, ld_dy, x, ld_x, type_, rows, cols, gamma, mean, rstd, dx, ld_dx, dgamma, dbeta, workspace, stream=0):
     """omc_layer_norm_backward: dx, and the gradients of gain and bias."""
-    _check(lib().omc_layer_norm_backward(dy, ld_dy, x, ld_x, type_, rows, cols, gamma, mean, rstd, dx, ld_dx, dgamma, dbeta, workspace,
-                                         stream), "omc_layer_norm_backward")
+    rc = (_calls or _load_calls()).layer_norm_backward(dy, ld_dy, x, ld_x, type_, rows, cols, gamma, mean, rstd, dx, ld_dx, dgamma, dbeta, workspace, stream)
+    if rc:
+        _check(rc, "omc_layer_norm_backward")

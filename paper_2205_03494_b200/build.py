@@ -8,12 +8,14 @@ import glob
 import os
 import subprocess
 import sys
+import sysconfig
 from concurrent.futures import ThreadPoolExecutor
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 OBJ = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libomc.so")
+CALLS = os.path.join(HERE, "_calls.so")        # Python entry points of the layer operators (csrc/binding.c)
 
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-O3", "-lineinfo", "-std=c++17",
               "-Xcompiler", "-fPIC", "--fmad=false", "-I", os.path.join(os.path.dirname(HERE), "include")]
@@ -63,6 +65,12 @@ def build(force: bool = False, verbose: bool = False) -> str:
         tmp = LIB + ".tmp.%d" % os.getpid()
         subprocess.check_call([_nvcc(), "-shared", "-o", tmp, *objs, "-cudart", "static"])
         os.replace(tmp, LIB)
+    binding = os.path.join(CSRC, "binding.c")
+    if force or not os.path.exists(CALLS) or os.path.getmtime(CALLS) < max(os.path.getmtime(binding), newest_dep):
+        tmp = CALLS + ".tmp.%d" % os.getpid()
+        subprocess.check_call([os.environ.get("CC", "gcc"), "-O2", "-Wall", "-shared", "-fPIC", "-I", sysconfig.get_paths()["include"],
+                               binding, "-o", tmp, "-L", HERE, "-l:libomc.so", "-Wl,-rpath,$ORIGIN"])
+        os.replace(tmp, CALLS)
     return LIB
 
 
