@@ -305,12 +305,18 @@ mx_matmul_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constan
             const uint32_t n = tn * BM + q * 32 + lane, m0 = tm * NT;
             const uint32_t acc = tmem_base + buf * C::ACC1 + ((uint32_t)(q * 32) << 16);
             T *out = y + (uint64_t)m0 * ldy + n;
+            const bool whole = m0 + NT <= M;                     // no column needs a check
             auto put = [&](int c, const uint32_t *v) {           // sixteen columns from c on
                 if (n >= N) return;
                 T *p = out + (uint64_t)c * ldy;
+                if (whole) {
 #pragma unroll
-                for (int j = 0; j < 16; ++j, p += ldy)
-                    if (m0 + c + j < M) *p = el::from_float<T>(__uint_as_float(v[j]));
+                    for (int j = 0; j < 16; ++j, p += ldy) *p = el::from_float<T>(__uint_as_float(v[j]));
+                } else {
+#pragma unroll
+                    for (int j = 0; j < 16; ++j, p += ldy)
+                        if (m0 + c + j < M) *p = el::from_float<T>(__uint_as_float(v[j]));
+                }
             };
             int c = half * (NT / 2), c_end = c + NT / 2;
             if constexpr (C::SHARED_COLS != 0) {

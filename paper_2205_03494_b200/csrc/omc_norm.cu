@@ -463,37 +463,43 @@ norm_backward_kernel(const T *dy, uint64_t ld_dy, const T *x, uint64_t ld_x, uin
         }
         row_dx += step * ld_dx;
     }
+    // the groups' sums side by side where the images were (2 x cols each), added in the groups' order
     __syncthreads();
-    float *columns = reinterpret_cast<float *>(images);    // 2 x cols: the groups' sums joined, in their order
-    for (uint32_t k = 0; k < groups; ++k) {
-        if (g.index == k)
-            R::each(cols, t, G, [&](int i, uint32_t c) {
-                const float dg = i & 1 ? sg[i / 2].y : sg[i / 2].x, db = i & 1 ? sb[i / 2].y : sb[i / 2].x;
-                columns[c] = k ? columns[c] + dg : dg;
-                columns[cols + c] = k ? columns[cols + c] + db : db;
-            });
-        __syncthreads();
-    }
+    float *columns = reinterpret_cast<float *>(images);
+    R::each(cols, t, G, [&](int i, uint32_t c) {
+        columns[g.index * 2 * cols + c] = i & 1 ? sg[i / 2].y : sg[i / 2].x;
+        columns[(g.index * 2 + 1) * cols + c] = i & 1 ? sb[i / 2].y : sb[i / 2].x;
+    });
+    __syncthreads();
     float *out = part + (uint64_t)blockIdx.x * 2 * cols;
-    for (uint32_t c = threadIdx.x; c < 2 * cols; c += blockDim.x) out[c] = columns[c];
+    for (uint32_t c = threadIdx.x; c < 2 * cols; c += blockDim.x) {
+        float sum = columns[c];
+        for (uint32_t k = 1; k < groups; ++k) sum += columns[k * 2 * cols + c];
+        out[c] = sum;
+    }
 }
 
-// Sums of the parts: 32 columns per CTA, eight threads to a column.
-__global__ void __launch_bounds__(THREADS)
+// Sums of the parts: 32 columns per CTA, 32 warps that take every 32nd part, then one that adds their sums.
+constexpr int FINISH_WARPS = 32;
+__global__ void __launch_bounds__(32 * FINISH_WARPS)
 norm_finish_kernel(const float *__restrict__ part, uint32_t parts, uint32_t cols, float *__restrict__ dgamma, float *__restrict__ dbeta)
 {
     el::enter_stream_order();
-    __shared__ float room[THREADS];
-    const uint32_t c = blockIdx.x * 32 + (threadIdx.x & 31);
+    __shared__ float room[FINISH_WARPS][33];
+    const uint32_t lane = threadIdx.x & 31, warp = threadIdx.x >> 5, c = blockIdx.x * 32 + lane;
     float s = 0.f;
     if (c < 2 * cols)
-        for (uint32_t p = threadIdx.x >> 5; p < parts; p += THREADS / 32) s += part[(uint64_t)p * 2 * cols + c];
-    room[threadIdx.x] = s;
+        for (uint32_t p = warp; p < parts; p += FINISH_WARPS) s += part[(uint64_t)p * 2 * cols + c];
+    room[warp][lane] = s;
     __syncthreads();
-    if (threadIdx.x < 32 && c < 2 * cols) {
-        for (int k = 1; k < THREADS / 32; ++k) s += room[threadIdx.x + 32 * k];
-        if (c < cols) dgamma[c] = s;
-        else dbeta[c - cols] = s;
+    // warp w adds up column w's sums, lane l holding warp l's
+    s = room[lane][warp];
+#pragma unroll
+    for (int d = 16; d >= 1; d >>= 1) s += __shfl_xor_sync(0xFFFFFFFFu, s, d);
+    const uint32_t k = blockIdx.x * 32 + warp;
+    if (lane == 0 && k < 2 * cols) {
+        if (k < cols) dgamma[k] = s;
+        else dbeta[k - cols] = s;
     }
 }
 
@@ -549,7 +555,7 @@ int backward_rows(const void *dy, uint64_t ld_dy, const void *x, uint64_t ld_x, 
     const uint32_t groups = warps >= 16 ? 1 : (16 / warps < MAX_GROUPS ? 16 / warps : MAX_GROUPS);
     const uint32_t ctas = (rows + groups - 1) / groups;
     const uint32_t ring = groups * STAGES * 2 * Row<T, VECTOR, E>::image_bytes(warps * 32);
-    const uint32_t smem = ring > 8 * cols ? ring : 8 * cols;
+    const uint32_t joined = groups * 8 * cols, smem = ring > joined ? ring : joined;
     const uint32_t most = E == 8 ? MAX_PARTS : MAX_PARTS / 2;      // as many CTAs as are resident
     *parts = ctas < most ? ctas : most;
     if (const int rc = el::allow_smem<norm_backward_kernel<T, VECTOR, E>>(smem)) return rc;
@@ -578,7 +584,7 @@ int backward(const void *dy, uint64_t ld_dy, const void *x, uint64_t ld_x, uint6
                                       ld_dy, static_cast<const T *>(x), ld_x, c, gamma, mean, rstd, static_cast<T *>(dx), ld_dx));
     }
     if (!rc)
-        rc = note_cuda(el::launch(norm_finish_kernel, dim3((2 * c + 31) / 32), THREADS, 0, 1, stream, static_cast<const float *>(part), parts, c,
+        rc = note_cuda(el::launch(norm_finish_kernel, dim3((2 * c + 31) / 32), 32 * FINISH_WARPS, 0, 1, stream, static_cast<const float *>(part), parts, c,
                                   dgamma, dbeta));
     return rc;
 }
