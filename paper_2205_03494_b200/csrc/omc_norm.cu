@@ -106,18 +106,20 @@ norm_columns_kernel(const T *__restrict__ dy, uint64_t ld_dy, const T *__restric
 }
 
 // ---- rows that fit in registers ------------------------------------------------------------------
-// A row is held by a group of `warps` warps, E values a thread; a CTA has several groups, each of which walks over
-// rows of its own.  The rows ahead are on their way into a ring of row images in shared memory (cp.async), so
-// that what is in flight takes no registers.
-//   VECTOR: rows start on 16-byte boundaries and are whole 16-byte chunks; chunk i G + t belongs to thread t (of G), which
-//   copies and reads it itself: no barrier.  Otherwise the image starts at the boundary below the row (never
-//   below the matrix), value i G + t belongs to thread t, and the group meets between copying and reading.
-template <typename T, bool VECTOR, int E>
+// A row is held by a group of G threads, E values each: 8 or 16 lanes of a warp (narrow rows: the warp works on four or
+// two rows at a time), a warp, or several warps.  Each group walks over rows of its own.  The rows ahead are on their
+// way into a ring of row images in shared memory (cp.async), so that what is in flight takes no registers.
+//   ALIGN  bytes on whose multiples every row begins and that divide its length: 16, 4 or that of one value.  Unit i G + t of a row,
+//          ALIGN bytes of it, belongs to thread t.  With 16 a thread copies and reads its own units: no barrier.  Otherwise the
+//          image starts at the 16-byte boundary below the row (never below the matrix), and the group meets
+//          between copying and reading.
+template <typename T, int ALIGN, int E>
 struct Row {
-    static constexpr uint32_t SIZE = sizeof(T), PER = 16 / SIZE;      // values of one chunk
-    static constexpr int CHUNKS = E / PER;                            // of a thread
+    static constexpr uint32_t SIZE = sizeof(T), PER = ALIGN / SIZE;   // values of a unit
+    static constexpr int UNITS = E / PER;                             // of a thread
+    static_assert(UNITS >= 1 && E % PER == 0, "");
 
-    static __host__ __device__ constexpr uint32_t image_bytes(uint32_t G) { return G * E * SIZE + (VECTOR ? 0 : 16); }
+    static __host__ __device__ constexpr uint32_t image_bytes(uint32_t G) { return G * E * SIZE + (ALIGN == 16 ? 0 : 16); }
 
     static __device__ __forceinline__ void copy16(uint32_t dst, const void *src, uint32_t bytes)      // the rest of the 16 becomes 0
     {
@@ -126,15 +128,16 @@ struct Row {
     static __device__ __forceinline__ void fetch(uint8_t *image, const T *row, bool first_row, uint32_t cols, uint32_t t, uint32_t G)
     {
         const uint32_t dst = (uint32_t)__cvta_generic_to_shared(image);
-        if constexpr (VECTOR) {
+        if constexpr (ALIGN == 16) {
 #pragma unroll
-            for (int i = 0; i < CHUNKS; ++i) {
+            for (int i = 0; i < UNITS; ++i) {
                 const uint32_t k = i * G + t;
                 if (k * PER < cols) copy16(dst + k * 16, row + k * PER, 16);
             }
         } else {
             const uint32_t skip = (uint32_t)(reinterpret_cast<uintptr_t>(row) & 15u), total = skip + cols * SIZE;
             const uint8_t *src = reinterpret_cast<const uint8_t *>(row) - skip;
+            constexpr int CHUNKS = (E * SIZE + 15) / 16;
 #pragma unroll
             for (int i = 0; i <= CHUNKS; ++i) {
                 const uint32_t k = i * G + t;
@@ -148,49 +151,49 @@ struct Row {
             }
         }
     }
-    static __device__ __forceinline__ void values(const uint8_t *image, const T *row, uint32_t cols, uint32_t t, uint32_t G, float *v)
+    static __device__ __forceinline__ void values(const uint8_t *image, const T *row, uint32_t t, uint32_t G, float *v)
     {
-        if constexpr (VECTOR) {
-            constexpr int N = el::Word<T>::N;
+        constexpr int N = el::Word<T>::N;
+        const uint8_t *p = image + (ALIGN == 16 ? 0 : reinterpret_cast<uintptr_t>(row) & 15u);      // (behind the row: never used)
 #pragma unroll
-            for (int i = 0; i < CHUNKS; ++i) {
-                const uint4 w = *reinterpret_cast<const uint4 *>(image + (i * G + t) * 16);
+        for (int i = 0; i < UNITS; ++i) {
+            if constexpr (ALIGN == 16) {
+                const uint4 w = *reinterpret_cast<const uint4 *>(p + (i * G + t) * 16);
                 el::Word<T>::unpack(w.x, v + i * PER);
                 el::Word<T>::unpack(w.y, v + i * PER + N);
                 el::Word<T>::unpack(w.z, v + i * PER + 2 * N);
                 el::Word<T>::unpack(w.w, v + i * PER + 3 * N);
+            } else if constexpr (ALIGN == 4) {
+                el::Word<T>::unpack(*reinterpret_cast<const uint32_t *>(p + (i * G + t) * 4), v + i * PER);
+            } else {
+                v[i] = el::to_float(*reinterpret_cast<const T *>(p + (i * G + t) * SIZE));
             }
-        } else {
-            const T *p = reinterpret_cast<const T *>(image + (reinterpret_cast<uintptr_t>(row) & 15u));
-#pragma unroll
-            for (int i = 0; i < E; ++i) v[i] = el::to_float(p[i * G + t]);       // (behind the row: never used)
         }
     }
     static __device__ __forceinline__ void store(T *row, uint32_t cols, uint32_t t, uint32_t G, const float *v)
     {
-        if constexpr (VECTOR) {
-            constexpr int N = el::Word<T>::N;
+        constexpr int N = el::Word<T>::N;
 #pragma unroll
-            for (int i = 0; i < CHUNKS; ++i) {
-                const uint32_t k = i * G + t;
-                const float *p = v + i * PER;
-                if (k * PER < cols)
-                    *reinterpret_cast<uint4 *>(row + k * PER) = make_uint4(el::Word<T>::pack(p), el::Word<T>::pack(p + N),
-                                                                           el::Word<T>::pack(p + 2 * N), el::Word<T>::pack(p + 3 * N));
-            }
-        } else {
-#pragma unroll
-            for (int i = 0; i < E; ++i)
-                if (i * G + t < cols) row[i * G + t] = el::from_float<T>(v[i]);
+        for (int i = 0; i < UNITS; ++i) {
+            const uint32_t c = (i * G + t) * PER;
+            const float *p = v + i * PER;
+            if (c >= cols) continue;
+            if constexpr (ALIGN == 16)
+                *reinterpret_cast<uint4 *>(row + c) = make_uint4(el::Word<T>::pack(p), el::Word<T>::pack(p + N), el::Word<T>::pack(p + 2 * N),
+                                                                 el::Word<T>::pack(p + 3 * N));
+            else if constexpr (ALIGN == 4)
+                *reinterpret_cast<uint32_t *>(row + c) = el::Word<T>::pack(p);
+            else
+                row[c] = el::from_float<T>(*p);
         }
     }
     // The thread's values of an FP32 vector of the row's length; 0 behind its end.
     static __device__ __forceinline__ void vector(const float *p, uint32_t cols, uint32_t t, uint32_t G, float *v)
     {
-        if constexpr (VECTOR) {
 #pragma unroll
-            for (int i = 0; i < CHUNKS; ++i) {
-                const uint32_t c = (i * G + t) * PER;
+        for (int i = 0; i < UNITS; ++i) {
+            const uint32_t c = (i * G + t) * PER;
+            if constexpr (PER % 4 == 0) {
 #pragma unroll
                 for (uint32_t j = 0; j < PER; j += 4) {
                     const float4 f = c < cols ? __ldg(reinterpret_cast<const float4 *>(p + c + j)) : make_float4(0.f, 0.f, 0.f, 0.f);
@@ -199,45 +202,36 @@ struct Row {
                     v[i * PER + j + 2] = f.z;
                     v[i * PER + j + 3] = f.w;
                 }
+            } else if constexpr (PER == 2) {
+                const float2 f = c < cols ? __ldg(reinterpret_cast<const float2 *>(p + c)) : make_float2(0.f, 0.f);
+                v[i * 2] = f.x;
+                v[i * 2 + 1] = f.y;
+            } else {
+                v[i] = c < cols ? __ldg(p + c) : 0.f;
             }
-        } else {
-#pragma unroll
-            for (int i = 0; i < E; ++i) v[i] = i * G + t < cols ? __ldg(p + i * G + t) : 0.f;
         }
     }
     // Sets the values behind the row's end.
     static __device__ __forceinline__ void fill(uint32_t cols, uint32_t t, uint32_t G, float *v, float to)
     {
-        if constexpr (VECTOR) {
 #pragma unroll
-            for (int i = 0; i < CHUNKS; ++i)
-                if ((i * G + t) * PER >= cols) {
+        for (int i = 0; i < UNITS; ++i)
+            if ((i * G + t) * PER >= cols) {
 #pragma unroll
-                    for (uint32_t j = 0; j < PER; ++j) v[i * PER + j] = to;
-                }
-        } else {
-#pragma unroll
-            for (int i = 0; i < E; ++i)
-                if (i * G + t >= cols) v[i] = to;
-        }
+                for (uint32_t j = 0; j < PER; ++j) v[i * PER + j] = to;
+            }
     }
     // Calls f(index of the value in v, column) for the values inside the row.
     template <typename F>
     static __device__ __forceinline__ void each(uint32_t cols, uint32_t t, uint32_t G, F f)
     {
-        if constexpr (VECTOR) {
 #pragma unroll
-            for (int i = 0; i < CHUNKS; ++i) {
-                const uint32_t c = (i * G + t) * PER;
-                if (c < cols) {
+        for (int i = 0; i < UNITS; ++i) {
+            const uint32_t c = (i * G + t) * PER;
+            if (c < cols) {
 #pragma unroll
-                    for (uint32_t j = 0; j < PER; ++j) f(i * PER + j, c + j);
-                }
+                for (uint32_t j = 0; j < PER; ++j) f(i * PER + j, c + j);
             }
-        } else {
-#pragma unroll
-            for (int i = 0; i < E; ++i)
-                if (i * G + t < cols) f(i, i * G + t);
         }
     }
 };
@@ -245,24 +239,28 @@ __device__ __forceinline__ void commit_copies() { asm volatile("cp.async.commit_
 template <int LEFT>
 __device__ __forceinline__ void wait_copies() { asm volatile("cp.async.wait_group %0;" ::"n"(LEFT) : "memory"); }
 
-// Sums over a group, known to all its threads.  Consecutive calls use the two halves of `room` in turn, so that
-// one barrier per call is enough: who writes a half again has passed the barrier of the call between.
+// Sums over a group, known to all its threads.  Groups of several warps (L = 32): consecutive calls use the two halves of
+// `room` in turn, so that one barrier per call is enough: who writes a half again has passed the barrier of the call between.
+template <int L>
 struct Group {
     uint32_t warps, index, thread;
     float *room;        // [2][32] of this group
     uint32_t turn;
 
+    __device__ __forceinline__ Group(uint32_t warps_, float *rooms)
+        : warps(warps_), index(threadIdx.x / (L * warps_)), thread(threadIdx.x - index * L * warps_), room(rooms + index * 64), turn(0) {}
+
     __device__ __forceinline__ void meet()
     {
-        if (warps > 1) asm volatile("bar.sync %0, %1;" ::"r"(index + 1), "r"(warps * 32) : "memory");
+        if (L == 32 && warps > 1) asm volatile("bar.sync %0, %1;" ::"r"(index + 1), "r"(warps * 32) : "memory");
         else __syncwarp();
     }
     // One value: every lane ends with the total.
     __device__ __forceinline__ float sum(float v)
     {
 #pragma unroll
-        for (int d = 16; d >= 1; d >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, d);
-        if (warps > 1) {
+        for (int d = L / 2; d >= 1; d >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, d);
+        if (L == 32 && warps > 1) {
             float *half = room + 32 * (turn & 1);
             ++turn;
             const uint32_t lane = threadIdx.x & 31;
@@ -274,15 +272,15 @@ struct Group {
         }
         return v;
     }
-    // Two values: the lower sixteen lanes add up the first, the upper sixteen the second.
+    // Two values: the lower half of the lanes adds up the first, the upper half the second.
     __device__ __forceinline__ float2 sum2(float a, float b)
     {
         const uint32_t lane = threadIdx.x & 31;
-        const bool upper = lane >= 16;
-        float v = (upper ? b : a) + __shfl_xor_sync(0xFFFFFFFFu, upper ? a : b, 16);
+        const bool upper = (lane & (L / 2)) != 0;
+        float v = (upper ? b : a) + __shfl_xor_sync(0xFFFFFFFFu, upper ? a : b, L / 2);
 #pragma unroll
-        for (int d = 8; d >= 1; d >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, d);
-        if (warps > 1) {
+        for (int d = L / 4; d >= 1; d >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, d);
+        if (L == 32 && warps > 1) {
             float *half = room + 32 * (turn & 1);
             ++turn;
             if ((lane & 15) == 0) half[(thread >> 5) + (upper ? 16 : 0)] = v;
@@ -291,39 +289,29 @@ struct Group {
 #pragma unroll
             for (int d = 8; d >= 1; d >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, d);
         }
-        return make_float2(__shfl_sync(0xFFFFFFFFu, v, 0), __shfl_sync(0xFFFFFFFFu, v, 16));
+        const float other = __shfl_xor_sync(0xFFFFFFFFu, v, L / 2);
+        return upper ? make_float2(other, v) : make_float2(v, other);
     }
 };
 
-constexpr int MAX_GROUPS = 15;      // named barriers 1 .. 15
-
-__device__ __forceinline__ Group make_group(uint32_t warps, float *room)
-{
-    Group g;
-    g.warps = warps;
-    g.index = threadIdx.x / (warps * 32);
-    g.thread = threadIdx.x - g.index * warps * 32;
-    g.room = room + g.index * 64;
-    g.turn = 0;
-    return g;
-}
+constexpr int MAX_GROUPS = 15;      // of several warps: named barriers 1 .. 15
 
 constexpr int STAGES = 3;      // row images of a group: two ahead of the one in work
 
 // Registers a thread of the forward kernel gets: what lets 1024, 768 or 512 threads share an SM.
-template <bool VECTOR, int E> constexpr int forward_registers = E == 8 ? 64 : VECTOR ? 80 : 128;
+template <int ALIGN, int E> constexpr int forward_registers = E == 8 ? 64 : ALIGN == 16 ? 80 : 128;
 
-template <typename T, bool VECTOR, int E>
-__global__ void __maxnreg__((forward_registers<VECTOR, E>))
+template <typename T, int ALIGN, int E, int L>
+__global__ void __maxnreg__((forward_registers<ALIGN, E>))
 norm_kernel(const T *x, uint32_t rows, uint32_t cols, uint64_t ld, const float *__restrict__ gamma, const float *__restrict__ beta, float eps,
             T *y, uint64_t ldy, float *__restrict__ mean_out, float *__restrict__ rstd_out, uint32_t warps)
 {
-    using R = Row<T, VECTOR, E>;
+    using R = Row<T, ALIGN, E>;
     constexpr int S = STAGES;
-    __shared__ float room[MAX_GROUPS * 64];
+    __shared__ float room[L == 32 ? 16 * 64 : 1];
     extern __shared__ __align__(16) uint8_t images[];
-    Group g = make_group(warps, room);
-    const uint32_t G = warps * 32, groups = blockDim.x / G, t = g.thread, bytes = R::image_bytes(G);
+    Group<L> g(warps, room);
+    const uint32_t G = warps * L, groups = blockDim.x / G, t = g.thread, bytes = R::image_bytes(G);
     uint8_t *ring = images + g.index * S * bytes;
     const float inv = 1.f / (float)cols;
     el::enter_stream_order();
@@ -344,12 +332,13 @@ norm_kernel(const T *x, uint32_t rows, uint32_t cols, uint64_t ld, const float *
     R::vector(gamma, cols, t, G, ga);
     R::vector(beta, cols, t, G, be);
     uint32_t now = 0, ahead = S - 1;
-    for (uint32_t row = first; row < rows; row += step) {
+    const uint32_t neighbour = L < 32 ? g.index % (32 / L) : 0u;      // a warp's groups go on as long as the first has a row
+    for (uint32_t row = first; row - neighbour < rows; row += step) {
         fetch(ahead);                                      // where the row before was: its group has met since
         wait_copies<S - 1>();
-        if (!VECTOR) g.meet();
+        if (ALIGN != 16) g.meet();
         float v[E];
-        R::values(ring + now * bytes, row_x, cols, t, G, v);
+        R::values(ring + now * bytes, row_x, t, G, v);
         now = now + 1 == S ? 0 : now + 1;
         ahead = ahead + 1 == S ? 0 : ahead + 1;
         if (!whole) R::fill(cols, t, G, v, 0.f);
@@ -369,29 +358,30 @@ norm_kernel(const T *x, uint32_t rows, uint32_t cols, uint64_t ld, const float *
 #pragma unroll
         for (int i = 0; i < E / 2; ++i)
             p[i] = fma2(mul2(p[i], twice(rstd)), make_float2(ga[2 * i], ga[2 * i + 1]), make_float2(be[2 * i], be[2 * i + 1]));
+        if (L < 32 && row >= rows) break;                  // the neighbours' last row
         R::store(row_y, cols, t, G, v);
         if (t == 0) {
             if (mean_out) mean_out[row] = mean;
             if (rstd_out) rstd_out[row] = rstd;
         }
-        if (!VECTOR) row_x += step * ld;
+        if (ALIGN != 16) row_x += step * ld;
         row_y += step * ldy;
     }
 }
 
 // dx, and this CTA's part of the column sums: each thread adds up its own columns over its group's rows in registers.
-template <typename T, bool VECTOR, int E>
-__global__ void __launch_bounds__(512, E == 8 ? 2 : 1)
+template <typename T, int ALIGN, int E, int L>
+__global__ void __launch_bounds__(E == 8 ? 384 : 512, E == 8 ? 2 : 1)
 norm_backward_kernel(const T *dy, uint64_t ld_dy, const T *x, uint64_t ld_x, uint32_t rows, uint32_t cols, const float *__restrict__ gamma,
                      const float *__restrict__ mean_in, const float *__restrict__ rstd_in, T *dx, uint64_t ld_dx, float *__restrict__ part,
                      uint32_t warps)
 {
-    using R = Row<T, VECTOR, E>;
+    using R = Row<T, ALIGN, E>;
     constexpr int S = STAGES;
-    __shared__ float room[MAX_GROUPS * 64];
+    __shared__ float room[L == 32 ? 16 * 64 : 1];
     extern __shared__ __align__(16) uint8_t images[];
-    Group g = make_group(warps, room);
-    const uint32_t G = warps * 32, groups = blockDim.x / G, t = g.thread, bytes = R::image_bytes(G);
+    Group<L> g(warps, room);
+    const uint32_t G = warps * L, groups = blockDim.x / G, t = g.thread, bytes = R::image_bytes(G);
     uint8_t *ring = images + g.index * S * 2 * bytes;      // x and dy
     const float inv = 1.f / (float)cols;
     el::enter_stream_order();
@@ -421,23 +411,29 @@ norm_backward_kernel(const T *dy, uint64_t ld_dy, const T *x, uint64_t ld_x, uin
         rstd = rstd_in[first];
     }
     uint32_t now = 0, ahead = S - 1;
-    for (uint32_t row = first; row < rows; row += step) {
+    const uint32_t neighbour = L < 32 ? g.index % (32 / L) : 0u;      // a warp's groups go on as long as the first has a row
+    for (uint32_t row = first; row - neighbour < rows; row += step) {
         fetch(ahead);                                      // where the row before was: its group has met since
-        const float mu = mean, rs = rstd;
+        float mu = mean, rs = rstd;
         if (row + step < rows) {
             mean = mean_in[row + step];
             rstd = rstd_in[row + step];
         }
         wait_copies<S - 1>();
-        if (!VECTOR) g.meet();
+        if (ALIGN != 16) g.meet();
         float h[E], d[E];
-        R::values(ring + now * 2 * bytes, row_x, cols, t, G, h);
-        R::values(ring + now * 2 * bytes + bytes, row_d, cols, t, G, d);
+        R::values(ring + now * 2 * bytes, row_x, t, G, h);
+        R::values(ring + now * 2 * bytes + bytes, row_d, t, G, d);
         now = now + 1 == S ? 0 : now + 1;
         ahead = ahead + 1 == S ? 0 : ahead + 1;
         if (!whole) {
             R::fill(cols, t, G, h, mu);
             R::fill(cols, t, G, d, 0.f);
+        }
+        if (L < 32 && row >= rows) {                       // no row of its own: nothing to add to the columns
+#pragma unroll
+            for (int i = 0; i < E; ++i) h[i] = d[i] = 0.f;
+            mu = rs = 0.f;
         }
         float ga[E];                                       // from L1 each time: registers are short here
         R::vector(gamma, cols, t, G, ga);
@@ -456,8 +452,9 @@ norm_backward_kernel(const T *dy, uint64_t ld_dy, const T *x, uint64_t ld_x, uin
         const float2 m1 = twice(-(m.x * inv)), m2 = twice(-(m.y * inv));
 #pragma unroll
         for (int i = 0; i < E / 2; ++i) pd[i] = mul2(fma2(ph[i], m2, add2(pd[i], m1)), twice(rs));
+        if (L < 32 && row >= rows) break;                  // the neighbours' last row
         R::store(row_dx, cols, t, G, d);
-        if (!VECTOR) {
+        if (ALIGN != 16) {
             row_x += step * ld_x;
             row_d += step * ld_dy;
         }
@@ -510,29 +507,63 @@ uint32_t parts_of(uint64_t rows) { return (uint32_t)(rows < MAX_PARTS ? rows : M
 
 bool shape_ok(uint64_t rows, uint64_t cols) { return cols >= 1 && rows < (1ull << 31) && cols < (1ull << 30); }
 
-// Whether 16-byte loads cover every row.
+// Bytes on whose multiples the matrix's rows begin and end: 16, 4 or the size of a value.
 template <typename T>
-bool vector_rows(const void *p, uint64_t ld, uint64_t cols)
+int align_of(const void *p, uint64_t ld, uint64_t cols)
 {
-    return el::aligned16(p) && ld * sizeof(T) % 16 == 0 && cols * sizeof(T) % 16 == 0;
+    const uint64_t all = reinterpret_cast<uintptr_t>(p) | (ld * sizeof(T)) | (cols * sizeof(T));
+    return all % 16 == 0 ? 16 : all % 4 == 0 ? 4 : (int)sizeof(T);
 }
 
 constexpr uint32_t REGISTER_COLS = 8192;      // 16 warps of 16 values a thread
 
-template <typename T, bool VECTOR, int E>
-int forward_rows(const void *x, uint32_t rows, uint32_t cols, uint64_t ld, const float *gamma, const float *beta, float eps, void *y,
-                 uint64_t ldy, float *mean, float *rstd, void *stream)
+// Calls f.operator()<ALIGN, E, L>() with the instantiation for rows of this width: narrow rows several to a warp, up to 256 values a
+// warp with eight a thread, longer ones with sixteen (per thread and row about 200 instructions do not depend on the number
+// of values: 32768 x 2048 BF16 backward 104 us with eight, 83 us with sixteen).
+template <int ALIGN, typename F>
+int with_width(uint32_t cols, F f)
 {
-    const uint32_t warps = (cols + 32 * E - 1) / (32 * E), groups = warps >= 8 ? 1 : 8 / warps;
-    const uint32_t ctas = (rows + groups - 1) / groups, threads = warps * groups * 32;
-    const uint32_t smem = groups * STAGES * Row<T, VECTOR, E>::image_bytes(warps * 32);
-    // as many CTAs as are resident
-    const uint32_t by_regs = 65536 / (threads * forward_registers<VECTOR, E>), by_smem = 220 * 1024 / (smem + 5 * 1024);
-    const uint32_t most = DEFAULT_SMS * (by_regs < by_smem ? by_regs : by_smem);
-    if (const int rc = el::allow_smem<norm_kernel<T, VECTOR, E>>(smem)) return rc;
-    return note_cuda(el::launch(norm_kernel<T, VECTOR, E>, dim3(ctas < most ? ctas : most), threads, smem, 1, stream,
-                                static_cast<const T *>(x), rows, cols, ld, gamma, beta, eps, static_cast<T *>(y), ldy, mean, rstd, warps));
+    if (cols <= 64) return f.template operator()<ALIGN, 8, 8>();
+    if (cols <= 128) return f.template operator()<ALIGN, 8, 16>();
+    if (cols <= 256) return f.template operator()<ALIGN, 8, 32>();
+    return f.template operator()<ALIGN, 16, 32>();
 }
+template <typename T, typename F>
+int with_rows(int align, uint32_t cols, F f)
+{
+    if (align == 16) return with_width<16>(cols, f);
+    if constexpr (sizeof(T) == 2) {
+        if (align == 2) return with_width<2>(cols, f);
+    }
+    return with_width<4>(cols, f);
+}
+
+template <typename T>
+struct Forward {
+    const void *x;
+    uint32_t rows, cols;
+    uint64_t ld;
+    const float *gamma, *beta;
+    float eps;
+    void *y;
+    uint64_t ldy;
+    float *mean, *rstd;
+    void *stream;
+
+    template <int ALIGN, int E, int L>
+    int operator()() const
+    {
+        const uint32_t warps = (cols + L * E - 1) / (L * E), G = warps * L, groups = G >= 256 ? 1 : 256 / G;
+        const uint32_t ctas = (rows + groups - 1) / groups, threads = groups * G;
+        const uint32_t smem = groups * STAGES * Row<T, ALIGN, E>::image_bytes(G);
+        // as many CTAs as are resident
+        const uint32_t by_regs = 65536 / (threads * forward_registers<ALIGN, E>), by_smem = 220 * 1024 / (smem + 5 * 1024);
+        const uint32_t most = DEFAULT_SMS * (by_regs < by_smem ? by_regs : by_smem);
+        if (const int rc = el::allow_smem<norm_kernel<T, ALIGN, E, L>>(smem)) return rc;
+        return note_cuda(el::launch(norm_kernel<T, ALIGN, E, L>, dim3(ctas < most ? ctas : most), threads, smem, 1, stream,
+                                    static_cast<const T *>(x), rows, cols, ld, gamma, beta, eps, static_cast<T *>(y), ldy, mean, rstd, warps));
+    }
+};
 
 template <typename T>
 int forward(const void *x, uint64_t rows, uint64_t cols, uint64_t ld, const float *gamma, const float *beta, float eps, void *y,
@@ -541,27 +572,40 @@ int forward(const void *x, uint64_t rows, uint64_t cols, uint64_t ld, const floa
     if (cols > REGISTER_COLS)
         return note_cuda(el::launch(norm_wide_kernel<T>, dim3((uint32_t)rows), THREADS, 0, 1, stream, static_cast<const T *>(x),
                                     (uint32_t)cols, ld, gamma, beta, eps, static_cast<T *>(y), ldy, mean, rstd));
-    const bool vec = vector_rows<T>(x, ld, cols) && vector_rows<T>(y, ldy, cols);
-    auto f = vec ? (cols <= 256 ? forward_rows<T, true, 8> : forward_rows<T, true, 16>)
-                 : (cols <= 256 ? forward_rows<T, false, 8> : forward_rows<T, false, 16>);
-    return f(x, (uint32_t)rows, (uint32_t)cols, ld, gamma, beta, eps, y, ldy, mean, rstd, stream);
+    const int ax = align_of<T>(x, ld, cols), ay = align_of<T>(y, ldy, cols);
+    return with_rows<T>(ax < ay ? ax : ay, (uint32_t)cols,
+                        Forward<T>{x, (uint32_t)rows, (uint32_t)cols, ld, gamma, beta, eps, y, ldy, mean, rstd, stream});
 }
 
-template <typename T, bool VECTOR, int E>
-int backward_rows(const void *dy, uint64_t ld_dy, const void *x, uint64_t ld_x, uint32_t rows, uint32_t cols, const float *gamma,
-                  const float *mean, const float *rstd, void *dx, uint64_t ld_dx, float *part, uint32_t *parts, void *stream)
-{
-    const uint32_t warps = (cols + 32 * E - 1) / (32 * E);
-    const uint32_t groups = warps >= 16 ? 1 : (16 / warps < MAX_GROUPS ? 16 / warps : MAX_GROUPS);
-    const uint32_t ctas = (rows + groups - 1) / groups;
-    const uint32_t ring = groups * STAGES * 2 * Row<T, VECTOR, E>::image_bytes(warps * 32);
-    const uint32_t joined = groups * 8 * cols, smem = ring > joined ? ring : joined;
-    const uint32_t most = E == 8 ? MAX_PARTS : MAX_PARTS / 2;      // as many CTAs as are resident
-    *parts = ctas < most ? ctas : most;
-    if (const int rc = el::allow_smem<norm_backward_kernel<T, VECTOR, E>>(smem)) return rc;
-    return note_cuda(el::launch(norm_backward_kernel<T, VECTOR, E>, dim3(*parts), warps * groups * 32, smem, 1, stream, static_cast<const T *>(dy), ld_dy,
-                                static_cast<const T *>(x), ld_x, rows, cols, gamma, mean, rstd, static_cast<T *>(dx), ld_dx, part, warps));
-}
+template <typename T>
+struct Backward {
+    const void *dy;
+    uint64_t ld_dy;
+    const void *x;
+    uint64_t ld_x;
+    uint32_t rows, cols;
+    const float *gamma, *mean, *rstd;
+    void *dx;
+    uint64_t ld_dx;
+    float *part;
+    uint32_t *parts;
+    void *stream;
+
+    template <int ALIGN, int E, int L>
+    int operator()() const
+    {
+        const uint32_t warps = (cols + L * E - 1) / (L * E), G = warps * L;
+        const uint32_t room = E == 8 ? 384 : 512, groups = G >= room ? 1 : warps == 1 || room / G < MAX_GROUPS ? room / G : MAX_GROUPS;
+        const uint32_t ctas = (rows + groups - 1) / groups;
+        const uint32_t ring = groups * STAGES * 2 * Row<T, ALIGN, E>::image_bytes(G);
+        const uint32_t joined = groups * 8 * cols, smem = ring > joined ? ring : joined;
+        const uint32_t most = E == 8 ? MAX_PARTS : MAX_PARTS / 2;      // as many CTAs as are resident
+        *parts = ctas < most ? ctas : most;
+        if (const int rc = el::allow_smem<norm_backward_kernel<T, ALIGN, E, L>>(smem)) return rc;
+        return note_cuda(el::launch(norm_backward_kernel<T, ALIGN, E, L>, dim3(*parts), groups * G, smem, 1, stream, static_cast<const T *>(dy),
+                                    ld_dy, static_cast<const T *>(x), ld_x, rows, cols, gamma, mean, rstd, static_cast<T *>(dx), ld_dx, part, warps));
+    }
+};
 
 template <typename T>
 int backward(const void *dy, uint64_t ld_dy, const void *x, uint64_t ld_x, uint64_t rows, uint64_t cols, const float *gamma,
@@ -571,10 +615,9 @@ int backward(const void *dy, uint64_t ld_dy, const void *x, uint64_t ld_x, uint6
     uint32_t parts = parts_of(rows);
     int rc = 0;
     if (rows && cols <= REGISTER_COLS) {
-        const bool vec = vector_rows<T>(dy, ld_dy, cols) && vector_rows<T>(x, ld_x, cols) && vector_rows<T>(dx, ld_dx, cols);
-        auto f = vec ? (cols <= 256 ? backward_rows<T, true, 8> : backward_rows<T, true, 16>)
-                     : (cols <= 256 ? backward_rows<T, false, 8> : backward_rows<T, false, 16>);
-        rc = f(dy, ld_dy, x, ld_x, (uint32_t)rows, c, gamma, mean, rstd, dx, ld_dx, part, &parts, stream);
+        const int ad = align_of<T>(dy, ld_dy, cols), ax = align_of<T>(x, ld_x, cols), ao = align_of<T>(dx, ld_dx, cols);
+        const int align = ad < ax ? (ad < ao ? ad : ao) : (ax < ao ? ax : ao);
+        rc = with_rows<T>(align, c, Backward<T>{dy, ld_dy, x, ld_x, (uint32_t)rows, c, gamma, mean, rstd, dx, ld_dx, part, &parts, stream});
     } else if (rows) {
         // the column sums first: dx may overwrite dy or x
         rc = note_cuda(el::launch(norm_columns_kernel<T>, dim3((c + THREADS - 1) / THREADS, parts), THREADS, 0, 1, stream,

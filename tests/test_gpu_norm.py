@@ -129,6 +129,17 @@ def test_backward(rows, cols, ty):
         assert (np.abs(host(bg.t[:cols]) - dy.sum(0)) <= deep * np.abs(dy).sum(0) + 1e-30).all()
 
 
+MORE = [(1000, 64), (999, 100), (513, 128), (1201, 66), (3, 17), (77, 130), (41, 258), (200, 1002), (31, 2050), (5, 8190), (1, 33), (6, 65)]
+
+
+@pytest.mark.parametrize("ty", list(TYPES))
+@pytest.mark.parametrize("rows,cols", MORE)
+def test_narrow_rows_and_rows_on_four_bytes(rows, cols, ty):
+    """Several rows to a warp, the last of them missing; rows that begin on multiples of 4 bytes but not of 16."""
+    test_forward(rows, cols, ty)
+    test_backward(rows, cols, ty)
+
+
 def test_backward_against_differences():
     """Central differences of the forward formula in 64 bits (step 1e-4: error about 1e-8 of the third derivative)."""
     rng = np.random.default_rng(3)
@@ -177,7 +188,7 @@ def test_large_mean_does_not_cancel(cols):
     assert (np.abs(host(y) - (v - v.mean(1, keepdims=True)) * want[:, None]) < 0.012).all()
 
 
-@pytest.mark.parametrize("rows,cols", [(40, 512), (30, 2048), (9, 1001), (5, 9000)])
+@pytest.mark.parametrize("rows,cols", [(40, 512), (30, 2048), (9, 1001), (5, 9000), (7, 50), (6, 100)])
 def test_non_finite_rows_stay_in_their_rows(rows, cols):
     """Inf and NaN make their own row NaN; in the backward pass also the column sums, which run over all rows."""
     rng = np.random.default_rng(2)
