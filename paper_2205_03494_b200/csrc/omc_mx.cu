@@ -6,6 +6,8 @@
 // the only rounding is the conversion to E2M1.
 #include <cuda_runtime.h>
 
+#include <type_traits>
+
 #include "element.cuh"
 #include "mx_encode.cuh"
 #include "mx_format.cuh"
@@ -175,7 +177,7 @@ __device__ __forceinline__ uint32_t code_place(uint32_t col, uint32_t chunk)
 }
 
 template <typename T, bool VECTOR, bool ROWS>
-__global__ void __launch_bounds__(256)
+__global__ void __launch_bounds__(256, sizeof(T) == 4 ? 3 : 4)
 quantise_tile_kernel(const T *__restrict__ x, uint32_t rows, uint32_t cols, uint64_t ld, uint8_t *__restrict__ codes,
                      uint8_t *__restrict__ scales, uint8_t *__restrict__ codes_t, uint8_t *__restrict__ scales_t)
 {
@@ -230,19 +232,17 @@ quantise_tile_kernel(const T *__restrict__ x, uint32_t rows, uint32_t cols, uint
     // a thread takes one block of 32 rows of two neighbouring columns
     {
         const int block = tid >> 6, pair = tid & 63;
-        float2 v[32];
+        using Pair = typename std::conditional<sizeof(T) == 4, float2, uint32_t>::type;      // two columns of a row as they are stored
+        Pair p[32];
         uint32_t top_a = 0, top_b = 0;
 #pragma unroll
         for (int i = 0; i < 32; ++i) {
-            const T *p = tile + (block * 32 + i) * TILE + pair * 2;
+            p[i] = *reinterpret_cast<const Pair *>(tile + (block * 32 + i) * TILE + pair * 2);
             if constexpr (sizeof(T) == 4) {
-                v[i] = *reinterpret_cast<const float2 *>(p);
-                top_a = max_magnitude<T>(top_a, __float_as_uint(v[i].x));
-                top_b = max_magnitude<T>(top_b, __float_as_uint(v[i].y));
+                top_a = max_magnitude<T>(top_a, __float_as_uint(p[i].x));
+                top_b = max_magnitude<T>(top_b, __float_as_uint(p[i].y));
             } else {
-                const uint32_t w = *reinterpret_cast<const uint32_t *>(p);
-                top_a = max_magnitude<T>(top_a, w);
-                Word<T>::unpack(w, reinterpret_cast<float *>(v + i));
+                top_a = max_magnitude<T>(top_a, p[i]);
             }
         }
         if constexpr (sizeof(T) == 2) {
@@ -251,22 +251,28 @@ quantise_tile_kernel(const T *__restrict__ x, uint32_t rows, uint32_t cols, uint
         }
         const uint32_t sa = mx::scale_of(fp32_bits<T>(top_a)), sb = mx::scale_of(fp32_bits<T>(top_b));
         const float2 f = make_float2(mx::inverse_scale(sa), mx::inverse_scale(sb));
+        uint32_t ca[4], cb[4];
 #pragma unroll
-        for (int i = 0; i < 32; ++i) v[i] = el::mul2(v[i], f);
+        for (int i = 0; i < 4; ++i) {
+            float u[8], w[8];
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            uint32_t c[4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                float u[8];
-#pragma unroll
-                for (int j = 0; j < 8; ++j) u[j] = h ? v[8 * i + j].y : v[8 * i + j].x;
-                c[i] = (h ? sb : sa) == mx::NAN_SCALE ? 0u : mx::encode8(u);
+            for (int j = 0; j < 8; ++j) {
+                float2 v;
+                if constexpr (sizeof(T) == 4) v = p[8 * i + j];
+                else Word<T>::unpack(p[8 * i + j], reinterpret_cast<float *>(&v));
+                v = el::mul2(v, f);
+                u[j] = v.x;
+                w[j] = v.y;
             }
-            const uint32_t col = tile_column<T>(pair * 2) + h;
-            *reinterpret_cast<uint4 *>(out + code_place<T>(col, block)) = make_uint4(c[0], c[1], c[2], c[3]);
-            atom_t[(col & 31) * 16 + (col >> 5) * 4 + block] = (uint8_t)(h ? sb : sa);
+            ca[i] = sa == mx::NAN_SCALE ? 0u : mx::encode8(u);
+            cb[i] = sb == mx::NAN_SCALE ? 0u : mx::encode8(w);
         }
+        const uint32_t col = tile_column<T>(pair * 2);
+        *reinterpret_cast<uint4 *>(out + code_place<T>(col, block)) = make_uint4(ca[0], ca[1], ca[2], ca[3]);
+        *reinterpret_cast<uint4 *>(out + code_place<T>(col + 1, block)) = make_uint4(cb[0], cb[1], cb[2], cb[3]);
+        uint8_t *scale = atom_t + (col & 31) * 16 + (col >> 5) * 4 + block;      // (an even column: its neighbour is 16 bytes on)
+        scale[0] = (uint8_t)sa;
+        scale[16] = (uint8_t)sb;
     }
     __syncthreads();
 
