@@ -153,7 +153,7 @@ def check_product(got, x, w, ty):
 
 PRODUCTS = [(1, 128, 256), (1, 1, 1), (2, 130, 64), (16, 64, 2048), (17, 777, 1000), (33, 128, 31), (64, 300, 4096), (65, 257, 513),
             (128, 128, 128), (129, 511, 96), (300, 384, 800), (1000, 640, 512), (256, 256, 256), (515, 1030, 2050), (1, 2048, 8192),
-            (2300, 2600, 768), (4, 40, 8160)]
+            (2300, 2600, 768), (4, 40, 8160), (4000, 3000, 4100), (130, 300, 8192), (700, 9000, 600), (100, 129, 5000)]
 
 
 @pytest.mark.parametrize("ty", list(TYPES))
