@@ -109,15 +109,18 @@ norm_columns_kernel(const T *__restrict__ dy, uint64_t ld_dy, const T *__restric
 // A row is held by a group of G threads, E values each: 8 or 16 lanes of a warp (narrow rows: the warp works on four or
 // two rows at a time), a warp, or several warps.  Each group walks over rows of its own.  The rows ahead are on their
 // way into a ring of row images in shared memory (cp.async), so that what is in flight takes no registers.
-//   ALIGN  bytes on whose multiples every row begins and that divide its length: 16, 4 or that of one value.  Unit i G + t of a row,
-//          ALIGN bytes of it, belongs to thread t.  With 16 a thread copies and reads its own units: no barrier.  Otherwise the
+//   ALIGN  bytes on whose multiples every row begins and that divide its length: 16, 4 or that of one value.  A row's units,
+//          ALIGN bytes each, are dealt out to the threads.  With 16 a thread copies and reads its own units: no barrier.  Otherwise the
 //          image starts at the 16-byte boundary below the row (never below the matrix), and the group meets
 //          between copying and reading.
-template <typename T, int ALIGN, int E>
+template <typename T, int ALIGN, int E, int L>
 struct Row {
     static constexpr uint32_t SIZE = sizeof(T), PER = ALIGN / SIZE;   // values of a unit
     static constexpr int UNITS = E / PER;                             // of a thread
     static_assert(UNITS >= 1 && E % PER == 0, "");
+
+    // unit i of thread t, without i L: a warp's units lie together, so that the others are at constant distances
+    static __device__ __forceinline__ uint32_t first(uint32_t t) { return L == 32 ? (t & ~31u) * UNITS + (t & 31u) : t; }
 
     static __host__ __device__ constexpr uint32_t image_bytes(uint32_t G) { return G * E * SIZE + (ALIGN == 16 ? 0 : 16); }
 
@@ -129,11 +132,10 @@ struct Row {
     {
         const uint32_t dst = (uint32_t)__cvta_generic_to_shared(image);
         if constexpr (ALIGN == 16) {
+            const uint32_t u = first(t);
 #pragma unroll
-            for (int i = 0; i < UNITS; ++i) {
-                const uint32_t k = i * G + t;
-                if (k * PER < cols) copy16(dst + k * 16, row + k * PER, 16);
-            }
+            for (int i = 0; i < UNITS; ++i)
+                if ((u + i * L) * PER < cols) copy16(dst + u * 16 + i * L * 16, row + u * PER + i * L * PER, 16);
         } else {
             const uint32_t skip = (uint32_t)(reinterpret_cast<uintptr_t>(row) & 15u), total = skip + cols * SIZE;
             const uint8_t *src = reinterpret_cast<const uint8_t *>(row) - skip;
@@ -151,48 +153,51 @@ struct Row {
             }
         }
     }
-    static __device__ __forceinline__ void values(const uint8_t *image, const T *row, uint32_t t, uint32_t G, float *v)
+    static __device__ __forceinline__ void values(const uint8_t *image, const T *row, uint32_t t, float *v)
     {
         constexpr int N = el::Word<T>::N;
-        const uint8_t *p = image + (ALIGN == 16 ? 0 : reinterpret_cast<uintptr_t>(row) & 15u);      // (behind the row: never used)
+        const uint8_t *p = image + (ALIGN == 16 ? 0 : reinterpret_cast<uintptr_t>(row) & 15u) + first(t) * ALIGN;      // (behind the row: never used)
 #pragma unroll
         for (int i = 0; i < UNITS; ++i) {
             if constexpr (ALIGN == 16) {
-                const uint4 w = *reinterpret_cast<const uint4 *>(p + (i * G + t) * 16);
+                const uint4 w = *reinterpret_cast<const uint4 *>(p + i * L * 16);
                 el::Word<T>::unpack(w.x, v + i * PER);
                 el::Word<T>::unpack(w.y, v + i * PER + N);
                 el::Word<T>::unpack(w.z, v + i * PER + 2 * N);
                 el::Word<T>::unpack(w.w, v + i * PER + 3 * N);
             } else if constexpr (ALIGN == 4) {
-                el::Word<T>::unpack(*reinterpret_cast<const uint32_t *>(p + (i * G + t) * 4), v + i * PER);
+                el::Word<T>::unpack(*reinterpret_cast<const uint32_t *>(p + i * L * 4), v + i * PER);
             } else {
-                v[i] = el::to_float(*reinterpret_cast<const T *>(p + (i * G + t) * SIZE));
+                v[i] = el::to_float(*reinterpret_cast<const T *>(p + i * L * SIZE));
             }
         }
     }
-    static __device__ __forceinline__ void store(T *row, uint32_t cols, uint32_t t, uint32_t G, const float *v)
+    static __device__ __forceinline__ void store(T *row, uint32_t cols, uint32_t t, const float *v)
     {
         constexpr int N = el::Word<T>::N;
+        const uint32_t c0 = first(t) * PER;
+        row += c0;
 #pragma unroll
         for (int i = 0; i < UNITS; ++i) {
-            const uint32_t c = (i * G + t) * PER;
+            constexpr uint32_t D = L * PER;
             const float *p = v + i * PER;
-            if (c >= cols) continue;
+            if (c0 + i * D >= cols) continue;
             if constexpr (ALIGN == 16)
-                *reinterpret_cast<uint4 *>(row + c) = make_uint4(el::Word<T>::pack(p), el::Word<T>::pack(p + N), el::Word<T>::pack(p + 2 * N),
+                *reinterpret_cast<uint4 *>(row + i * D) = make_uint4(el::Word<T>::pack(p), el::Word<T>::pack(p + N), el::Word<T>::pack(p + 2 * N),
                                                                  el::Word<T>::pack(p + 3 * N));
             else if constexpr (ALIGN == 4)
-                *reinterpret_cast<uint32_t *>(row + c) = el::Word<T>::pack(p);
+                *reinterpret_cast<uint32_t *>(row + i * D) = el::Word<T>::pack(p);
             else
-                row[c] = el::from_float<T>(*p);
+                row[i * D] = el::from_float<T>(*p);
         }
     }
     // The thread's values of an FP32 vector of the row's length; 0 behind its end.
-    static __device__ __forceinline__ void vector(const float *p, uint32_t cols, uint32_t t, uint32_t G, float *v)
+    static __device__ __forceinline__ void vector(const float *p, uint32_t cols, uint32_t t, float *v)
     {
+        const uint32_t u = first(t);
 #pragma unroll
         for (int i = 0; i < UNITS; ++i) {
-            const uint32_t c = (i * G + t) * PER;
+            const uint32_t c = (u + i * L) * PER;
             if constexpr (PER % 4 == 0) {
 #pragma unroll
                 for (uint32_t j = 0; j < PER; j += 4) {
@@ -212,22 +217,24 @@ struct Row {
         }
     }
     // Sets the values behind the row's end.
-    static __device__ __forceinline__ void fill(uint32_t cols, uint32_t t, uint32_t G, float *v, float to)
+    static __device__ __forceinline__ void fill(uint32_t cols, uint32_t t, float *v, float to)
     {
+        const uint32_t u = first(t);
 #pragma unroll
         for (int i = 0; i < UNITS; ++i)
-            if ((i * G + t) * PER >= cols) {
+            if ((u + i * L) * PER >= cols) {
 #pragma unroll
                 for (uint32_t j = 0; j < PER; ++j) v[i * PER + j] = to;
             }
     }
     // Calls f(index of the value in v, column) for the values inside the row.
     template <typename F>
-    static __device__ __forceinline__ void each(uint32_t cols, uint32_t t, uint32_t G, F f)
+    static __device__ __forceinline__ void each(uint32_t cols, uint32_t t, F f)
     {
+        const uint32_t u = first(t);
 #pragma unroll
         for (int i = 0; i < UNITS; ++i) {
-            const uint32_t c = (i * G + t) * PER;
+            const uint32_t c = (u + i * L) * PER;
             if (c < cols) {
 #pragma unroll
                 for (uint32_t j = 0; j < PER; ++j) f(i * PER + j, c + j);
@@ -299,14 +306,14 @@ constexpr int MAX_GROUPS = 15;      // of several warps: named barriers 1 .. 15
 constexpr int STAGES = 3;      // row images of a group: two ahead of the one in work
 
 // Registers a thread of the forward kernel gets: what lets 1024, 768 or 512 threads share an SM.
-template <int ALIGN, int E> constexpr int forward_registers = E == 8 ? 64 : ALIGN == 16 ? 80 : 128;
+template <int ALIGN, int E> constexpr int forward_registers = E == 8 ? 64 : E == 16 && ALIGN == 16 ? 80 : 128;
 
 template <typename T, int ALIGN, int E, int L>
 __global__ void __maxnreg__((forward_registers<ALIGN, E>))
 norm_kernel(const T *x, uint32_t rows, uint32_t cols, uint64_t ld, const float *__restrict__ gamma, const float *__restrict__ beta, float eps,
             T *y, uint64_t ldy, float *__restrict__ mean_out, float *__restrict__ rstd_out, uint32_t warps)
 {
-    using R = Row<T, ALIGN, E>;
+    using R = Row<T, ALIGN, E, L>;
     constexpr int S = STAGES;
     __shared__ float room[L == 32 ? 16 * 64 : 1];
     extern __shared__ __align__(16) uint8_t images[];
@@ -329,8 +336,8 @@ norm_kernel(const T *x, uint32_t rows, uint32_t cols, uint64_t ld, const float *
 #pragma unroll
     for (int s = 0; s < S - 1; ++s) fetch(s);
     float ga[E], be[E];
-    R::vector(gamma, cols, t, G, ga);
-    R::vector(beta, cols, t, G, be);
+    R::vector(gamma, cols, t, ga);
+    R::vector(beta, cols, t, be);
     uint32_t now = 0, ahead = S - 1;
     const uint32_t neighbour = L < 32 ? g.index % (32 / L) : 0u;      // a warp's groups go on as long as the first has a row
     for (uint32_t row = first; row - neighbour < rows; row += step) {
@@ -338,16 +345,16 @@ norm_kernel(const T *x, uint32_t rows, uint32_t cols, uint64_t ld, const float *
         wait_copies<S - 1>();
         if (ALIGN != 16) g.meet();
         float v[E];
-        R::values(ring + now * bytes, row_x, t, G, v);
+        R::values(ring + now * bytes, row_x, t, v);
         now = now + 1 == S ? 0 : now + 1;
         ahead = ahead + 1 == S ? 0 : ahead + 1;
-        if (!whole) R::fill(cols, t, G, v, 0.f);
+        if (!whole) R::fill(cols, t, v, 0.f);
         float2 *p = reinterpret_cast<float2 *>(v);
         float2 s = twice(0.f);
 #pragma unroll
         for (int i = 0; i < E / 2; ++i) s = add2(s, p[i]);
         const float mean = g.sum(s.x + s.y) * inv;
-        if (!whole) R::fill(cols, t, G, v, mean);
+        if (!whole) R::fill(cols, t, v, mean);
         s = twice(0.f);
 #pragma unroll
         for (int i = 0; i < E / 2; ++i) {
@@ -359,7 +366,7 @@ norm_kernel(const T *x, uint32_t rows, uint32_t cols, uint64_t ld, const float *
         for (int i = 0; i < E / 2; ++i)
             p[i] = fma2(mul2(p[i], twice(rstd)), make_float2(ga[2 * i], ga[2 * i + 1]), make_float2(be[2 * i], be[2 * i + 1]));
         if (L < 32 && row >= rows) break;                  // the neighbours' last row
-        R::store(row_y, cols, t, G, v);
+        R::store(row_y, cols, t, v);
         if (t == 0) {
             if (mean_out) mean_out[row] = mean;
             if (rstd_out) rstd_out[row] = rstd;
@@ -376,7 +383,7 @@ norm_backward_kernel(const T *dy, uint64_t ld_dy, const T *x, uint64_t ld_x, uin
                      const float *__restrict__ mean_in, const float *__restrict__ rstd_in, T *dx, uint64_t ld_dx, float *__restrict__ part,
                      uint32_t warps)
 {
-    using R = Row<T, ALIGN, E>;
+    using R = Row<T, ALIGN, E, L>;
     constexpr int S = STAGES;
     __shared__ float room[L == 32 ? 16 * 64 : 1];
     extern __shared__ __align__(16) uint8_t images[];
@@ -422,13 +429,13 @@ norm_backward_kernel(const T *dy, uint64_t ld_dy, const T *x, uint64_t ld_x, uin
         wait_copies<S - 1>();
         if (ALIGN != 16) g.meet();
         float h[E], d[E];
-        R::values(ring + now * 2 * bytes, row_x, t, G, h);
-        R::values(ring + now * 2 * bytes + bytes, row_d, t, G, d);
+        R::values(ring + now * 2 * bytes, row_x, t, h);
+        R::values(ring + now * 2 * bytes + bytes, row_d, t, d);
         now = now + 1 == S ? 0 : now + 1;
         ahead = ahead + 1 == S ? 0 : ahead + 1;
         if (!whole) {
-            R::fill(cols, t, G, h, mu);
-            R::fill(cols, t, G, d, 0.f);
+            R::fill(cols, t, h, mu);
+            R::fill(cols, t, d, 0.f);
         }
         if (L < 32 && row >= rows) {                       // no row of its own: nothing to add to the columns
 #pragma unroll
@@ -436,7 +443,7 @@ norm_backward_kernel(const T *dy, uint64_t ld_dy, const T *x, uint64_t ld_x, uin
             mu = rs = 0.f;
         }
         float ga[E];                                       // from L1 each time: registers are short here
-        R::vector(gamma, cols, t, G, ga);
+        R::vector(gamma, cols, t, ga);
         float2 *ph = reinterpret_cast<float2 *>(h), *pd = reinterpret_cast<float2 *>(d);
         float2 s1 = twice(0.f), s2 = twice(0.f);
 #pragma unroll
@@ -453,7 +460,7 @@ norm_backward_kernel(const T *dy, uint64_t ld_dy, const T *x, uint64_t ld_x, uin
 #pragma unroll
         for (int i = 0; i < E / 2; ++i) pd[i] = mul2(fma2(ph[i], m2, add2(pd[i], m1)), twice(rs));
         if (L < 32 && row >= rows) break;                  // the neighbours' last row
-        R::store(row_dx, cols, t, G, d);
+        R::store(row_dx, cols, t, d);
         if (ALIGN != 16) {
             row_x += step * ld_x;
             row_d += step * ld_dy;
@@ -463,7 +470,7 @@ norm_backward_kernel(const T *dy, uint64_t ld_dy, const T *x, uint64_t ld_x, uin
     // the groups' sums side by side where the images were (2 x cols each), added in the groups' order
     __syncthreads();
     float *columns = reinterpret_cast<float *>(images);
-    R::each(cols, t, G, [&](int i, uint32_t c) {
+    R::each(cols, t, [&](int i, uint32_t c) {
         columns[g.index * 2 * cols + c] = i & 1 ? sg[i / 2].y : sg[i / 2].x;
         columns[(g.index * 2 + 1) * cols + c] = i & 1 ? sb[i / 2].y : sb[i / 2].x;
     });
@@ -553,9 +560,14 @@ struct Forward {
     template <int ALIGN, int E, int L>
     int operator()() const
     {
+        // Without sums to keep over the rows there is room for 32 values a thread (8000 x 8192 BF16 61 us with 16, 42 us with 32;
+        // 32768 x 2048 46.5 and 44.8 us); off the 16-byte boundaries they spill.
+        if constexpr (ALIGN == 16 && E == 16) {
+            if (cols > 512) return this->template operator()<16, 32, 32>();
+        }
         const uint32_t warps = (cols + L * E - 1) / (L * E), G = warps * L, groups = G >= 256 ? 1 : 256 / G;
         const uint32_t ctas = (rows + groups - 1) / groups, threads = groups * G;
-        const uint32_t smem = groups * STAGES * Row<T, ALIGN, E>::image_bytes(G);
+        const uint32_t smem = groups * STAGES * Row<T, ALIGN, E, L>::image_bytes(G);
         // as many CTAs as are resident
         const uint32_t by_regs = 65536 / (threads * forward_registers<ALIGN, E>), by_smem = 220 * 1024 / (smem + 5 * 1024);
         const uint32_t most = DEFAULT_SMS * (by_regs < by_smem ? by_regs : by_smem);
@@ -597,7 +609,7 @@ struct Backward {
         const uint32_t warps = (cols + L * E - 1) / (L * E), G = warps * L;
         const uint32_t room = E == 8 ? 384 : 512, groups = G >= room ? 1 : warps == 1 || room / G < MAX_GROUPS ? room / G : MAX_GROUPS;
         const uint32_t ctas = (rows + groups - 1) / groups;
-        const uint32_t ring = groups * STAGES * 2 * Row<T, ALIGN, E>::image_bytes(G);
+        const uint32_t ring = groups * STAGES * 2 * Row<T, ALIGN, E, L>::image_bytes(G);
         const uint32_t joined = groups * 8 * cols, smem = ring > joined ? ring : joined;
         const uint32_t most = E == 8 ? MAX_PARTS : MAX_PARTS / 2;      // as many CTAs as are resident
         *parts = ctas < most ? ctas : most;
