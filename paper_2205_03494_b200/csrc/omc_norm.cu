@@ -52,15 +52,18 @@ norm_wide_kernel(const T *x, uint32_t cols, uint64_t ld, const float *__restrict
     T *yr = y + row * ldy;
     float s = 0.f;
     for (uint32_t c = threadIdx.x; c < cols; c += THREADS) s += el::to_float(xr[c]);
-    const float mean = cta_sum(s, room) / (float)cols;
+    const float near = cta_sum(s, room) / (float)cols;
     s = 0.f;
+    float s1 = 0.f;
     for (uint32_t c = threadIdx.x; c < cols; c += THREADS) {
-        const float d = el::to_float(xr[c]) - mean;
+        const float d = el::to_float(xr[c]) - near;
+        s1 += d;
         s = __fmaf_rn(d, d, s);
     }
-    const float rstd = 1.f / sqrtf(cta_sum(s, room) / (float)cols + eps);
+    const float off = cta_sum(s1, room) / (float)cols, mean = near + off;      // (the first mean corrected)
+    const float rstd = __frsqrt_rn(fmaxf(__fmaf_rn(-off, off, cta_sum(s, room) / (float)cols), 0.f) + eps);
     for (uint32_t c = threadIdx.x; c < cols; c += THREADS)
-        yr[c] = el::from_float<T>(__fmaf_rn((el::to_float(xr[c]) - mean) * rstd, gamma[c], beta[c]));
+        yr[c] = el::from_float<T>(__fmaf_rn((el::to_float(xr[c]) - near - off) * rstd, gamma[c], beta[c]));
     if (threadIdx.x == 0) {
         if (mean_out) mean_out[row] = mean;
         if (rstd_out) rstd_out[row] = rstd;
@@ -359,18 +362,23 @@ norm_kernel(const T *x, uint32_t rows, uint32_t cols, uint64_t ld, const float *
         float2 s = twice(0.f);
 #pragma unroll
         for (int i = 0; i < E / 2; ++i) s = add2(s, p[i]);
-        const float mean = g.sum(s.x + s.y) * inv;
-        if (!whole) R::fill(cols, t, v, mean);
+        // the mean of the deviations from the first mean corrects it: a row of equal values leaves zeros, not the
+        // rounding of the sum times 1 / sqrt(eps)
+        const float near = g.sum(s.x + s.y) * inv;
+        if (!whole) R::fill(cols, t, v, near);
         s = twice(0.f);
+        float2 s1 = twice(0.f);
 #pragma unroll
         for (int i = 0; i < E / 2; ++i) {
-            p[i] = add2(p[i], twice(-mean));
+            p[i] = add2(p[i], twice(-near));
+            s1 = add2(s1, p[i]);
             s = fma2(p[i], p[i], s);
         }
-        const float rstd = __frsqrt_rn(g.sum(s.x + s.y) * inv + eps);
+        const float2 m = g.sum2(s1.x + s1.y, s.x + s.y);
+        const float off = m.x * inv, mean = near + off, rstd = __frsqrt_rn(fmaxf(__fmaf_rn(-off, off, m.y * inv), 0.f) + eps);
 #pragma unroll
         for (int i = 0; i < E / 2; ++i)
-            p[i] = fma2(mul2(p[i], twice(rstd)), make_float2(ga[2 * i], ga[2 * i + 1]), make_float2(be[2 * i], be[2 * i + 1]));
+            p[i] = fma2(mul2(add2(p[i], twice(-off)), twice(rstd)), make_float2(ga[2 * i], ga[2 * i + 1]), make_float2(be[2 * i], be[2 * i + 1]));
         if (L < 32 && row >= rows) break;                  // the neighbours' last row
         R::store(row_y, cols, t, v);
         if (t == 0) {

@@ -172,6 +172,20 @@ def test_backward_against_differences():
         assert abs((loss(x, g, b + e) - loss(x, g, b - e)) / (2 * h) - got_b[c]) < 1e-5
 
 
+@pytest.mark.parametrize("cols", [33, 100, 300, 1000, 1023, 2048, 5000, 9000])
+def test_rows_of_equal_values_give_the_bias(cols):
+    """Padding frames: the deviations are zero, whatever the sum rounds to.  A first mean that is off by D u |x| leaves
+    D u |x| u after its correction, times 1 / sqrt(eps) = 316 and a gain below 2: under 1e-9 for |x| < 2, so that y is the bias
+    to half a unit of the last place."""
+    x = torch.tensor([0.3, -1.7, 0.1, 1.2345], device="cuda")[:, None].expand(4, cols).contiguous()
+    gamma, beta = torch.rand(cols, device="cuda") + 0.5, torch.rand(cols, device="cuda") + 0.5
+    y, mean = torch.empty_like(x), torch.empty(4, device="cuda")
+    omc.layer_norm(x.data_ptr(), omc.F32, 4, cols, cols, gamma.data_ptr(), beta.data_ptr(), EPS, y.data_ptr(), cols, mean.data_ptr(), 0,
+                   stream=stream())
+    assert np.abs(host(y) - host(beta)).max() < 2e-7
+    assert (np.abs(host(mean) - host(x[:, 0])) <= 2.0 ** -23 * np.abs(host(x[:, 0]))).all()
+
+
 @pytest.mark.parametrize("cols", [512, 1000, 2048, 9000])
 def test_large_mean_does_not_cancel(cols):
     """Mean 1000, deviation 1: the variance is taken around the mean, not as a difference of large squares."""
