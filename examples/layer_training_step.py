@@ -61,7 +61,7 @@ class Layer:
         return arena[self.plan.full_off[i]:self.plan.full_off[i] + self.plan.numel[i]]
 
     def load(self):
-        """This round's weights: decompressed from the store, the matrix quantised along both axes."""
+        """The current weights: decompressed from the store, the matrix quantised along both axes."""
         p, st = self.plan, self.stream
         p.decompress(self.packed.data_ptr(), self.resid.data_ptr(), self.sb.data_ptr(), self.full.data_ptr(), stream=st)
         omc.mx_quantise(self.view(self.full, 0).data_ptr(), omc.F32, self.n, self.k, self.k, *[t.data_ptr() for t in self.w + self.wt], stream=st)
