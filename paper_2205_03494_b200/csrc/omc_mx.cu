@@ -41,7 +41,7 @@ __device__ __forceinline__ uint32_t gather_scales(uint32_t scale, int lane)
 // A CTA of the row kernels takes a strip of columns, 32 bytes of values a lane (blockIdx.x), of eight rows at a time, a row a
 // warp, and walks down the matrix: from row to row a warp's addresses move by constants.  It asks for the next AHEAD
 // rows' pieces while it works on one.
-constexpr int AHEAD = 3;
+template <bool VECTOR> constexpr int AHEAD = VECTOR ? 3 : 2;                   // (with three, turned rows spill: 16384 x 8191 BF16 100 us, with two 79)
 template <typename T> constexpr int LANE_VALUES = 32 / (int)sizeof(T);         // 8 or 16
 template <typename T> constexpr uint32_t STRIP = 32 * LANE_VALUES<T>;          // columns: 256 or 512
 // CTAs on an SM, as the registers of the pieces on their way allow.
@@ -59,7 +59,7 @@ __device__ __forceinline__ uint64_t row_offset(uint32_t r, uint32_t ksteps)
 // only partly inside are fetched alone (lane 0 the first, lane 1 the last): nothing outside the row is read.
 template <typename T>
 struct Turned {
-    static constexpr int E = LANE_VALUES<T>, PLACES = 4 / (int)sizeof(T);      // places of a word
+    static constexpr int PLACES = 4 / (int)sizeof(T);      // of a word
     uint32_t w[8], edge;
 
     static __device__ __forceinline__ uint32_t odd(const T *row) { return PLACES == 2 ? (uint32_t)(reinterpret_cast<uintptr_t>(row) >> 1) & 1u : 0u; }
@@ -123,8 +123,8 @@ quantise_rows_kernel(const T *__restrict__ x, uint32_t rows, uint32_t cols, uint
     const bool inside = col / 2 < rb, stores = lane % (128 / E) == 0 && block / 8 < ksteps;
     uint8_t *const strip = scales + (uint64_t)(block / 8) * 1024 + (block / 4 & 1) * 512;
     el::enter_stream_order();
-    uint32_t w[AHEAD][8];
-    Turned<T> t[VECTOR ? 1 : AHEAD];
+    uint32_t w[VECTOR ? AHEAD<VECTOR> : 1][8];
+    Turned<T> t[VECTOR ? 1 : AHEAD<VECTOR>];
     auto fetch = [&](int i) {
         if (coming < rows) {
             if constexpr (VECTOR) load<T, true, E>(src, lane * E, n, w[i]);
@@ -134,10 +134,10 @@ quantise_rows_kernel(const T *__restrict__ x, uint32_t rows, uint32_t cols, uint
         src += src_step;
     };
 #pragma unroll
-    for (int i = 0; i < AHEAD; ++i) fetch(i);
+    for (int i = 0; i < AHEAD<VECTOR>; ++i) fetch(i);
     while (row < rows) {
 #pragma unroll
-        for (int i = 0; i < AHEAD; ++i) {
+        for (int i = 0; i < AHEAD<VECTOR>; ++i) {
             if (row >= rows) break;
             uint32_t scale, c[E / 8];
             if constexpr (!VECTOR) {
@@ -195,38 +195,60 @@ quantise_tile_kernel(const T *__restrict__ x, uint32_t rows, uint32_t cols, uint
     const uint64_t rb = mx::row_bytes(cols), rb_t = mx::row_bytes(rows);
     el::enter_stream_order();
 
-    // 8 or 16 lanes take 128 columns of a row, 32 bytes a lane; four rows are asked for at a time
+    // 8 or 16 lanes take 128 columns of a row, 32 bytes a lane
     constexpr int E = LANE_VALUES<T>, LANES = TILE / E, STEP = 256 / LANES, BATCH = 4;
     const uint32_t lane_col = (tid % LANES) * E, col = c0 + lane_col;
+    auto put_row = [&](uint32_t r, const uint32_t *w) {      // codes and scales along row r of the tile
+        uint32_t scale, c[E / 8];
+        encode_block<T, E>(w, c, scale);
+        if (r0 + r < rows && col / 2 < rb) {
+            uint8_t *to = codes + (r0 + r) * rb + col / 2;
+            if constexpr (E == 16) *reinterpret_cast<uint2 *>(to) = make_uint2(c[0], c[1]);
+            else *reinterpret_cast<uint32_t *>(to) = c[0];
+        }
+        const uint32_t s = gather_scales<E>(scale, lane);
+        if (tid % LANES == 0) *reinterpret_cast<uint32_t *>(atom + (r & 31) * 16 + (r >> 5) * 4) = s;
+    };
+    if constexpr (VECTOR) {
+        // four rows are asked for at a time, and encoded along the rows on their way to shared memory
 #pragma unroll
-    for (int i0 = 0; i0 < TILE / STEP; i0 += BATCH) {
-        uint32_t w[BATCH][8];
+        for (int i0 = 0; i0 < TILE / STEP; i0 += BATCH) {
+            uint32_t w[BATCH][8];
 #pragma unroll
-        for (int i = 0; i < BATCH; ++i) {
-            const uint32_t r = r0 + (i0 + i) * STEP + tid / LANES;
-            if (r < rows) {
-                load<T, VECTOR, E>(x + (uint64_t)r * ld, col, cols, w[i]);
-            } else {
+            for (int i = 0; i < BATCH; ++i) {
+                const uint32_t r = r0 + (i0 + i) * STEP + tid / LANES;
+                if (r < rows) {
+                    load<T, true, E>(x + (uint64_t)r * ld, col, cols, w[i]);
+                } else {
 #pragma unroll
-                for (int j = 0; j < 8; ++j) w[i][j] = 0u;
+                    for (int j = 0; j < 8; ++j) w[i][j] = 0u;
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < BATCH; ++i) {
+                const uint32_t r = (i0 + i) * STEP + tid / LANES;
+                T *dst = tile + r * TILE + lane_col / 2;
+                *reinterpret_cast<uint4 *>(dst) = make_uint4(w[i][0], w[i][1], w[i][2], w[i][3]);
+                *reinterpret_cast<uint4 *>(dst + TILE / 2) = make_uint4(w[i][4], w[i][5], w[i][6], w[i][7]);
+                if constexpr (ROWS) put_row(r, w[i]);
             }
         }
-#pragma unroll
-        for (int i = 0; i < BATCH; ++i) {
-            const uint32_t r = (i0 + i) * STEP + tid / LANES;
-            T *dst = tile + r * TILE + lane_col / 2;
-            *reinterpret_cast<uint4 *>(dst) = make_uint4(w[i][0], w[i][1], w[i][2], w[i][3]);
-            *reinterpret_cast<uint4 *>(dst + TILE / 2) = make_uint4(w[i][4], w[i][5], w[i][6], w[i][7]);
-            if constexpr (ROWS) {
-                uint32_t scale, c[E / 8];
-                encode_block<T, E>(w[i], c, scale);
-                if (r0 + r < rows && col / 2 < rb) {
-                    uint8_t *to = codes + (r0 + r) * rb + col / 2;
-                    if constexpr (E == 16) *reinterpret_cast<uint2 *>(to) = make_uint2(c[0], c[1]);
-                    else *reinterpret_cast<uint32_t *>(to) = c[0];
-                }
-                const uint32_t s = gather_scales<E>(scale, lane);
-                if (tid % LANES == 0) *reinterpret_cast<uint32_t *>(atom + (r & 31) * 16 + (r >> 5) * 4) = s;
+    } else {
+        // off the 16-byte boundaries neighbouring lanes take neighbouring values, a column a thread
+        const uint32_t c = tid % TILE, half = LANE_VALUES<T> / 2, place = c / (2 * half) * half + c % half + (c / half & 1) * (TILE / 2);
+        const T *src = x + (uint64_t)(r0 + tid / TILE) * ld + c0 + c;
+#pragma unroll 16
+        for (uint32_t r = tid / TILE; r < TILE; r += 2, src += 2 * ld)
+            tile[r * TILE + place] = r0 + r < rows && c0 + c < cols ? *src : el::from_float<T>(0.f);
+        if constexpr (ROWS) {
+            __syncthreads();
+#pragma unroll 2
+            for (int i = 0; i < TILE / STEP; ++i) {
+                const uint32_t r = i * STEP + tid / LANES;
+                const T *row = tile + r * TILE + lane_col / 2;
+                const uint4 a = *reinterpret_cast<const uint4 *>(row), b = *reinterpret_cast<const uint4 *>(row + TILE / 2);
+                const uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+                put_row(r, w);
             }
         }
     }
