@@ -363,9 +363,23 @@ dequantise_kernel(const uint8_t *__restrict__ codes, const uint8_t *__restrict__
             T *mine = turned[threadIdx.x >> 5];
             const uint32_t n = min(256u, cols - blockIdx.x * 256);
             const uint32_t odd = sizeof(T) == 2 ? (uint32_t)(reinterpret_cast<uintptr_t>(to) >> 1) & 1u : 0u;      // values before the first boundary
-            __syncwarp();
+            // value e goes to place odd + e: with odd = 1 a lane's words are its own moved by a half, led by its neighbour's last value
+            uint32_t w[8 / N];
 #pragma unroll
-            for (int j = 0; j < 8; ++j) mine[odd + lane * 8 + j] = el::from_float<T>(v[j]);      // value e at odd + e
+            for (int j = 0; j < 8 / N; ++j) w[j] = Word<T>::pack(v + N * j);
+            __syncwarp();
+            if constexpr (sizeof(T) == 2) {
+                const uint32_t before = __shfl_up_sync(0xFFFFFFFFu, w[3], 1);
+                if (odd) {
+                    if (lane == 31) mine[256] = el::from_float<T>(v[7]);
+                    w[3] = __byte_perm(w[2], w[3], 0x5432);
+                    w[2] = __byte_perm(w[1], w[2], 0x5432);
+                    w[1] = __byte_perm(w[0], w[1], 0x5432);
+                    w[0] = __byte_perm(before, w[0], 0x5432);
+                }
+            }
+#pragma unroll
+            for (int j = 0; j < 8 / N; j += 4) *reinterpret_cast<uint4 *>(mine + lane * 8 + j * N) = make_uint4(w[j], w[j + 1], w[j + 2], w[j + 3]);
             __syncwarp();
             if constexpr (sizeof(T) == 2) {
                 // pair p: places 2 p and 2 p + 1, values 2 p - odd and 2 p + 1 - odd
