@@ -321,43 +321,54 @@ quantise_tile_kernel(const T *__restrict__ x, uint32_t rows, uint32_t cols, uint
     }
 }
 
-// A warp takes 256 columns of a row.  Rows off the 16-byte boundaries are turned in shared memory, so that neighbouring
-// lanes store neighbouring values (16-bit types in pairs that lie on 4-byte boundaries).
+// A warp takes a strip of a row, 32 bytes of values a lane, stored at once: two 16-byte stores would write every 32-byte
+// sector in two halves (8192 x 2048 FP32 17 us instead of 11).  Rows off the 16-byte boundaries, 256 columns at a time, are
+// turned in shared memory, so that neighbouring lanes store neighbouring values (16-bit types in pairs that lie on 4-byte boundaries).
+template <typename T, bool VECTOR> constexpr uint32_t VALUES_STRIP = VECTOR ? STRIP<T> : 256;
+
 template <typename T, bool VECTOR>
 __global__ void __launch_bounds__(32 * WARPS)
 dequantise_kernel(const uint8_t *__restrict__ codes, const uint8_t *__restrict__ scales, uint32_t rows, uint32_t cols,
                   T *__restrict__ out, uint64_t ld)
 {
-    constexpr int N = Word<T>::N;
+    constexpr int N = Word<T>::N, E = VALUES_STRIP<T, VECTOR> / 32;
     __shared__ __align__(16) T turned[VECTOR ? 1 : WARPS][VECTOR ? 8 : 256 + 8];
     const uint32_t ksteps = (cols + 255) / 256;
     const int lane = threadIdx.x & 31;
     const uint64_t rb = mx::row_bytes(cols);
-    const uint32_t col = blockIdx.x * 256 + lane * 8;
+    const uint32_t col = blockIdx.x * VALUES_STRIP<T, VECTOR> + lane * E;
     el::enter_stream_order();
     for (uint32_t row = blockIdx.y * WARPS + (threadIdx.x >> 5); row < rows; row += gridDim.y * WARPS) {
-        float v[8];
+        float v[E];
         if (col < cols) {
-            mx::decode8(*reinterpret_cast<const uint32_t *>(codes + row * rb + col / 2), v);
-            const float2 s = el::twice(mx::scale_value(scales[mx::scale_offset(row, blockIdx.x * 8 + (lane >> 2), ksteps)]));
+            const uint8_t *src = codes + row * rb + col / 2;
+            const float2 s = el::twice(mx::scale_value(scales[mx::scale_offset(row, col / 32, ksteps)]));
+            if constexpr (E == 16) {
+                const uint2 c = *reinterpret_cast<const uint2 *>(src);
+                mx::decode8(c.x, v);
+                mx::decode8(c.y, v + 8);
+            } else {
+                mx::decode8(*reinterpret_cast<const uint32_t *>(src), v);
+            }
 #pragma unroll
-            for (int j = 0; j < 4; ++j) reinterpret_cast<float2 *>(v)[j] = el::mul2(reinterpret_cast<float2 *>(v)[j], s);
+            for (int j = 0; j < E / 2; ++j) reinterpret_cast<float2 *>(v)[j] = el::mul2(reinterpret_cast<float2 *>(v)[j], s);
         }
-        T *to = out + row * ld + blockIdx.x * 256;
-        if (VECTOR) {
-            if (N == 1 && col + 8 <= cols && (reinterpret_cast<uintptr_t>(to) & 31u) == 0) {
-                // whole 32-byte sectors: two 16-byte stores would write every sector in two halves
-                asm volatile("st.global.v8.f32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
-                             ::"l"(to + lane * 8), "f"(v[0]), "f"(v[1]), "f"(v[2]), "f"(v[3]), "f"(v[4]), "f"(v[5]), "f"(v[6]), "f"(v[7]) : "memory");
-            } else if (col + 8 <= cols) {
+        T *to = out + row * ld + blockIdx.x * VALUES_STRIP<T, VECTOR>;
+        if constexpr (VECTOR) {
+            T *dst = to + lane * E;
+            uint32_t w[8];
 #pragma unroll
-                for (int j = 0; j < 8; j += 4 * N)
-                    *reinterpret_cast<uint4 *>(to + lane * 8 + j) = make_uint4(Word<T>::pack(v + j), Word<T>::pack(v + j + N),
-                                                                               Word<T>::pack(v + j + 2 * N), Word<T>::pack(v + j + 3 * N));
+            for (int j = 0; j < 8; ++j) w[j] = Word<T>::pack(v + N * j);
+            if (col + E <= cols && (reinterpret_cast<uintptr_t>(dst) & 31u) == 0) {
+                asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
+                             ::"l"(dst), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]), "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7]) : "memory");
+            } else if (col + E <= cols) {
+                *reinterpret_cast<uint4 *>(dst) = make_uint4(w[0], w[1], w[2], w[3]);
+                *reinterpret_cast<uint4 *>(dst + E / 2) = make_uint4(w[4], w[5], w[6], w[7]);
             } else {
 #pragma unroll
-                for (int j = 0; j < 8; ++j)
-                    if (col + j < cols) to[lane * 8 + j] = el::from_float<T>(v[j]);
+                for (int j = 0; j < E; ++j)
+                    if (col + j < cols) dst[j] = el::from_float<T>(v[j]);
             }
         } else {
             T *mine = turned[threadIdx.x >> 5];
@@ -433,7 +444,7 @@ template <typename T, bool VECTOR>
 int dequantise(const uint8_t *codes, const uint8_t *scales, uint32_t rows, uint32_t cols, void *out, uint64_t ld, void *stream)
 {
     const uint32_t groups = (rows + WARPS - 1) / WARPS;
-    return note_cuda(el::launch(dequantise_kernel<T, VECTOR>, dim3((cols + 255) / 256, groups < 65535 ? groups : 65535), 32 * WARPS, 0, 1, stream,
+    return note_cuda(el::launch(dequantise_kernel<T, VECTOR>, dim3((cols + VALUES_STRIP<T, VECTOR> - 1) / VALUES_STRIP<T, VECTOR>, groups < 65535 ? groups : 65535), 32 * WARPS, 0, 1, stream,
                                 codes, scales, rows, cols, static_cast<T *>(out), ld));
 }
 
