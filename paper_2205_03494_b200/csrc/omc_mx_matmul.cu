@@ -257,8 +257,8 @@ mx_matmul_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constan
             const uint32_t d = tmem_base + buf * C::ACC1;
             for (uint32_t k = k_begin; k < k_end; ++k, ++it) {
                 const int s = it % NS;
-                ok = mbar_wait(full(s), (it / NS) & 1u, WAIT_LIMIT);
-                ok = ok && mbar_wait(scaled(it % C::SLOTS), (it / C::SLOTS) & 1u, WAIT_LIMIT);
+                ok = mbar_wait_held(full(s), (it / NS) & 1u);
+                ok = ok && mbar_wait_held(scaled(it % C::SLOTS), (it / C::SLOTS) & 1u);
                 if (!ok) break;
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
                 const uint32_t a = base + s * C::STAGE, b = a + TILE_W_BYTES;
@@ -276,7 +276,7 @@ mx_matmul_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constan
         for (uint32_t it = 0; it < steps; ++it) {
             const int s = it % NS;
             if (it >= (uint32_t)C::SLOTS) ok = mbar_wait(empty((it - C::SLOTS) % NS), ((it - C::SLOTS) / NS) & 1u, WAIT_LIMIT);      // columns are free
-            ok = ok && mbar_wait(full(s), (it / NS) & 1u, WAIT_LIMIT);
+            ok = ok && mbar_wait_held(full(s), (it / NS) & 1u);
             ok = __all_sync(0xFFFFFFFFu, ok);
             if (!ok) break;
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
@@ -300,7 +300,7 @@ mx_matmul_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constan
             const uint32_t buf = lt & 1u;
             uint32_t tn, tm;
             tile_of(t, tiles_n, tiles_m, tn, tm);
-            ok = mbar_wait(acc_full(buf), (lt >> 1) & 1u, WAIT_LIMIT);
+            ok = mbar_wait_held(acc_full(buf), (lt >> 1) & 1u);
             ok = __all_sync(0xFFFFFFFFu, ok);
             if (t + step >= ntiles) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
             if (!ok || splits > 1) break;
@@ -484,7 +484,7 @@ mx_matmul_narrow_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_
         const uint32_t steps = k_end - k_begin;
         auto bring_scales = [&](uint32_t it) {            // its columns were last read NS steps ago, before the stage was refilled
             const int s = it % NS;
-            if (!mbar_wait(full(s), (it / NS) & 1u, WAIT_LIMIT)) return false;
+            if (!mbar_wait_held(full(s), (it / NS) & 1u)) return false;
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
             const uint32_t sc = base + s * C::STAGE + TILE_W_BYTES + C::TILE_X_BYTES;
             const uint32_t ta = tmem_base + C::D_COLS + s * 2 * SCALE_COLS, tb = ta + SCALE_COLS;
@@ -542,7 +542,7 @@ mx_matmul_narrow_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_
     if (warp >= 2) {
         asm volatile("bar.sync 1, 160;" ::: "memory");
         read_slot();
-        ok = mbar_wait(done, 0u, WAIT_LIMIT) && ok;
+        ok = mbar_wait_held(done, 0u) && ok;
         ok = __all_sync(0xFFFFFFFFu, ok);
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
     }

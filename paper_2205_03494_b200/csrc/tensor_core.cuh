@@ -38,6 +38,21 @@ __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, uint32_
     }
     return false;
 }
+// The same for waits that may be long: a poll lets the hardware hold the thread for up to 10 us (it goes on as soon as the phase
+// completes), which issues fewer instructions meanwhile; the limit is then about a second.
+__device__ __forceinline__ bool mbar_wait_held(uint32_t bar, uint32_t parity)
+{
+    for (uint32_t i = 0; i < (1u << 17); ++i) {
+        uint32_t ok;
+        asm volatile(
+            "{\n\t.reg .pred p;\n\t"
+            "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n\t"
+            "selp.u32 %0, 1, 0, p;\n\t}"
+            : "=r"(ok) : "r"(bar), "r"(parity), "r"(10000u) : "memory");
+        if (ok) return true;
+    }
+    return false;
+}
 __device__ __forceinline__ void tma_load_2d(uint32_t dst, const CUtensorMap *map, int x, int y, uint32_t bar)
 {
     asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
