@@ -4,7 +4,7 @@
 // or four lanes, so that the largest magnitude takes one or two shuffles; along the columns a tile of 128 x 128 goes
 // through shared memory and a thread holds whole blocks.  The scale is a power of two, so that scaling is exact and
 // the only rounding is the conversion to E2M1.
-// Memory bounds the kernels along the rows and back (16384 x 8192 BF16 52 us, 6.5 TB/s; 8192 x 2048 FP32 back 11.8 us, 6.4 TB/s:
+// Memory bounds the kernels along the rows and back (16384 x 8192 BF16 52 us, 6.5 TB/s; 8192 x 2048 FP32 back 11.0 us, 6.9 TB/s:
 // the rate of a plain copy); both ways at once the instructions do (8192 x 8192 BF16 40 us, 5.2 TB/s; 8192 x 2048 FP32
 // 17.7 us, 4.8 TB/s): each value is scaled and rounded twice.  Copying the tile past the registers (cp.async) was slower, 54 us.
 #include <cuda_runtime.h>
