@@ -407,7 +407,7 @@ int omc_mx_quantise(const void *x, int type, uint64_t rows, uint64_t cols, uint6
 
 /*
  * omc_mx_dequantise -- the values of a quantised rows x cols matrix, rounded to `type` (FP32 and BF16
- * hold every value of the format but BF16's and FP32's own underflow; FP16 saturates to Inf).
+ * hold all of them below 2^128, larger ones become Inf; FP16 rounds and overflows as usual).
  */
 int omc_mx_dequantise(const uint8_t *codes, const uint8_t *scales, uint64_t rows, uint64_t cols, void *out, int type,
                       uint64_t ld, void *stream);
@@ -429,7 +429,8 @@ int omc_mx_matmul(const uint8_t *x_codes, const uint8_t *x_scales, uint64_t M, c
  * omc_mx_linear -- the forward product from activations that are not quantised yet: exactly
  * omc_mx_quantise of x along its rows followed by omc_mx_matmul with W.
  *   workspace  device, 16-byte aligned, codes_bytes + scales_bytes of omc_mx_sizes(M, K); contents
- *              undefined afterwards.
+ *              undefined afterwards (with at most 16 rows it is not used).  Calls that may overlap on
+ *              the GPU need workspaces of their own.
  */
 int omc_mx_linear(const void *x, int type, uint64_t M, uint64_t K, uint64_t ldx, const uint8_t *w_codes, const uint8_t *w_scales,
                   uint64_t N, void *y, int y_type, uint64_t ldy, uint8_t *workspace, uint32_t *status, void *stream);
@@ -450,7 +451,8 @@ int omc_layer_norm(const void *x, int type, uint64_t rows, uint64_t cols, uint64
  *   dx = rstd * (g - mean(g) - xhat * mean(g * xhat)),   dgamma = sum over rows of dy * xhat,   dbeta = sum over rows of dy.
  *   dgamma, dbeta  device, cols floats, 16-byte aligned, written (zeros for rows = 0); a place in a
  *                  gradient arena will do.  The order of the additions is fixed: same input, same bits.
- *   workspace      device, 16-byte aligned, omc_layer_norm_workspace(rows, cols) bytes, undefined afterwards.
+ *   workspace      device, 16-byte aligned, omc_layer_norm_workspace(rows, cols) bytes, undefined afterwards;
+ *                  one for each call that may overlap with another on the GPU.
  *   dx may be the same matrix as dy or x.
  */
 int omc_layer_norm_workspace(uint64_t rows, uint64_t cols, uint64_t *bytes);

@@ -119,6 +119,18 @@ __device__ __forceinline__ void store_remote(uint32_t cluster_addr, float v)
 {
     asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(cluster_addr), "f"(v) : "memory");
 }
+// Before a CTA ends, also after a wait that ran out: its copies have landed (`issued` stages were filled, in turn) ...
+template <typename F>
+__device__ __forceinline__ void copies_landed(uint32_t issued, uint32_t stages, F full)
+{
+    for (uint32_t it = issued > stages ? issued - stages : 0u; it < issued; ++it) mbar_wait_held(full(it % stages), (it / stages) & 1u);
+}
+// ... and what was issued to the tensor cores has finished (a barrier for this alone).
+__device__ __forceinline__ void products_finished(uint32_t bar)
+{
+    umma_commit(bar);
+    mbar_wait_held(bar, 0u);
+}
 // Four neighbouring values of a row of Y, as many of them as the row has.
 template <typename T>
 __device__ __forceinline__ void put4(T *p, uint32_t left, float4 v)
@@ -158,7 +170,7 @@ struct Cfg {
     static constexpr int D_COLS = NT;
     static constexpr int SHARED_COLS = NT == 256 ? 80 : 0;                // (3 x 24, in whole loads of 16)
     static constexpr int ACC1 = D_COLS - SHARED_COLS, SCALES = ACC1 + D_COLS;
-    static constexpr int BARRIERS = 2 * NSTAGES + 6 + SLOTS;
+    static constexpr int BARRIERS = 2 * NSTAGES + 7 + SLOTS;
     static constexpr int SMEM = NSTAGES * STAGE + 1024 + 256;
     static_assert(STAGE % 1024 == 0 && SMEM <= 227 * 1024 && 8 * BARRIERS + 8 <= 256, "");
     static_assert(SCALES + SLOTS * SLOT_COLS <= 512 && BM * NT * 4 <= NSTAGES * STAGE, "");
@@ -185,14 +197,14 @@ mx_matmul_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constan
     extern __shared__ uint8_t smem_raw[];
     const uint32_t base = (saddr(smem_raw) + 1023u) & ~1023u;
     uint8_t *const base_ptr = smem_raw + (base - saddr(smem_raw));
-    const uint32_t bars = base + NS * C::STAGE;      // full[NS], empty[NS], acc_full[2], acc_shared[2], acc_empty[2], scaled[SLOTS]; tmem slot
+    const uint32_t bars = base + NS * C::STAGE;      // full[NS], empty[NS], acc_full[2], acc_shared[2], acc_empty[2], scaled[SLOTS], drained; tmem slot
     auto full = [&](int s) { return bars + 8u * s; };
     auto empty = [&](int s) { return bars + 8u * (NS + s); };
     auto acc_full = [&](int b) { return bars + 8u * (2 * NS + b); };
     auto acc_shared = [&](int b) { return bars + 8u * (2 * NS + 2 + b); };      // the shared columns have been read
     auto acc_empty = [&](int b) { return bars + 8u * (2 * NS + 4 + b); };       // all have
     auto scaled = [&](int s) { return bars + 8u * (2 * NS + 6 + s); };          // a step's scales are in tensor memory
-    const uint32_t tmem_slot = bars + 8u * C::BARRIERS;
+    const uint32_t drained = bars + 8u * (C::BARRIERS - 1), tmem_slot = bars + 8u * C::BARRIERS;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     // with divided K a cluster has one tile, and a CTA of it a range of its K steps
     const uint32_t rank = splits > 1 ? cluster_cta_rank() : 0u;
@@ -205,6 +217,7 @@ mx_matmul_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constan
     if (tid == 0) {
         for (int s = 0; s < NS; ++s) { mbar_init(full(s), 1); mbar_init(empty(s), 1); }
         for (int s = 0; s < C::SLOTS; ++s) mbar_init(scaled(s), SCALE_THREADS);
+        mbar_init(drained, 1);
         for (int b = 0; b < 2; ++b) {
             mbar_init(acc_full(b), 1);
             mbar_init(acc_shared(b), EPILOGUE_THREADS);
@@ -247,6 +260,7 @@ mx_matmul_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constan
                 if (C::X_BLOCKS == 2) bulk_load(sc + 2 * SCALE_BYTES, xs1 + (uint64_t)k * SCALE_BYTES, SCALE_BYTES, full(s));
             }
         }
+        copies_landed(it, NS, full);
     } else if (tid == 32) {
         uint32_t it = 0, lt = 0;
         for (uint32_t t = first; t < ntiles && ok; t += step, ++lt) {
@@ -271,6 +285,7 @@ mx_matmul_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constan
             }
             if (ok) umma_commit(acc_full(buf));
         }
+        if (!ok) products_finished(drained);
     } else if (warp >= 12) {
         const uint32_t quarter = (uint32_t)((warp & 3) * 32) << 16;
         for (uint32_t it = 0; it < steps; ++it) {
@@ -399,7 +414,7 @@ struct Narrow {
     static constexpr int NSTAGES = (SMEM - 1024 - 256) / STAGE;
     static constexpr int D_COLS = NT < 32 ? 32 : NT, TMEM_COLS = 256;
     static constexpr int THREADS = 192;
-    static_assert(STAGE % 1024 == 0 && D_COLS + NSTAGES * 2 * SCALE_COLS <= TMEM_COLS && 8 * (2 * NSTAGES + 2) <= 256, "");
+    static_assert(STAGE % 1024 == 0 && D_COLS + NSTAGES * 2 * SCALE_COLS <= TMEM_COLS && 8 * (2 * NSTAGES + 3) <= 256, "");
     static_assert(BM * NT * 4 <= NSTAGES * STAGE, "a partial result fits where the stages were");
 };
 
@@ -431,10 +446,10 @@ mx_matmul_narrow_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_
     extern __shared__ uint8_t smem_raw[];
     const uint32_t base = (saddr(smem_raw) + 1023u) & ~1023u;
     uint8_t *const base_ptr = smem_raw + (base - saddr(smem_raw));
-    const uint32_t bars = base + NS * C::STAGE;           // full[NS], empty[NS], done, tmem slot
+    const uint32_t bars = base + NS * C::STAGE;           // full[NS], empty[NS], done, drained, tmem slot
     auto full = [&](int s) { return bars + 8u * s; };
     auto empty = [&](int s) { return bars + 8u * (NS + s); };
-    const uint32_t done = bars + 8u * (2 * NS), tmem_slot = done + 8u;
+    const uint32_t done = bars + 8u * (2 * NS), drained = done + 8u, tmem_slot = drained + 8u;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const uint32_t rank = splits > 1 ? cluster_cta_rank() : 0u;
     const uint32_t tile_n = blockIdx.x / splits;
@@ -446,6 +461,7 @@ mx_matmul_narrow_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_
         if constexpr (VALUES) arrivals += 8 * source.rows;
         for (int s = 0; s < NS; ++s) { mbar_init(full(s), arrivals); mbar_init(empty(s), 1); }
         mbar_init(done, 1);
+        mbar_init(drained, 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     __syncthreads();
@@ -467,7 +483,8 @@ mx_matmul_narrow_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_
     bool ok = true;
     if (tid == 0) {
         const uint8_t *ws = w_scales + (uint64_t)tile_n * ksteps * SCALE_BYTES;
-        for (uint32_t k = k_begin, it = 0; k < k_end; ++k, ++it) {
+        uint32_t it = 0;
+        for (uint32_t k = k_begin; k < k_end; ++k, ++it) {
             const int s = it % NS;
             if (it >= (uint32_t)NS) ok = mbar_wait(empty(s), ((it / NS) - 1) & 1u, WAIT_LIMIT);
             if (!ok) break;
@@ -480,6 +497,7 @@ mx_matmul_narrow_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_
                 bulk_load(a + TILE_W_BYTES + C::TILE_X_BYTES + SCALE_BYTES, x_scales + (uint64_t)k * SCALE_BYTES, SCALE_BYTES, full(s));
             }
         }
+        copies_landed(it, NS, full);
     } else if (tid == 32) {
         const uint32_t steps = k_end - k_begin;
         auto bring_scales = [&](uint32_t it) {            // its columns were last read NS steps ago, before the stage was refilled
@@ -509,6 +527,7 @@ mx_matmul_narrow_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_
             umma_commit(empty(s));
         }
         if (ok) umma_commit(done);
+        else products_finished(drained);
     } else if (VALUES && warp >= 2) {
         if constexpr (VALUES) {
             const uint32_t t = tid - 64, team = 8 * source.rows, r = t % team / 8, block = t % 8;
