@@ -81,7 +81,8 @@ __device__ __forceinline__ float2 twice(float v) { return make_float2(v, v); }
 
 // Every kernel of the layer operators lets its successor start early and waits for the kernel before it here,
 // in every CTA and before any global access: a CTA that left without waiting could let the successor's wait end
-// while that earlier kernel still runs.
+// while that earlier kernel still runs.  What it writes may be what this kernel reads, within this kernel's own
+// lifetime: inputs are read by ordinary loads, never by those for memory that nobody writes meanwhile (so no __restrict__ on them).
 __device__ __forceinline__ void enter_stream_order()
 {
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");

@@ -104,7 +104,7 @@ struct Turned {
 // Along the rows only.
 template <typename T, bool VECTOR>
 __global__ void __launch_bounds__(32 * WARPS, ROWS_CTAS)
-quantise_rows_kernel(const T *__restrict__ x, uint32_t rows, uint32_t cols, uint64_t ld, uint8_t *__restrict__ codes,
+quantise_rows_kernel(const T *x, uint32_t rows, uint32_t cols, uint64_t ld, uint8_t *__restrict__ codes,
                      uint8_t *__restrict__ scales)
 {
     constexpr int E = LANE_VALUES<T>;
@@ -181,7 +181,7 @@ __device__ __forceinline__ uint32_t code_place(uint32_t col, uint32_t chunk)
 
 template <typename T, bool VECTOR, bool ROWS>
 __global__ void __launch_bounds__(256, sizeof(T) == 4 ? 3 : 4)
-quantise_tile_kernel(const T *__restrict__ x, uint32_t rows, uint32_t cols, uint64_t ld, uint8_t *__restrict__ codes,
+quantise_tile_kernel(const T *x, uint32_t rows, uint32_t cols, uint64_t ld, uint8_t *__restrict__ codes,
                      uint8_t *__restrict__ scales, uint8_t *__restrict__ codes_t, uint8_t *__restrict__ scales_t)
 {
     extern __shared__ __align__(16) uint8_t smem[];
@@ -328,7 +328,7 @@ template <typename T, bool VECTOR> constexpr uint32_t VALUES_STRIP = VECTOR ? ST
 
 template <typename T, bool VECTOR>
 __global__ void __launch_bounds__(32 * WARPS)
-dequantise_kernel(const uint8_t *__restrict__ codes, const uint8_t *__restrict__ scales, uint32_t rows, uint32_t cols,
+dequantise_kernel(const uint8_t *codes, const uint8_t *scales, uint32_t rows, uint32_t cols,
                   T *__restrict__ out, uint64_t ld)
 {
     constexpr int N = Word<T>::N, E = VALUES_STRIP<T, VECTOR> / 32;

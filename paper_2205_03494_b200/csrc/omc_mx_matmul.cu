@@ -189,7 +189,7 @@ __device__ __forceinline__ void tile_of(uint32_t t, uint32_t tiles_n, uint32_t t
 template <int NT, typename T>
 __global__ void __launch_bounds__(THREADS, 1)
 mx_matmul_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_x,
-                 const uint8_t *__restrict__ w_scales, const uint8_t *__restrict__ x_scales, T *__restrict__ y, uint64_t ldy,
+                 const uint8_t *w_scales, const uint8_t *x_scales, T *__restrict__ y, uint64_t ldy,
                  uint32_t M, uint32_t N, uint32_t K, uint32_t splits, uint32_t *status)
 {
     using C = Cfg<NT>;
@@ -436,7 +436,7 @@ struct Nothing {};
 template <int NT, typename T, typename SOURCE>
 __global__ void __launch_bounds__(Narrow<NT>::THREADS)
 mx_matmul_narrow_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_x,
-                        const uint8_t *__restrict__ w_scales, const uint8_t *__restrict__ x_scales, SOURCE source, T *__restrict__ y, uint64_t ldy,
+                        const uint8_t *w_scales, const uint8_t *x_scales, SOURCE source, T *__restrict__ y, uint64_t ldy,
                         uint32_t M, uint32_t N, uint32_t K, uint32_t splits, uint32_t *status)
 {
     constexpr bool VALUES = !std::is_same<SOURCE, Nothing>::value;

@@ -6,7 +6,7 @@
 //
 // One pass over memory: a row stays on the chip between its moments and its results, and the column sums of the
 // backward pass stay in registers over all rows of a group.  Rows of up to 8192 values; longer ones are read again.
-// Measured (BF16, 32768 x 2048): forward 45 us, 5.9 TB/s, bound by memory; backward 75 us, 5.4 TB/s, bound by
+// Measured (BF16, 32768 x 2048): forward 44 us, 6.1 TB/s, bound by memory; backward 75 us, 5.4 TB/s, bound by
 // instructions (about 20 per value) at the sixteen warps that its sums leave room for.  Rows off the 4-byte boundaries take twice as
 // long (16000 x 2047: 44 and 59 us): every value is stored on its own.
 #include <cuda_runtime.h>
@@ -39,10 +39,10 @@ __device__ __forceinline__ float cta_sum(float v, float *room)
     return s;
 }
 
-// Any width: a CTA per row, three passes over it.  (y may be x, dx may be dy or x: no __restrict__ on them.)
+// Any width: a CTA per row, three passes over it.
 template <typename T>
 __global__ void __launch_bounds__(THREADS)
-norm_wide_kernel(const T *x, uint32_t cols, uint64_t ld, const float *__restrict__ gamma, const float *__restrict__ beta,
+norm_wide_kernel(const T *x, uint32_t cols, uint64_t ld, const float *gamma, const float *beta,
                  float eps, T *y, uint64_t ldy, float *__restrict__ mean_out, float *__restrict__ rstd_out)
 {
     el::enter_stream_order();
@@ -73,7 +73,7 @@ norm_wide_kernel(const T *x, uint32_t cols, uint64_t ld, const float *__restrict
 template <typename T>
 __global__ void __launch_bounds__(THREADS)
 norm_backward_wide_kernel(const T *dy, uint64_t ld_dy, const T *x, uint64_t ld_x, uint32_t cols,
-                          const float *__restrict__ gamma, const float *__restrict__ mean_in, const float *__restrict__ rstd_in,
+                          const float *gamma, const float *mean_in, const float *rstd_in,
                           T *dx, uint64_t ld_dx)
 {
     el::enter_stream_order();
@@ -98,8 +98,8 @@ norm_backward_wide_kernel(const T *dy, uint64_t ld_dy, const T *x, uint64_t ld_x
 // Column sums of part of the rows: a thread per column, blockIdx.y the part.
 template <typename T>
 __global__ void __launch_bounds__(THREADS)
-norm_columns_kernel(const T *__restrict__ dy, uint64_t ld_dy, const T *__restrict__ x, uint64_t ld_x, uint32_t rows, uint32_t cols,
-                    const float *__restrict__ mean_in, const float *__restrict__ rstd_in, float *__restrict__ part)
+norm_columns_kernel(const T *dy, uint64_t ld_dy, const T *x, uint64_t ld_x, uint32_t rows, uint32_t cols,
+                    const float *mean_in, const float *rstd_in, float *__restrict__ part)
 {
     el::enter_stream_order();
     const uint32_t c = blockIdx.x * THREADS + threadIdx.x;
@@ -210,18 +210,18 @@ struct Row {
             if constexpr (PER % 4 == 0) {
 #pragma unroll
                 for (uint32_t j = 0; j < PER; j += 4) {
-                    const float4 f = c < cols ? __ldg(reinterpret_cast<const float4 *>(p + c + j)) : make_float4(0.f, 0.f, 0.f, 0.f);
+                    const float4 f = c < cols ? *reinterpret_cast<const float4 *>(p + c + j) : make_float4(0.f, 0.f, 0.f, 0.f);
                     v[i * PER + j] = f.x;
                     v[i * PER + j + 1] = f.y;
                     v[i * PER + j + 2] = f.z;
                     v[i * PER + j + 3] = f.w;
                 }
             } else if constexpr (PER == 2) {
-                const float2 f = c < cols ? __ldg(reinterpret_cast<const float2 *>(p + c)) : make_float2(0.f, 0.f);
+                const float2 f = c < cols ? *reinterpret_cast<const float2 *>(p + c) : make_float2(0.f, 0.f);
                 v[i * 2] = f.x;
                 v[i * 2 + 1] = f.y;
             } else {
-                v[i] = c < cols ? __ldg(p + c) : 0.f;
+                v[i] = c < cols ? p[c] : 0.f;
             }
         }
     }
@@ -319,7 +319,7 @@ template <int ALIGN, int E> constexpr int forward_registers = E == 8 ? 64 : E ==
 
 template <typename T, int ALIGN, int E, int L>
 __global__ void __maxnreg__((forward_registers<ALIGN, E>))
-norm_kernel(const T *x, uint32_t rows, uint32_t cols, uint64_t ld, const float *__restrict__ gamma, const float *__restrict__ beta, float eps,
+norm_kernel(const T *x, uint32_t rows, uint32_t cols, uint64_t ld, const float *gamma, const float *beta, float eps,
             T *y, uint64_t ldy, float *__restrict__ mean_out, float *__restrict__ rstd_out, uint32_t warps)
 {
     using R = Row<T, ALIGN, E, L>;
@@ -393,8 +393,8 @@ norm_kernel(const T *x, uint32_t rows, uint32_t cols, uint64_t ld, const float *
 // dx, and this CTA's part of the column sums: each thread adds up its own columns over its group's rows in registers.
 template <typename T, int ALIGN, int E, int L>
 __global__ void __launch_bounds__(E == 8 ? 384 : 512, E == 8 ? 2 : 1)
-norm_backward_kernel(const T *dy, uint64_t ld_dy, const T *x, uint64_t ld_x, uint32_t rows, uint32_t cols, const float *__restrict__ gamma,
-                     const float *__restrict__ mean_in, const float *__restrict__ rstd_in, T *dx, uint64_t ld_dx, float *__restrict__ part,
+norm_backward_kernel(const T *dy, uint64_t ld_dy, const T *x, uint64_t ld_x, uint32_t rows, uint32_t cols, const float *gamma,
+                     const float *mean_in, const float *rstd_in, T *dx, uint64_t ld_dx, float *__restrict__ part,
                      uint32_t warps)
 {
     using R = Row<T, ALIGN, E, L>;
@@ -500,7 +500,7 @@ norm_backward_kernel(const T *dy, uint64_t ld_dy, const T *x, uint64_t ld_x, uin
 // Sums of the parts: 32 columns per CTA, 32 warps that take every 32nd part, then one that adds their sums.
 constexpr int FINISH_WARPS = 32;
 __global__ void __launch_bounds__(32 * FINISH_WARPS)
-norm_finish_kernel(const float *__restrict__ part, uint32_t parts, uint32_t cols, float *__restrict__ dgamma, float *__restrict__ dbeta)
+norm_finish_kernel(const float *part, uint32_t parts, uint32_t cols, float *__restrict__ dgamma, float *__restrict__ dbeta)
 {
     el::enter_stream_order();
     __shared__ float room[FINISH_WARPS][33];
@@ -574,8 +574,8 @@ struct Forward {
     template <int ALIGN, int E, int L>
     int operator()() const
     {
-        // Without sums to keep over the rows there is room for 32 values a thread (8000 x 8192 BF16 61 us with 16, 42 us with 32;
-        // 32768 x 2048 46.5 and 44.8 us); off the 16-byte boundaries they spill.
+        // Without sums to keep over the rows there is room for 32 values a thread (8000 x 8192 BF16 61 us with 16, 45 us with 32;
+        // 32768 x 2048 46.5 and 44 us); off the 16-byte boundaries they spill.
         if constexpr (ALIGN == 16 && E == 16) {
             if (cols > 512) return this->template operator()<16, 32, 32>();
         }
