@@ -440,6 +440,9 @@ int omc_mx_linear(const void *x, int type, uint64_t M, uint64_t K, uint64_t ldx,
  * variance taken around the mean (two passes over the row, which stays on the chip).
  *   gamma, beta  device, cols floats, 16-byte aligned (a norm variable of the store's arenas).
  *   mean, rstd   device, rows floats each, written; either may be NULL.
+ *   A row that holds an Inf or a NaN has rstd = NaN and y = NaN, its mean is what its sum is (Inf of one sign stays Inf).
+ *   A finite FP32 row whose squared deviations pass the largest FP32 value has rstd = 0 and y = beta; one whose sum
+ *   does has mean = +-Inf, rstd = 0 and y = NaN.
  *   rows = 0 is allowed and does nothing.  x and y may be the same matrix.
  */
 int omc_layer_norm(const void *x, int type, uint64_t rows, uint64_t cols, uint64_t ld, const float *gamma, const float *beta,

@@ -39,6 +39,18 @@ __device__ __forceinline__ float cta_sum(float v, float *room)
     return s;
 }
 
+// The mean of the deviations from a first mean corrects it, unless that mean is not finite (Inf stays Inf, NaN NaN) or the
+// deviations overflowed.
+__device__ __forceinline__ float finite_or_0(float v) { return isfinite(v) ? v : 0.f; }
+// Variance from the mean squared deviation `around` a mean that is `off` from the right one.  Not below zero after rounding,
+// but a NaN stays one (fmaxf would make it 0); where the squares overflowed it is Inf, since off is finite.
+__device__ __forceinline__ float variance(float around, float off)
+{
+    float v;
+    asm("max.NaN.f32 %0, %1, 0f00000000;" : "=f"(v) : "f"(__fmaf_rn(-off, off, around)));
+    return v;
+}
+
 // Any width: a CTA per row, three passes over it.
 template <typename T>
 __global__ void __launch_bounds__(THREADS)
@@ -60,8 +72,8 @@ norm_wide_kernel(const T *x, uint32_t cols, uint64_t ld, const float *gamma, con
         s1 += d;
         s = __fmaf_rn(d, d, s);
     }
-    const float off = cta_sum(s1, room) / (float)cols, mean = near + off;      // (the first mean corrected)
-    const float rstd = __frsqrt_rn(fmaxf(__fmaf_rn(-off, off, cta_sum(s, room) / (float)cols), 0.f) + eps);
+    const float off = finite_or_0(cta_sum(s1, room) / (float)cols), mean = near + off;
+    const float rstd = __frsqrt_rn(variance(cta_sum(s, room) / (float)cols, off) + eps);
     for (uint32_t c = threadIdx.x; c < cols; c += THREADS)
         yr[c] = el::from_float<T>(__fmaf_rn((el::to_float(xr[c]) - near - off) * rstd, gamma[c], beta[c]));
     if (threadIdx.x == 0) {
@@ -365,17 +377,18 @@ norm_kernel(const T *x, uint32_t rows, uint32_t cols, uint64_t ld, const float *
         // the mean of the deviations from the first mean corrects it: a row of equal values leaves zeros, not the
         // rounding of the sum times 1 / sqrt(eps)
         const float near = g.sum(s.x + s.y) * inv;
-        if (!whole) R::fill(cols, t, v, near);
+#pragma unroll
+        for (int i = 0; i < E / 2; ++i) p[i] = add2(p[i], twice(-near));
+        if (!whole) R::fill(cols, t, v, 0.f);              // (not the mean before: Inf - Inf)
         s = twice(0.f);
         float2 s1 = twice(0.f);
 #pragma unroll
         for (int i = 0; i < E / 2; ++i) {
-            p[i] = add2(p[i], twice(-near));
             s1 = add2(s1, p[i]);
             s = fma2(p[i], p[i], s);
         }
         const float2 m = g.sum2(s1.x + s1.y, s.x + s.y);
-        const float off = m.x * inv, mean = near + off, rstd = __frsqrt_rn(fmaxf(__fmaf_rn(-off, off, m.y * inv), 0.f) + eps);
+        const float off = finite_or_0(m.x * inv), mean = near + off, rstd = __frsqrt_rn(variance(m.y * inv, off) + eps);
 #pragma unroll
         for (int i = 0; i < E / 2; ++i)
             p[i] = fma2(mul2(add2(p[i], twice(-off)), twice(rstd)), make_float2(ga[2 * i], ga[2 * i + 1]), make_float2(be[2 * i], be[2 * i + 1]));
