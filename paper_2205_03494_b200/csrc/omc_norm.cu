@@ -15,6 +15,7 @@
 
 #include "element.cuh"
 #include "omc_internal.h"
+#include "row_copy.h"
 
 namespace {
 
@@ -149,7 +150,7 @@ struct Row {
     {
         asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
     }
-    static __device__ __forceinline__ void fetch(uint8_t *image, const T *row, bool first_row, uint32_t cols, uint32_t t, uint32_t G)
+    static __device__ __forceinline__ void fetch(uint8_t *image, const T *row, bool from_below, uint32_t cols, uint32_t t, uint32_t G)
     {
         const uint32_t dst = (uint32_t)__cvta_generic_to_shared(image);
         if constexpr (ALIGN == 16) {
@@ -158,14 +159,14 @@ struct Row {
             for (int i = 0; i < UNITS; ++i)
                 if ((u + i * L) * PER < cols) copy16(dst + u * 16 + i * L * 16, row + u * PER + i * L * PER, 16);
         } else {
-            const uint32_t skip = (uint32_t)(reinterpret_cast<uintptr_t>(row) & 15u), total = skip + cols * SIZE;
+            const uint32_t skip = row_skip(reinterpret_cast<uintptr_t>(row)), total = skip + cols * SIZE;
             const uint8_t *src = reinterpret_cast<const uint8_t *>(row) - skip;
             constexpr int CHUNKS = (E * SIZE + 15) / 16;
 #pragma unroll
             for (int i = 0; i <= CHUNKS; ++i) {
                 const uint32_t k = i * G + t;
                 if (k * 16 >= total) break;
-                if (k == 0 && skip && first_row) {          // nothing before the matrix is read
+                if (by_value(k, from_below)) {              // nothing before the matrix is read
                     for (uint32_t j = skip; j < 16 && j < total; j += SIZE)
                         *reinterpret_cast<T *>(image + j) = *reinterpret_cast<const T *>(src + j);
                 } else {
@@ -177,7 +178,7 @@ struct Row {
     static __device__ __forceinline__ void values(const uint8_t *image, const T *row, uint32_t t, float *v)
     {
         constexpr int N = el::Word<T>::N;
-        const uint8_t *p = image + (ALIGN == 16 ? 0 : reinterpret_cast<uintptr_t>(row) & 15u) + first(t) * ALIGN;      // (behind the row: never used)
+        const uint8_t *p = image + (ALIGN == 16 ? 0 : row_skip(reinterpret_cast<uintptr_t>(row))) + first(t) * ALIGN;      // (behind the row: never used)
 #pragma unroll
         for (int i = 0; i < UNITS; ++i) {
             if constexpr (ALIGN == 16) {
@@ -332,7 +333,8 @@ template <int ALIGN, int E> constexpr int forward_registers = E == 8 ? 64 : E ==
 template <typename T, int ALIGN, int E, int L>
 __global__ void __maxnreg__((forward_registers<ALIGN, E>))
 norm_kernel(const T *x, uint32_t rows, uint32_t cols, uint64_t ld, const float *gamma, const float *beta, float eps,
-            T *y, uint64_t ldy, float *__restrict__ mean_out, float *__restrict__ rstd_out, uint32_t warps)
+            T *y, uint64_t ldy, float *__restrict__ mean_out, float *__restrict__ rstd_out, uint32_t warps,
+            uint32_t below)
 {
     using R = Row<T, ALIGN, E, L>;
     constexpr int S = STAGES;
@@ -349,7 +351,7 @@ norm_kernel(const T *x, uint32_t rows, uint32_t cols, uint64_t ld, const float *
     T *row_y = y + (uint64_t)first * ldy;
     uint32_t coming = first;                               // the row to fetch next (no overflow: rows < 2^31, step < 2^14)
     auto fetch = [&](uint32_t s) {
-        if (coming < rows) R::fetch(ring + s * bytes, src, coming == 0, cols, t, G);
+        if (coming < rows) R::fetch(ring + s * bytes, src, coming < below, cols, t, G);
         commit_copies();
         coming += step;
         src += step * ld;
@@ -408,7 +410,7 @@ template <typename T, int ALIGN, int E, int L>
 __global__ void __launch_bounds__(E == 8 ? 384 : 512, E == 8 ? 2 : 1)
 norm_backward_kernel(const T *dy, uint64_t ld_dy, const T *x, uint64_t ld_x, uint32_t rows, uint32_t cols, const float *gamma,
                      const float *mean_in, const float *rstd_in, T *dx, uint64_t ld_dx, float *__restrict__ part,
-                     uint32_t warps)
+                     uint32_t warps, uint32_t below_x, uint32_t below_d)
 {
     using R = Row<T, ALIGN, E, L>;
     constexpr int S = STAGES;
@@ -426,8 +428,8 @@ norm_backward_kernel(const T *dy, uint64_t ld_dy, const T *x, uint64_t ld_x, uin
     uint32_t coming = first;                               // the row to fetch next (no overflow: rows < 2^31, step < 2^14)
     auto fetch = [&](uint32_t s) {
         if (coming < rows) {
-            R::fetch(ring + s * 2 * bytes, src_x, coming == 0, cols, t, G);
-            R::fetch(ring + s * 2 * bytes + bytes, src_d, coming == 0, cols, t, G);
+            R::fetch(ring + s * 2 * bytes, src_x, coming < below_x, cols, t, G);
+            R::fetch(ring + s * 2 * bytes + bytes, src_d, coming < below_d, cols, t, G);
         }
         commit_copies();
         coming += step;
@@ -600,7 +602,8 @@ struct Forward {
         const uint32_t most = DEFAULT_SMS * (by_regs < by_smem ? by_regs : by_smem);
         if (const int rc = el::allow_smem<norm_kernel<T, ALIGN, E, L>>(smem)) return rc;
         return note_cuda(el::launch(norm_kernel<T, ALIGN, E, L>, dim3(ctas < most ? ctas : most), threads, smem, 1, stream,
-                                    static_cast<const T *>(x), rows, cols, ld, gamma, beta, eps, static_cast<T *>(y), ldy, mean, rstd, warps));
+                                    static_cast<const T *>(x), rows, cols, ld, gamma, beta, eps, static_cast<T *>(y), ldy, mean, rstd, warps,
+                                    rows_from_below(reinterpret_cast<uintptr_t>(x), ld * sizeof(T))));
     }
 };
 
@@ -642,7 +645,8 @@ struct Backward {
         *parts = ctas < most ? ctas : most;
         if (const int rc = el::allow_smem<norm_backward_kernel<T, ALIGN, E, L>>(smem)) return rc;
         return note_cuda(el::launch(norm_backward_kernel<T, ALIGN, E, L>, dim3(*parts), groups * G, smem, 1, stream, static_cast<const T *>(dy),
-                                    ld_dy, static_cast<const T *>(x), ld_x, rows, cols, gamma, mean, rstd, static_cast<T *>(dx), ld_dx, part, warps));
+                                    ld_dy, static_cast<const T *>(x), ld_x, rows, cols, gamma, mean, rstd, static_cast<T *>(dx), ld_dx, part, warps,
+                                    rows_from_below(reinterpret_cast<uintptr_t>(x), ld_x * sizeof(T)), rows_from_below(reinterpret_cast<uintptr_t>(dy), ld_dy * sizeof(T))));
     }
 };
 
