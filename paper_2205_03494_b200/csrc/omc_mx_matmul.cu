@@ -34,6 +34,7 @@
 #include "element.cuh"
 #include "mx_encode.cuh"
 #include "mx_format.cuh"
+#include "mx_schedule.h"
 #include "omc_internal.h"
 #include "tensor_core.cuh"
 
@@ -46,7 +47,8 @@ namespace {
 using namespace omc;
 using namespace omc::tc;
 
-constexpr int BM = 128, BK = 256;                     // W rows per CTA; K per stage (128 bytes of codes)
+constexpr int BM = mx::TILE_W, BK = mx::STEP_K;       // W rows per CTA; K per stage (128 bytes of codes)
+static_assert(mx::LAID_OUT_SMS == DEFAULT_SMS, "");
 constexpr int INSTR_K = 64;                           // K of one tcgen05.mma with 4-bit inputs
 constexpr int TILE_W_BYTES = BM * BK / 2;
 constexpr int SCALE_BYTES = 1024;                     // scales of 128 rows x 256 columns
@@ -621,31 +623,22 @@ struct Product {
     void *stream;
 };
 
-uint32_t ksteps_of(const Product &p) { return (p.K + BK - 1) / BK; }
-template <int NT>
-uint64_t tiles_of(const Product &p) { return (uint64_t)((p.N + BM - 1) / BM) * ((p.M + NT - 1) / NT); }
-
 template <int NT, typename T>
-int launch(const Product &p)
+int launch(const Product &p, uint32_t splits)
 {
     using C = Cfg<NT>;
     CUtensorMap map_w, map_x;
     if (!make_codes_map(&map_w, p.w_codes, p.N, p.K, BM) || !make_codes_map(&map_x, p.x_codes, p.M, p.K, NT)) return OMC_ERR_CUDA;
     if (const int rc = el::allow_smem<mx_matmul_kernel<NT, T>>(C::SMEM)) return rc;
-    const uint32_t sms = el::sm_count(), ksteps = ksteps_of(p);
-    const uint64_t tiles = tiles_of<NT>(p);
+    const uint64_t tiles = mx::tiles_of(p.M, p.N, NT), sms = el::sm_count();
     if (tiles >= (1ull << 31)) return OMC_ERR_INVALID_ARG;
-    // Divide K while the clusters still fit on the device at once.  Joining the parts takes about 2 us, a step 0.34 us
-    // (128 x 8192 x 8192: 15.0 us undivided, 11.7 us in two; 1999 x 512 x 2048: 6.4 us undivided, 7.5 us in two).
-    uint32_t splits = 1;
-    while (splits < 4 && tiles * splits * 2 <= sms && ksteps >= 16) splits *= 2;
-    const uint32_t grid = splits > 1 ? (uint32_t)tiles * splits : tiles < sms ? (uint32_t)tiles : sms;
+    const uint32_t grid = (uint32_t)(splits > 1 ? tiles * splits : tiles < sms ? tiles : sms);
     return note_cuda(el::launch(mx_matmul_kernel<NT, T>, dim3(grid), THREADS, C::SMEM, splits, p.stream, map_w, map_x, p.w_scales, p.x_scales,
                                 static_cast<T *>(p.y), p.ldy, p.M, p.N, p.K, splits, p.status));
 }
 
 template <int NT, typename T, typename SOURCE>
-int launch_narrow(const Product &p, SOURCE source)
+int launch_narrow(const Product &p, uint32_t splits, SOURCE source)
 {
     using C = Narrow<NT>;
     CUtensorMap map_w, map_x;
@@ -656,25 +649,21 @@ int launch_narrow(const Product &p, SOURCE source)
         map_x = map_w;      // not used
     }
     if (const int rc = el::allow_smem<mx_matmul_narrow_kernel<NT, T, SOURCE>>(C::SMEM)) return rc;
-    const uint32_t tiles = (uint32_t)tiles_of<NT>(p), ksteps = ksteps_of(p);
-    // divide K while all CTAs are resident at once, two to an SM, and a CTA keeps two steps (joining takes 0.5 us, a step 0.4 us)
-    uint32_t splits = 1;
-    while (splits < 8 && (uint64_t)tiles * splits <= el::sm_count() && ksteps >= splits * 4) splits *= 2;
-    return note_cuda(el::launch(mx_matmul_narrow_kernel<NT, T, SOURCE>, dim3(tiles * splits), C::THREADS, C::SMEM, splits, p.stream, map_w, map_x,
+    return note_cuda(el::launch(mx_matmul_narrow_kernel<NT, T, SOURCE>, dim3((uint32_t)mx::tiles_of(p.M, p.N, NT) * splits), C::THREADS, C::SMEM, splits, p.stream, map_w, map_x,
                                 p.w_scales, p.x_scales, source, static_cast<T *>(p.y), p.ldy, p.M, p.N, p.K, splits, p.status));
 }
 
-// Up to 64 rows of X: the narrowest tile that holds them all.  More: tiles of 128 or 256 rows, whichever takes less time by
-// its number of rounds over the SMs; measured, a round takes about 0.35 (K steps + 2) us with 128 rows, 0.36 (K steps + 5) us
-// with 256 (1024 x 2048 x 2048: 6.7 and 7.7 us; 3000 x 1000 x 1000: 7.1 and 6.6 us).
 template <typename T>
 int launch_any(const Product &p)
 {
-    if (p.M <= 16) return launch_narrow<16, T>(p, Nothing());
-    if (p.M <= 32) return launch_narrow<32, T>(p, Nothing());
-    if (p.M <= 64) return launch_narrow<64, T>(p, Nothing());
-    const uint64_t sms = el::sm_count(), rounds128 = (tiles_of<128>(p) + sms - 1) / sms, rounds256 = (tiles_of<256>(p) + sms - 1) / sms;
-    return rounds128 * (ksteps_of(p) + 2) <= rounds256 * (ksteps_of(p) + 5) ? launch<128, T>(p) : launch<256, T>(p);
+    const mx::Schedule s = mx::schedule_of(p.M, p.N, p.K);
+    switch (s.tile) {
+    case 16: return launch_narrow<16, T>(p, s.splits, Nothing());
+    case 32: return launch_narrow<32, T>(p, s.splits, Nothing());
+    case 64: return launch_narrow<64, T>(p, s.splits, Nothing());
+    case 128: return launch<128, T>(p, s.splits);
+    default: return launch<256, T>(p, s.splits);
+    }
 }
 
 // At most this many rows of values are quantised inside the product.
@@ -686,7 +675,9 @@ int product_of_values(const Product &p, const void *x, uint64_t ld, int type)
     uint32_t rows = 1;
     while (rows < p.M) rows *= 2;
     const Values<TX> v = {static_cast<const TX *>(x), ld, rows, el::aligned16(x) && ld * sizeof(TX) % 16 == 0};
-    return type == OMC_TYPE_F32 ? launch_narrow<16, float>(p, v) : type == OMC_TYPE_F16 ? launch_narrow<16, __half>(p, v) : launch_narrow<16, __nv_bfloat16>(p, v);
+    const uint32_t splits = mx::schedule_of(p.M, p.N, p.K).splits;
+    return type == OMC_TYPE_F32   ? launch_narrow<16, float>(p, splits, v)
+           : type == OMC_TYPE_F16 ? launch_narrow<16, __half>(p, splits, v) : launch_narrow<16, __nv_bfloat16>(p, splits, v);
 }
 
 int product(const Product &p, int type)
