@@ -22,7 +22,8 @@ inline uint64_t tiles_of(uint64_t M, uint64_t N, uint32_t tile) { return (N + TI
 // More: tiles of 128 or 256 rows, whichever takes less time by its number of rounds over the SMs; measured, a round takes about
 // 0.35 (K steps + 2) us with 128 rows, 0.36 (K steps + 5) us with 256 (1024 x 2048 x 2048: 6.7 and 7.7 us; 3000 x 1000 x 1000:
 // 7.1 and 6.6 us).  K is divided while the clusters still fit on the SMs at once: joining the parts takes about 2 us, a step
-// 0.34 us (128 x 8192 x 8192: 15.0 us undivided, 11.7 us in two; 1999 x 512 x 2048: 6.4 us undivided, 7.5 us in two).
+// 0.34 us (128 x 8192 x 8192: 15.0 us undivided, 11.7 us in two; 1999 x 512 x 2048: 6.4 us undivided, 7.5 us in two).  Tiles of 256
+// rows are taken only where those of 128 need two rounds, so there are too many of them to divide K.
 inline Schedule schedule_of(uint64_t M, uint64_t N, uint64_t K)
 {
     const uint64_t ksteps = (K + STEP_K - 1) / STEP_K;
@@ -34,7 +35,7 @@ inline Schedule schedule_of(uint64_t M, uint64_t N, uint64_t K)
     }
     const uint64_t rounds128 = (tiles_of(M, N, 128) + LAID_OUT_SMS - 1) / LAID_OUT_SMS, rounds256 = (tiles_of(M, N, 256) + LAID_OUT_SMS - 1) / LAID_OUT_SMS;
     s.tile = rounds128 * (ksteps + 2) <= rounds256 * (ksteps + 5) ? 128u : 256u;
-    while (s.splits < 4 && tiles_of(M, N, s.tile) * s.splits * 2 <= LAID_OUT_SMS && ksteps >= 16) s.splits *= 2;
+    while (s.tile == 128 && s.splits < 4 && tiles_of(M, N, s.tile) * s.splits * 2 <= LAID_OUT_SMS && ksteps >= 16) s.splits *= 2;
     return s;
 }
 

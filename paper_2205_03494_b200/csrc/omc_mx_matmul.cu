@@ -170,12 +170,13 @@ struct Cfg {
     static constexpr int NSTAGES = 208 * 1024 / STAGE;
     static constexpr int SLOTS = NT == 256 ? 3 : 4, SLOT_COLS = (1 + X_BLOCKS) * SCALE_COLS;
     static constexpr int D_COLS = NT;
+    static constexpr bool DIVIDES = NT == 128;                            // K may be divided among a cluster's CTAs (few tiles: never of 256 rows)
     static constexpr int SHARED_COLS = NT == 256 ? 80 : 0;                // (3 x 24, in whole loads of 16)
     static constexpr int ACC1 = D_COLS - SHARED_COLS, SCALES = ACC1 + D_COLS;
     static constexpr int BARRIERS = 2 * NSTAGES + 7 + SLOTS;
     static constexpr int SMEM = NSTAGES * STAGE + 1024 + 256;
     static_assert(STAGE % 1024 == 0 && SMEM <= 227 * 1024 && 8 * BARRIERS + 8 <= 256, "");
-    static_assert(SCALES + SLOTS * SLOT_COLS <= 512 && BM * NT * 4 <= NSTAGES * STAGE, "");
+    static_assert(SCALES + SLOTS * SLOT_COLS <= 512 && (!DIVIDES || BM * NT * 4 <= NSTAGES * STAGE), "");
 };
 
 // Tiles in the order in which the CTAs take them: bands of sixteen tiles of W's rows, so that the tiles in work
@@ -320,7 +321,7 @@ mx_matmul_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constan
             ok = mbar_wait_held(acc_full(buf), (lt >> 1) & 1u);
             ok = __all_sync(0xFFFFFFFFu, ok);
             if (t + step >= ntiles) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-            if (!ok || splits > 1) break;
+            if (!ok || (C::DIVIDES && splits > 1)) break;
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
             const uint32_t n = tn * BM + q * 32 + lane, m0 = tm * NT;
             const uint32_t acc = tmem_base + buf * C::ACC1 + ((uint32_t)(q * 32) << 16);
@@ -369,7 +370,7 @@ mx_matmul_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constan
             mbar_arrive(acc_empty(buf));
         }
     }
-    if (splits > 1) {
+    if (C::DIVIDES && splits > 1) {
         uint32_t tn, tm;
         tile_of(first, tiles_n, tiles_m, tn, tm);
         const uint32_t m0 = tm * NT, mine = NT / splits;

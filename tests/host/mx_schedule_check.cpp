@@ -36,6 +36,7 @@ int main()
                     if (s.splits > 1 && (steps < 2 * s.splits || ctas > 2 * LAID_OUT_SMS)) return fail("few rows, division", M, N, K);
                 } else {
                     if (M <= 64 || (s.tile != 128 && s.tile != 256)) return fail("tile", M, N, K);
+                    if (s.tile == 256 && s.splits != 1) return fail("division of a tile of 256 rows, which its kernel cannot", M, N, K);
                     // a CTA owns at least 32 rows of the tile and four steps, and every cluster has its SMs
                     if (s.splits > 1 && (s.tile / s.splits < 32 || steps < 4 * s.splits || ctas > LAID_OUT_SMS)) return fail("division of a tile", M, N, K);
                 }
