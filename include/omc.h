@@ -419,7 +419,9 @@ int omc_mx_dequantise(const uint8_t *codes, const uint8_t *scales, uint64_t rows
  *   y       device, M x N of `type`, written; any ldy >= N, element-aligned.
  *   status  device, one 32-bit word of the caller's, cleared by the caller: set non-zero by a kernel
  *           that gave up waiting for one of its own copies (y is then incomplete; the context stays
- *           usable).  Not expected to happen; the bounded wait exists so that a fault cannot hang the GPU.
+ *           usable).  Not expected to happen; the bounded wait exists so that a fault cannot hang the GPU.  (Bounded are
+ *           the waits for copies, products and their results.  Those for the kernel before on the stream, for tensor memory that other
+ *           work on the GPU holds and for the other CTAs of a cluster, which end because their own waits do, have no limit.)
  * A NaN block of X or W makes the rows or columns of Y that it enters NaN.  M <= 128 * 65535.
  */
 int omc_mx_matmul(const uint8_t *x_codes, const uint8_t *x_scales, uint64_t M, const uint8_t *w_codes, const uint8_t *w_scales,
@@ -434,6 +436,15 @@ int omc_mx_matmul(const uint8_t *x_codes, const uint8_t *x_scales, uint64_t M, c
  */
 int omc_mx_linear(const void *x, int type, uint64_t M, uint64_t K, uint64_t ldx, const uint8_t *w_codes, const uint8_t *w_scales,
                   uint64_t N, void *y, int y_type, uint64_t ldy, uint8_t *workspace, uint32_t *status, void *stream);
+
+/*
+ * omc_mx_inject_wait_timeout -- diagnostics for the bounded waits of the two calls above.  The first CTA of the next product that
+ * the calling thread launches announces its copies without issuing them and gives up each wait after `polls` polls
+ * (1 .. 2^16, of up to 10 us each): its waits run out with no copy in flight, it sets the status word and returns, and what it would have
+ * written to y is garbage.  The other CTAs are not touched, nor is any later call.  Host only.  For tests of the give-up path: nothing
+ * faults, hangs or reads out of bounds.
+ */
+int omc_mx_inject_wait_timeout(uint32_t polls);
 
 /*
  * omc_layer_norm -- y = (x - mean) * rstd * gamma + beta per row, rstd = 1 / sqrt(variance + eps), the

@@ -25,7 +25,7 @@ EXPORTS = ["omc_strerror", "omc_last_cuda_error", "omc_plan", "omc_plan_destroy"
            "omc_plan_var", "omc_plan_division", "omc_plan_prepare", "omc_plan_status", "omc_plan_inject_wait_timeout", "omc_compress", "omc_decompress",
            "omc_update_recompress", "omc_update_recompress_host", "omc_transition", "omc_aggregate", "omc_aggregate_sum", "omc_aggregate_add", "omc_divide", "omc_matmul",
            "omc_compress_var_static", "omc_static_status", "omc_mx_sizes", "omc_mx_quantise", "omc_mx_dequantise", "omc_mx_matmul",
-           "omc_mx_linear", "omc_layer_norm", "omc_layer_norm_workspace", "omc_layer_norm_backward"]
+           "omc_mx_linear", "omc_mx_inject_wait_timeout", "omc_layer_norm", "omc_layer_norm_workspace", "omc_layer_norm_backward"]
 STATIC_MAX_NUMEL = 1 << 28
 
 
@@ -91,6 +91,7 @@ def lib():
         L.omc_mx_dequantise.argtypes = [vp, vp, u64, u64, vp, i32, u64, vp]
         L.omc_mx_matmul.argtypes = [vp, vp, u64, vp, vp, u64, u64, vp, i32, u64, vp, vp]
         L.omc_mx_linear.argtypes = [vp, i32, u64, u64, u64, vp, vp, u64, vp, i32, u64, vp, vp, vp]
+        L.omc_mx_inject_wait_timeout.argtypes = [C.c_uint32]
         L.omc_layer_norm.argtypes = [vp, i32, u64, u64, u64, vp, vp, C.c_float, vp, u64, vp, vp, vp]
         L.omc_layer_norm_workspace.argtypes = [u64, u64, u64p]
         L.omc_layer_norm_backward.argtypes = [vp, u64, vp, u64, i32, u64, u64, vp, vp, vp, vp, u64, vp, vp, vp, vp]
@@ -308,6 +309,11 @@ def mx_linear(x, type_, M, K, ldx, w_codes, w_scales, N, y, y_type, ldy, workspa
     rc = (_calls or _load_calls()).mx_linear(x, type_, M, K, ldx, w_codes, w_scales, N, y, y_type, ldy, workspace, status, stream)
     if rc:
         _check(rc, "omc_mx_linear")
+
+
+def mx_inject_wait_timeout(polls: int):
+    """omc_mx_inject_wait_timeout: the first CTA of this thread's next product gives up its waits (diagnostics)."""
+    _check(lib().omc_mx_inject_wait_timeout(int(polls)), "omc_mx_inject_wait_timeout")
 
 
 def layer_norm(x, type_, rows, cols, ld, gamma, beta, eps, y, ldy, mean=0, rstd=0, stream=0):

@@ -123,16 +123,22 @@ __device__ __forceinline__ void store_remote(uint32_t cluster_addr, float v)
 }
 // Before a CTA ends, also after a wait that ran out: its copies have landed (`issued` stages were filled, in turn) ...
 template <typename F>
-__device__ __forceinline__ void copies_landed(uint32_t issued, uint32_t stages, F full)
+__device__ __forceinline__ void copies_landed(uint32_t issued, uint32_t stages, uint32_t limit, F full)
 {
-    for (uint32_t it = issued > stages ? issued - stages : 0u; it < issued; ++it) mbar_wait_held(full(it % stages), (it / stages) & 1u);
+    for (uint32_t it = issued > stages ? issued - stages : 0u; it < issued; ++it) mbar_wait_held(full(it % stages), (it / stages) & 1u, limit);
 }
 // ... and what was issued to the tensor cores has finished (a barrier for this alone).
 __device__ __forceinline__ void products_finished(uint32_t bar)
 {
     umma_commit(bar);
-    mbar_wait_held(bar, 0u);
+    mbar_wait_held(bar, 0u, HELD_LIMIT);
 }
+// Diagnostics (omc_mx_inject_wait_timeout): the first CTA gives up each wait after `polls` polls (0: the default limits)
+// and announces its copies without issuing them.
+struct Trial {
+    uint32_t polls;
+    __device__ __forceinline__ bool here() const { return polls != 0u && blockIdx.x == 0; }
+};
 // Four neighbouring values of a row of Y, as many of them as the row has.
 template <typename T>
 __device__ __forceinline__ void put4(T *p, uint32_t left, float4 v)
@@ -193,7 +199,7 @@ template <int NT, typename T>
 __global__ void __launch_bounds__(THREADS, 1)
 mx_matmul_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_x,
                  const uint8_t *w_scales, const uint8_t *x_scales, T *__restrict__ y, uint64_t ldy,
-                 uint32_t M, uint32_t N, uint32_t K, uint32_t splits, uint32_t *status)
+                 uint32_t M, uint32_t N, uint32_t K, uint32_t splits, uint32_t *status, Trial trial)
 {
     using C = Cfg<NT>;
     constexpr int NS = C::NSTAGES;
@@ -209,6 +215,7 @@ mx_matmul_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constan
     auto scaled = [&](int s) { return bars + 8u * (2 * NS + 6 + s); };          // a step's scales are in tensor memory
     const uint32_t drained = bars + 8u * (C::BARRIERS - 1), tmem_slot = bars + 8u * C::BARRIERS;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const uint32_t limit = trial.here() ? trial.polls : WAIT_LIMIT, held = trial.here() ? trial.polls : HELD_LIMIT;
     // with divided K a cluster has one tile, and a CTA of it a range of its K steps
     const uint32_t rank = splits > 1 ? cluster_cta_rank() : 0u;
     const uint32_t ksteps = (K + BK - 1) / BK;
@@ -252,10 +259,11 @@ mx_matmul_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constan
             const uint8_t *xs1 = x_scales + (uint64_t)min(xb + 1, x_blocks - 1) * ksteps * SCALE_BYTES;      // (no such rows: any scales)
             for (uint32_t k = k_begin; k < k_end; ++k, ++it) {
                 const int s = it % NS;
-                if (it >= (uint32_t)NS) ok = mbar_wait(empty(s), ((it / NS) - 1) & 1u, WAIT_LIMIT);
+                if (it >= (uint32_t)NS) ok = mbar_wait(empty(s), ((it / NS) - 1) & 1u, limit);
                 if (!ok) break;
                 const uint32_t a = base + s * C::STAGE, sc = a + TILE_W_BYTES + C::TILE_X_BYTES;
                 mbar_expect_tx(full(s), C::STAGE);
+                if (trial.here()) continue;
                 tma_load_2d(a, &map_w, (int)(k * (BK / 2)), (int)(tn * BM), full(s));
                 tma_load_2d(a + TILE_W_BYTES, &map_x, (int)(k * (BK / 2)), (int)(tm * NT), full(s));
                 bulk_load(sc, ws + (uint64_t)k * SCALE_BYTES, SCALE_BYTES, full(s));
@@ -263,19 +271,19 @@ mx_matmul_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constan
                 if (C::X_BLOCKS == 2) bulk_load(sc + 2 * SCALE_BYTES, xs1 + (uint64_t)k * SCALE_BYTES, SCALE_BYTES, full(s));
             }
         }
-        copies_landed(it, NS, full);
+        copies_landed(it, NS, held, full);
     } else if (tid == 32) {
         uint32_t it = 0, lt = 0;
         for (uint32_t t = first; t < ntiles && ok; t += step, ++lt) {
             const uint32_t buf = lt & 1u;
-            if (C::SHARED_COLS && lt >= 1) ok = mbar_wait(acc_shared(buf ^ 1u), ((lt - 1) >> 1) & 1u, WAIT_LIMIT);     // of the tile before
-            if (ok && lt >= 2) ok = mbar_wait(acc_empty(buf), ((lt >> 1) - 1) & 1u, WAIT_LIMIT);                       // of the one before that
+            if (C::SHARED_COLS && lt >= 1) ok = mbar_wait(acc_shared(buf ^ 1u), ((lt - 1) >> 1) & 1u, limit);     // of the tile before
+            if (ok && lt >= 2) ok = mbar_wait(acc_empty(buf), ((lt >> 1) - 1) & 1u, limit);                       // of the one before that
             if (!ok) break;
             const uint32_t d = tmem_base + buf * C::ACC1;
             for (uint32_t k = k_begin; k < k_end; ++k, ++it) {
                 const int s = it % NS;
-                ok = mbar_wait_held(full(s), (it / NS) & 1u);
-                ok = ok && mbar_wait_held(scaled(it % C::SLOTS), (it / C::SLOTS) & 1u);
+                ok = mbar_wait_held(full(s), (it / NS) & 1u, held);
+                ok = ok && mbar_wait_held(scaled(it % C::SLOTS), (it / C::SLOTS) & 1u, held);
                 if (!ok) break;
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
                 const uint32_t a = base + s * C::STAGE, b = a + TILE_W_BYTES;
@@ -293,8 +301,8 @@ mx_matmul_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constan
         const uint32_t quarter = (uint32_t)((warp & 3) * 32) << 16;
         for (uint32_t it = 0; it < steps; ++it) {
             const int s = it % NS;
-            if (it >= (uint32_t)C::SLOTS) ok = mbar_wait(empty((it - C::SLOTS) % NS), ((it - C::SLOTS) / NS) & 1u, WAIT_LIMIT);      // columns are free
-            ok = ok && mbar_wait_held(full(s), (it / NS) & 1u);
+            if (it >= (uint32_t)C::SLOTS) ok = mbar_wait(empty((it - C::SLOTS) % NS), ((it - C::SLOTS) / NS) & 1u, limit);      // columns are free
+            ok = ok && mbar_wait_held(full(s), (it / NS) & 1u, held);
             ok = __all_sync(0xFFFFFFFFu, ok);
             if (!ok) break;
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
@@ -318,7 +326,7 @@ mx_matmul_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constan
             const uint32_t buf = lt & 1u;
             uint32_t tn, tm;
             tile_of(t, tiles_n, tiles_m, tn, tm);
-            ok = mbar_wait_held(acc_full(buf), (lt >> 1) & 1u);
+            ok = mbar_wait_held(acc_full(buf), (lt >> 1) & 1u, held);
             ok = __all_sync(0xFFFFFFFFu, ok);
             if (t + step >= ntiles) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
             if (!ok || (C::DIVIDES && splits > 1)) break;
@@ -440,7 +448,7 @@ template <int NT, typename T, typename SOURCE>
 __global__ void __launch_bounds__(Narrow<NT>::THREADS)
 mx_matmul_narrow_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_x,
                         const uint8_t *w_scales, const uint8_t *x_scales, SOURCE source, T *__restrict__ y, uint64_t ldy,
-                        uint32_t M, uint32_t N, uint32_t K, uint32_t splits, uint32_t *status)
+                        uint32_t M, uint32_t N, uint32_t K, uint32_t splits, uint32_t *status, Trial trial)
 {
     constexpr bool VALUES = !std::is_same<SOURCE, Nothing>::value;
     static_assert(!VALUES || NT == 16, "sixteen rows of eight blocks are a thread each");
@@ -454,6 +462,7 @@ mx_matmul_narrow_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_
     auto empty = [&](int s) { return bars + 8u * (NS + s); };
     const uint32_t done = bars + 8u * (2 * NS), drained = done + 8u, tmem_slot = drained + 8u;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const uint32_t limit = trial.here() ? trial.polls : WAIT_LIMIT, held = trial.here() ? trial.polls : HELD_LIMIT;
     const uint32_t rank = splits > 1 ? cluster_cta_rank() : 0u;
     const uint32_t tile_n = blockIdx.x / splits;
     const uint32_t ksteps = (K + BK - 1) / BK;
@@ -489,10 +498,11 @@ mx_matmul_narrow_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_
         uint32_t it = 0;
         for (uint32_t k = k_begin; k < k_end; ++k, ++it) {
             const int s = it % NS;
-            if (it >= (uint32_t)NS) ok = mbar_wait(empty(s), ((it / NS) - 1) & 1u, WAIT_LIMIT);
+            if (it >= (uint32_t)NS) ok = mbar_wait(empty(s), ((it / NS) - 1) & 1u, limit);
             if (!ok) break;
             const uint32_t a = base + s * C::STAGE;
             mbar_expect_tx(full(s), VALUES ? TILE_W_BYTES + SCALE_BYTES : C::STAGE);
+            if (trial.here()) continue;
             tma_load_2d(a, &map_w, (int)(k * (BK / 2)), (int)(tile_n * BM), full(s));
             bulk_load(a + TILE_W_BYTES + C::TILE_X_BYTES, ws + (uint64_t)k * SCALE_BYTES, SCALE_BYTES, full(s));
             if constexpr (!VALUES) {
@@ -500,12 +510,12 @@ mx_matmul_narrow_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_
                 bulk_load(a + TILE_W_BYTES + C::TILE_X_BYTES + SCALE_BYTES, x_scales + (uint64_t)k * SCALE_BYTES, SCALE_BYTES, full(s));
             }
         }
-        copies_landed(it, NS, full);
+        copies_landed(it, NS, held, full);
     } else if (tid == 32) {
         const uint32_t steps = k_end - k_begin;
         auto bring_scales = [&](uint32_t it) {            // its columns were last read NS steps ago, before the stage was refilled
             const int s = it % NS;
-            if (!mbar_wait_held(full(s), (it / NS) & 1u)) return false;
+            if (!mbar_wait_held(full(s), (it / NS) & 1u, held)) return false;
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
             const uint32_t sc = base + s * C::STAGE + TILE_W_BYTES + C::TILE_X_BYTES;
             const uint32_t ta = tmem_base + C::D_COLS + s * 2 * SCALE_COLS, tb = ta + SCALE_COLS;
@@ -547,7 +557,7 @@ mx_matmul_narrow_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_
                     mx::load<typename SOURCE::Type, false, 32>(source.x + r * source.ld, col, K, w);
                 }
                 mx::encode_block<typename SOURCE::Type, 32>(w, codes, scale);
-                if (it >= (uint32_t)NS) ok = mbar_wait(empty(s), ((it / NS) - 1) & 1u, WAIT_LIMIT);
+                if (it >= (uint32_t)NS) ok = mbar_wait(empty(s), ((it / NS) - 1) & 1u, limit);
                 if (!ok) break;
                 uint8_t *tile = base_ptr + s * C::STAGE + TILE_W_BYTES;
                 // 128-byte swizzle: 16-byte chunk c of row r sits at chunk c ^ (r mod 8)
@@ -564,7 +574,7 @@ mx_matmul_narrow_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_
     if (warp >= 2) {
         asm volatile("bar.sync 1, 160;" ::: "memory");
         read_slot();
-        ok = mbar_wait_held(done, 0u) && ok;
+        ok = mbar_wait_held(done, 0u, held) && ok;
         ok = __all_sync(0xFFFFFFFFu, ok);
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
     }
@@ -615,6 +625,15 @@ bool make_codes_map(CUtensorMap *m, const void *ptr, uint64_t rows, uint64_t col
               CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+// What omc_mx_inject_wait_timeout asked for, for the calling thread's next product.
+thread_local Trial next_trial = {0u};
+Trial take_trial()
+{
+    const Trial t = next_trial;
+    next_trial = {0u};
+    return t;
+}
+
 struct Product {
     const uint8_t *x_codes, *x_scales, *w_codes, *w_scales;
     uint32_t M, N, K;
@@ -635,7 +654,7 @@ int launch(const Product &p, uint32_t splits)
     if (tiles >= (1ull << 31)) return OMC_ERR_INVALID_ARG;
     const uint32_t grid = (uint32_t)(splits > 1 ? tiles * splits : tiles < sms ? tiles : sms);
     return note_cuda(el::launch(mx_matmul_kernel<NT, T>, dim3(grid), THREADS, C::SMEM, splits, p.stream, map_w, map_x, p.w_scales, p.x_scales,
-                                static_cast<T *>(p.y), p.ldy, p.M, p.N, p.K, splits, p.status));
+                                static_cast<T *>(p.y), p.ldy, p.M, p.N, p.K, splits, p.status, take_trial()));
 }
 
 template <int NT, typename T, typename SOURCE>
@@ -651,7 +670,7 @@ int launch_narrow(const Product &p, uint32_t splits, SOURCE source)
     }
     if (const int rc = el::allow_smem<mx_matmul_narrow_kernel<NT, T, SOURCE>>(C::SMEM)) return rc;
     return note_cuda(el::launch(mx_matmul_narrow_kernel<NT, T, SOURCE>, dim3((uint32_t)mx::tiles_of(p.M, p.N, NT) * splits), C::THREADS, C::SMEM, splits, p.stream, map_w, map_x,
-                                p.w_scales, p.x_scales, source, static_cast<T *>(p.y), p.ldy, p.M, p.N, p.K, splits, p.status));
+                                p.w_scales, p.x_scales, source, static_cast<T *>(p.y), p.ldy, p.M, p.N, p.K, splits, p.status, take_trial()));
 }
 
 template <typename T>
@@ -725,4 +744,11 @@ extern "C" int omc_mx_linear(const void *x, int type, uint64_t M, uint64_t K, ui
     const int rc = omc_mx_quantise(x, type, M, K, ldx, workspace, scales, nullptr, nullptr, stream);
     if (rc) return rc;
     return product({workspace, scales, w_codes, w_scales, (uint32_t)M, (uint32_t)N, (uint32_t)K, y, ldy, status, stream}, y_type);
+}
+
+extern "C" int omc_mx_inject_wait_timeout(uint32_t polls)
+{
+    if (polls < 1 || polls > (1u << 16)) return OMC_ERR_INVALID_ARG;
+    next_trial = {polls};
+    return OMC_OK;
 }

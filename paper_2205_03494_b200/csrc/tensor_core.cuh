@@ -39,10 +39,11 @@ __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, uint32_
     return false;
 }
 // The same for waits that may be long: a poll lets the hardware hold the thread for up to 10 us (it goes on as soon as the phase
-// completes), which issues fewer instructions meanwhile; the limit is then about a second.
-__device__ __forceinline__ bool mbar_wait_held(uint32_t bar, uint32_t parity)
+// completes), which issues fewer instructions meanwhile; HELD_LIMIT is then about a second.
+constexpr uint32_t HELD_LIMIT = 1u << 17;
+__device__ __forceinline__ bool mbar_wait_held(uint32_t bar, uint32_t parity, uint32_t limit)
 {
-    for (uint32_t i = 0; i < (1u << 17); ++i) {
+    for (uint32_t i = 0; i < limit; ++i) {
         uint32_t ok;
         asm volatile(
             "{\n\t.reg .pred p;\n\t"
