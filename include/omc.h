@@ -438,13 +438,16 @@ int omc_mx_linear(const void *x, int type, uint64_t M, uint64_t K, uint64_t ldx,
                   uint64_t N, void *y, int y_type, uint64_t ldy, uint8_t *workspace, uint32_t *status, void *stream);
 
 /*
- * omc_mx_inject_wait_timeout -- diagnostics for the bounded waits of the two calls above.  The first CTA of the next product that
- * the calling thread launches announces its copies without issuing them and gives up each wait after `polls` polls
- * (1 .. 2^16, of up to 10 us each): its waits run out with no copy in flight, it sets the status word and returns, and what it would have
- * written to y is garbage.  The other CTAs are not touched, nor is any later call.  Host only.  For tests of the give-up path: nothing
+ * omc_mx_inject_wait_timeout -- diagnostics for the bounded waits of the two calls above.  In the next product with FP32 results that
+ * the calling thread launches every wait gives up after `polls` polls (1 .. 2^16, of up to 10 us each), and in its first CTA, by `what`,
+ *   OMC_MX_COPIES_MISSING   the copies are announced without being issued: the waits run out with no copy in flight;
+ *   OMC_MX_RESULTS_LATE     the waits for results give up at once, with the products still on their way.
+ * The CTA sets the status word and ends; what it would have written to y is garbage or not written.  (The other CTAs' waits end long
+ * before that many polls, if there are a thousand or more.)  No later call is touched.  Host only.  For tests of the give-up path: nothing
  * faults, hangs or reads out of bounds.
  */
-int omc_mx_inject_wait_timeout(uint32_t polls);
+enum { OMC_MX_COPIES_MISSING = 1, OMC_MX_RESULTS_LATE = 2 };
+int omc_mx_inject_wait_timeout(uint32_t polls, int what);
 
 /*
  * omc_layer_norm -- y = (x - mean) * rstd * gamma + beta per row, rstd = 1 / sqrt(variance + eps), the

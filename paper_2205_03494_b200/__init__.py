@@ -20,6 +20,7 @@ PLAN_PVT, PLAN_WEIGHTS_ONLY = 1, 2
 PLAN_DEFAULT = PLAN_PVT | PLAN_WEIGHTS_ONLY
 FORMAT_FIXED_POINT = 1
 F32, F16, BF16 = 0, 1, 2       # OMC_TYPE_*
+MX_COPIES_MISSING, MX_RESULTS_LATE = 1, 2
 
 EXPORTS = ["omc_strerror", "omc_last_cuda_error", "omc_plan", "omc_plan_destroy", "omc_plan_seed", "omc_plan_sizes",
            "omc_plan_var", "omc_plan_division", "omc_plan_prepare", "omc_plan_status", "omc_plan_inject_wait_timeout", "omc_compress", "omc_decompress",
@@ -91,7 +92,7 @@ def lib():
         L.omc_mx_dequantise.argtypes = [vp, vp, u64, u64, vp, i32, u64, vp]
         L.omc_mx_matmul.argtypes = [vp, vp, u64, vp, vp, u64, u64, vp, i32, u64, vp, vp]
         L.omc_mx_linear.argtypes = [vp, i32, u64, u64, u64, vp, vp, u64, vp, i32, u64, vp, vp, vp]
-        L.omc_mx_inject_wait_timeout.argtypes = [C.c_uint32]
+        L.omc_mx_inject_wait_timeout.argtypes = [C.c_uint32, i32]
         L.omc_layer_norm.argtypes = [vp, i32, u64, u64, u64, vp, vp, C.c_float, vp, u64, vp, vp, vp]
         L.omc_layer_norm_workspace.argtypes = [u64, u64, u64p]
         L.omc_layer_norm_backward.argtypes = [vp, u64, vp, u64, i32, u64, u64, vp, vp, vp, vp, u64, vp, vp, vp, vp]
@@ -311,9 +312,9 @@ def mx_linear(x, type_, M, K, ldx, w_codes, w_scales, N, y, y_type, ldy, workspa
         _check(rc, "omc_mx_linear")
 
 
-def mx_inject_wait_timeout(polls: int):
+def mx_inject_wait_timeout(polls: int, what: int):
     """omc_mx_inject_wait_timeout: the first CTA of this thread's next product gives up its waits (diagnostics)."""
-    _check(lib().omc_mx_inject_wait_timeout(int(polls)), "omc_mx_inject_wait_timeout")
+    _check(lib().omc_mx_inject_wait_timeout(int(polls), int(what)), "omc_mx_inject_wait_timeout")
 
 
 def layer_norm(x, type_, rows, cols, ld, gamma, beta, eps, y, ldy, mean=0, rstd=0, stream=0):

@@ -127,17 +127,38 @@ __device__ __forceinline__ void copies_landed(uint32_t issued, uint32_t stages, 
 {
     for (uint32_t it = issued > stages ? issued - stages : 0u; it < issued; ++it) mbar_wait_held(full(it % stages), (it / stages) & 1u, limit);
 }
-// ... and what was issued to the tensor cores has finished (a barrier for this alone).
+// ... and what was issued to the tensor cores has finished, whichever thread's wait it was (a barrier for this alone).
 __device__ __forceinline__ void products_finished(uint32_t bar)
 {
     umma_commit(bar);
     mbar_wait_held(bar, 0u, HELD_LIMIT);
 }
-// Diagnostics (omc_mx_inject_wait_timeout): the first CTA gives up each wait after `polls` polls (0: the default limits)
-// and announces its copies without issuing them.
+// A thread whose wait ran out says so to the caller and, through a word of shared memory, to the CTA's issuing thread, which asks
+// behind a barrier.  (A barrier that joins the threads' answers costs 1024 x 2048 x 2048 1.5 %.)
+__device__ __forceinline__ void shared_word(uint32_t addr, uint32_t v) { asm volatile("st.shared.u32 [%0], %1;" ::"r"(addr), "r"(v) : "memory"); }
+__device__ __forceinline__ uint32_t shared_word(uint32_t addr)
+{
+    uint32_t v;
+    asm volatile("ld.shared.u32 %0, [%1];" : "=r"(v) : "r"(addr) : "memory");
+    return v;
+}
+__device__ __forceinline__ void give_up(uint32_t *status, uint32_t gave_up)
+{
+    atomicExch(status, 1u);
+    shared_word(gave_up, 1u);
+}
+// The waits' limits: constants, and for omc_mx_inject_wait_timeout, in kernels of their own (limits that are variables cost
+// 1024 x 2048 x 2048 5 %, 16384 x 2048 x 8192 0.8 %), the given number of polls; the first CTA then announces its copies without issuing them, or gives up the waits
+// for results at once, with the products on their way.
+struct Usual {
+    static constexpr uint32_t polls = WAIT_LIMIT, held = HELD_LIMIT;
+    static __device__ __forceinline__ bool missing() { return false; }
+    static __device__ __forceinline__ uint32_t results() { return held; }
+};
 struct Trial {
-    uint32_t polls;
-    __device__ __forceinline__ bool here() const { return polls != 0u && blockIdx.x == 0; }
+    uint32_t polls, held, what;
+    __device__ __forceinline__ bool missing() const { return what == OMC_MX_COPIES_MISSING && blockIdx.x == 0; }
+    __device__ __forceinline__ uint32_t results() const { return what == OMC_MX_RESULTS_LATE && blockIdx.x == 0 ? 0u : held; }
 };
 // Four neighbouring values of a row of Y, as many of them as the row has.
 template <typename T>
@@ -195,27 +216,26 @@ __device__ __forceinline__ void tile_of(uint32_t t, uint32_t tiles_n, uint32_t t
     tn = band * 16 + in_band - tm * width;
 }
 
-template <int NT, typename T>
+template <int NT, typename T, typename WAITS>
 __global__ void __launch_bounds__(THREADS, 1)
 mx_matmul_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_x,
                  const uint8_t *w_scales, const uint8_t *x_scales, T *__restrict__ y, uint64_t ldy,
-                 uint32_t M, uint32_t N, uint32_t K, uint32_t splits, uint32_t *status, Trial trial)
+                 uint32_t M, uint32_t N, uint32_t K, uint32_t splits, uint32_t *status, WAITS waits)
 {
     using C = Cfg<NT>;
     constexpr int NS = C::NSTAGES;
     extern __shared__ uint8_t smem_raw[];
     const uint32_t base = (saddr(smem_raw) + 1023u) & ~1023u;
     uint8_t *const base_ptr = smem_raw + (base - saddr(smem_raw));
-    const uint32_t bars = base + NS * C::STAGE;      // full[NS], empty[NS], acc_full[2], acc_shared[2], acc_empty[2], scaled[SLOTS], drained; tmem slot
+    const uint32_t bars = base + NS * C::STAGE;      // full[NS], empty[NS], acc_full[2], acc_shared[2], acc_empty[2], scaled[SLOTS], drained; tmem slot, gave_up
     auto full = [&](int s) { return bars + 8u * s; };
     auto empty = [&](int s) { return bars + 8u * (NS + s); };
     auto acc_full = [&](int b) { return bars + 8u * (2 * NS + b); };
     auto acc_shared = [&](int b) { return bars + 8u * (2 * NS + 2 + b); };      // the shared columns have been read
     auto acc_empty = [&](int b) { return bars + 8u * (2 * NS + 4 + b); };       // all have
     auto scaled = [&](int s) { return bars + 8u * (2 * NS + 6 + s); };          // a step's scales are in tensor memory
-    const uint32_t drained = bars + 8u * (C::BARRIERS - 1), tmem_slot = bars + 8u * C::BARRIERS;
+    const uint32_t drained = bars + 8u * (C::BARRIERS - 1), tmem_slot = bars + 8u * C::BARRIERS, gave_up = tmem_slot + 4u;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-    const uint32_t limit = trial.here() ? trial.polls : WAIT_LIMIT, held = trial.here() ? trial.polls : HELD_LIMIT;
     // with divided K a cluster has one tile, and a CTA of it a range of its K steps
     const uint32_t rank = splits > 1 ? cluster_cta_rank() : 0u;
     const uint32_t ksteps = (K + BK - 1) / BK;
@@ -228,6 +248,7 @@ mx_matmul_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constan
         for (int s = 0; s < NS; ++s) { mbar_init(full(s), 1); mbar_init(empty(s), 1); }
         for (int s = 0; s < C::SLOTS; ++s) mbar_init(scaled(s), SCALE_THREADS);
         mbar_init(drained, 1);
+        shared_word(gave_up, 0u);
         for (int b = 0; b < 2; ++b) {
             mbar_init(acc_full(b), 1);
             mbar_init(acc_shared(b), EPILOGUE_THREADS);
@@ -259,11 +280,11 @@ mx_matmul_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constan
             const uint8_t *xs1 = x_scales + (uint64_t)min(xb + 1, x_blocks - 1) * ksteps * SCALE_BYTES;      // (no such rows: any scales)
             for (uint32_t k = k_begin; k < k_end; ++k, ++it) {
                 const int s = it % NS;
-                if (it >= (uint32_t)NS) ok = mbar_wait(empty(s), ((it / NS) - 1) & 1u, limit);
+                if (it >= (uint32_t)NS) ok = mbar_wait(empty(s), ((it / NS) - 1) & 1u, waits.polls);
                 if (!ok) break;
                 const uint32_t a = base + s * C::STAGE, sc = a + TILE_W_BYTES + C::TILE_X_BYTES;
                 mbar_expect_tx(full(s), C::STAGE);
-                if (trial.here()) continue;
+                if (waits.missing()) continue;
                 tma_load_2d(a, &map_w, (int)(k * (BK / 2)), (int)(tn * BM), full(s));
                 tma_load_2d(a + TILE_W_BYTES, &map_x, (int)(k * (BK / 2)), (int)(tm * NT), full(s));
                 bulk_load(sc, ws + (uint64_t)k * SCALE_BYTES, SCALE_BYTES, full(s));
@@ -271,19 +292,19 @@ mx_matmul_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constan
                 if (C::X_BLOCKS == 2) bulk_load(sc + 2 * SCALE_BYTES, xs1 + (uint64_t)k * SCALE_BYTES, SCALE_BYTES, full(s));
             }
         }
-        copies_landed(it, NS, held, full);
+        copies_landed(it, NS, waits.held, full);
     } else if (tid == 32) {
         uint32_t it = 0, lt = 0;
         for (uint32_t t = first; t < ntiles && ok; t += step, ++lt) {
             const uint32_t buf = lt & 1u;
-            if (C::SHARED_COLS && lt >= 1) ok = mbar_wait(acc_shared(buf ^ 1u), ((lt - 1) >> 1) & 1u, limit);     // of the tile before
-            if (ok && lt >= 2) ok = mbar_wait(acc_empty(buf), ((lt >> 1) - 1) & 1u, limit);                       // of the one before that
+            if (C::SHARED_COLS && lt >= 1) ok = mbar_wait(acc_shared(buf ^ 1u), ((lt - 1) >> 1) & 1u, waits.polls);     // of the tile before
+            if (ok && lt >= 2) ok = mbar_wait(acc_empty(buf), ((lt >> 1) - 1) & 1u, waits.polls);                       // of the one before that
             if (!ok) break;
             const uint32_t d = tmem_base + buf * C::ACC1;
             for (uint32_t k = k_begin; k < k_end; ++k, ++it) {
                 const int s = it % NS;
-                ok = mbar_wait_held(full(s), (it / NS) & 1u, held);
-                ok = ok && mbar_wait_held(scaled(it % C::SLOTS), (it / C::SLOTS) & 1u, held);
+                ok = mbar_wait_held(full(s), (it / NS) & 1u, waits.held);
+                ok = ok && mbar_wait_held(scaled(it % C::SLOTS), (it / C::SLOTS) & 1u, waits.held);
                 if (!ok) break;
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
                 const uint32_t a = base + s * C::STAGE, b = a + TILE_W_BYTES;
@@ -296,13 +317,12 @@ mx_matmul_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constan
             }
             if (ok) umma_commit(acc_full(buf));
         }
-        if (!ok) products_finished(drained);
     } else if (warp >= 12) {
         const uint32_t quarter = (uint32_t)((warp & 3) * 32) << 16;
         for (uint32_t it = 0; it < steps; ++it) {
             const int s = it % NS;
-            if (it >= (uint32_t)C::SLOTS) ok = mbar_wait(empty((it - C::SLOTS) % NS), ((it - C::SLOTS) / NS) & 1u, limit);      // columns are free
-            ok = ok && mbar_wait_held(full(s), (it / NS) & 1u, held);
+            if (it >= (uint32_t)C::SLOTS) ok = mbar_wait(empty((it - C::SLOTS) % NS), ((it - C::SLOTS) / NS) & 1u, waits.polls);      // columns are free
+            ok = ok && mbar_wait_held(full(s), (it / NS) & 1u, waits.held);
             ok = __all_sync(0xFFFFFFFFu, ok);
             if (!ok) break;
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
@@ -326,7 +346,7 @@ mx_matmul_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constan
             const uint32_t buf = lt & 1u;
             uint32_t tn, tm;
             tile_of(t, tiles_n, tiles_m, tn, tm);
-            ok = mbar_wait_held(acc_full(buf), (lt >> 1) & 1u, held);
+            ok = mbar_wait_held(acc_full(buf), (lt >> 1) & 1u, waits.results());
             ok = __all_sync(0xFFFFFFFFu, ok);
             if (t + step >= ntiles) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
             if (!ok || (C::DIVIDES && splits > 1)) break;
@@ -404,10 +424,12 @@ mx_matmul_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constan
         cluster_barrier();                                 // the parts of this CTA's rows have arrived
         add_parts(reinterpret_cast<const float4 *>(base_ptr) + lane, warp, THREADS / 32, splits, mine, m0 + rank * mine, M, tn * BM + lane * 4, N, y, ldy);
     }
-    if (!ok) atomicExch(status, 1u);
+    if (!ok) give_up(status, gave_up);
     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
     __syncwarp();
     __syncthreads();
+    if (tid == 32 && shared_word(gave_up)) products_finished(drained);
+    __syncwarp();
     if (warp == 1)
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"((uint32_t)TMEM_COLS) : "memory");
 }
@@ -444,11 +466,11 @@ struct Nothing {};
 // X quantised already (SOURCE = Nothing: map_x, x_scales), or at most 16 rows of values of type TX (SOURCE = Values<TX>), which warps 2-5 of
 // every CTA quantise for themselves on the way into the operand tile: a thread a block, 8 `rows` threads a K step, the other threads
 // the steps after it.  Tile rows behind `rows` stay as they are: they only enter columns that nobody reads.
-template <int NT, typename T, typename SOURCE>
+template <int NT, typename T, typename SOURCE, typename WAITS>
 __global__ void __launch_bounds__(Narrow<NT>::THREADS)
 mx_matmul_narrow_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_x,
                         const uint8_t *w_scales, const uint8_t *x_scales, SOURCE source, T *__restrict__ y, uint64_t ldy,
-                        uint32_t M, uint32_t N, uint32_t K, uint32_t splits, uint32_t *status, Trial trial)
+                        uint32_t M, uint32_t N, uint32_t K, uint32_t splits, uint32_t *status, WAITS waits)
 {
     constexpr bool VALUES = !std::is_same<SOURCE, Nothing>::value;
     static_assert(!VALUES || NT == 16, "sixteen rows of eight blocks are a thread each");
@@ -457,12 +479,11 @@ mx_matmul_narrow_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_
     extern __shared__ uint8_t smem_raw[];
     const uint32_t base = (saddr(smem_raw) + 1023u) & ~1023u;
     uint8_t *const base_ptr = smem_raw + (base - saddr(smem_raw));
-    const uint32_t bars = base + NS * C::STAGE;           // full[NS], empty[NS], done, drained, tmem slot
+    const uint32_t bars = base + NS * C::STAGE;           // full[NS], empty[NS], done, drained; tmem slot, gave_up
     auto full = [&](int s) { return bars + 8u * s; };
     auto empty = [&](int s) { return bars + 8u * (NS + s); };
-    const uint32_t done = bars + 8u * (2 * NS), drained = done + 8u, tmem_slot = drained + 8u;
+    const uint32_t done = bars + 8u * (2 * NS), drained = done + 8u, tmem_slot = drained + 8u, gave_up = tmem_slot + 4u;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-    const uint32_t limit = trial.here() ? trial.polls : WAIT_LIMIT, held = trial.here() ? trial.polls : HELD_LIMIT;
     const uint32_t rank = splits > 1 ? cluster_cta_rank() : 0u;
     const uint32_t tile_n = blockIdx.x / splits;
     const uint32_t ksteps = (K + BK - 1) / BK;
@@ -474,6 +495,7 @@ mx_matmul_narrow_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_
         for (int s = 0; s < NS; ++s) { mbar_init(full(s), arrivals); mbar_init(empty(s), 1); }
         mbar_init(done, 1);
         mbar_init(drained, 1);
+        shared_word(gave_up, 0u);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     __syncthreads();
@@ -498,11 +520,11 @@ mx_matmul_narrow_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_
         uint32_t it = 0;
         for (uint32_t k = k_begin; k < k_end; ++k, ++it) {
             const int s = it % NS;
-            if (it >= (uint32_t)NS) ok = mbar_wait(empty(s), ((it / NS) - 1) & 1u, limit);
+            if (it >= (uint32_t)NS) ok = mbar_wait(empty(s), ((it / NS) - 1) & 1u, waits.polls);
             if (!ok) break;
             const uint32_t a = base + s * C::STAGE;
             mbar_expect_tx(full(s), VALUES ? TILE_W_BYTES + SCALE_BYTES : C::STAGE);
-            if (trial.here()) continue;
+            if (waits.missing()) continue;
             tma_load_2d(a, &map_w, (int)(k * (BK / 2)), (int)(tile_n * BM), full(s));
             bulk_load(a + TILE_W_BYTES + C::TILE_X_BYTES, ws + (uint64_t)k * SCALE_BYTES, SCALE_BYTES, full(s));
             if constexpr (!VALUES) {
@@ -510,12 +532,12 @@ mx_matmul_narrow_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_
                 bulk_load(a + TILE_W_BYTES + C::TILE_X_BYTES + SCALE_BYTES, x_scales + (uint64_t)k * SCALE_BYTES, SCALE_BYTES, full(s));
             }
         }
-        copies_landed(it, NS, held, full);
+        copies_landed(it, NS, waits.held, full);
     } else if (tid == 32) {
         const uint32_t steps = k_end - k_begin;
         auto bring_scales = [&](uint32_t it) {            // its columns were last read NS steps ago, before the stage was refilled
             const int s = it % NS;
-            if (!mbar_wait_held(full(s), (it / NS) & 1u, held)) return false;
+            if (!mbar_wait_held(full(s), (it / NS) & 1u, waits.held)) return false;
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
             const uint32_t sc = base + s * C::STAGE + TILE_W_BYTES + C::TILE_X_BYTES;
             const uint32_t ta = tmem_base + C::D_COLS + s * 2 * SCALE_COLS, tb = ta + SCALE_COLS;
@@ -540,7 +562,6 @@ mx_matmul_narrow_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_
             umma_commit(empty(s));
         }
         if (ok) umma_commit(done);
-        else products_finished(drained);
     } else if (VALUES && warp >= 2) {
         if constexpr (VALUES) {
             const uint32_t t = tid - 64, team = 8 * source.rows, r = t % team / 8, block = t % 8;
@@ -557,7 +578,7 @@ mx_matmul_narrow_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_
                     mx::load<typename SOURCE::Type, false, 32>(source.x + r * source.ld, col, K, w);
                 }
                 mx::encode_block<typename SOURCE::Type, 32>(w, codes, scale);
-                if (it >= (uint32_t)NS) ok = mbar_wait(empty(s), ((it / NS) - 1) & 1u, limit);
+                if (it >= (uint32_t)NS) ok = mbar_wait(empty(s), ((it / NS) - 1) & 1u, waits.polls);
                 if (!ok) break;
                 uint8_t *tile = base_ptr + s * C::STAGE + TILE_W_BYTES;
                 // 128-byte swizzle: 16-byte chunk c of row r sits at chunk c ^ (r mod 8)
@@ -574,7 +595,7 @@ mx_matmul_narrow_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_
     if (warp >= 2) {
         asm volatile("bar.sync 1, 160;" ::: "memory");
         read_slot();
-        ok = mbar_wait_held(done, 0u, held) && ok;
+        ok = mbar_wait_held(done, 0u, waits.results()) && ok;
         ok = __all_sync(0xFFFFFFFFu, ok);
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
     }
@@ -601,9 +622,11 @@ mx_matmul_narrow_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_
         }
         asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
     }
-    if (!ok) atomicExch(status, 1u);
+    if (!ok) give_up(status, gave_up);
     __syncwarp();
     __syncthreads();
+    if (tid == 32 && shared_word(gave_up)) products_finished(drained);
+    __syncwarp();
     if (splits > 1) {
         cluster_barrier();                                 // the parts of this CTA's rows have arrived
         add_parts(reinterpret_cast<const float4 *>(base_ptr) + lane, warp, C::THREADS / 32, splits, mine, rank * mine, M, tile_n * BM + lane * 4, N, y, ldy);
@@ -625,12 +648,12 @@ bool make_codes_map(CUtensorMap *m, const void *ptr, uint64_t rows, uint64_t col
               CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-// What omc_mx_inject_wait_timeout asked for, for the calling thread's next product.
-thread_local Trial next_trial = {0u};
+// What omc_mx_inject_wait_timeout asked for, for the calling thread's next product with FP32 results (what = 0: nothing).
+thread_local Trial next_trial = {0u, 0u, 0u};
 Trial take_trial()
 {
     const Trial t = next_trial;
-    next_trial = {0u};
+    next_trial = {0u, 0u, 0u};
     return t;
 }
 
@@ -643,22 +666,22 @@ struct Product {
     void *stream;
 };
 
-template <int NT, typename T>
-int launch(const Product &p, uint32_t splits)
+template <int NT, typename T, typename WAITS>
+int launch(const Product &p, uint32_t splits, WAITS waits)
 {
     using C = Cfg<NT>;
     CUtensorMap map_w, map_x;
     if (!make_codes_map(&map_w, p.w_codes, p.N, p.K, BM) || !make_codes_map(&map_x, p.x_codes, p.M, p.K, NT)) return OMC_ERR_CUDA;
-    if (const int rc = el::allow_smem<mx_matmul_kernel<NT, T>>(C::SMEM)) return rc;
+    if (const int rc = el::allow_smem<mx_matmul_kernel<NT, T, WAITS>>(C::SMEM)) return rc;
     const uint64_t tiles = mx::tiles_of(p.M, p.N, NT), sms = el::sm_count();
     if (tiles >= (1ull << 31)) return OMC_ERR_INVALID_ARG;
     const uint32_t grid = (uint32_t)(splits > 1 ? tiles * splits : tiles < sms ? tiles : sms);
-    return note_cuda(el::launch(mx_matmul_kernel<NT, T>, dim3(grid), THREADS, C::SMEM, splits, p.stream, map_w, map_x, p.w_scales, p.x_scales,
-                                static_cast<T *>(p.y), p.ldy, p.M, p.N, p.K, splits, p.status, take_trial()));
+    return note_cuda(el::launch(mx_matmul_kernel<NT, T, WAITS>, dim3(grid), THREADS, C::SMEM, splits, p.stream, map_w, map_x, p.w_scales, p.x_scales,
+                                static_cast<T *>(p.y), p.ldy, p.M, p.N, p.K, splits, p.status, waits));
 }
 
-template <int NT, typename T, typename SOURCE>
-int launch_narrow(const Product &p, uint32_t splits, SOURCE source)
+template <int NT, typename T, typename SOURCE, typename WAITS>
+int launch_narrow(const Product &p, uint32_t splits, SOURCE source, WAITS waits)
 {
     using C = Narrow<NT>;
     CUtensorMap map_w, map_x;
@@ -668,21 +691,21 @@ int launch_narrow(const Product &p, uint32_t splits, SOURCE source)
     } else {
         map_x = map_w;      // not used
     }
-    if (const int rc = el::allow_smem<mx_matmul_narrow_kernel<NT, T, SOURCE>>(C::SMEM)) return rc;
-    return note_cuda(el::launch(mx_matmul_narrow_kernel<NT, T, SOURCE>, dim3((uint32_t)mx::tiles_of(p.M, p.N, NT) * splits), C::THREADS, C::SMEM, splits, p.stream, map_w, map_x,
-                                p.w_scales, p.x_scales, source, static_cast<T *>(p.y), p.ldy, p.M, p.N, p.K, splits, p.status, take_trial()));
+    if (const int rc = el::allow_smem<mx_matmul_narrow_kernel<NT, T, SOURCE, WAITS>>(C::SMEM)) return rc;
+    return note_cuda(el::launch(mx_matmul_narrow_kernel<NT, T, SOURCE, WAITS>, dim3((uint32_t)mx::tiles_of(p.M, p.N, NT) * splits), C::THREADS, C::SMEM, splits, p.stream, map_w, map_x,
+                                p.w_scales, p.x_scales, source, static_cast<T *>(p.y), p.ldy, p.M, p.N, p.K, splits, p.status, waits));
 }
 
-template <typename T>
-int launch_any(const Product &p)
+template <typename T, typename WAITS>
+int launch_any(const Product &p, WAITS waits)
 {
     const mx::Schedule s = mx::schedule_of(p.M, p.N, p.K);
     switch (s.tile) {
-    case 16: return launch_narrow<16, T>(p, s.splits, Nothing());
-    case 32: return launch_narrow<32, T>(p, s.splits, Nothing());
-    case 64: return launch_narrow<64, T>(p, s.splits, Nothing());
-    case 128: return launch<128, T>(p, s.splits);
-    default: return launch<256, T>(p, s.splits);
+    case 16: return launch_narrow<16, T>(p, s.splits, Nothing(), waits);
+    case 32: return launch_narrow<32, T>(p, s.splits, Nothing(), waits);
+    case 64: return launch_narrow<64, T>(p, s.splits, Nothing(), waits);
+    case 128: return launch<128, T>(p, s.splits, waits);
+    default: return launch<256, T>(p, s.splits, waits);
     }
 }
 
@@ -696,13 +719,18 @@ int product_of_values(const Product &p, const void *x, uint64_t ld, int type)
     while (rows < p.M) rows *= 2;
     const Values<TX> v = {static_cast<const TX *>(x), ld, rows, el::aligned16(x) && ld * sizeof(TX) % 16 == 0};
     const uint32_t splits = mx::schedule_of(p.M, p.N, p.K).splits;
-    return type == OMC_TYPE_F32   ? launch_narrow<16, float>(p, splits, v)
-           : type == OMC_TYPE_F16 ? launch_narrow<16, __half>(p, splits, v) : launch_narrow<16, __nv_bfloat16>(p, splits, v);
+    if (type == OMC_TYPE_F16) return launch_narrow<16, __half>(p, splits, v, Usual());
+    if (type == OMC_TYPE_BF16) return launch_narrow<16, __nv_bfloat16>(p, splits, v, Usual());
+    const Trial trial = take_trial();
+    return trial.what ? launch_narrow<16, float>(p, splits, v, trial) : launch_narrow<16, float>(p, splits, v, Usual());
 }
 
 int product(const Product &p, int type)
 {
-    return type == OMC_TYPE_F32 ? launch_any<float>(p) : type == OMC_TYPE_F16 ? launch_any<__half>(p) : launch_any<__nv_bfloat16>(p);
+    if (type == OMC_TYPE_F16) return launch_any<__half>(p, Usual());
+    if (type == OMC_TYPE_BF16) return launch_any<__nv_bfloat16>(p, Usual());
+    const Trial trial = take_trial();
+    return trial.what ? launch_any<float>(p, trial) : launch_any<float>(p, Usual());
 }
 
 bool product_shape_ok(uint64_t M, uint64_t N, uint64_t K)
@@ -746,9 +774,9 @@ extern "C" int omc_mx_linear(const void *x, int type, uint64_t M, uint64_t K, ui
     return product({workspace, scales, w_codes, w_scales, (uint32_t)M, (uint32_t)N, (uint32_t)K, y, ldy, status, stream}, y_type);
 }
 
-extern "C" int omc_mx_inject_wait_timeout(uint32_t polls)
+extern "C" int omc_mx_inject_wait_timeout(uint32_t polls, int what)
 {
-    if (polls < 1 || polls > (1u << 16)) return OMC_ERR_INVALID_ARG;
-    next_trial = {polls};
+    if (polls < 1 || polls > (1u << 16) || (what != OMC_MX_COPIES_MISSING && what != OMC_MX_RESULTS_LATE)) return OMC_ERR_INVALID_ARG;
+    next_trial = {polls, polls, (uint32_t)what};
     return OMC_OK;
 }

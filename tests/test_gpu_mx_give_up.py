@@ -1,6 +1,6 @@
 """The give-up path of the 4-bit products' bounded waits, run in the one form that cannot fault or hang: omc_mx_inject_wait_timeout
-makes the first CTA of the next product announce its copies without issuing them, so that its waits run out.  It has to set the
-status word and end, the other CTAs' results have to be right, nothing may be written outside Y, and the next call gives the same
+makes the first CTA of the next product announce its copies without issuing them, so that its waits run out, or give up the waits
+for results while its products are on their way (tensor memory may be let go only after them).  It has to set the status word and end, the other CTAs' results have to be right, nothing may be written outside Y, and the next call gives the same
 bits as one before it."""
 import numpy as np
 import pytest
@@ -75,9 +75,15 @@ def check(name, linear, inject):
 @pytest.mark.parametrize("linear", [False, True], ids=["matmul", "linear"])
 @pytest.mark.parametrize("name", list(SHAPES))
 def test_copies_that_never_arrive(name, linear):
-    check(name, linear, lambda: omc.mx_inject_wait_timeout(1 << 8))
+    check(name, linear, lambda: omc.mx_inject_wait_timeout(1 << 10, omc.MX_COPIES_MISSING))
+
+
+@pytest.mark.parametrize("linear", [False, True], ids=["matmul", "linear"])
+@pytest.mark.parametrize("name", list(SHAPES))
+def test_results_given_up_with_products_on_their_way(name, linear):
+    check(name, linear, lambda: omc.mx_inject_wait_timeout(1 << 14, omc.MX_RESULTS_LATE))
 
 
 def test_injection_argument_checks():
-    assert omc.lib().omc_mx_inject_wait_timeout(0) == -1
-    assert omc.lib().omc_mx_inject_wait_timeout((1 << 16) + 1) == -1
+    for polls, what in ((0, 1), ((1 << 16) + 1, 1), (10, 0), (10, 3)):
+        assert omc.lib().omc_mx_inject_wait_timeout(polls, what) == -1
