@@ -424,6 +424,9 @@ mx_matmul_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constan
         cluster_barrier();                                 // the parts of this CTA's rows have arrived
         add_parts(reinterpret_cast<const float4 *>(base_ptr) + lane, warp, THREADS / 32, splits, mine, m0 + rank * mine, M, tn * BM + lane * 4, N, y, ldy);
     }
+    // The first tile's number keeps a register to the end, as the join would make it: if the loops over the tiles may count in that
+    // register, the compiler's code for them is 2 % slower (16384 x 2048 x 8192 109.1 instead of 107.0 us).
+    if constexpr (!C::DIVIDES) asm volatile("" ::"r"(first));
     if (!ok) give_up(status, gave_up);
     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
     __syncwarp();
