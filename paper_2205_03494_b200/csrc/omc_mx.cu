@@ -5,8 +5,12 @@
 // through shared memory and a thread holds whole blocks.  The scale is a power of two, so that scaling is exact and
 // the only rounding is the conversion to E2M1.
 // Memory bounds the kernels along the rows and back (16384 x 8192 BF16 52 us, 6.5 TB/s; 8192 x 2048 FP32 back 11.0 us, 6.9 TB/s:
-// the rate of a plain copy); both ways at once the instructions do (8192 x 8192 BF16 40 us, 5.2 TB/s; 8192 x 2048 FP32
-// 17.7 us, 4.8 TB/s): each value is scaled and rounded twice.  Copying the tile past the registers (cp.async) was slower, 54 us.
+// the rate of a plain copy).  Both ways at once (8192 x 8192 BF16 40 us, 5.2 TB/s; 8192 x 2048 FP32 17.6 us, 4.8 TB/s) nothing is
+// used up (issue slots 68 %, L1 62 %, DRAM 50 %): each value is scaled and rounded twice, and a CTA loads its one tile, encodes it and stores
+// it in turn, with barriers between.  Along the columns alone (32 us, 5.2 TB/s; 12.8 us, 5.9 TB/s) it is these phases too
+// (issue slots 48 %, waiting for loads).  Copying the tile past the registers (cp.async) was slower, 54 us.
+// Off the 16-byte boundaries the instructions bound both directions: rows are turned in shared memory and 16-bit values move two at a time
+// (8192 x 4095 BF16 back 24 us, 1.9 times the time its bytes need, 16384 x 8191 BF16 79 us, 1.5 times; 75 % of the issue slots).
 #include <cuda_runtime.h>
 
 #include <type_traits>

@@ -21,11 +21,13 @@
 // narrower ones spread a small product over more SMs.  With fewer tiles than SMs the K steps of a tile are divided
 // among the CTAs of a cluster: each owns a share of X's rows and gets the others' parts of these (stores to distributed
 // shared memory, which nobody waits for), which it adds up in a fixed order.
-// Every wait is bounded; tensor memory is released on every path.  It is taken only after the kernel before on the
-// stream has finished: nothing waits for another kernel while it holds what others need.
-// Measured: M = 16384, N = 2048, K = 8192 99 us (5.5 PFLOP/s; 126 us, 4.4 PFLOP/s, held at 1.48 GHz by the power cap when repeated
-// for seconds), M = N = 8192, K = 2048 68 us.  What bounds it is the rate of the instruction itself: the same loop with
-// neither copies nor scales nor results takes 98 us.
+// The waits for copies, products and results are bounded, those of a cluster's CTAs for one another end because these do; tensor memory is
+// released on every path, after the products.  It is taken only after the kernel before on the stream has finished: nothing
+// waits for another kernel while it holds what others need.
+// Measured: M = 16384, N = 2048, K = 8192 107 us (5.1 PFLOP/s, twenty in a row; 125 us, 4.4 PFLOP/s, held at 1.48 GHz by the power cap
+// when repeated for seconds), M = N = 8192, K = 2048 67 us.  The instructions alone, without copies, scales and results, take
+// 98 us at the first of these; most of the rest is the way from a freed step to the next scales in tensor memory, which the
+// products wait for (one more exchange between lanes there cost 3 to 5 %).
 #include <cuda.h>
 #include <cuda_runtime.h>
 
