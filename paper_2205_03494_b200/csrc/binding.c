@@ -8,16 +8,19 @@
 
 #include "../../include/omc.h"
 
-/* -1 in *bad if an argument is no integer in range (the exception is set). */
+/* -1 in *bad if an argument is no integer in range (the exception is set).  Whatever stands for an integer is one (numpy's, say). */
 static uint64_t whole(PyObject *o, int *bad)
 {
-    if (o == Py_None) return 0;
-    const unsigned long long v = PyLong_AsUnsignedLongLong(o);
+    if (o == Py_None || *bad) return 0;
+    PyObject *n = PyLong_Check(o) ? Py_NewRef(o) : PyNumber_Index(o);
+    const unsigned long long v = n ? PyLong_AsUnsignedLongLong(n) : (unsigned long long)-1;
+    Py_XDECREF(n);
     if (v == (unsigned long long)-1 && PyErr_Occurred()) *bad = -1;
     return v;
 }
 static int small(PyObject *o, int *bad)
 {
+    if (*bad) return 0;
     const long v = PyLong_AsLong(o);
     if (v == -1 && PyErr_Occurred()) *bad = -1;
     if (v != (int)v) {
@@ -28,6 +31,7 @@ static int small(PyObject *o, int *bad)
 }
 static float real(PyObject *o, int *bad)
 {
+    if (*bad) return 0.f;
     const double v = PyFloat_AsDouble(o);
     if (v == -1.0 && PyErr_Occurred()) *bad = -1;
     return (float)v;
