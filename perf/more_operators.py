@@ -272,7 +272,7 @@ def _gate(case):
 def _room(rows, cols):
     """Codes and scales of a quantised rows x cols matrix."""
     import paper_2205_03494_b200 as omc
-    codes, scales = omc.i8_sizes(rows, cols)
+    codes, scales = omc.byte_sizes(rows, cols)
     return torch.empty(codes, dtype=torch.uint8, device="cuda"), torch.empty(scales, dtype=torch.uint8, device="cuda")
 
 
@@ -286,20 +286,20 @@ def _buffers(case):
     if op == "round_trip":
         r, c = case["rows"], case["cols"]
         d["q"], d["y"] = _room(r, c), new(r, c)
-        d["workspace"] = space(omc.i8_quantise_workspace_bytes(r, c))
+        d["workspace"] = space(omc.byte_quantise_workspace_bytes(r, c))
         if case["both"]:
             d["qt"], d["yt"] = _room(c, r), new(c, r)
         return d
     m, k = case["m"], case["k"]
     if op == "linear":
-        d["y"], d["workspace"] = new(m, case["n"]), space(sum(omc.i8_sizes(m, k)))
+        d["y"], d["workspace"] = new(m, case["n"]), space(sum(omc.byte_sizes(m, k)))
     elif op == "linear_backward":
         n = case["n"]
-        d["q"], d["qt"], d["workspace"] = _room(m, n), _room(n, m), space(omc.i8_quantise_workspace_bytes(m, n))
+        d["q"], d["qt"], d["workspace"] = _room(m, n), _room(n, m), space(omc.byte_quantise_workspace_bytes(m, n))
         d["dx"], d["dw"] = new(m, k), new(n, k, dtype=torch.float32)
     elif op == "gated":
         f = case["f"]
-        d["y"], d["workspace"] = new(m, f), space(sum(omc.i8_sizes(m, k)))
+        d["y"], d["workspace"] = new(m, f), space(sum(omc.byte_sizes(m, k)))
         if case["keep"]:
             d["kept"] = new(m, 2 * f)
     elif op == "gated_backward":
@@ -319,32 +319,32 @@ def _own(s):
     if op == "round_trip":
         r, c, q = case["rows"], case["cols"], s["q"]
         qt = s.get("qt")
-        omc.i8_quantise(s["x"].data_ptr(), ty, r, c, c, q[0].data_ptr(), q[1].data_ptr(), qt[0].data_ptr() if qt else 0,
+        omc.byte_quantise(s["x"].data_ptr(), ty, r, c, c, q[0].data_ptr(), q[1].data_ptr(), qt[0].data_ptr() if qt else 0,
                         qt[1].data_ptr() if qt else 0, s["workspace"].data_ptr(), stream=st)
-        omc.i8_dequantise(q[0].data_ptr(), q[1].data_ptr(), r, c, s["y"].data_ptr(), ty, c, stream=st)
+        omc.byte_dequantise(q[0].data_ptr(), q[1].data_ptr(), r, c, s["y"].data_ptr(), ty, c, stream=st)
         if not qt:
             return s["y"]
-        omc.i8_dequantise(qt[0].data_ptr(), qt[1].data_ptr(), c, r, s["yt"].data_ptr(), ty, r, stream=st)
+        omc.byte_dequantise(qt[0].data_ptr(), qt[1].data_ptr(), c, r, s["yt"].data_ptr(), ty, r, stream=st)
         return s["y"], s["yt"]
     m, k = case["m"], case["k"]
     if op == "linear":
         n = case["n"]
-        omc.i8_linear(s["x"].data_ptr(), ty, m, k, k, s["w"][0].data_ptr(), s["w"][1].data_ptr(), n, s["y"].data_ptr(), ty, n,
+        omc.byte_linear(s["x"].data_ptr(), ty, m, k, k, s["w"][0].data_ptr(), s["w"][1].data_ptr(), n, s["y"].data_ptr(), ty, n,
                       s["workspace"].data_ptr(), s["status"].data_ptr(), stream=st)
         return s["y"]
     if op == "linear_backward":
         n, q, qt = case["n"], s["q"], s["qt"]
-        omc.i8_quantise(s["dy"].data_ptr(), ty, m, n, n, q[0].data_ptr(), q[1].data_ptr(), qt[0].data_ptr(), qt[1].data_ptr(),
+        omc.byte_quantise(s["dy"].data_ptr(), ty, m, n, n, q[0].data_ptr(), q[1].data_ptr(), qt[0].data_ptr(), qt[1].data_ptr(),
                         s["workspace"].data_ptr(), stream=st)
-        omc.i8_matmul(q[0].data_ptr(), q[1].data_ptr(), m, s["wt"][0].data_ptr(), s["wt"][1].data_ptr(), k, n, s["dx"].data_ptr(), ty, k,
+        omc.byte_matmul(q[0].data_ptr(), q[1].data_ptr(), m, s["wt"][0].data_ptr(), s["wt"][1].data_ptr(), k, n, s["dx"].data_ptr(), ty, k,
                       s["status"].data_ptr(), stream=st)
-        omc.i8_matmul(qt[0].data_ptr(), qt[1].data_ptr(), n, s["xt"][0].data_ptr(), s["xt"][1].data_ptr(), k, m, s["dw"].data_ptr(), omc.F32, k,
+        omc.byte_matmul(qt[0].data_ptr(), qt[1].data_ptr(), n, s["xt"][0].data_ptr(), s["xt"][1].data_ptr(), k, m, s["dw"].data_ptr(), omc.F32, k,
                       s["status"].data_ptr(), stream=st)
         return s["dx"], s["dw"]
     f, act = case["f"], _gate(case)
     if op == "gated":
         kept = s.get("kept")
-        omc.i8_gated_linear(s["x"].data_ptr(), ty, m, k, k, s["w"][0].data_ptr(), s["w"][1].data_ptr(), f, act, s["y"].data_ptr(), ty, f,
+        omc.byte_gated_linear(s["x"].data_ptr(), ty, m, k, k, s["w"][0].data_ptr(), s["w"][1].data_ptr(), f, act, s["y"].data_ptr(), ty, f,
                             0 if kept is None else kept.data_ptr(), 2 * f, s["workspace"].data_ptr(), s["status"].data_ptr(), stream=st)
         return s["y"] if kept is None else (s["y"], kept)
     if op == "gated_backward":
@@ -353,9 +353,9 @@ def _own(s):
     q, qt = s["q"], s["qt"]
     omc.gated_backward(s["dy"].data_ptr(), f, s["pre"].data_ptr(), 2 * f, ty, m, f, act, 0, 0, q[0].data_ptr(), q[1].data_ptr(),
                        qt[0].data_ptr(), qt[1].data_ptr(), s["workspace"].data_ptr(), stream=st)
-    omc.i8_matmul(q[0].data_ptr(), q[1].data_ptr(), m, s["wt"][0].data_ptr(), s["wt"][1].data_ptr(), k, 2 * f, s["dx"].data_ptr(), ty, k,
+    omc.byte_matmul(q[0].data_ptr(), q[1].data_ptr(), m, s["wt"][0].data_ptr(), s["wt"][1].data_ptr(), k, 2 * f, s["dx"].data_ptr(), ty, k,
                   s["status"].data_ptr(), stream=st)
-    omc.i8_matmul(qt[0].data_ptr(), qt[1].data_ptr(), 2 * f, s["xt"][0].data_ptr(), s["xt"][1].data_ptr(), k, m, s["dw"].data_ptr(), ty, k,
+    omc.byte_matmul(qt[0].data_ptr(), qt[1].data_ptr(), 2 * f, s["xt"][0].data_ptr(), s["xt"][1].data_ptr(), k, m, s["dw"].data_ptr(), ty, k,
                   s["status"].data_ptr(), stream=st)
     return s["dx"], s["dw"]
 
