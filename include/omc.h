@@ -477,6 +477,94 @@ int omc_layer_norm_backward(const void *dy, uint64_t ld_dy, const void *x, uint6
                             const float *gamma, const float *mean, const float *rstd, void *dx, uint64_t ld_dx, float *dgamma,
                             float *dbeta, void *workspace, void *stream);
 
+/* ----------------------------------------------------------------------------------------------
+ * The same layer at eight bits, and a gated layer.  Two operands of a product in 8-bit integers with one FP32 scale for each row
+ * (a token, or an output channel) need no scale inside the sum: it is a sum of integers, exact in 32 bits, and the order of its
+ * additions does not show.  The paper's convolution modules gate (GLU), and so do the feed-forward layers that came after it.
+ *
+ * The 8-bit format: every row of a matrix has the scale
+ *     s = max(largest magnitude of the row / 127, 2^-126),    and the codes    q = nearest integer to x * r, ties to even, r = 1 / s,
+ * s and r rounded to FP32, x * r not rounded before it is made an integer; -127 <= q <= 127, and a code stands for q * s.  A row that
+ * holds an Inf or a NaN has the scale NaN and codes 0: it makes the row or column of a product that it enters NaN.
+ * Layout of a quantised rows x cols matrix (sizes: omc_byte_sizes):
+ *   codes   row r at byte r * 16 * ceil(cols / 16), a byte each; those behind the last column are 0.
+ *   scales  rows floats.
+ * The codes of a variable that the store holds as S1I0F7 have this layout too, if its rows are whole 16 bytes: with s / 128 (Sec. 2.3) in every
+ * row's place of `scales` they are an operand of the products below as they stand (a variable's b has no place here: plan it without PVT).
+ * omc_byte_sizes: host only; 1 <= rows, cols < 2^31; scales_bytes is a multiple of 16.  Either output pointer may be NULL.
+ */
+int omc_byte_sizes(uint64_t rows, uint64_t cols, uint64_t *codes_bytes, uint64_t *scales_bytes);
+
+/*
+ * omc_byte_quantise -- x (rows x cols) to eight bits along its rows (codes, scales: rows x cols), and/or along its columns (codes_t, scales_t: the
+ * quantised cols x rows transpose, a scale for each column of x).  One of the two pairs may be NULL, NULL.
+ *   x  device, read only.    codes, codes_t  device, 16-byte aligned, scales, scales_t  4-byte aligned; written.
+ *   workspace  device, 16-byte aligned, omc_byte_quantise_workspace(rows, cols) bytes, undefined afterwards; may be NULL if codes_t is.  Calls that
+ *              may overlap on the GPU need workspaces of their own.
+ */
+int omc_byte_quantise_workspace(uint64_t rows, uint64_t cols, uint64_t *bytes);
+int omc_byte_quantise(const void *x, int type, uint64_t rows, uint64_t cols, uint64_t ld, int8_t *codes, float *scales, int8_t *codes_t, float *scales_t,
+                    void *workspace, void *stream);
+
+/* omc_byte_dequantise -- the values of a quantised rows x cols matrix, q * s rounded to FP32 and then to `type`. */
+int omc_byte_dequantise(const int8_t *codes, const float *scales, uint64_t rows, uint64_t cols, void *out, int type, uint64_t ld, void *stream);
+
+/*
+ * omc_byte_matmul -- Y = X W^T of two quantised matrices, X M x K and W N x K, K < 2^17: y = (sum * sx) * sw with the sum exact, rounded to
+ * FP32 after each step and to `type` at the end, the same bits for any M, N and place in the matrix.  Forward Y = X W^T; backward dX = dY W
+ * (W quantised along N: the transposed pair of omc_byte_quantise) and dW = dY^T X (both quantised along the rows of the batch).
+ *   codes   device, 16-byte aligned, scales 4-byte aligned.
+ *   y       device, M x N of `type`, written; any ldy >= N, element-aligned; overlaps no input.
+ *   status  device, as for omc_mx_matmul.      M <= 128 * 65535.
+ */
+int omc_byte_matmul(const int8_t *x_codes, const float *x_scales, uint64_t M, const int8_t *w_codes, const float *w_scales, uint64_t N, uint64_t K, void *y,
+                  int type, uint64_t ldy, uint32_t *status, void *stream);
+
+/*
+ * omc_byte_linear -- the forward product from activations that are not quantised yet: exactly omc_byte_quantise of x along its rows followed by
+ * omc_byte_matmul with W.
+ *   workspace  device, 16-byte aligned, codes_bytes + scales_bytes of omc_byte_sizes(M, K); contents undefined afterwards.  Calls that may overlap
+ *              on the GPU need workspaces of their own.
+ */
+int omc_byte_linear(const void *x, int type, uint64_t M, uint64_t K, uint64_t ldx, const int8_t *w_codes, const float *w_scales, uint64_t N, void *y,
+                  int y_type, uint64_t ldy, uint8_t *workspace, uint32_t *status, void *stream);
+
+/*
+ * omc_byte_gated -- both projections of a gated layer, the activation and the product in one kernel:
+ *     a = X Wg^T,  b = X Wv^T,  y = act(a) * b
+ * with W = (Wg; Wv), 2F x K, the gate's rows first, quantised along K.  a and b are what omc_byte_matmul gives in FP32; y is rounded once.
+ *   activation  OMC_GATE_SIGMOID 1 / (1 + e^-a) (the gated linear unit), OMC_GATE_SILU a / (1 + e^-a), OMC_GATE_GELU a (1 + erf(a / sqrt 2)) / 2.
+ *   y       device, M x F of `type`, written; any ldy >= F.
+ *   pre     device, M x 2F of `type`, written: (a | b) for the backward pass, any ld_pre >= 2F; NULL if it is not wanted.
+ *   The others as for omc_byte_matmul.  omc_byte_gated_linear: from activations that are not quantised yet, as omc_byte_linear.
+ */
+enum { OMC_GATE_SIGMOID = 0, OMC_GATE_SILU = 1, OMC_GATE_GELU = 2 };
+int omc_byte_gated(const int8_t *x_codes, const float *x_scales, uint64_t M, const int8_t *w_codes, const float *w_scales, uint64_t F, uint64_t K,
+                 int activation, void *y, int type, uint64_t ldy, void *pre, uint64_t ld_pre, uint32_t *status, void *stream);
+int omc_byte_gated_linear(const void *x, int type, uint64_t M, uint64_t K, uint64_t ldx, const int8_t *w_codes, const float *w_scales, uint64_t F,
+                        int activation, void *y, int y_type, uint64_t ldy, void *pre, uint64_t ld_pre, uint8_t *workspace, uint32_t *status, void *stream);
+
+/*
+ * omc_byte_inject_wait_timeout -- diagnostics for the bounded waits of the four calls above, as omc_mx_inject_wait_timeout is for its own: the next
+ * product with FP32 results and more than four rows that the calling thread launches gives up its waits after `polls` polls (1 .. 2^16), and its
+ * first CTA (or pair of CTAs) announces its copies without issuing them, or gives up the waits for results with the products on their way.
+ */
+enum { OMC_BYTE_COPIES_MISSING = 1, OMC_BYTE_RESULTS_LATE = 2 };
+int omc_byte_inject_wait_timeout(uint32_t polls, int what);
+
+/*
+ * omc_gated_backward -- from dy (rows x F) and pre = (a | b) (rows x 2F), both of `type`:
+ *     dpre = (dy b act'(a) | dy act(a)),  rows x 2F
+ * in any of three forms (at least one): dpre of `type`; its 8-bit form along its rows (codes, scales: rows x 2F) and along its columns (codes_t,
+ * scales_t: 2F x rows), exactly omc_byte_quantise of dpre, which need not be stored.  With them the gradients of a gated layer are two products:
+ * dX = codes * (W quantised along 2F)^T and dW = codes_t * (X quantised along the rows of the batch)^T.
+ *   dpre       device, written, overlaps neither dy nor pre (else OMC_ERR_INVALID_ARG); NULL if it is not wanted.
+ *   workspace  device, 16-byte aligned, omc_gated_backward_workspace(rows, F) bytes, undefined afterwards; may be NULL if codes_t is.
+ */
+int omc_gated_backward_workspace(uint64_t rows, uint64_t F, uint64_t *bytes);
+int omc_gated_backward(const void *dy, uint64_t ld_dy, const void *pre, uint64_t ld_pre, int type, uint64_t rows, uint64_t F, int activation,
+                       void *dpre, uint64_t ld_dpre, int8_t *codes, float *scales, int8_t *codes_t, float *scales_t, void *workspace, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

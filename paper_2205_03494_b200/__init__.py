@@ -21,12 +21,16 @@ PLAN_DEFAULT = PLAN_PVT | PLAN_WEIGHTS_ONLY
 FORMAT_FIXED_POINT = 1
 F32, F16, BF16 = 0, 1, 2       # OMC_TYPE_*
 MX_COPIES_MISSING, MX_RESULTS_LATE = 1, 2
+BYTE_COPIES_MISSING, BYTE_RESULTS_LATE = 1, 2
+GATE_SIGMOID, GATE_SILU, GATE_GELU = 0, 1, 2       # OMC_GATE_*
 
 EXPORTS = ["omc_strerror", "omc_last_cuda_error", "omc_plan", "omc_plan_destroy", "omc_plan_seed", "omc_plan_sizes",
            "omc_plan_var", "omc_plan_division", "omc_plan_prepare", "omc_plan_status", "omc_plan_inject_wait_timeout", "omc_compress", "omc_decompress",
            "omc_update_recompress", "omc_update_recompress_host", "omc_transition", "omc_aggregate", "omc_aggregate_sum", "omc_aggregate_add", "omc_divide", "omc_matmul",
            "omc_compress_var_static", "omc_static_status", "omc_mx_sizes", "omc_mx_quantise", "omc_mx_dequantise", "omc_mx_matmul",
-           "omc_mx_linear", "omc_mx_inject_wait_timeout", "omc_layer_norm", "omc_layer_norm_workspace", "omc_layer_norm_backward"]
+           "omc_mx_linear", "omc_mx_inject_wait_timeout", "omc_layer_norm", "omc_layer_norm_workspace", "omc_layer_norm_backward",
+           "omc_byte_sizes", "omc_byte_quantise_workspace", "omc_byte_quantise", "omc_byte_dequantise", "omc_byte_matmul", "omc_byte_linear", "omc_byte_gated",
+           "omc_byte_gated_linear", "omc_byte_inject_wait_timeout", "omc_gated_backward_workspace", "omc_gated_backward"]
 STATIC_MAX_NUMEL = 1 << 28
 
 
@@ -96,6 +100,17 @@ def lib():
         L.omc_layer_norm.argtypes = [vp, i32, u64, u64, u64, vp, vp, C.c_float, vp, u64, vp, vp, vp]
         L.omc_layer_norm_workspace.argtypes = [u64, u64, u64p]
         L.omc_layer_norm_backward.argtypes = [vp, u64, vp, u64, i32, u64, u64, vp, vp, vp, vp, u64, vp, vp, vp, vp]
+        L.omc_byte_sizes.argtypes = [u64, u64, u64p, u64p]
+        L.omc_byte_quantise_workspace.argtypes = [u64, u64, u64p]
+        L.omc_byte_quantise.argtypes = [vp, i32, u64, u64, u64, vp, vp, vp, vp, vp, vp]
+        L.omc_byte_dequantise.argtypes = [vp, vp, u64, u64, vp, i32, u64, vp]
+        L.omc_byte_matmul.argtypes = [vp, vp, u64, vp, vp, u64, u64, vp, i32, u64, vp, vp]
+        L.omc_byte_linear.argtypes = [vp, i32, u64, u64, u64, vp, vp, u64, vp, i32, u64, vp, vp, vp]
+        L.omc_byte_gated.argtypes = [vp, vp, u64, vp, vp, u64, u64, i32, vp, i32, u64, vp, u64, vp, vp]
+        L.omc_byte_gated_linear.argtypes = [vp, i32, u64, u64, u64, vp, vp, u64, i32, vp, i32, u64, vp, u64, vp, vp, vp]
+        L.omc_byte_inject_wait_timeout.argtypes = [C.c_uint32, i32]
+        L.omc_gated_backward_workspace.argtypes = [u64, u64, u64p]
+        L.omc_gated_backward.argtypes = [vp, u64, vp, u64, i32, u64, u64, i32, vp, u64, vp, vp, vp, vp, vp, vp]
         _lib = L
     return _lib
 
@@ -336,3 +351,81 @@ def layer_norm_backward(dy, ld_dy, x, ld_x, type_, rows, cols, gamma, mean, rstd
     rc = (_calls or _load_calls()).layer_norm_backward(dy, ld_dy, x, ld_x, type_, rows, cols, gamma, mean, rstd, dx, ld_dx, dgamma, dbeta, workspace, stream)
     if rc:
         _check(rc, "omc_layer_norm_backward")
+
+
+# ---- the layer at eight bits, and gated layers ---------------------------------------------------
+
+def byte_sizes(rows: int, cols: int):
+    """omc_byte_sizes: (bytes of the codes, bytes of the scales) of a quantised rows x cols matrix."""
+    a, b = C.c_uint64(), C.c_uint64()
+    _check(lib().omc_byte_sizes(int(rows), int(cols), C.byref(a), C.byref(b)), "omc_byte_sizes")
+    return a.value, b.value
+
+
+def byte_quantise_workspace_bytes(rows: int, cols: int) -> int:
+    """omc_byte_quantise_workspace: workspace of byte_quantise along the columns."""
+    n = C.c_uint64()
+    _check(lib().omc_byte_quantise_workspace(int(rows), int(cols), C.byref(n)), "omc_byte_quantise_workspace")
+    return n.value
+
+
+def byte_quantise(x, type_, rows, cols, ld, codes=0, scales=0, codes_t=0, scales_t=0, workspace=0, stream=0):
+    """omc_byte_quantise: x to eight bits along its rows and/or (the _t pair, which needs the workspace) along its columns."""
+    rc = (_calls or _load_calls()).byte_quantise(x, type_, rows, cols, ld, codes, scales, codes_t, scales_t, workspace, stream)
+    if rc:
+        _check(rc, "omc_byte_quantise")
+
+
+def byte_dequantise(codes, scales, rows, cols, out, type_, ld, stream=0):
+    """omc_byte_dequantise: the values of a quantised matrix."""
+    rc = (_calls or _load_calls()).byte_dequantise(codes, scales, rows, cols, out, type_, ld, stream)
+    if rc:
+        _check(rc, "omc_byte_dequantise")
+
+
+def byte_matmul(x_codes, x_scales, M, w_codes, w_scales, N, K, y, type_, ldy, status, stream=0):
+    """omc_byte_matmul: Y = X W^T of two quantised matrices."""
+    rc = (_calls or _load_calls()).byte_matmul(x_codes, x_scales, M, w_codes, w_scales, N, K, y, type_, ldy, status, stream)
+    if rc:
+        _check(rc, "omc_byte_matmul")
+
+
+def byte_linear(x, type_, M, K, ldx, w_codes, w_scales, N, y, y_type, ldy, workspace, status, stream=0):
+    """omc_byte_linear: Y = X W^T with X quantised on the way (workspace: sum(byte_sizes(M, K)) bytes)."""
+    rc = (_calls or _load_calls()).byte_linear(x, type_, M, K, ldx, w_codes, w_scales, N, y, y_type, ldy, workspace, status, stream)
+    if rc:
+        _check(rc, "omc_byte_linear")
+
+
+def byte_gated(x_codes, x_scales, M, w_codes, w_scales, F, K, activation, y, type_, ldy, pre, ld_pre, status, stream=0):
+    """omc_byte_gated: y = act(X Wg^T) * (X Wv^T), W = (Wg; Wv) of 2F rows; pre (M x 2F) = both products, or 0."""
+    rc = (_calls or _load_calls()).byte_gated(x_codes, x_scales, M, w_codes, w_scales, F, K, activation, y, type_, ldy, pre, ld_pre, status, stream)
+    if rc:
+        _check(rc, "omc_byte_gated")
+
+
+def byte_gated_linear(x, type_, M, K, ldx, w_codes, w_scales, F, activation, y, y_type, ldy, pre, ld_pre, workspace, status, stream=0):
+    """omc_byte_gated_linear: the gated layer with X quantised on the way (workspace: sum(byte_sizes(M, K)) bytes)."""
+    rc = (_calls or _load_calls()).byte_gated_linear(x, type_, M, K, ldx, w_codes, w_scales, F, activation, y, y_type, ldy, pre, ld_pre, workspace, status, stream)
+    if rc:
+        _check(rc, "omc_byte_gated_linear")
+
+
+def byte_inject_wait_timeout(polls: int, what: int):
+    """omc_byte_inject_wait_timeout: the first CTA of this thread's next product gives up its waits (diagnostics)."""
+    _check(lib().omc_byte_inject_wait_timeout(int(polls), int(what)), "omc_byte_inject_wait_timeout")
+
+
+def gated_backward_workspace_bytes(rows: int, F: int) -> int:
+    """omc_gated_backward_workspace: workspace of gated_backward along the columns."""
+    n = C.c_uint64()
+    _check(lib().omc_gated_backward_workspace(int(rows), int(F), C.byref(n)), "omc_gated_backward_workspace")
+    return n.value
+
+
+def gated_backward(dy, ld_dy, pre, ld_pre, type_, rows, F, activation, dpre=0, ld_dpre=0, codes=0, scales=0, codes_t=0, scales_t=0, workspace=0, stream=0):
+    """omc_gated_backward: (dy b act'(a) | dy act(a)) of pre = (a | b), as it is and / or at eight bits along its rows and its columns."""
+    rc = (_calls or _load_calls()).gated_backward(dy, ld_dy, pre, ld_pre, type_, rows, F, activation, dpre, ld_dpre, codes, scales, codes_t, scales_t, workspace,
+                                                  stream)
+    if rc:
+        _check(rc, "omc_gated_backward")
