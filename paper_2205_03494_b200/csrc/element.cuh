@@ -79,6 +79,13 @@ __device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c)
 }
 __device__ __forceinline__ float2 twice(float v) { return make_float2(v, v); }
 
+// 32 bytes, to a 32-byte boundary.
+__device__ __forceinline__ void store32(void *p, const uint32_t *w)
+{
+    asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
+                 ::"l"(p), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]), "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7]) : "memory");
+}
+
 // Every kernel of the layer operators lets its successor start early and waits for the kernel before it here,
 // in every CTA and before any global access: a CTA that left without waiting could let the successor's wait end
 // while that earlier kernel still runs.  What it writes may be what this kernel reads, within this kernel's own

@@ -1,14 +1,18 @@
 // Quantisation to 8-bit integers (i8_format.cuh) along the rows and / or the columns of what a source gives: a matrix in memory, or
 // gradients computed from several (omc_gated.cu).
 //
-// A row's scale follows from the whole row, a column's from the whole column, so at least one of the two needs the values twice.
-// First kernel: a row in the registers of 32 .. 512 threads, sixteen-byte pieces a thread; its largest magnitude by shuffles (and
-// one barrier), its codes at once; each thread keeps the largest magnitudes of its own columns over all rows that it sees, which it
-// leaves in the workspace, one set a CTA.  Second kernel: a CTA joins these sets for a strip of 128 columns and takes the strip's
-// rows, 128 at a time: four rows of a piece a thread, whose codes of one column make a word that goes to shared memory, and from there
-// 128 bytes of a column at a time to memory.  It starts with the rows that the first kernel read last, which the L2 cache still holds.
+// Along the rows alone one kernel reads the values once: a row in the registers of 32 .. 512 threads, sixteen-byte pieces a thread; its largest
+// magnitude by shuffles (and a barrier of the row's own threads), then its codes.
+// A column's scale follows from the whole column, so its values are needed twice.  A first kernel only takes maxima: a warp walks down a window
+// of columns, keeps the largest magnitudes of its columns in registers (a CTA leaves one set in the workspace) and leaves the largest magnitude of
+// each row's piece of the window.  A second kernel joins these for a strip of 64 or 128 columns and its rows, and makes the codes along both axes
+// from one more read: four rows of a piece a thread; along the rows they go out as they are, along the columns the codes of four rows make a word that
+// goes to shared memory, and from there 64 or 128 bytes of a column at a time to memory.  It starts with the rows that the first kernel read last,
+// which the L2 cache still holds.
 // Magnitudes are compared as bit patterns, two 16-bit values in one instruction: their order is that of the values, Inf and NaN on top.
 #pragma once
+#include <type_traits>
+
 #include "element.cuh"
 #include "i8_format.cuh"
 #include "mx_encode.cuh"
@@ -23,31 +27,100 @@ using mx::max_magnitude;
 
 template <typename T> constexpr int PIECE = 16 / (int)sizeof(T);               // values of a piece: 8 or 4
 template <typename T> constexpr uint32_t MAGNITUDE = sizeof(T) == 4 ? 0x7FFFFFFFu : 0x7FFF7FFFu;
-constexpr uint32_t MOST_PARTS = 296;                                           // sets of column maxima: two CTAs on each of 148 SMs
 constexpr int ROW_THREADS = 512;                                               // of the widest group that shares a row
-constexpr int STRIP = 128, STRIP_ROWS = 128, STRIP_THREADS = 256;              // tile of the second kernel
+constexpr int MAXIMA_WARPS = 8, MAXIMA_CTAS = DEFAULT_SMS * 3;                 // of the first kernel: warps of a CTA, CTAs
+constexpr int STRIP_THREADS = 256;                                             // of the second kernel
 
-// Bytes of the sets of `values` columns' maxima (as FP32 magnitudes, the widest).
-inline uint64_t parts_bytes(uint64_t rows, uint64_t values)
+// Pieces of a warp's window of columns in the first kernel, and CTAs that share a window's rows: their sets of maxima.
+template <int OUT> constexpr int WINDOW_PIECES = OUT == 1 ? 4 : 2;
+inline uint64_t shares_of(uint64_t rows, uint64_t windows)
 {
-    return (rows < MOST_PARTS ? rows : MOST_PARTS) * ((values + 7) / 8 * 8) * 4;
+    const uint64_t most = windows < (uint64_t)MAXIMA_CTAS ? MAXIMA_CTAS / windows : 1, all = (rows + MAXIMA_WARPS - 1) / MAXIMA_WARPS;
+    return all < most ? all : most;
+}
+// Bytes of the sets of `cols` columns' maxima and of the rows' maxima in the windows, of any type: widest words, fewest and most windows.
+inline uint64_t maxima_bytes(uint64_t rows, uint64_t cols, int out)
+{
+    const uint64_t sets = shares_of(rows, (cols + 1023) / 1024) * out * ((cols + 7) / 8 * 8) * 4, windows = (cols + 255) / 256;
+    return (sets + 15) / 16 * 16 + windows * ((rows + 3) / 4 * 4) * 4;
 }
 
+// A matrix's bytes: its first, and behind its last.
+struct Span {
+    uintptr_t first, last;
+};
+template <typename T>
+Span span_of(const T *x, uint64_t ld, uint64_t rows, uint64_t cols)
+{
+    return {reinterpret_cast<uintptr_t>(x), reinterpret_cast<uintptr_t>(x + (rows - 1) * ld + cols)};
+}
+
+// A piece on its way.  WHOLE, rows on 16-byte boundaries and a multiple of 16 bytes wide: its four words.  Else the two aligned sixteens that hold it, which
+// `words` shifts, where all bytes of both lie between the matrix's first and last ones; the other pieces, and those cut off by the row's end, `words`
+// reads value by value.  (Loads are predicated, never one side of a branch: where registers meet after a branch the compiler copies them, which waits for
+// the load.  8192 x 8192 BF16, first kernel, 44 us with a branch.)
+template <typename T, bool WHOLE>
+struct Piece {
+    static constexpr int E = PIECE<T>;
+    uint4 a, b;
+    static __device__ __forceinline__ bool shifted(const T *at, uint32_t left, const Span &span)
+    {
+        const uintptr_t low = reinterpret_cast<uintptr_t>(at) & ~(uintptr_t)15;
+        return left >= (uint32_t)E && low >= span.first && low + 32 <= span.last;
+    }
+    // From `at` on, `left` values of the row.
+    __device__ __forceinline__ void load(const T *at, uint32_t left, const Span &span)
+    {
+        if constexpr (WHOLE) {
+            a = *reinterpret_cast<const uint4 *>(at);
+        } else if (shifted(at, left, span)) {
+            const uint4 *low = reinterpret_cast<const uint4 *>(reinterpret_cast<uintptr_t>(at) & ~(uintptr_t)15);
+            a = low[0];
+            b = low[1];
+        }
+    }
+    __device__ __forceinline__ void words(const T *at, uint32_t left, const Span &span, uint32_t *out) const
+    {
+        if constexpr (WHOLE) {
+            out[0] = a.x, out[1] = a.y, out[2] = a.z, out[3] = a.w;
+        } else {
+            const uint32_t skip = (uint32_t)reinterpret_cast<uintptr_t>(at), w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+            uint32_t v[6], u[5];
+#pragma unroll
+            for (int i = 0; i < 6; ++i) v[i] = skip & 8 ? w[i + 2] : w[i];
+#pragma unroll
+            for (int i = 0; i < 5; ++i) u[i] = skip & 4 ? v[i + 1] : v[i];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) out[i] = sizeof(T) == 4 ? u[i] : __funnelshift_r(u[i], u[i + 1], (skip & 2) * 8);
+            if (!shifted(at, left, span)) mx::load<T, false, E>(at, 0, left, out);
+        }
+    }
+};
+
 // A matrix in memory.
-template <typename T_, bool VECTOR>
+template <typename T_, bool WHOLE>
 struct Matrix {
     using T = T_;
-    static constexpr int IN = 1, OUT = 1;         // pieces read and made at a place
+    static constexpr int OUT = 1, HEAVY = WHOLE ? 0 : 1;           // pieces made at a place; whether loads take more registers than those of whole rows
+    static constexpr bool WHOLE_ROWS = WHOLE;
     const T *x;
     uint64_t ld;
-    __device__ __forceinline__ void fetch(uint32_t row, uint32_t col, uint32_t cols, uint32_t (*raw)[4]) const
+    Span span;
+    struct Raw {
+        Piece<T, WHOLE> x;
+    };
+    __device__ __forceinline__ void fetch(uint32_t row, uint32_t col, uint32_t cols, Raw &raw) const { raw.x.load(x + row * ld + col, cols - col, span); }
+    // Four rows' pieces from one address on (whole pieces of whole rows).
+    __device__ __forceinline__ void fetch4(uint32_t row, uint32_t col, Raw *raw) const
     {
-        mx::load<T, VECTOR, PIECE<T>>(x + row * ld, col, cols, raw[0]);
-    }
-    __device__ __forceinline__ void make(const uint32_t (*raw)[4], uint32_t (*out)[4]) const
-    {
+        const T *p = x + row * ld + col;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) out[0][i] = raw[0][i];
+        for (int i = 0; i < 4; ++i, p += ld) raw[i].x.a = *reinterpret_cast<const uint4 *>(p);
+    }
+    // Of a place that was fetched.
+    __device__ __forceinline__ void make(uint32_t row, uint32_t col, uint32_t cols, const Raw &raw, uint32_t (*out)[4]) const
+    {
+        raw.x.words(x + row * ld + col, cols - col, span, out[0]);
     }
     __device__ __forceinline__ void emit(uint32_t, uint32_t, uint32_t, const uint32_t (*)[4]) const {}
 };
@@ -69,22 +142,23 @@ __device__ __forceinline__ void encode_piece(const uint32_t *w, float r, bool na
 #pragma unroll
     for (int i = 0; i < 4; ++i) Word<T>::unpack(w[i], v + N * i);
 #pragma unroll
-    for (int i = 0; i < E; i += 2) {
-        const float2 q = el::fma2(make_float2(v[i], v[i + 1]), el::twice(r), el::twice(TO_INTEGER));
-        v[i] = q.x;
-        v[i + 1] = q.y;
-    }
+    for (int i = 0; i < E; ++i) v[i] = __fmaf_rn(v[i], r, TO_INTEGER);
 #pragma unroll
     for (int i = 0; i < E / 4; ++i) codes[i] = nan ? 0u : bytes4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
 }
 
+template <int E>
+__device__ __forceinline__ void store_whole(int8_t *at, const uint32_t *codes)
+{
+    if constexpr (E == 8) *reinterpret_cast<uint2 *>(at) = make_uint2(codes[0], codes[1]);
+    else *reinterpret_cast<uint32_t *>(at) = codes[0];
+}
 // A piece's codes into a row of codes from byte `at` on, `n` of them.
 template <int E>
 __device__ __forceinline__ void store_codes(int8_t *row, uint64_t at, uint32_t n, const uint32_t *codes)
 {
     if (n >= (uint32_t)E && at % E == 0) {
-        if constexpr (E == 8) *reinterpret_cast<uint2 *>(row + at) = make_uint2(codes[0], codes[1]);
-        else *reinterpret_cast<uint32_t *>(row + at) = codes[0];
+        store_whole<E>(row + at, codes);
     } else {
 #pragma unroll
         for (int i = 0; i < E; ++i)
@@ -92,112 +166,103 @@ __device__ __forceinline__ void store_codes(int8_t *row, uint64_t at, uint32_t n
     }
 }
 
+// A piece of half o of a row of codes.  One half: zeros behind the last column up to the row's end belong to the pieces there; two: the second
+// half starts where the first one ends, and pad_row writes the zeros.
+template <int E, int OUT>
+__device__ __forceinline__ void store_row_piece(int8_t *row, int o, uint32_t col, uint32_t cols, uint64_t pitch, const uint32_t *codes)
+{
+    if (OUT == 1 && col < pitch) store_codes<E>(row, col, E, codes);
+    if (OUT > 1 && col < cols) store_codes<E>(row, (uint64_t)o * cols + col, cols - col, codes);
+}
+__device__ __forceinline__ void pad_row(int8_t *row, uint64_t from, uint64_t pitch)
+{
+    for (uint64_t c = from; c < pitch; ++c) row[c] = 0;
+}
+
 struct RowsOut {
     int8_t *codes;            // rows of `pitch` bytes, OUT * cols codes
     float *scales;
     uint64_t pitch;
-    uint4 *parts;             // [CTA][OUT][pieces of a row] magnitudes
 };
 
-// First kernel.  A row's threads: 2^group_log of them, P pieces each, piece p of thread t at column (p 2^group_log + t) E.  Without ROWS
-// a row is not needed whole: blockIdx.y is a window of it.
-template <typename SRC, int P, int THREADS, bool ROWS, bool COLS>
-__global__ void __launch_bounds__(THREADS) rows_kernel(SRC src, uint32_t rows, uint32_t cols, uint32_t group_log, RowsOut out)
+// A CTA's window of columns and share of the rows: blockIdx.x counts the shares of the first window, then those of the next.
+struct Place {
+    uint32_t shares;
+    __device__ __forceinline__ uint32_t window() const { return blockIdx.x / shares; }
+    __device__ __forceinline__ uint32_t share() const { return blockIdx.x % shares; }
+};
+
+// CTAs on an SM, as the registers allow.
+template <typename SRC, int P, int THREADS> constexpr int ROWS_CTAS = THREADS > 256 ? 1 : SRC::HEAVY ? 2 : P > 2 ? 3 : 4;
+
+// Along the rows.  A row's threads: 2^group_log of them, P pieces each, piece p of thread t at column (p 2^group_log + t) E.  While a row is worked
+// on the next AHEAD ones are on their way.  Without ROWS only what the source emits, window by window.
+template <typename SRC, int P, int THREADS, bool ROWS>
+__global__ void __launch_bounds__(THREADS, ROWS_CTAS<SRC, P, THREADS>) rows_kernel(SRC src, uint32_t rows, uint32_t cols, uint32_t group_log, Place place, RowsOut out)
 {
     using T = typename SRC::T;
-    constexpr int E = PIECE<T>, IN = SRC::IN, OUT = SRC::OUT;
+    constexpr int E = PIECE<T>, OUT = SRC::OUT, AHEAD = SRC::HEAVY ? 1 : 2;
     __shared__ uint32_t slots[2][THREADS / 32];
-    __shared__ uint4 joined[COLS ? THREADS : 1];
     const uint32_t tid = threadIdx.x, group = 1u << group_log, t = tid & (group - 1), g = tid >> group_log, together = THREADS >> group_log;
-    const uint32_t window = ROWS ? 0u : blockIdx.y * (group * P * E);
+    const uint32_t window = ROWS ? 0u : place.window() * (group * P * E);
     const uint32_t first_warp = g << (group_log - 5);
     el::enter_stream_order();
-    uint32_t raw[P][IN][4], most[COLS ? P : 1][COLS ? OUT : 1][4];
+    typename SRC::Raw raw[AHEAD][P];
     auto column = [&](int p) { return window + (((uint32_t)p << group_log) + t) * E; };
-    auto fetch = [&](uint32_t row) {
+    auto fetch = [&](uint32_t row, typename SRC::Raw *r) {
 #pragma unroll
         for (int p = 0; p < P; ++p)
-            if (row < rows && column(p) < cols) src.fetch(row, column(p), cols, raw[p]);
+            if (row < rows && column(p) < cols) src.fetch(row, column(p), cols, r[p]);
     };
+    const uint32_t step = place.shares * together;
+    uint32_t base = place.share() * together, turn = 0;
 #pragma unroll
-    for (int p = 0; p < P; ++p) {
+    for (int a = 0; a < AHEAD; ++a) fetch(base + a * step + g, raw[a]);
+    while (base < rows) {
 #pragma unroll
-        for (int i = 0; i < IN * 4; ++i) raw[p][i / 4][i % 4] = 0u;
-        if constexpr (COLS) {
+        for (int a = 0; a < AHEAD; ++a) {
+            if (base >= rows) break;
+            const uint32_t row = base + g;
+            uint32_t w[P][OUT][4];
 #pragma unroll
-            for (int i = 0; i < OUT * 4; ++i) most[p][i / 4][i % 4] = 0u;
-        }
-    }
-    const uint32_t step = gridDim.x * together;
-    uint32_t base = blockIdx.x * together, turn = 0;
-    fetch(base + g);
-    for (; base < rows; base += step, turn ^= 1u) {
-        const uint32_t row = base + g;
-        uint32_t w[P][OUT][4], top = 0u;
+            for (int p = 0; p < P; ++p) {
+                if (row < rows && column(p) < cols) {
+                    src.make(row, column(p), cols, raw[a][p], w[p]);
+                    src.emit(row, column(p), cols, w[p]);
+                } else {
 #pragma unroll
-        for (int p = 0; p < P; ++p) {
-            src.make(raw[p], w[p]);
-            if (row < rows && column(p) < cols) src.emit(row, column(p), cols, w[p]);
-        }
-        fetch(row + step);
-        if constexpr (ROWS || COLS) {
-            const bool here = row < rows;             // (behind the last row the pieces are those of a row before it)
-#pragma unroll
-            for (int p = 0; p < P; ++p)
-#pragma unroll
-                for (int i = 0; i < OUT * 4; ++i) {
-                    const uint32_t m = w[p][i / 4][i % 4] & MAGNITUDE<T>;
-                    if constexpr (ROWS) top = max_magnitude<T>(top, m);
-                    if constexpr (COLS) most[p][i / 4][i % 4] = here ? max_magnitude<T>(most[p][i / 4][i % 4], m) : most[p][i / 4][i % 4];
+                    for (int i = 0; i < OUT * 4; ++i) w[p][i / 4][i % 4] = 0u;
                 }
-        }
-        if constexpr (ROWS) {
-            top = __reduce_max_sync(0xFFFFFFFFu, top_bits<T>(top));
-            if (group_log > 5) {                      // the same for all threads
-                if ((tid & 31) == 0) slots[turn][tid >> 5] = top;
-                __syncthreads();
-                for (uint32_t i = 0; i < group >> 5; ++i) top = max(top, slots[turn][first_warp + i]);
             }
-            if (row < rows) {
-                const Scale s = scale_of(top);
-                int8_t *to = out.codes + row * out.pitch;
+            fetch(row + AHEAD * step, raw[a]);
+            if constexpr (ROWS) {
+                uint32_t top = 0u;
 #pragma unroll
-                for (int p = 0; p < P; ++p)
+                for (int i = 0; i < P * OUT * 4; ++i) top = max_magnitude<T>(top, w[i / (OUT * 4)][i / 4 % OUT][i % 4] & MAGNITUDE<T>);
+                top = __reduce_max_sync(0xFFFFFFFFu, top_bits<T>(top));
+                if (group_log > 5) {                  // a barrier of the row's own threads
+                    if ((tid & 31) == 0) slots[turn][tid >> 5] = top;
+                    asm volatile("bar.sync %0, %1;" ::"r"(g + 1), "r"(group) : "memory");
+                    for (uint32_t i = 0; i < group >> 5; ++i) top = max(top, slots[turn][first_warp + i]);
+                    turn ^= 1u;
+                }
+                if (row < rows) {
+                    const Scale s = scale_of(top);
+                    int8_t *to = out.codes + row * out.pitch;
 #pragma unroll
-                    for (int o = 0; o < OUT; ++o) {
-                        uint32_t c[E / 4];
-                        encode_piece<T>(w[p][o], s.r, s.nan(), c);
-                        // one piece a place: zeros behind the last column up to the row's end; two: the second half starts where the first one ends
-                        if (OUT == 1 && column(p) < out.pitch) store_codes<E>(to, column(p), E, c);
-                        if (OUT > 1 && column(p) < cols) store_codes<E>(to, (uint64_t)o * cols + column(p), cols - column(p), c);
-                    }
-                if (OUT > 1)
-                    for (uint64_t c = (uint64_t)OUT * cols + t; c < out.pitch; c += group) to[c] = 0;
-                if (t == 0) out.scales[row] = s.s;
-            }
-        }
-    }
-    if constexpr (COLS) {
-        const uint32_t pieces = (cols + E - 1) / E;
+                    for (int p = 0; p < P; ++p)
 #pragma unroll
-        for (int p = 0; p < P; ++p)
-#pragma unroll
-            for (int o = 0; o < OUT; ++o) {
-                uint32_t *m = most[p][o];
-                if (together > 1) {
-                    __syncthreads();
-                    joined[tid] = make_uint4(m[0], m[1], m[2], m[3]);
-                    __syncthreads();
-                    if (g == 0)
-                        for (uint32_t i = 1; i < together; ++i) {
-                            const uint4 q = joined[i * group + t];
-                            m[0] = max_magnitude<T>(m[0], q.x), m[1] = max_magnitude<T>(m[1], q.y);
-                            m[2] = max_magnitude<T>(m[2], q.z), m[3] = max_magnitude<T>(m[3], q.w);
+                        for (int o = 0; o < OUT; ++o) {
+                            uint32_t c[E / 4];
+                            encode_piece<T>(w[p][o], s.r, s.nan(), c);
+                            store_row_piece<E, OUT>(to, o, column(p), cols, out.pitch, c);
                         }
+                    if (OUT > 1 && t == 0) pad_row(to, (uint64_t)OUT * cols, out.pitch);
+                    if (t == 0) out.scales[row] = s.s;
                 }
-                if (g == 0 && column(p) < cols)
-                    out.parts[((uint64_t)blockIdx.x * OUT + o) * pieces + column(p) / E] = make_uint4(m[0], m[1], m[2], m[3]);
             }
+            base += step;
+        }
     }
 }
 
@@ -207,14 +272,15 @@ template <typename SRC>
 __global__ void __launch_bounds__(WIDE_THREADS) wide_rows_kernel(SRC src, uint32_t rows, uint32_t cols, RowsOut out)
 {
     using T = typename SRC::T;
-    constexpr int E = PIECE<T>, IN = SRC::IN, OUT = SRC::OUT;
+    constexpr int E = PIECE<T>, OUT = SRC::OUT;
     __shared__ uint32_t slots[WIDE_THREADS / 32];
     el::enter_stream_order();
     for (uint32_t row = blockIdx.x; row < rows; row += gridDim.x) {
-        uint32_t raw[IN][4], w[OUT][4], top = 0u;
+        typename SRC::Raw raw;
+        uint32_t w[OUT][4], top = 0u;
         for (uint32_t col = threadIdx.x * E; col < cols; col += WIDE_THREADS * E) {
             src.fetch(row, col, cols, raw);
-            src.make(raw, w);
+            src.make(row, col, cols, raw, w);
             src.emit(row, col, cols, w);
 #pragma unroll
             for (int i = 0; i < OUT * 4; ++i) top = max_magnitude<T>(top, w[i / 4][i % 4] & MAGNITUDE<T>);
@@ -227,7 +293,7 @@ __global__ void __launch_bounds__(WIDE_THREADS) wide_rows_kernel(SRC src, uint32
         int8_t *to = out.codes + row * out.pitch;
         for (uint32_t col = threadIdx.x * E; col < cols; col += WIDE_THREADS * E) {
             src.fetch(row, col, cols, raw);
-            src.make(raw, w);
+            src.make(row, col, cols, raw, w);
 #pragma unroll
             for (int o = 0; o < OUT; ++o) {
                 uint32_t c[E / 4];
@@ -235,39 +301,157 @@ __global__ void __launch_bounds__(WIDE_THREADS) wide_rows_kernel(SRC src, uint32
                 store_codes<E>(to, (uint64_t)o * cols + col, cols - col, c);
             }
         }
-        for (uint64_t c = (uint64_t)OUT * cols + threadIdx.x; c < out.pitch; c += WIDE_THREADS) to[c] = 0;
-        if (threadIdx.x == 0) out.scales[row] = s.s;
+        if (threadIdx.x == 0) {
+            pad_row(to, (uint64_t)OUT * cols, out.pitch);
+            out.scales[row] = s.s;
+        }
         __syncthreads();
     }
 }
 
+// What the first kernel leaves for the second.
+struct Maxima {
+    uint4 *cols;              // [set][OUT][pieces of a row] magnitudes
+    uint32_t *rows;           // [window][row] magnitudes as FP32 bits
+    uint32_t sets, windows;
+};
+
+// First kernel.
+template <typename SRC, bool ROWS>
+__global__ void __launch_bounds__(32 * MAXIMA_WARPS, SRC::HEAVY ? 2 : 3) maxima_kernel(SRC src, uint32_t rows, uint32_t cols, Place place, Maxima out)
+{
+    using T = typename SRC::T;
+    constexpr int E = PIECE<T>, OUT = SRC::OUT, P = WINDOW_PIECES<OUT>, AHEAD = SRC::HEAVY ? 1 : 2;
+    __shared__ uint4 joined[32 * MAXIMA_WARPS];
+    const uint32_t lane = threadIdx.x & 31, warp = threadIdx.x >> 5, window = place.window() * (32 * P * E);
+    el::enter_stream_order();
+    typename SRC::Raw raw[AHEAD][P];
+    uint32_t most[P][OUT][4];
+    auto column = [&](int p) { return window + (p * 32 + lane) * E; };
+    auto fetch = [&](uint32_t row, typename SRC::Raw *r) {
+#pragma unroll
+        for (int p = 0; p < P; ++p)
+            if (row < rows && column(p) < cols) src.fetch(row, column(p), cols, r[p]);
+    };
+#pragma unroll
+    for (int i = 0; i < P * OUT * 4; ++i) most[i / (OUT * 4)][i / 4 % OUT][i % 4] = 0u;
+    const uint32_t step = place.shares * MAXIMA_WARPS;
+    uint32_t row = place.share() * MAXIMA_WARPS + warp;
+#pragma unroll
+    for (int a = 0; a < AHEAD; ++a) fetch(row + a * step, raw[a]);
+    while (row < rows) {
+#pragma unroll
+        for (int a = 0; a < AHEAD; ++a) {
+            if (row >= rows) break;
+            uint32_t top = 0u;
+#pragma unroll
+            for (int p = 0; p < P; ++p) {
+                if (column(p) < cols) {
+                    uint32_t w[OUT][4];
+                    src.make(row, column(p), cols, raw[a][p], w);
+                    src.emit(row, column(p), cols, w);
+#pragma unroll
+                    for (int i = 0; i < OUT * 4; ++i) {
+                        const uint32_t m = w[i / 4][i % 4] & MAGNITUDE<T>;
+                        if constexpr (ROWS) top = max_magnitude<T>(top, m);
+                        most[p][i / 4][i % 4] = max_magnitude<T>(most[p][i / 4][i % 4], m);
+                    }
+                }
+            }
+            fetch(row + AHEAD * step, raw[a]);
+            if constexpr (ROWS) {
+                top = __reduce_max_sync(0xFFFFFFFFu, top_bits<T>(top));
+                if (lane == 0) out.rows[(uint64_t)place.window() * rows + row] = top;
+            }
+            row += step;
+        }
+    }
+    const uint32_t pieces = (cols + E - 1) / E;
+#pragma unroll
+    for (int p = 0; p < P; ++p)
+#pragma unroll
+        for (int o = 0; o < OUT; ++o) {
+            uint32_t *m = most[p][o];
+            __syncthreads();
+            joined[threadIdx.x] = make_uint4(m[0], m[1], m[2], m[3]);
+            __syncthreads();
+            if (warp == 0) {
+                for (uint32_t i = 1; i < MAXIMA_WARPS; ++i) {
+                    const uint4 q = joined[i * 32 + lane];
+                    m[0] = max_magnitude<T>(m[0], q.x), m[1] = max_magnitude<T>(m[1], q.y);
+                    m[2] = max_magnitude<T>(m[2], q.z), m[3] = max_magnitude<T>(m[3], q.w);
+                }
+                if (column(p) < cols) out.cols[((uint64_t)place.share() * OUT + o) * pieces + column(p) / E] = make_uint4(m[0], m[1], m[2], m[3]);
+            }
+        }
+}
+
 struct ColsOut {
-    const uint4 *parts;
-    uint32_t n_parts;
     int8_t *codes;            // OUT * cols rows of `pitch` bytes, `rows` codes
     float *scales;
     uint64_t pitch;
 };
 
-// Second kernel: blockIdx.x is a strip of 128 columns and a share of the row tiles, the last ones first.
+// Second kernel: blockIdx.x is a strip of sixteen pieces of columns and a share of the row tiles, the last ones first.  The next tile's loads are
+// on their way while a tile's codes go to memory.
 template <typename SRC>
-__global__ void __launch_bounds__(STRIP_THREADS, 2) cols_kernel(SRC src, uint32_t rows, uint32_t cols, uint32_t strips, uint32_t tiles_each, ColsOut out)
+struct Strip {
+    static constexpr int E = PIECE<typename SRC::T>, COLS = 16 * E, SWEEPS = SRC::OUT == 1 ? 2 : 1;     // 128 or 64 columns; loads of 64 rows at a time
+    static constexpr int ROWS = 64 * SWEEPS, WORDS = ROWS / 4;                                         // of a tile; of a column of its codes
+    static constexpr int CTAS = SRC::OUT == 1 && !SRC::HEAVY ? 3 : 2;                                  // on an SM, as the registers allow
+    static constexpr int WORDS_ALL = SRC::OUT * COLS * WORDS;
+    // Column e of piece p is column e 16 + p of the tile in shared memory.  Its words are turned by the piece (an even number), so that a warp's
+    // stores, sixteen pieces of two words each, fall into different banks.
+    static __device__ __forceinline__ uint32_t turned(uint32_t piece) { return WORDS == 32 ? piece * 2 : (piece >> 1) * 2; }
+};
+template <typename SRC, bool ROWS>
+__global__ void __launch_bounds__(STRIP_THREADS, Strip<SRC>::CTAS) codes_kernel(SRC src, uint32_t rows, uint32_t cols, uint32_t strips, uint32_t tiles_each, Maxima in,
+                                                                               RowsOut out_r, ColsOut out)
 {
     using T = typename SRC::T;
-    constexpr int E = PIECE<T>, IN = SRC::IN, OUT = SRC::OUT, ACROSS = STRIP / E, DOWN = STRIP_THREADS / ACROSS, SWEEP = DOWN * 4;
-    constexpr int TOGETHER = IN == 1 ? 2 : 1;                      // sweeps whose loads are on their way at a time
-    __shared__ __align__(16) uint32_t tile[OUT * STRIP * STRIP_ROWS / 4];
-    __shared__ float factor[OUT * STRIP];
-    __shared__ uint32_t any_nan;
-    const uint32_t tid = threadIdx.x, piece = tid % ACROSS, down = tid / ACROSS;
-    const uint32_t strip = blockIdx.x % strips, share = blockIdx.x / strips, tiles = (rows + STRIP_ROWS - 1) / STRIP_ROWS;
+    using S = Strip<SRC>;
+    constexpr int E = S::E, OUT = SRC::OUT, COLS = S::COLS, WORDS = S::WORDS, SWEEPS = S::SWEEPS;
+    __shared__ __align__(16) uint32_t tiles_smem[2 * S::WORDS_ALL];            // two tiles, in turn: one barrier a tile
+    __shared__ __align__(16) float factor[OUT * COLS], row_factor[2][ROWS ? S::ROWS : 4];
+    __shared__ uint32_t any_nan, nan_rows[2];
+    const uint32_t tid = threadIdx.x, piece = tid % 16, down = tid / 16;
+    const uint32_t strip = blockIdx.x % strips, share = blockIdx.x / strips, tiles = (rows + S::ROWS - 1) / S::ROWS;
     const uint32_t end = tiles - share * tiles_each, begin = end > tiles_each ? end - tiles_each : 0u;
-    const uint32_t col = strip * STRIP + piece * E;
-    if (tid == 0) any_nan = 0u;
+    const uint32_t col = strip * COLS + piece * E;
+    if (tid == 0) any_nan = nan_rows[0] = nan_rows[1] = 0u;
+    __syncthreads();
     el::enter_stream_order();
-    // the strip's magnitudes: DOWN threads share the sets of a piece, and join what they found in shared memory
+    typename SRC::Raw raw[SWEEPS * 4];
+    auto row_of = [&](uint32_t t, int k) { return t * S::ROWS + k / 4 * 64 + down * 4 + k % 4; };
+    const bool whole_strip = (strip + 1) * COLS <= cols;
+    auto fetch = [&](uint32_t t) {
+        if (SRC::WHOLE_ROWS && whole_strip && (t + 1) * S::ROWS <= rows) {
+#pragma unroll
+            for (int k = 0; k < SWEEPS; ++k) src.fetch4(row_of(t, k * 4), col, raw + k * 4);
+            return;
+        }
+#pragma unroll
+        for (int k = 0; k < SWEEPS * 4; ++k)
+            if (row_of(t, k) < rows && col < cols) src.fetch(row_of(t, k), col, cols, raw[k]);
+    };
+    auto rows_of = [&](uint32_t t) {                               // a tile's rows' factors, a row a thread; the first strip stores the scales
+        if constexpr (ROWS) {
+            const uint32_t row = t * S::ROWS + tid;
+            if (tid < S::ROWS && row < rows) {
+                uint32_t top = 0u;
+                for (uint32_t i = 0; i < in.windows; ++i) top = max(top, in.rows[(uint64_t)i * rows + row]);
+                const Scale s = scale_of(top);
+                row_factor[t & 1u][tid] = s.r;
+                if (s.nan()) nan_rows[t & 1u] = t + 1;             // (no other tile's number)
+                if (strip == 0) out_r.scales[row] = s.s;
+            }
+        }
+    };
+    fetch(end - 1);
+    rows_of(end - 1);
+    // the strip's magnitudes: sixteen threads share the sets of a piece, and join what they found in shared memory
     const uint32_t pieces = (cols + E - 1) / E;
-    uint4 *const found = reinterpret_cast<uint4 *>(tile);          // [DOWN][ACROSS]
+    uint4 *const found = reinterpret_cast<uint4 *>(tiles_smem);    // [16][16]
 #pragma unroll
     for (int o = 0; o < OUT; ++o) {
         uint4 m = make_uint4(0u, 0u, 0u, 0u);
@@ -277,90 +461,122 @@ __global__ void __launch_bounds__(STRIP_THREADS, 2) cols_kernel(SRC src, uint32_
         };
         if (col < cols)
 #pragma unroll 4
-            for (uint32_t i = down; i < out.n_parts; i += DOWN) join(out.parts[((uint64_t)i * OUT + o) * pieces + col / E]);
+            for (uint32_t i = down; i < in.sets; i += 16) join(in.cols[((uint64_t)i * OUT + o) * pieces + col / E]);
         __syncthreads();
         found[tid] = m;
         __syncthreads();
         if (down == 0) {
-            for (int i = 1; i < DOWN; ++i) join(found[i * ACROSS + piece]);
+            for (int i = 1; i < 16; ++i) join(found[i * 16 + piece]);
             const uint32_t w[4] = {m.x, m.y, m.z, m.w};
 #pragma unroll
             for (int e = 0; e < E; ++e) {
                 const uint32_t bits = fp32_bits<T>(sizeof(T) == 4 ? w[e % 4] : w[e / 2] >> (16 * (e & 1)) & 0xFFFFu);
                 const Scale s = scale_of(bits);
-                factor[o * STRIP + piece * E + e] = s.r;
+                factor[o * COLS + piece * E + e] = s.r;
                 if (s.nan()) any_nan = 1u;
                 if (begin == 0 && col + e < cols) out.scales[(uint64_t)o * cols + col + e] = s.s;
             }
         }
     }
     __syncthreads();
-    float r[OUT][E];
-#pragma unroll
-    for (int i = 0; i < OUT * E; ++i) r[i / E][i % E] = factor[i / E * STRIP + piece * E + i % E];
     const bool masked = any_nan != 0u;
 
+    // what a thread brings from the tile to memory: chunk `chunk` of columns STEP places apart, which are STEP / 16 columns of its piece p apart
+    constexpr int CHUNKS = WORDS / 4, STEP = STRIP_THREADS / CHUNKS;
+    const uint32_t chunk = tid % CHUNKS, slot = tid / CHUNKS, p_out = slot % 16, turned = S::turned(p_out), first_col = strip * COLS + p_out * E + slot / 16;
+    int8_t *const to_cols = out.codes + (uint64_t)first_col * out.pitch + chunk * 16;
     for (uint32_t t = end; t-- > begin;) {
-        const uint32_t r0 = t * STRIP_ROWS;
-#pragma unroll 1
-        for (int sweep0 = 0; sweep0 < STRIP_ROWS / SWEEP; sweep0 += TOGETHER) {
-            uint32_t raw[TOGETHER][4][IN][4];
+        uint32_t *const tile = tiles_smem + (t & 1u) * S::WORDS_ALL;
+        const bool masked_rows = ROWS && nan_rows[t & 1u] == t + 1;
+        // FULL: the tile lies inside the matrix, nothing needs a check
+        auto work = [&](auto full) {
+            constexpr bool FULL = decltype(full)::value;
 #pragma unroll
-            for (int k = 0; k < TOGETHER * 4; ++k) {
-                const uint32_t row = r0 + ((sweep0 + k / 4) * DOWN + down) * 4 + k % 4;
-#pragma unroll
-                for (int j = 0; j < IN * 4; ++j) raw[k / 4][k % 4][j / 4][j % 4] = 0u;
-                if (row < rows && col < cols) src.fetch(row, col, cols, raw[k / 4][k % 4]);
-            }
-#pragma unroll
-            for (int k = 0; k < TOGETHER; ++k) {
-                const uint32_t four = (sweep0 + k) * DOWN + down;
-                float v[OUT][4][E];
+            for (int k = 0; k < SWEEPS; ++k) {
+                constexpr int N = Word<T>::N;
+                uint32_t w[4][OUT][4];
+                int8_t *to = nullptr;
+                float4 r4 = make_float4(0.f, 0.f, 0.f, 0.f);
+                if constexpr (ROWS) {
+                    to = out_r.codes + (uint64_t)row_of(t, k * 4) * out_r.pitch;
+                    r4 = *reinterpret_cast<const float4 *>(&row_factor[t & 1u][k * 64 + down * 4]);
+                }
+                const float rs[4] = {r4.x, r4.y, r4.z, r4.w};
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    uint32_t w[OUT][4];
-                    src.make(raw[k][i], w);
+                    const uint32_t row = row_of(t, k * 4 + i);
+                    if (FULL || (row < rows && col < cols)) {
+                        src.make(row, col, cols, raw[k * 4 + i], w[i]);
+                    } else {
 #pragma unroll
-                    for (int j = 0; j < OUT * 4; ++j) Word<T>::unpack(w[j / 4][j % 4], &v[j / 4][i][j % 4 * Word<T>::N]);
+                        for (int j = 0; j < OUT * 4; ++j) w[i][j / 4][j % 4] = 0u;
+                    }
+                    if constexpr (ROWS) {
+                        if (FULL || row < rows) {
+#pragma unroll
+                            for (int o = 0; o < OUT; ++o) {
+                                uint32_t c[E / 4];
+                                encode_piece<T>(w[i][o], rs[i], false, c);
+                                if (masked_rows && rs[i] == 0.f)
+#pragma unroll
+                                    for (int j = 0; j < E / 4; ++j) c[j] = 0u;
+                                if (FULL && OUT == 1) store_whole<E>(to + col, c);
+                                else store_row_piece<E, OUT>(to, o, col, cols, out_r.pitch, c);
+                            }
+                            if (OUT > 1 && strip == strips - 1 && piece == 0) pad_row(to, (uint64_t)OUT * cols, out_r.pitch);
+                        }
+                        to += out_r.pitch;
+                    }
                 }
-                // word `four` of a column, turned by the piece so that a warp's stores fall into different banks
-                const uint32_t place = four ^ (piece * (32 / ACROSS));
+                const uint32_t place = (k * 16 + down) ^ S::turned(piece);
 #pragma unroll
                 for (int o = 0; o < OUT; ++o)
 #pragma unroll
                     for (int e = 0; e < E; e += 2) {
-                        float2 q[4];
+                        const float2 r = *reinterpret_cast<const float2 *>(factor + o * COLS + piece * E + e);
+                        float p[4], q[4];
 #pragma unroll
-                        for (int i = 0; i < 4; ++i)
-                            q[i] = el::fma2(make_float2(v[o][i][e], v[o][i][e + 1]), make_float2(r[o][e], r[o][e + 1]), el::twice(TO_INTEGER));
-                        uint32_t a = bytes4(q[0].x, q[1].x, q[2].x, q[3].x), b = bytes4(q[0].y, q[1].y, q[2].y, q[3].y);
-                        if (masked) {
-                            if (r[o][e] == 0.f) a = 0u;
-                            if (r[o][e + 1] == 0.f) b = 0u;
+                        for (int i = 0; i < 4; ++i) {
+                            float v[2];
+                            if constexpr (N == 2) Word<T>::unpack(w[i][o][e / 2], v);
+                            else v[0] = __uint_as_float(w[i][o][e % 4]), v[1] = __uint_as_float(w[i][o][(e + 1) % 4]);
+                            p[i] = __fmaf_rn(v[0], r.x, TO_INTEGER);
+                            q[i] = __fmaf_rn(v[1], r.y, TO_INTEGER);
                         }
-                        tile[(o * STRIP + piece * E + e) * 32 + place] = a;
-                        tile[(o * STRIP + piece * E + e + 1) * 32 + place] = b;
+                        uint32_t a = bytes4(p[0], p[1], p[2], p[3]), b = bytes4(q[0], q[1], q[2], q[3]);
+                        if (masked) {
+                            if (r.x == 0.f) a = 0u;
+                            if (r.y == 0.f) b = 0u;
+                        }
+                        tile[(o * COLS + e * 16 + piece) * WORDS + place] = a;
+                        tile[(o * COLS + e * 16 + 16 + piece) * WORDS + place] = b;
                     }
             }
+        };
+        if (whole_strip && (t + 1) * S::ROWS <= rows) work(std::true_type());
+        else work(std::false_type());
+        if (t > begin) {
+            fetch(t - 1);
+            rows_of(t - 1);
         }
         __syncthreads();
+        const uint32_t *const from = tile + slot * WORDS + ((chunk ^ (turned >> 2)) * 4);
+        int8_t *const at = to_cols + (uint64_t)t * S::ROWS;
+        const bool inside = (uint64_t)t * S::ROWS + chunk * 16 < out.pitch;
 #pragma unroll
-        for (int i = 0; i < OUT * STRIP * 8 / STRIP_THREADS; ++i) {
-            const uint32_t n = i * STRIP_THREADS + tid, c = n >> 3, chunk = n & 7, in_strip = c % STRIP;
-            const uint32_t at = strip * STRIP + in_strip, first = r0 + chunk * 16;
-            if (at < cols && first < out.pitch) {
-                const uint32_t turned = in_strip / E * (32 / ACROSS);
-                uint4 q = *reinterpret_cast<const uint4 *>(tile + c * 32 + ((chunk ^ (turned >> 2)) * 4));
-                if (turned & 1) q = make_uint4(q.y, q.x, q.w, q.z);
+        for (int i = 0; i < OUT * COLS / STEP; ++i) {
+            constexpr int PER = COLS / STEP;               // steps in a half
+            const uint32_t more = i % PER * (STEP / 16);
+            if (inside && first_col + more < cols) {
+                uint4 q = *reinterpret_cast<const uint4 *>(from + i * STEP * WORDS);
                 if (turned & 2) q = make_uint4(q.z, q.w, q.x, q.y);
-                *reinterpret_cast<uint4 *>(out.codes + ((uint64_t)(c / STRIP) * cols + at) * out.pitch + first) = q;
+                *reinterpret_cast<uint4 *>(at + ((uint64_t)(i / PER) * cols + more) * out.pitch) = q;
             }
         }
-        __syncthreads();
     }
 }
 
-// Threads that share a row (a power of two, 32 at least) and pieces a thread.
+// Threads that share a row (32 or a power of two from 128 on) and pieces a thread.
 struct Group {
     uint32_t log, pieces;
     bool fits;
@@ -372,64 +588,69 @@ Group group_of(uint64_t cols)
     const uint64_t pieces = (cols + PIECE<T> - 1) / PIECE<T>;
     Group g = {5, 1, true};
     while ((int)g.pieces < MOST_P && pieces > 32u * g.pieces) g.pieces *= 2;
+    if (pieces > 32u * g.pieces) {
+        g.log = 7;
+        if (pieces <= 256) g.pieces = 2;
+    }
     while ((1u << g.log) < (uint32_t)ROW_THREADS && pieces > ((uint64_t)g.pieces << g.log)) ++g.log;
     g.fits = pieces <= ((uint64_t)g.pieces << g.log);
     return g;
 }
 
-template <typename SRC, int P, int THREADS, bool ROWS, bool COLS>
-int launch_rows(const SRC &src, uint32_t rows, uint32_t cols, uint32_t group_log, const RowsOut &out, uint32_t &parts, void *stream)
+template <typename SRC, int P, int THREADS, bool ROWS>
+int launch_rows(const SRC &src, uint32_t rows, uint32_t cols, uint32_t group_log, const RowsOut &out, void *stream)
 {
-    const uint32_t together = THREADS >> group_log;
+    const uint32_t together = THREADS >> group_log, most = (uint32_t)DEFAULT_SMS * ROWS_CTAS<SRC, P, THREADS>;
     const uint64_t window = (uint64_t)(P * PIECE<typename SRC::T>) << group_log;
     const uint32_t windows = ROWS ? 1u : (uint32_t)((cols + window - 1) / window);
-    const uint32_t most = COLS ? MOST_PARTS : (uint32_t)DEFAULT_SMS * (THREADS > 256 ? 2u : 4u);
     uint32_t ctas = (rows + together - 1) / together;
     if (ctas > most) ctas = most;
-    parts = ctas;
-    return note_cuda(el::launch(rows_kernel<SRC, P, THREADS, ROWS, COLS>, dim3(ctas, windows), THREADS, 0, 1, stream, src, rows, cols, group_log, out));
+    return note_cuda(el::launch(rows_kernel<SRC, P, THREADS, ROWS>, dim3(ctas * windows), THREADS, 0, 1, stream, src, rows, cols, group_log, Place{ctas}, out));
 }
 
-template <typename SRC, int MOST_P, bool ROWS, bool COLS>
-int launch_rows_by_width(const SRC &src, uint32_t rows, uint32_t cols, const Group &g, const RowsOut &out, uint32_t &parts, void *stream)
+// CTAs of 256 threads, or of a whole wider group.
+template <typename SRC, int MOST_P, bool ROWS>
+int launch_rows_by_width(const SRC &src, uint32_t rows, uint32_t cols, const Group &g, const RowsOut &out, void *stream)
 {
-    if ((1u << g.log) == (uint32_t)ROW_THREADS) return launch_rows<SRC, MOST_P, ROW_THREADS, ROWS, COLS>(src, rows, cols, g.log, out, parts, stream);
+    if ((1 << g.log) == ROW_THREADS) return launch_rows<SRC, MOST_P, ROW_THREADS, ROWS>(src, rows, cols, g.log, out, stream);
     if constexpr (MOST_P > 2)
-        if (g.pieces > 2) return launch_rows<SRC, MOST_P, 256, ROWS, COLS>(src, rows, cols, g.log, out, parts, stream);
-    if (g.pieces == 2) return launch_rows<SRC, 2, 256, ROWS, COLS>(src, rows, cols, g.log, out, parts, stream);
-    return launch_rows<SRC, 1, 256, ROWS, COLS>(src, rows, cols, g.log, out, parts, stream);
+        if (g.pieces > 2) return launch_rows<SRC, MOST_P, 256, ROWS>(src, rows, cols, g.log, out, stream);
+    if (g.pieces == 2) return launch_rows<SRC, 2, 256, ROWS>(src, rows, cols, g.log, out, stream);
+    return launch_rows<SRC, 1, 256, ROWS>(src, rows, cols, g.log, out, stream);
+}
+
+template <typename SRC, bool ROWS>
+int launch_both(const SRC &src, uint32_t rows, uint32_t cols, const RowsOut &ro, const ColsOut &co, void *workspace, void *stream)
+{
+    using S = Strip<SRC>;
+    const uint32_t window = 32 * WINDOW_PIECES<SRC::OUT> * PIECE<typename SRC::T>, windows = (uint32_t)(((uint64_t)cols + window - 1) / window), sets = (uint32_t)shares_of(rows, windows);
+    const uint64_t pieces = (cols + S::E - 1) / S::E;
+    uint4 *const maxima = static_cast<uint4 *>(workspace);
+    const Maxima m = {maxima, reinterpret_cast<uint32_t *>(maxima + sets * SRC::OUT * pieces), sets, windows};
+    if (const int rc = note_cuda(el::launch(maxima_kernel<SRC, ROWS>, dim3(sets * windows), 32 * MAXIMA_WARPS, 0, 1, stream, src, rows, cols, Place{sets}, m))) return rc;
+    const uint32_t strips = (cols + S::COLS - 1) / S::COLS, tiles = (rows + S::ROWS - 1) / S::ROWS, resident = DEFAULT_SMS * S::CTAS;
+    uint32_t shares = strips < resident ? resident / strips : 1u;          // all CTAs at once
+    if (shares > tiles) shares = tiles;
+    const uint32_t each = (tiles + shares - 1) / shares;
+    shares = (tiles + each - 1) / each;
+    return note_cuda(el::launch(codes_kernel<SRC, ROWS>, dim3(strips * shares), STRIP_THREADS, 0, 1, stream, src, rows, cols, strips, each, m, ro, co));
 }
 
 // Along the rows (codes) and / or the columns (codes_t) of a source; with neither, what the source emits alone.
 template <int MOST_P, typename SRC>
 int quantise(const SRC &src, uint32_t rows, uint32_t cols, int8_t *codes, float *scales, int8_t *codes_t, float *scales_t, void *workspace, void *stream)
 {
-    using T = typename SRC::T;
-    const Group g = group_of<T, MOST_P>(cols);
-    const RowsOut ro = {codes, scales, row_bytes((uint64_t)SRC::OUT * cols), static_cast<uint4 *>(workspace)};
-    uint32_t parts = 0;
-    int rc = OMC_OK;
-    const bool wide = codes && !g.fits;
-    if (wide) {
-        const uint32_t most = DEFAULT_SMS * 4;
-        rc = note_cuda(el::launch(wide_rows_kernel<SRC>, dim3(rows < most ? rows : most), WIDE_THREADS, 0, 1, stream, src, rows, cols, ro));
-        if (rc || !codes_t) return rc;
+    const RowsOut ro = {codes, scales, row_bytes((uint64_t)SRC::OUT * cols)};
+    const ColsOut co = {codes_t, scales_t, row_bytes(rows)};
+    if (codes_t) return codes ? launch_both<SRC, true>(src, rows, cols, ro, co, workspace, stream) : launch_both<SRC, false>(src, rows, cols, ro, co, workspace, stream);
+    const Group g = group_of<typename SRC::T, MOST_P>(cols);
+    if (!codes) {
+        if constexpr (SRC::OUT > 1) return launch_rows_by_width<SRC, MOST_P, false>(src, rows, cols, g, ro, stream);
+        return OMC_OK;
     }
-    if (codes && !wide)
-        rc = codes_t ? launch_rows_by_width<SRC, MOST_P, true, true>(src, rows, cols, g, ro, parts, stream)
-                     : launch_rows_by_width<SRC, MOST_P, true, false>(src, rows, cols, g, ro, parts, stream);
-    else if (codes_t)
-        rc = launch_rows_by_width<SRC, MOST_P, false, true>(src, rows, cols, g, ro, parts, stream);
-    else if constexpr (SRC::OUT > 1)
-        rc = launch_rows_by_width<SRC, MOST_P, false, false>(src, rows, cols, g, ro, parts, stream);
-    if (rc || !codes_t) return rc;
-    const uint32_t strips = (cols + STRIP - 1) / STRIP, tiles = (rows + STRIP_ROWS - 1) / STRIP_ROWS;
-    uint32_t shares = (DEFAULT_SMS * 3 + strips - 1) / strips;
-    if (shares > tiles) shares = tiles;
-    const uint32_t each = (tiles + shares - 1) / shares;
-    shares = (tiles + each - 1) / each;
-    const ColsOut co = {ro.parts, parts, codes_t, scales_t, row_bytes(rows)};
-    return note_cuda(el::launch(cols_kernel<SRC>, dim3(strips * shares), STRIP_THREADS, 0, 1, stream, src, rows, cols, strips, each, co));
+    if (g.fits) return launch_rows_by_width<SRC, MOST_P, true>(src, rows, cols, g, ro, stream);
+    const uint32_t most = DEFAULT_SMS * 4;
+    return note_cuda(el::launch(wide_rows_kernel<SRC>, dim3(rows < most ? rows : most), WIDE_THREADS, 0, 1, stream, src, rows, cols, ro));
 }
 
 }  // namespace i8

@@ -18,52 +18,92 @@ namespace {
 using namespace omc;
 using el::Word;
 
-// Values back: a thread takes sixteen codes.
-template <typename T, bool VECTOR>
+// Values back.  Rows on 32-byte boundaries: a thread makes 32 bytes, 8 or 16 values, with one store.
+template <typename T>
 __global__ void __launch_bounds__(256) dequantise_kernel(const int8_t *codes, const float *scales, uint32_t rows, uint32_t cols, T *__restrict__ out, uint64_t ld)
 {
-    constexpr int N = Word<T>::N;
+    constexpr int N = Word<T>::N, E = 8 * N;
     el::enter_stream_order();
-    const uint32_t chunks = (cols + 15) / 16;
-    const uint64_t all = (uint64_t)rows * chunks, step = (uint64_t)gridDim.x * 256;
+    const uint32_t chunks = (cols + E - 1) / E;
+    const uint64_t all = (uint64_t)rows * chunks, step = (uint64_t)gridDim.x * 256, pitch = i8::row_bytes(cols);
     for (uint64_t i = (uint64_t)blockIdx.x * 256 + threadIdx.x; i < all; i += step) {
-        const uint32_t row = (uint32_t)(i / chunks), col = (uint32_t)(i - (uint64_t)row * chunks) * 16;
-        const uint4 q = *reinterpret_cast<const uint4 *>(codes + i * 16);
+        const uint32_t row = (uint32_t)(i / chunks), col = (uint32_t)(i - (uint64_t)row * chunks) * E;
+        const int8_t *from = codes + row * pitch + col;
+        uint32_t w[E / 4];
+        if constexpr (E == 16) {
+            const uint4 q = *reinterpret_cast<const uint4 *>(from);
+            w[0] = q.x, w[1] = q.y, w[2] = q.z, w[3] = q.w;
+        } else {
+            const uint2 q = *reinterpret_cast<const uint2 *>(from);
+            w[0] = q.x, w[1] = q.y;
+        }
         const float s = scales[row];
-        const uint32_t w[4] = {q.x, q.y, q.z, q.w};
-        float v[16];
+        float v[E];
 #pragma unroll
-        for (int j = 0; j < 16; ++j) v[j] = (float)(int8_t)(w[j / 4] >> (8 * (j & 3))) * s;
+        for (int j = 0; j < E; ++j) v[j] = (float)(int8_t)(w[j / 4] >> (8 * (j & 3))) * s;
         T *to = out + row * ld + col;
-        if (VECTOR && col + 16 <= cols) {
+        if (col + E <= cols) {
+            uint32_t o[8];
 #pragma unroll
-            for (int j = 0; j < 16 / N; j += 4)
-                *reinterpret_cast<uint4 *>(to + j * N) = make_uint4(Word<T>::pack(v + j * N), Word<T>::pack(v + (j + 1) * N), Word<T>::pack(v + (j + 2) * N), Word<T>::pack(v + (j + 3) * N));
+            for (int j = 0; j < 8; ++j) o[j] = Word<T>::pack(v + j * N);
+            el::store32(to, o);
         } else {
 #pragma unroll
-            for (int j = 0; j < 16; ++j)
+            for (int j = 0; j < E; ++j)
                 if (col + j < cols) to[j] = el::from_float<T>(v[j]);
         }
     }
 }
-
-template <typename T, bool VECTOR>
-int dequantise(const int8_t *codes, const float *scales, uint32_t rows, uint32_t cols, void *out, uint64_t ld, void *stream)
+// Other rows: neighbouring lanes make neighbouring words (of 16-bit types two values from the word's boundary on, whose halves at the row's ends
+// are stored alone), four of them a thread, 32 apart; a warp a piece of 128 words of a row.
+template <typename T>
+__global__ void __launch_bounds__(256) dequantise_words_kernel(const int8_t *codes, const float *scales, uint32_t rows, uint32_t cols, T *__restrict__ out, uint64_t ld)
 {
-    const uint64_t ctas = ((uint64_t)rows * ((cols + 15) / 16) + 255) / 256, most = DEFAULT_SMS * 8;
-    return note_cuda(el::launch(dequantise_kernel<T, VECTOR>, dim3((uint32_t)(ctas < most ? ctas : most)), 256, 0, 1, stream, codes, scales, rows, cols,
-                                static_cast<T *>(out), ld));
+    constexpr uint32_t N = Word<T>::N;
+    el::enter_stream_order();
+    const uint32_t lane = threadIdx.x & 31, pieces = (cols / N + 1 + 127) / 128;
+    const uint64_t all = (uint64_t)rows * pieces, step = (uint64_t)gridDim.x * 8, pitch = i8::row_bytes(cols);
+    for (uint64_t i = (uint64_t)blockIdx.x * 8 + (threadIdx.x >> 5); i < all; i += step) {
+        const uint32_t row = (uint32_t)(i / pieces), word = (uint32_t)(i - (uint64_t)row * pieces) * 128 + lane;
+        T *const to = out + row * ld;
+        const uint32_t odd = N == 2 ? (uint32_t)(reinterpret_cast<uintptr_t>(to) >> 1) & 1u : 0u;
+        const int8_t *const from = codes + row * pitch;
+        const float s = scales[row];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const uint32_t place = (word + 32 * j) * N;        // value place - odd is the word's first one
+            float v[2] = {0.f, 0.f};
+            const bool before = N == 2 && odd > place, first = !before && place - odd < cols, second = N == 2 && place + 1 - odd < cols;
+            if (first) v[0] = (float)from[place - odd] * s;
+            if (second) v[1] = (float)from[place + 1 - odd] * s;
+            T *const p = to + place - odd;
+            if (N == 1 ? first : first && second) *reinterpret_cast<uint32_t *>(p) = Word<T>::pack(v);
+            else if (first) p[0] = el::from_float<T>(v[0]);
+            else if (second) p[1] = el::from_float<T>(v[1]);
+        }
+    }
 }
 
-template <typename T, bool VECTOR>
+template <typename T>
+int dequantise(const int8_t *codes, const float *scales, uint32_t rows, uint32_t cols, void *out, uint64_t ld, void *stream)
+{
+    constexpr uint64_t N = Word<T>::N;
+    const bool whole = reinterpret_cast<uintptr_t>(out) % 32 == 0 && ld * sizeof(T) % 32 == 0;
+    const uint64_t threads = whole ? (uint64_t)rows * ((cols + 8 * N - 1) / (8 * N)) : (uint64_t)rows * ((cols / N + 1 + 127) / 128) * 32;
+    const uint64_t ctas = (threads + 255) / 256, most = DEFAULT_SMS * 8;
+    return note_cuda(el::launch(whole ? dequantise_kernel<T> : dequantise_words_kernel<T>, dim3((uint32_t)(ctas < most ? ctas : most)), 256, 0, 1, stream, codes,
+                                scales, rows, cols, static_cast<T *>(out), ld));
+}
+
+template <typename T, bool WHOLE>
 int quantise(const void *x, uint64_t ld, uint32_t rows, uint32_t cols, int8_t *codes, float *scales, int8_t *codes_t, float *scales_t, void *workspace,
              void *stream)
 {
-    const i8::Matrix<T, VECTOR> src = {static_cast<const T *>(x), ld};
+    const T *const m = static_cast<const T *>(x);
+    const i8::Matrix<T, WHOLE> src = {m, ld, i8::span_of(m, ld, rows, cols)};
     return i8::quantise<4>(src, rows, cols, codes, scales, codes_t, scales_t, workspace, stream);
 }
 
-bool vector_rows(const void *p, uint64_t ld, int type) { return el::aligned16(p) && ld * el::size_of(type) % 16 == 0; }
 bool aligned4(const void *p) { return reinterpret_cast<uintptr_t>(p) % 4 == 0; }
 
 }  // namespace
@@ -80,7 +120,7 @@ extern "C" int omc_byte_quantise_workspace(uint64_t rows, uint64_t cols, uint64_
 {
     if (!bytes) return OMC_ERR_NULL_PTR;
     if (!i8_shape_ok(rows, cols)) return OMC_ERR_INVALID_ARG;
-    *bytes = i8::parts_bytes(rows, cols);
+    *bytes = i8::maxima_bytes(rows, cols, 1);
     return OMC_OK;
 }
 
@@ -93,9 +133,9 @@ extern "C" int omc_byte_quantise(const void *x, int type, uint64_t rows, uint64_
     if (reinterpret_cast<uintptr_t>(x) % el::size_of(type) || !el::aligned16(codes) || !aligned4(scales) || !el::aligned16(codes_t) ||
         !aligned4(scales_t) || !el::aligned16(workspace))
         return OMC_ERR_MISALIGNED;
-    const bool vec = vector_rows(x, ld, type);
+    const bool whole = el::aligned16(x) && ld * el::size_of(type) % 16 == 0 && cols * el::size_of(type) % 16 == 0;
     const uint32_t r = (uint32_t)rows, c = (uint32_t)cols;
-#define OMC_CALL(T) (vec ? quantise<T, true>(x, ld, r, c, codes, scales, codes_t, scales_t, workspace, stream) \
+#define OMC_CALL(T) (whole ? quantise<T, true>(x, ld, r, c, codes, scales, codes_t, scales_t, workspace, stream) \
                          : quantise<T, false>(x, ld, r, c, codes, scales, codes_t, scales_t, workspace, stream))
     return type == OMC_TYPE_F32 ? OMC_CALL(float) : type == OMC_TYPE_F16 ? OMC_CALL(__half) : OMC_CALL(__nv_bfloat16);
 #undef OMC_CALL
@@ -107,9 +147,7 @@ extern "C" int omc_byte_dequantise(const int8_t *codes, const float *scales, uin
     if (!codes || !scales || !out) return OMC_ERR_NULL_PTR;
     if (!i8_shape_ok(rows, cols) || ld < cols) return OMC_ERR_INVALID_ARG;
     if (reinterpret_cast<uintptr_t>(out) % el::size_of(type) || !el::aligned16(codes) || !aligned4(scales)) return OMC_ERR_MISALIGNED;
-    const bool vec = vector_rows(out, ld, type);
     const uint32_t r = (uint32_t)rows, c = (uint32_t)cols;
-#define OMC_CALL(T) (vec ? dequantise<T, true>(codes, scales, r, c, out, ld, stream) : dequantise<T, false>(codes, scales, r, c, out, ld, stream))
-    return type == OMC_TYPE_F32 ? OMC_CALL(float) : type == OMC_TYPE_F16 ? OMC_CALL(__half) : OMC_CALL(__nv_bfloat16);
-#undef OMC_CALL
+    return type == OMC_TYPE_F32 ? dequantise<float>(codes, scales, r, c, out, ld, stream)
+           : type == OMC_TYPE_F16 ? dequantise<__half>(codes, scales, r, c, out, ld, stream) : dequantise<__nv_bfloat16>(codes, scales, r, c, out, ld, stream);
 }

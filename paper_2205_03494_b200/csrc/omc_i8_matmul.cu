@@ -6,8 +6,8 @@
 // two rows of W for a column of its result, one of each half of W, as two columns of the same accumulator.
 //
 // Three kernels:
-//   pairs   large products: pairs of SMs share tiles of 256 x 256 (gated: 256 x 128, whose operand is 128 rows of either half of W).
-//   small   few rows, or few tiles: W's rows are the 128 lanes of tensor memory, 16 .. 128 rows of X the columns, so that few rows of X
+//   tile    tiles of 128 rows of X on an SM or 256 on a pair of SMs; X's rows are the lanes of tensor memory.
+//   small   few rows, or few tiles and long sums: W's rows are the 128 lanes, 16 .. 64 rows of X the columns, so that few rows of X
 //           waste nothing; K divided among the CTAs of a cluster where there are few tiles.
 //   rows    up to four rows of X: no tensor cores, a warp multiplies four rows of W as they come from memory (dp4a); values that are
 //           not quantised yet are quantised by every CTA for itself.
@@ -158,26 +158,32 @@ __device__ __forceinline__ void values16(const uint32_t *v, const i8::RowScale &
     }
 }
 
-// ---- large products: pairs of SMs ----------------------------------------------------------------------
-// Two CTAs of a cluster share a tile of 256 rows of X by 256 rows of W: each holds 128 rows of either for a K step (32 KB, six steps on
-// their way), the leader issues products of 256 x 256 x 32 whose upper half accumulates in its own tensor memory and whose lower half in its
-// peer's, and each CTA stores its 128 rows.  In the gated layer the leader holds 128 rows of the gate's half of W and its peer the
-// same rows of the other half: columns 0 .. 127 of the accumulator are a, columns 128 .. 255 are b.
+// ---- tiles of 128 or 256 rows of X ---------------------------------------------------------------------
+// CG CTAs, a cluster, share a tile of 128 CG rows of X by BN rows of W (gated: BN / 2 of either half).  With two, each holds 128 rows of X and
+// BN / 2 rows of W for a K step (32 KB for the largest tile, six steps on their way), the leader issues products of 256 x BN x 32 whose upper half
+// accumulates in its own tensor memory and whose lower half in its peer's, and each CTA stores its 128 rows.  In the gated layer the accumulator's
+// first BN / 2 columns are a, the others b: with two CTAs the leader holds the gate's rows and its peer the same rows of the other half.
 // Barriers as their waiters need them: full (in the leader, the bytes of both CTAs' copies), empty and acc_full (in each CTA, a commit
-// reaches both), acc_empty (in the leader, an arrival of each of the sixteen warps that store results).
+// reaches both), acc_empty (in the leader, an arrival of each of the warps that store results).
 // Every wait is bounded, and a role whose wait ran out leaves its loop, so that both CTAs reach the closing barrier on every path.
 // Tensor memory is taken after the kernel before on the stream has finished and let go after the products.
-template <bool STAGED>
-struct Pair {
-    static constexpr int STAGE = 2 * TILE_BYTES, NSTAGES = STAGED ? 5 : 6;
+template <int CG, int BN, bool GATED>
+struct Tile {
+    static constexpr int W_ROWS = BN / CG;                           // of a CTA
+    static constexpr int STAGE = TILE_BYTES + W_ROWS * BK;
     static constexpr int THREADS = 320, STORE_WARPS = 8;
-    static constexpr int SCALES = 2 * 256 * 4;                       // of W's rows, of two tiles
-    static constexpr int ROOM = STAGED ? STORE_WARPS * 32 * 17 * 4 : 0;      // sixteen columns of a warp's rows on their way to Y
+    static constexpr int SCALES = 2 * BN * 4;                        // of W's rows, of two tiles
+    // results on their way from a warp to memory: boxes of 64 bytes of 32 rows, three a warp (or 16 columns of rows off the 16-byte boundaries)
+    static constexpr int BOX = 32 * 64, BOXES = 3, ROOM = STORE_WARPS * BOXES * BOX;
+    static_assert(BOXES * BOX >= 32 * 17 * 4, "");
+    static constexpr int FIT = (220 * 1024 - SCALES - ROOM - 1024 - 256) / STAGE, NSTAGES = FIT < 8 ? FIT : 8;
     static constexpr int BARRIERS = 2 * NSTAGES + 5;
     static constexpr int SMEM = NSTAGES * STAGE + SCALES + ROOM + 1024 + 256;
-    static_assert(8 * BARRIERS + 8 <= 256 && SMEM <= 220 * 1024, "");
+    static constexpr int TMEM_COLS = 2 * BN;
+    static constexpr int COLS = GATED ? BN / 2 : BN;                 // of Y
+    static constexpr int W_BOX = GATED ? BN / 2 : W_ROWS;            // rows of a copy
+    static_assert(STAGE % 1024 == 0 && NSTAGES >= 4 && 8 * BARRIERS + 8 <= 256, "");
 };
-constexpr int TMEM_COLS = 512;
 
 // Barrier of the 256 threads that store results, and whether all of them say yes: they leave their loop together or not at all.
 __device__ __forceinline__ bool together256(bool ok)
@@ -191,7 +197,7 @@ __device__ __forceinline__ bool together256(bool ok)
         : "=r"(all) : "r"((uint32_t)ok) : "memory");
     return all != 0u;
 }
-// Tiles in the order in which the pairs take them: bands of eight tiles of W's rows, so that the tiles in work at a time form a
+// Tiles in the order in which they are taken: bands of eight tiles of W's rows, so that the tiles in work at a time form a
 // block of about eight by nine and share their operands in L2.
 __device__ __forceinline__ void tile_of(uint32_t t, uint32_t tiles_n, uint32_t tiles_m, uint32_t &tn, uint32_t &tm)
 {
@@ -201,55 +207,77 @@ __device__ __forceinline__ void tile_of(uint32_t t, uint32_t tiles_n, uint32_t t
     tn = band * 8 + in_band - tm * width;
 }
 
-// Sixteen neighbouring values of each lane's row, from column `col` on, to a matrix of `cols` columns.  Rows that start on 16-byte
-// boundaries: each lane its own.  Others (STAGED): through shared memory, so that neighbouring lanes store neighbouring values.
-template <typename T, bool STAGED>
+// Sixteen neighbouring values of each lane's row, from column `col` on, to a matrix of `cols` columns whose rows start anywhere: through shared memory,
+// so that neighbouring lanes store neighbouring values.
+template <typename T>
 __device__ __forceinline__ void store16(const float *f, T *to, uint64_t ld, uint32_t row0, uint32_t rows, uint32_t col, uint32_t cols, int lane, uint32_t *room)
 {
-    constexpr int N = Word<T>::N;
-    if constexpr (STAGED) {
-        __syncwarp();
+    __syncwarp();
 #pragma unroll
-        for (int j = 0; j < 16; ++j) {
-            const T v = el::from_float<T>(f[j]);
-            if constexpr (sizeof(T) == 4) room[lane * 17 + j] = *reinterpret_cast<const uint32_t *>(&v);
-            else room[lane * 17 + j] = *reinterpret_cast<const uint16_t *>(&v);
-        }
-        __syncwarp();
-        const uint32_t c = lane & 15;
-        if (col + c < cols) {
+    for (int j = 0; j < 16; ++j) {
+        const T v = el::from_float<T>(f[j]);
+        if constexpr (sizeof(T) == 4) room[lane * 17 + j] = *reinterpret_cast<const uint32_t *>(&v);
+        else room[lane * 17 + j] = *reinterpret_cast<const uint16_t *>(&v);
+    }
+    __syncwarp();
+    const uint32_t c = lane & 15;
+    if (col + c < cols) {
 #pragma unroll 4
-            for (int i = 0; i < 16; ++i) {
-                const uint32_t r = 2 * i + (lane >> 4);
-                if (row0 + r < rows) {
-                    T *p = to + (uint64_t)(row0 + r) * ld + col + c;
-                    if constexpr (sizeof(T) == 4) *reinterpret_cast<uint32_t *>(p) = room[r * 17 + c];
-                    else *reinterpret_cast<uint16_t *>(p) = (uint16_t)room[r * 17 + c];
-                }
+        for (int i = 0; i < 16; ++i) {
+            const uint32_t r = 2 * i + (lane >> 4);
+            if (row0 + r < rows) {
+                T *p = to + (uint64_t)(row0 + r) * ld + col + c;
+                if constexpr (sizeof(T) == 4) *reinterpret_cast<uint32_t *>(p) = room[r * 17 + c];
+                else *reinterpret_cast<uint16_t *>(p) = (uint16_t)room[r * 17 + c];
             }
-        }
-    } else {
-        if (row0 + lane >= rows) return;
-        T *p = to + (uint64_t)(row0 + lane) * ld + col;
-        if (col + 16 <= cols) {
-#pragma unroll
-            for (int j = 0; j < 16 / N; j += 4)
-                *reinterpret_cast<uint4 *>(p + j * N) = make_uint4(Word<T>::pack(f + j * N), Word<T>::pack(f + (j + 1) * N), Word<T>::pack(f + (j + 2) * N), Word<T>::pack(f + (j + 3) * N));
-        } else {
-#pragma unroll
-            for (int j = 0; j < 16; ++j)
-                if (col + j < cols) p[j] = el::from_float<T>(f[j]);
         }
     }
 }
 
-template <typename T, bool GATED, bool STAGED, typename WAITS>
-__global__ void __launch_bounds__(Pair<STAGED>::THREADS, 1)
-i8_pair_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_w, Result<T> o, WAITS waits)
+// Rows on 16-byte boundaries: a warp's boxes of 32 rows x 64 bytes go out as bulk tensor stores, which write whole sectors and clip at the matrix's ends.
+// (They clip whole pieces of 16 bytes: a matrix 257 FP32 values wide got 260 written.)
+// (With each lane storing its own row, 32 bytes at a time, the stores took the load/store unit's time: 8192 x 8192 x 256 BF16 46.7 us.)
+// Sixteen values of a lane's row into a box, from its 16-byte piece `piece` on; 64-byte swizzle: piece p of row r sits at piece p ^ (r / 2 mod 4).
+template <typename T>
+__device__ __forceinline__ void box16(uint32_t box, int piece, const float *f, int lane)
 {
-    using C = Pair<STAGED>;
-    constexpr int NS = C::NSTAGES, TN = GATED ? 128 : 256;           // columns of Y in a tile
-    constexpr uint32_t IDESC = instr_desc(256, 256);
+    constexpr int N = Word<T>::N;
+#pragma unroll
+    for (int i = 0; i < 16 / (4 * N); ++i) {
+        const uint32_t at = box + lane * 64 + (((piece + i) ^ ((lane >> 1) & 3)) << 4);
+        asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(Word<T>::pack(f + (4 * i) * N)), "r"(Word<T>::pack(f + (4 * i + 1) * N)),
+                     "r"(Word<T>::pack(f + (4 * i + 2) * N)), "r"(Word<T>::pack(f + (4 * i + 3) * N)) : "memory");
+    }
+}
+// Waits until at most PENDING of this warp's stores still read their boxes.
+template <int PENDING>
+__device__ __forceinline__ void boxes_free(int lane)
+{
+    if (lane == 0) asm volatile("cp.async.bulk.wait_group.read %0;" ::"n"(PENDING) : "memory");
+    __syncwarp();
+}
+__device__ __forceinline__ void boxes_written() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); __syncwarp(); }
+__device__ __forceinline__ void send_box(uint32_t box, const CUtensorMap *map, uint32_t col, uint32_t row, int lane)
+{
+    if (lane == 0) {
+        asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.bulk_group [%0, {%1, %2}], [%3];" ::"l"(map), "r"(col), "r"(row), "r"(box) : "memory");
+        asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+    }
+}
+
+// Where Y, a and b go, as tensor maps (rows on 16-byte boundaries).
+struct Targets {
+    CUtensorMap y, a, b;
+};
+
+template <int CG, int BN, typename T, bool GATED, typename WAITS>
+__global__ void __launch_bounds__(Tile<CG, BN, GATED>::THREADS, 1)
+i8_tile_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_w, const __grid_constant__ Targets to, Result<T> o, uint32_t whole,
+               WAITS waits)
+{
+    using C = Tile<CG, BN, GATED>;
+    constexpr int NS = C::NSTAGES, TN = C::COLS, TM = 128 * CG;
+    constexpr uint32_t IDESC = instr_desc(TM, BN);
     extern __shared__ uint8_t smem_raw[];
     const uint32_t base = (saddr(smem_raw) + 1023u) & ~1023u;
     uint8_t *const base_ptr = smem_raw + (base - saddr(smem_raw));
@@ -261,56 +289,72 @@ i8_pair_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant_
     auto acc_empty = [&](int b) { return bars + 8u * (2 * NS + 2 + b); };
     const uint32_t drained = bars + 8u * (C::BARRIERS - 1), tmem_slot = bars + 8u * C::BARRIERS, gave_up = tmem_slot + 4u;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-    const uint32_t rank = cluster_cta_rank();                        // 0: the leader
+    const uint32_t rank = CG == 2 ? cluster_cta_rank() : 0u;         // 0: the leader
     const uint32_t ksteps = (o.K + BK - 1) / BK;
-    const uint32_t tiles_m = (o.M + 255) / 256, tiles_n = (o.N + TN - 1) / TN, ntiles = tiles_m * tiles_n;
-    const uint32_t pair = blockIdx.x >> 1, npairs = gridDim.x >> 1;
+    const uint32_t tiles_m = (o.M + TM - 1) / TM, tiles_n = (o.N + TN - 1) / TN, ntiles = tiles_m * tiles_n;
+    const uint32_t unit = blockIdx.x / CG, units = gridDim.x / CG;
+    auto commit = [&](uint32_t bar) {
+        if constexpr (CG == 2) umma_commit_pair(bar);
+        else umma_commit(bar);
+    };
 
     if (tid == 0) {
         for (int s = 0; s < NS; ++s) { mbar_init(full(s), 1); mbar_init(empty(s), 1); }
-        for (int b = 0; b < 2; ++b) { mbar_init(acc_full(b), 1); mbar_init(acc_empty(b), 2 * C::STORE_WARPS); }
+        for (int b = 0; b < 2; ++b) { mbar_init(acc_full(b), 1); mbar_init(acc_empty(b), CG * C::STORE_WARPS); }
         mbar_init(drained, 1);
         shared_word(gave_up, 0u);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     asm volatile("griddepcontrol.wait;" ::: "memory");
-    if (warp == 1) {          // the same warp of both CTAs takes the pair's tensor memory
-        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(tmem_slot), "r"((uint32_t)TMEM_COLS) : "memory");
-        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+    if (warp == 1) {          // with two CTAs the same warp of both takes the pair's tensor memory
+        if constexpr (CG == 2) {
+            asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(tmem_slot), "r"((uint32_t)C::TMEM_COLS) : "memory");
+            asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+        } else {
+            asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(tmem_slot), "r"((uint32_t)C::TMEM_COLS) : "memory");
+            asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+        }
     }
     fence_before();
     __syncthreads();
-    cluster_barrier();
+    if constexpr (CG == 2) cluster_barrier();
     fence_after();
     const uint32_t tmem_base = shared_word(tmem_slot);
 
     bool ok = true;
     if (tid == 0) {
         uint32_t it = 0;
-        for (uint32_t t = pair; t < ntiles && ok; t += npairs) {
+        for (uint32_t t = unit; t < ntiles && ok; t += units) {
             uint32_t tn, tm;
             tile_of(t, tiles_n, tiles_m, tn, tm);
-            const int xr = (int)(tm * 256 + rank * 128), wr = GATED ? (int)(tn * 128 + rank * o.N) : (int)(tn * 256 + rank * 128);
+            const int xr = (int)(tm * TM + rank * 128), wr = (int)(tn * TN + (CG == 2 ? rank * (GATED ? o.N : (uint32_t)C::W_ROWS) : 0u));
             for (uint32_t k = 0; k < ksteps; ++k, ++it) {
                 const int s = it % NS;
                 if (it >= (uint32_t)NS) ok = mbar_wait(empty(s), ((it / NS) - 1) & 1u, waits.polls);
                 if (!ok) break;
-                if (rank == 0) mbar_expect_tx(full(s), 2 * C::STAGE);          // the bytes of both CTAs
-                if (waits.missing(pair)) continue;
-                const uint32_t a = base + s * C::STAGE, lead_full = map_to_cta(full(s), 0u);
-                tma_load_2d_pair(a, &map_x, (int)(k * BK), xr, lead_full);
-                tma_load_2d_pair(a + TILE_BYTES, &map_w, (int)(k * BK), wr, lead_full);
+                if (rank == 0) mbar_expect_tx(full(s), CG * C::STAGE);          // the bytes of both CTAs
+                if (waits.missing(unit)) continue;
+                const uint32_t a = base + s * C::STAGE;
+                if constexpr (CG == 2) {
+                    const uint32_t lead_full = map_to_cta(full(s), 0u);
+                    tma_load_2d_pair(a, &map_x, (int)(k * BK), xr, lead_full);
+                    tma_load_2d_pair(a + TILE_BYTES, &map_w, (int)(k * BK), wr, lead_full);
+                } else {
+                    tma_load_2d(a, &map_x, (int)(k * BK), xr, full(s));
+                    tma_load_2d(a + TILE_BYTES, &map_w, (int)(k * BK), wr, full(s));
+                    if constexpr (GATED) tma_load_2d(a + TILE_BYTES + C::W_BOX * BK, &map_w, (int)(k * BK), wr + (int)o.N, full(s));
+                }
             }
         }
         if (rank == 0) copies_landed(it, NS, waits.held, full);
     } else if (tid == 32 && rank == 0) {
         uint32_t it = 0, lt = 0;
-        for (uint32_t t = pair; t < ntiles && ok; t += npairs, ++lt) {
+        for (uint32_t t = unit; t < ntiles && ok; t += units, ++lt) {
             const uint32_t buf = lt & 1u;
             if (lt >= 2) ok = mbar_wait(acc_empty(buf), ((lt >> 1) - 1) & 1u, waits.polls);
             if (!ok) break;
             fence_after();
-            const uint32_t d = tmem_base + buf * 256u;
+            const uint32_t d = tmem_base + buf * BN;
             for (uint32_t k = 0; k < ksteps; ++k, ++it) {
                 const int s = it % NS;
                 ok = mbar_wait_held(full(s), (it / NS) & 1u, waits.held);
@@ -318,55 +362,92 @@ i8_pair_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant_
                 fence_after();
                 const uint32_t a = base + s * C::STAGE, b = a + TILE_BYTES;
 #pragma unroll
-                for (int i = 0; i < BK / INSTR_K; ++i)
-                    mma_i8_pair(d, umma_desc(a + i * INSTR_K), umma_desc(b + i * INSTR_K), IDESC, (k | (uint32_t)i) != 0);
-                umma_commit_pair(empty(s));          // the stage goes back to both producers
+                for (int i = 0; i < BK / INSTR_K; ++i) {
+                    if constexpr (CG == 2) mma_i8_pair(d, umma_desc(a + i * INSTR_K), umma_desc(b + i * INSTR_K), IDESC, (k | (uint32_t)i) != 0);
+                    else mma_i8(d, umma_desc(a + i * INSTR_K), umma_desc(b + i * INSTR_K), IDESC, (k | (uint32_t)i) != 0);
+                }
+                commit(empty(s));          // the stage goes back to both producers
             }
-            if (ok) umma_commit_pair(acc_full(buf));
+            if (ok) commit(acc_full(buf));
         }
     } else if (warp >= 2) {
         const int q = warp & 3, half = (warp - 2) >> 2, mine = tid - 64;
-        uint32_t *const room = reinterpret_cast<uint32_t *>(base_ptr + NS * C::STAGE + C::SCALES) + (STAGED ? (warp - 2) * 32 * 17 : 0);
-        uint32_t lt = 0;
-        for (uint32_t t = pair; t < ntiles; t += npairs, ++lt) {
+        constexpr int PER_BOX = 64 / (int)sizeof(T);      // columns: 32 or 16
+        const uint32_t boxes = base + NS * C::STAGE + C::SCALES + (warp - 2) * C::BOXES * C::BOX;
+        uint32_t *const room = reinterpret_cast<uint32_t *>(base_ptr + NS * C::STAGE + C::SCALES + (warp - 2) * C::BOXES * C::BOX);
+        uint32_t lt = 0, box = 0;                          // the next box, of three in turn
+        // the store of a box clips at multiples of 16 bytes only: the last columns of other widths go out one by one
+        const bool ends_whole = o.N * sizeof(T) % 16 == 0;
+        auto boxed = [&](uint32_t col) { return whole && (ends_whole || col + PER_BOX <= o.N); };
+        for (uint32_t t = unit; t < ntiles; t += units, ++lt) {
             const uint32_t buf = lt & 1u;
             uint32_t tn, tm;
             tile_of(t, tiles_n, tiles_m, tn, tm);
             // the scales of the tile's rows of W, one a thread (a buffer is written again two tiles later: a barrier lies between)
-            const uint32_t w_row = GATED ? tn * 128 + (mine & 127) : tn * 256 + mine;
-            scales[buf * 256 + mine] = w_row < o.N ? o.w_scales[w_row + (GATED && mine >= 128 ? o.N : 0u)] : 0.f;
-            const uint32_t row0 = tm * 256 + rank * 128 + q * 32;
+            if (mine < BN) {
+                const uint32_t w_row = tn * TN + (GATED ? mine % TN : mine);
+                scales[buf * BN + mine] = w_row < o.N ? o.w_scales[w_row + (GATED && mine >= TN ? o.N : 0u)] : 0.f;
+            }
+            const uint32_t row0 = tm * TM + rank * 128 + q * 32;
             const i8::RowScale xs(row0 + lane < o.M ? o.x_scales[row0 + lane] : 0.f);
             const bool any_big = __any_sync(0xFFFFFFFFu, xs.big());
-            ok = together256(mbar_wait_held(acc_full(buf), (lt >> 1) & 1u, waits.results(pair)));
-            if (t + npairs >= ntiles) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+            ok = together256(mbar_wait_held(acc_full(buf), (lt >> 1) & 1u, waits.results(unit)));
+            if (t + units >= ntiles) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
             if (!ok) break;
             fence_after();
-            const uint32_t acc = tmem_base + buf * 256u + ((uint32_t)(q * 32) << 16);
-            const float4 *ws = reinterpret_cast<const float4 *>(scales + buf * 256);
+            const uint32_t acc = tmem_base + buf * BN + ((uint32_t)(q * 32) << 16);
+            const float4 *ws = reinterpret_cast<const float4 *>(scales + buf * BN);
             const uint32_t col0 = tn * TN;
+            const bool rows_here = row0 < o.M;             // of this warp
             if constexpr (GATED) {
 #pragma unroll 1
-                for (int c = half * 64; c < half * 64 + 64 && col0 + c < o.N; c += 16) {
+                for (int c = half * (TN / 2); c < (half + 1) * (TN / 2) && col0 + c < o.N; c += 16) {
                     uint32_t v[16], u[16];
                     tmem_load16(acc + c, v);
-                    tmem_load16(acc + 128 + c, u);
+                    tmem_load16(acc + TN + c, u);
                     tmem_wait();
                     loaded16(v);
                     loaded16(u);
                     float a[16], b[16], y[16];
                     values16(v, xs, any_big, ws + c / 4, a);
-                    values16(u, xs, any_big, ws + 32 + c / 4, b);
-                    if (o.pre) {
-                        store16<T, STAGED>(a, o.pre, o.ld_pre, row0, o.M, col0 + c, o.N, lane, room);
-                        store16<T, STAGED>(b, o.pre + o.N, o.ld_pre, row0, o.M, col0 + c, o.N, lane, room);
-                    }
+                    values16(u, xs, any_big, ws + TN / 4 + c / 4, b);
                     gate16(o.act, a, b, y);
-                    store16<T, STAGED>(y, o.y, o.ldy, row0, o.M, col0 + c, o.N, lane, room);
+                    const int in_box = c % PER_BOX, piece = in_box * (int)sizeof(T) / 16;
+                    if (boxed(col0 + c - in_box)) {
+                        const uint32_t y_box = boxes + box * C::BOX;
+                        if (in_box == 0) {
+                            if (o.pre) boxes_free<0>(lane);
+                            else boxes_free<C::BOXES - 1>(lane);
+                        }
+                        box16<T>(y_box, piece, y, lane);
+                        if (o.pre) {
+                            box16<T>(boxes + C::BOX, piece, a, lane);
+                            box16<T>(boxes + 2 * C::BOX, piece, b, lane);
+                        }
+                        if (in_box + 16 == PER_BOX || c + 16 == (half + 1) * (TN / 2) || col0 + c + 16 >= o.N) {
+                            boxes_written();
+                            if (rows_here) {
+                                const uint32_t col = col0 + c - in_box;
+                                send_box(y_box, &to.y, col, row0, lane);
+                                if (o.pre) {
+                                    send_box(boxes + C::BOX, &to.a, col, row0, lane);
+                                    send_box(boxes + 2 * C::BOX, &to.b, col, row0, lane);
+                                }
+                            }
+                            if (!o.pre) box = box == C::BOXES - 1 ? 0 : box + 1;
+                        }
+                    } else {
+                        boxes_free<0>(lane);
+                        if (o.pre) {
+                            store16<T>(a, o.pre, o.ld_pre, row0, o.M, col0 + c, o.N, lane, room);
+                            store16<T>(b, o.pre + o.N, o.ld_pre, row0, o.M, col0 + c, o.N, lane, room);
+                        }
+                        store16<T>(y, o.y, o.ldy, row0, o.M, col0 + c, o.N, lane, room);
+                    }
                 }
             } else {
 #pragma unroll 1
-                for (int c = half * 128; c < half * 128 + 128 && col0 + c < o.N; c += 32) {
+                for (int c = half * (TN / 2); c < (half + 1) * (TN / 2) && col0 + c < o.N; c += 32) {
                     uint32_t v[32];
                     tmem_load16(acc + c, v);
                     tmem_load16(acc + c + 16, v + 16);
@@ -376,27 +457,49 @@ i8_pair_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant_
                     float f[32];
                     values16(v, xs, any_big, ws + c / 4, f);
                     values16(v + 16, xs, any_big, ws + c / 4 + 4, f + 16);
-                    store16<T, STAGED>(f, o.y, o.ldy, row0, o.M, col0 + c, o.N, lane, room);
-                    store16<T, STAGED>(f + 16, o.y, o.ldy, row0, o.M, col0 + c + 16, o.N, lane, room);
+#pragma unroll
+                    for (int part = 0; part < 32 / PER_BOX; ++part) {
+                        const uint32_t col = col0 + c + part * PER_BOX, here = boxes + box * C::BOX;
+                        if (col >= o.N) break;
+                        if (boxed(col)) {
+                            boxes_free<C::BOXES - 1>(lane);
+#pragma unroll
+                            for (int i = 0; i < PER_BOX; i += 16) box16<T>(here, i * (int)sizeof(T) / 16, f + part * PER_BOX + i, lane);
+                            boxes_written();
+                            if (rows_here) send_box(here, &to.y, col, row0, lane);
+                            box = box == C::BOXES - 1 ? 0 : box + 1;
+                        } else {
+                            boxes_free<0>(lane);
+#pragma unroll
+                            for (int i = 0; i < PER_BOX; i += 16) store16<T>(f + part * PER_BOX + i, o.y, o.ldy, row0, o.M, col + i, o.N, lane, room);
+                        }
+                    }
                 }
             }
             fence_before();
             __syncwarp();
-            if (lane == 0) arrive_at(map_to_cta(acc_empty(buf), 0u));
+            if (lane == 0) {
+                if constexpr (CG == 2) arrive_at(map_to_cta(acc_empty(buf), 0u));
+                else mbar_arrive(acc_empty(buf));
+            }
         }
+        if (lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
+        __syncwarp();
     }
     if (!ok) give_up(o.status, gave_up);
     fence_before();
     __syncthreads();
     // what was issued has finished, whichever thread's wait ran out (if none of the leader's did, its results were all waited for)
     if (tid == 32 && rank == 0 && shared_word(gave_up)) {
-        umma_commit_pair(drained);
+        commit(drained);
         mbar_wait_held(drained, 0u, HELD_LIMIT);
     }
     __syncthreads();
-    cluster_barrier();                     // neither CTA ends or lets go of tensor memory while the other may still signal it
-    if (warp == 1)
-        asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"((uint32_t)TMEM_COLS) : "memory");
+    if constexpr (CG == 2) cluster_barrier();          // neither CTA ends or lets go of tensor memory while the other may still signal it
+    if (warp == 1) {
+        if constexpr (CG == 2) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"((uint32_t)C::TMEM_COLS) : "memory");
+        else asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"((uint32_t)C::TMEM_COLS) : "memory");
+    }
 }
 
 // ---- few rows of X or few tiles ------------------------------------------------------------------------
@@ -756,12 +859,12 @@ i8_rows_kernel(SOURCE source, const int8_t *w_codes, const float *w_scales, void
 }
 
 // ---- launches ------------------------------------------------------------------------------------------------
-// Codes as bytes: boxes of box_rows rows x 128 bytes, 128-byte swizzle, zeros outside the matrix (whatever pads its rows).
+// Codes as bytes, the zeros that pad the rows included: boxes of box_rows rows x 128 bytes, 128-byte swizzle, zeros outside.
 bool make_codes_map(CUtensorMap *m, const void *ptr, uint64_t rows, uint64_t cols, uint32_t box_rows)
 {
     EncodeTiledFn fn = encode_fn();
     if (!fn) return false;
-    const cuuint64_t dims[2] = {cols, rows};
+    const cuuint64_t dims[2] = {i8::row_bytes(cols), rows};
     const cuuint64_t strides[1] = {i8::row_bytes(cols)};
     const cuuint32_t box[2] = {BK, box_rows};
     const cuuint32_t elem[2] = {1, 1};
@@ -802,17 +905,44 @@ Result<T> result_of(const Product &p)
     return {p.x_scales, p.w_scales, static_cast<T *>(p.y), static_cast<T *>(p.pre), p.ldy, p.ld_pre, p.M, p.N, p.K, p.act, p.status};
 }
 
-template <typename T, bool GATED, bool STAGED, typename WAITS>
-int launch_pairs(const Product &p, WAITS waits)
+// A result matrix, boxes of 32 rows x 64 bytes, 64-byte swizzle.
+template <typename T>
+bool make_result_map(CUtensorMap *m, T *p, uint64_t rows, uint64_t cols, uint64_t ld)
 {
-    using C = Pair<STAGED>;
+    EncodeTiledFn fn = encode_fn();
+    if (!fn) return false;
+    const cuuint64_t dims[2] = {cols, rows};
+    const cuuint64_t strides[1] = {ld * sizeof(T)};
+    const cuuint32_t box[2] = {64 / (uint32_t)sizeof(T), 32};
+    const cuuint32_t elem[2] = {1, 1};
+    const CUtensorMapDataType type = sizeof(T) == 4 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_UINT16;
+    return fn(m, type, 2, p, dims, strides, box, elem, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_NONE,
+              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+// Whether rows start on 16-byte boundaries, and `second` values on from there.
+template <typename T>
+bool whole_rows(const T *p, uint64_t ld, uint64_t second)
+{
+    return ((uint64_t)reinterpret_cast<uintptr_t>(p) | ld * sizeof(T) | second * sizeof(T)) % 16 == 0;
+}
+
+template <int CG, int BN, typename T, bool GATED, typename WAITS>
+int launch_tiles(const Product &p, WAITS waits)
+{
+    using C = Tile<CG, BN, GATED>;
     CUtensorMap map_x, map_w;
-    if (!make_codes_map(&map_x, p.x_codes, p.M, p.K, 128) || !make_codes_map(&map_w, p.w_codes, p.w_rows(), p.K, 128)) return OMC_ERR_CUDA;
-    if (const int rc = el::allow_smem<i8_pair_kernel<T, GATED, STAGED, WAITS>>(C::SMEM)) return rc;
-    const uint64_t tiles = (uint64_t)((p.M + 255) / 256) * ((p.N + (GATED ? 127 : 255)) / (GATED ? 128 : 256)), pairs = el::sm_count() > 2 ? el::sm_count() / 2 : 1;
+    if (!make_codes_map(&map_x, p.x_codes, p.M, p.K, 128) || !make_codes_map(&map_w, p.w_codes, p.w_rows(), p.K, C::W_BOX)) return OMC_ERR_CUDA;
+    if (const int rc = el::allow_smem<i8_tile_kernel<CG, BN, T, GATED, WAITS>>(C::SMEM)) return rc;
+    const uint64_t tiles = (uint64_t)((p.M + 128 * CG - 1) / (128 * CG)) * ((p.N + C::COLS - 1) / C::COLS), units = el::sm_count() > CG ? el::sm_count() / CG : 1;
     if (tiles >= (1ull << 31)) return OMC_ERR_INVALID_ARG;
-    return note_cuda(el::launch(i8_pair_kernel<T, GATED, STAGED, WAITS>, dim3(2 * (uint32_t)(tiles < pairs ? tiles : pairs)), C::THREADS, C::SMEM, 2, p.stream,
-                                map_x, map_w, result_of<T>(p), waits));
+    const Result<T> r = result_of<T>(p);
+    Targets to = {};
+    // (a tensor map's pitch is below 2^40 bytes)
+    const bool whole = whole_rows(r.y, r.ldy, 0) && r.ldy < (1ull << 37) && (!r.pre || (whole_rows(r.pre, r.ld_pre, p.N) && r.ld_pre < (1ull << 37)));
+    if (whole && !make_result_map(&to.y, r.y, p.M, p.N, r.ldy)) return OMC_ERR_CUDA;
+    if (whole && r.pre && (!make_result_map(&to.a, r.pre, p.M, p.N, r.ld_pre) || !make_result_map(&to.b, r.pre + p.N, p.M, p.N, r.ld_pre))) return OMC_ERR_CUDA;
+    return note_cuda(el::launch(i8_tile_kernel<CG, BN, T, GATED, WAITS>, dim3(CG * (uint32_t)(tiles < units ? tiles : units)), C::THREADS, C::SMEM, CG, p.stream,
+                                map_x, map_w, to, r, (uint32_t)whole, waits));
 }
 
 template <int NT, typename T, bool GATED, typename WAITS>
@@ -832,17 +962,14 @@ template <typename T, bool GATED, typename WAITS>
 int launch_any(const Product &p, WAITS waits)
 {
     const i8::Schedule s = i8::schedule_of(p.M, p.N, p.K, GATED);
-    const uint64_t size = sizeof(T);
-    // rows of Y (and of what is kept, whose second half starts N values on) on 16-byte boundaries
-    const bool whole = el::aligned16(p.y) && p.ldy * size % 16 == 0 && (!p.pre || (el::aligned16(p.pre) && p.ld_pre * size % 16 == 0 && p.N * size % 16 == 0));
-    switch (s.tile) {
-    case 16: return launch_small<16, T, GATED>(p, s.splits, waits);
-    case 32: return launch_small<32, T, GATED>(p, s.splits, waits);
-    case 64: return launch_small<64, T, GATED>(p, s.splits, waits);
-    case 128:
-        if constexpr (!GATED) return launch_small<128, T, GATED>(p, s.splits, waits);
+    switch (s.kernel) {
+    case i8::PAIR_256: return launch_tiles<2, 256, T, GATED>(p, waits);
+    case i8::PAIR_128: return launch_tiles<2, 128, T, GATED>(p, waits);
+    case i8::ONE_128: return launch_tiles<1, 128, T, GATED>(p, waits);
+    case i8::SMALL_16: return launch_small<16, T, GATED>(p, s.splits, waits);
+    case i8::SMALL_32: return launch_small<32, T, GATED>(p, s.splits, waits);
+    default: return launch_small<64, T, GATED>(p, s.splits, waits);
     }
-    return whole ? launch_pairs<T, GATED, false>(p, waits) : launch_pairs<T, GATED, true>(p, waits);
 }
 
 template <int MT, bool GATED, typename SOURCE>
