@@ -16,31 +16,32 @@ using el::Word;
 template <typename T_, bool WHOLE, int ACT>
 struct Gradients {
     using T = T_;
-    static constexpr int OUT = 2, HEAVY = 1;
+    static constexpr int OUT = 2, HEAVY = WHOLE ? 1 : 2;
     static constexpr bool WHOLE_ROWS = WHOLE;
     const T *dy, *pre;
     T *dpre;                  // NULL: not wanted
     uint64_t ld_dy, ld_pre, ld_dpre;
-    uint32_t width;
-    i8::Span span_dy, span_pre;
+    uint32_t rows, width;
     struct Raw {
         i8::Piece<T, WHOLE> g, a, b;
     };
+    template <bool FULL>
     __device__ __forceinline__ void fetch(uint32_t row, uint32_t col, uint32_t cols, Raw &raw) const
     {
+        const bool in = FULL || i8::inside<T>(row, rows, col, cols);
         const T *const p = pre + row * ld_pre + col;
-        raw.g.load(dy + row * ld_dy + col, cols - col, span_dy);
-        raw.a.load(p, cols - col, span_pre);
-        raw.b.load(p + width, cols - col, span_pre);
+        raw.g.load(dy + row * ld_dy + col, in);
+        raw.a.load(p, in);
+        raw.b.load(p + width, in);
     }
     __device__ __forceinline__ void fetch4(uint32_t row, uint32_t col, Raw *raw) const
     {
         const T *p = dy + row * ld_dy + col, *q = pre + row * ld_pre + col;
 #pragma unroll
         for (int i = 0; i < 4; ++i, p += ld_dy, q += ld_pre) {
-            raw[i].g.a = *reinterpret_cast<const uint4 *>(p);
-            raw[i].a.a = *reinterpret_cast<const uint4 *>(q);
-            raw[i].b.a = *reinterpret_cast<const uint4 *>(q + width);
+            raw[i].g.load(p, true);
+            raw[i].a.load(q, true);
+            raw[i].b.load(q + width, true);
         }
     }
     static __device__ __forceinline__ void make_with(const uint32_t *gs, const uint32_t *as, const uint32_t *bs, uint32_t (*out)[4])
@@ -66,13 +67,15 @@ struct Gradients {
             }
         }
     }
+    template <bool FULL>
     __device__ __forceinline__ void make(uint32_t row, uint32_t col, uint32_t cols, const Raw &raw, uint32_t (*out)[4]) const
     {
         uint32_t g[4], a[4], b[4];
+        const bool in = FULL || i8::inside<T>(row, rows, col, cols);
         const T *const p = pre + row * ld_pre + col;
-        raw.g.words(dy + row * ld_dy + col, cols - col, span_dy, g);
-        raw.a.words(p, cols - col, span_pre, a);
-        raw.b.words(p + width, cols - col, span_pre, b);
+        raw.g.words(dy + row * ld_dy + col, cols - col, in, g);
+        raw.a.words(p, cols - col, in, a);
+        raw.b.words(p + width, cols - col, in, b);
         make_with(g, a, b, out);
     }
     __device__ __forceinline__ void emit(uint32_t row, uint32_t col, uint32_t cols, const uint32_t (*w)[4]) const
@@ -115,8 +118,7 @@ template <typename T, bool WHOLE, int ACT>
 int backward(const Backward &c)
 {
     const T *const g = static_cast<const T *>(c.dy), *const p = static_cast<const T *>(c.pre);
-    const Gradients<T, WHOLE, ACT> src = {g, p, static_cast<T *>(c.dpre), c.ld_dy, c.ld_pre, c.ld_dpre, c.width, i8::span_of(g, c.ld_dy, c.rows, c.width),
-                                          i8::span_of(p, c.ld_pre, c.rows, 2ull * c.width)};
+    const Gradients<T, WHOLE, ACT> src = {g, p, static_cast<T *>(c.dpre), c.ld_dy, c.ld_pre, c.ld_dpre, c.rows, c.width};
     return i8::quantise<2>(src, c.rows, c.width, c.codes, c.scales, c.codes_t, c.scales_t, c.workspace, c.stream);
 }
 template <int ACT>

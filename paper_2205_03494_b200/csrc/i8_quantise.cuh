@@ -29,13 +29,16 @@ template <typename T> constexpr int PIECE = 16 / (int)sizeof(T);               /
 template <typename T> constexpr uint32_t MAGNITUDE = sizeof(T) == 4 ? 0x7FFFFFFFu : 0x7FFF7FFFu;
 constexpr int ROW_THREADS = 512;                                               // of the widest group that shares a row
 constexpr int MAXIMA_WARPS = 8, MAXIMA_CTAS = DEFAULT_SMS * 3;                 // of the first kernel: warps of a CTA, CTAs
-constexpr int STRIP_THREADS = 256;                                             // of the second kernel
+constexpr int STRIP_THREADS = 128;                                             // of the second kernel
 
 // Pieces of a warp's window of columns in the first kernel, and CTAs that share a window's rows: their sets of maxima.
 template <int OUT> constexpr int WINDOW_PIECES = OUT == 1 ? 4 : 2;
 inline uint64_t shares_of(uint64_t rows, uint64_t windows)
 {
-    const uint64_t most = windows < (uint64_t)MAXIMA_CTAS ? MAXIMA_CTAS / windows : 1, all = (rows + MAXIMA_WARPS - 1) / MAXIMA_WARPS;
+    // (every CTA of the second kernel reads all sets: of narrow matrices there are as many as SMs and no more)
+    uint64_t most = windows < (uint64_t)MAXIMA_CTAS ? MAXIMA_CTAS / windows : 1;
+    if (most > DEFAULT_SMS) most = DEFAULT_SMS;
+    const uint64_t all = (rows + MAXIMA_WARPS - 1) / MAXIMA_WARPS;
     return all < most ? all : most;
 }
 // Bytes of the sets of `cols` columns' maxima and of the rows' maxima in the windows, of any type: widest words, fewest and most windows.
@@ -45,41 +48,24 @@ inline uint64_t maxima_bytes(uint64_t rows, uint64_t cols, int out)
     return (sets + 15) / 16 * 16 + windows * ((rows + 3) / 4 * 4) * 4;
 }
 
-// A matrix's bytes: its first, and behind its last.
-struct Span {
-    uintptr_t first, last;
-};
-template <typename T>
-Span span_of(const T *x, uint64_t ld, uint64_t rows, uint64_t cols)
-{
-    return {reinterpret_cast<uintptr_t>(x), reinterpret_cast<uintptr_t>(x + (rows - 1) * ld + cols)};
-}
-
-// A piece on its way.  WHOLE, rows on 16-byte boundaries and a multiple of 16 bytes wide: its four words.  Else the two aligned sixteens that hold it, which
-// `words` shifts, where all bytes of both lie between the matrix's first and last ones; the other pieces, and those cut off by the row's end, `words`
-// reads value by value.  (Loads are predicated, never one side of a branch: where registers meet after a branch the compiler copies them, which waits for
-// the load.  8192 x 8192 BF16, first kernel, 44 us with a branch.)
+// A piece on its way.  WHOLE, rows on 16-byte boundaries and a multiple of 16 bytes wide: its four words.  Else, of a piece that is `inside`, the two aligned
+// sixteens that hold it, which `words` shifts; the others `words` reads value by value.  (Loads are predicated, never one side of a branch: where registers
+// meet after a branch the compiler copies them, which waits for the load.  8192 x 8192 BF16, first kernel, 44 us with a branch, 31 us without.)
 template <typename T, bool WHOLE>
 struct Piece {
     static constexpr int E = PIECE<T>;
     uint4 a, b;
-    static __device__ __forceinline__ bool shifted(const T *at, uint32_t left, const Span &span)
-    {
-        const uintptr_t low = reinterpret_cast<uintptr_t>(at) & ~(uintptr_t)15;
-        return left >= (uint32_t)E && low >= span.first && low + 32 <= span.last;
-    }
-    // From `at` on, `left` values of the row.
-    __device__ __forceinline__ void load(const T *at, uint32_t left, const Span &span)
+    __device__ __forceinline__ void load(const T *at, bool inside)
     {
         if constexpr (WHOLE) {
             a = *reinterpret_cast<const uint4 *>(at);
-        } else if (shifted(at, left, span)) {
+        } else if (inside) {
             const uint4 *low = reinterpret_cast<const uint4 *>(reinterpret_cast<uintptr_t>(at) & ~(uintptr_t)15);
             a = low[0];
             b = low[1];
         }
     }
-    __device__ __forceinline__ void words(const T *at, uint32_t left, const Span &span, uint32_t *out) const
+    __device__ __forceinline__ void words(const T *at, uint32_t left, bool inside, uint32_t *out) const
     {
         if constexpr (WHOLE) {
             out[0] = a.x, out[1] = a.y, out[2] = a.z, out[3] = a.w;
@@ -92,10 +78,17 @@ struct Piece {
             for (int i = 0; i < 5; ++i) u[i] = skip & 4 ? v[i + 1] : v[i];
 #pragma unroll
             for (int i = 0; i < 4; ++i) out[i] = sizeof(T) == 4 ? u[i] : __funnelshift_r(u[i], u[i + 1], (skip & 2) * 8);
-            if (!shifted(at, left, span)) mx::load<T, false, E>(at, 0, left, out);
+            if (!inside) mx::load<T, false, E>(at, 0, left, out);
         }
     }
 };
+// Whether the two aligned sixteens around a piece lie inside its matrix: a whole piece of any row but the first and the last, of rows of 32 bytes
+// at least (the first begins in the row before it at the earliest, the second ends in the row behind it at the latest).
+template <typename T>
+__device__ __forceinline__ bool inside(uint32_t row, uint32_t rows, uint32_t col, uint32_t cols)
+{
+    return row - 1u < rows - 2u && rows > 2u && col + PIECE<T> <= cols && cols >= 2 * PIECE<T>;
+}
 
 // A matrix in memory.
 template <typename T_, bool WHOLE>
@@ -105,22 +98,28 @@ struct Matrix {
     static constexpr bool WHOLE_ROWS = WHOLE;
     const T *x;
     uint64_t ld;
-    Span span;
+    uint32_t rows;
     struct Raw {
         Piece<T, WHOLE> x;
     };
-    __device__ __forceinline__ void fetch(uint32_t row, uint32_t col, uint32_t cols, Raw &raw) const { raw.x.load(x + row * ld + col, cols - col, span); }
-    // Four rows' pieces from one address on (whole pieces of whole rows).
+    // FULL: the place is known to be inside.
+    template <bool FULL>
+    __device__ __forceinline__ void fetch(uint32_t row, uint32_t col, uint32_t cols, Raw &raw) const
+    {
+        raw.x.load(x + row * ld + col, FULL || inside<T>(row, rows, col, cols));
+    }
+    // Four rows' pieces from one address on, all inside.
     __device__ __forceinline__ void fetch4(uint32_t row, uint32_t col, Raw *raw) const
     {
         const T *p = x + row * ld + col;
 #pragma unroll
-        for (int i = 0; i < 4; ++i, p += ld) raw[i].x.a = *reinterpret_cast<const uint4 *>(p);
+        for (int i = 0; i < 4; ++i, p += ld) raw[i].x.load(p, true);
     }
     // Of a place that was fetched.
+    template <bool FULL>
     __device__ __forceinline__ void make(uint32_t row, uint32_t col, uint32_t cols, const Raw &raw, uint32_t (*out)[4]) const
     {
-        raw.x.words(x + row * ld + col, cols - col, span, out[0]);
+        raw.x.words(x + row * ld + col, cols - col, FULL || inside<T>(row, rows, col, cols), out[0]);
     }
     __device__ __forceinline__ void emit(uint32_t, uint32_t, uint32_t, const uint32_t (*)[4]) const {}
 };
@@ -212,7 +211,7 @@ __global__ void __launch_bounds__(THREADS, ROWS_CTAS<SRC, P, THREADS>) rows_kern
     auto fetch = [&](uint32_t row, typename SRC::Raw *r) {
 #pragma unroll
         for (int p = 0; p < P; ++p)
-            if (row < rows && column(p) < cols) src.fetch(row, column(p), cols, r[p]);
+            if (row < rows && column(p) < cols) src.template fetch<false>(row, column(p), cols, r[p]);
     };
     const uint32_t step = place.shares * together;
     uint32_t base = place.share() * together, turn = 0;
@@ -227,7 +226,7 @@ __global__ void __launch_bounds__(THREADS, ROWS_CTAS<SRC, P, THREADS>) rows_kern
 #pragma unroll
             for (int p = 0; p < P; ++p) {
                 if (row < rows && column(p) < cols) {
-                    src.make(row, column(p), cols, raw[a][p], w[p]);
+                    src.template make<false>(row, column(p), cols, raw[a][p], w[p]);
                     src.emit(row, column(p), cols, w[p]);
                 } else {
 #pragma unroll
@@ -279,8 +278,8 @@ __global__ void __launch_bounds__(WIDE_THREADS) wide_rows_kernel(SRC src, uint32
         typename SRC::Raw raw;
         uint32_t w[OUT][4], top = 0u;
         for (uint32_t col = threadIdx.x * E; col < cols; col += WIDE_THREADS * E) {
-            src.fetch(row, col, cols, raw);
-            src.make(row, col, cols, raw, w);
+            src.template fetch<false>(row, col, cols, raw);
+            src.template make<false>(row, col, cols, raw, w);
             src.emit(row, col, cols, w);
 #pragma unroll
             for (int i = 0; i < OUT * 4; ++i) top = max_magnitude<T>(top, w[i / 4][i % 4] & MAGNITUDE<T>);
@@ -292,8 +291,8 @@ __global__ void __launch_bounds__(WIDE_THREADS) wide_rows_kernel(SRC src, uint32
         const Scale s = scale_of(top);
         int8_t *to = out.codes + row * out.pitch;
         for (uint32_t col = threadIdx.x * E; col < cols; col += WIDE_THREADS * E) {
-            src.fetch(row, col, cols, raw);
-            src.make(row, col, cols, raw, w);
+            src.template fetch<false>(row, col, cols, raw);
+            src.template make<false>(row, col, cols, raw, w);
 #pragma unroll
             for (int o = 0; o < OUT; ++o) {
                 uint32_t c[E / 4];
@@ -331,7 +330,7 @@ __global__ void __launch_bounds__(32 * MAXIMA_WARPS, SRC::HEAVY ? 2 : 3) maxima_
     auto fetch = [&](uint32_t row, typename SRC::Raw *r) {
 #pragma unroll
         for (int p = 0; p < P; ++p)
-            if (row < rows && column(p) < cols) src.fetch(row, column(p), cols, r[p]);
+            if (row < rows && column(p) < cols) src.template fetch<false>(row, column(p), cols, r[p]);
     };
 #pragma unroll
     for (int i = 0; i < P * OUT * 4; ++i) most[i / (OUT * 4)][i / 4 % OUT][i % 4] = 0u;
@@ -348,7 +347,7 @@ __global__ void __launch_bounds__(32 * MAXIMA_WARPS, SRC::HEAVY ? 2 : 3) maxima_
             for (int p = 0; p < P; ++p) {
                 if (column(p) < cols) {
                     uint32_t w[OUT][4];
-                    src.make(row, column(p), cols, raw[a][p], w);
+                    src.template make<false>(row, column(p), cols, raw[a][p], w);
                     src.emit(row, column(p), cols, w);
 #pragma unroll
                     for (int i = 0; i < OUT * 4; ++i) {
@@ -392,13 +391,14 @@ struct ColsOut {
     uint64_t pitch;
 };
 
-// Second kernel: blockIdx.x is a strip of sixteen pieces of columns and a share of the row tiles, the last ones first.  The next tile's loads are
-// on their way while a tile's codes go to memory.
+// Second kernel: blockIdx.x is a strip of sixteen pieces of columns and a share of the row tiles, the last ones first.  A thread takes four rows of a
+// piece at a time, a CTA a sweep of 32 rows; the loads of the next sweeps are on their way.
 template <typename SRC>
 struct Strip {
-    static constexpr int E = PIECE<typename SRC::T>, COLS = 16 * E, SWEEPS = SRC::OUT == 1 ? 2 : 1;     // 128 or 64 columns; loads of 64 rows at a time
-    static constexpr int ROWS = 64 * SWEEPS, WORDS = ROWS / 4;                                         // of a tile; of a column of its codes
-    static constexpr int CTAS = SRC::OUT == 1 && !SRC::HEAVY ? 3 : 2;                                  // on an SM, as the registers allow
+    static constexpr int E = PIECE<typename SRC::T>, COLS = 16 * E, SWEEPS = SRC::OUT == 1 ? 4 : 2;     // 128 or 64 columns; sweeps of a tile
+    static constexpr int AHEAD = SRC::OUT == 1 && !SRC::HEAVY ? 2 : 1;
+    static constexpr int ROWS = 32 * SWEEPS, WORDS = ROWS / 4;                                         // of a tile; of a column of its codes
+    static constexpr int CTAS = SRC::OUT == 1 ? (SRC::HEAVY ? 4 : 5) : SRC::HEAVY == 2 ? 2 : 3;        // on an SM, as the registers allow
     static constexpr int WORDS_ALL = SRC::OUT * COLS * WORDS;
     // Column e of piece p is column e 16 + p of the tile in shared memory.  Its words are turned by the piece (an even number), so that a warp's
     // stores, sixteen pieces of two words each, fall into different banks.
@@ -410,7 +410,8 @@ __global__ void __launch_bounds__(STRIP_THREADS, Strip<SRC>::CTAS) codes_kernel(
 {
     using T = typename SRC::T;
     using S = Strip<SRC>;
-    constexpr int E = S::E, OUT = SRC::OUT, COLS = S::COLS, WORDS = S::WORDS, SWEEPS = S::SWEEPS;
+    constexpr int E = S::E, OUT = SRC::OUT, COLS = S::COLS, WORDS = S::WORDS, SWEEPS = S::SWEEPS, AHEAD = S::AHEAD, DOWN = STRIP_THREADS / 16;
+    static_assert(DOWN * 4 == 32 && S::ROWS <= STRIP_THREADS, "");
     __shared__ __align__(16) uint32_t tiles_smem[2 * S::WORDS_ALL];            // two tiles, in turn: one barrier a tile
     __shared__ __align__(16) float factor[OUT * COLS], row_factor[2][ROWS ? S::ROWS : 4];
     __shared__ uint32_t any_nan, nan_rows[2];
@@ -421,18 +422,21 @@ __global__ void __launch_bounds__(STRIP_THREADS, Strip<SRC>::CTAS) codes_kernel(
     if (tid == 0) any_nan = nan_rows[0] = nan_rows[1] = 0u;
     __syncthreads();
     el::enter_stream_order();
-    typename SRC::Raw raw[SWEEPS * 4];
-    auto row_of = [&](uint32_t t, int k) { return t * S::ROWS + k / 4 * 64 + down * 4 + k % 4; };
+    typename SRC::Raw raw[AHEAD][4];
+    auto row_of = [&](uint32_t t, int k) { return t * S::ROWS + k * 32 + down * 4; };      // the first of four, in sweep k of tile t
     const bool whole_strip = (strip + 1) * COLS <= cols;
-    auto fetch = [&](uint32_t t) {
-        if (SRC::WHOLE_ROWS && whole_strip && (t + 1) * S::ROWS <= rows) {
+    // a tile that lies inside the matrix, where nothing needs a check (rows that start anywhere: off its first and last row)
+    auto full = [&](uint32_t t) {
+        return whole_strip && (SRC::WHOLE_ROWS ? (t + 1) * S::ROWS <= rows : t > 0 && (t + 1) * S::ROWS < rows && cols >= 2 * E);
+    };
+    auto fetch = [&](uint32_t t, int k, typename SRC::Raw *r) {
+        if (full(t)) {
+            src.fetch4(row_of(t, k), col, r);
+        } else {
 #pragma unroll
-            for (int k = 0; k < SWEEPS; ++k) src.fetch4(row_of(t, k * 4), col, raw + k * 4);
-            return;
+            for (int i = 0; i < 4; ++i)
+                if (row_of(t, k) + i < rows && col < cols) src.template fetch<false>(row_of(t, k) + i, col, cols, r[i]);
         }
-#pragma unroll
-        for (int k = 0; k < SWEEPS * 4; ++k)
-            if (row_of(t, k) < rows && col < cols) src.fetch(row_of(t, k), col, cols, raw[k]);
     };
     auto rows_of = [&](uint32_t t) {                               // a tile's rows' factors, a row a thread; the first strip stores the scales
         if constexpr (ROWS) {
@@ -447,11 +451,12 @@ __global__ void __launch_bounds__(STRIP_THREADS, Strip<SRC>::CTAS) codes_kernel(
             }
         }
     };
-    fetch(end - 1);
+#pragma unroll
+    for (int k = 0; k < AHEAD; ++k) fetch(end - 1, k, raw[k]);
     rows_of(end - 1);
-    // the strip's magnitudes: sixteen threads share the sets of a piece, and join what they found in shared memory
+    // the strip's magnitudes: eight threads share the sets of a piece, and join what they found in shared memory
     const uint32_t pieces = (cols + E - 1) / E;
-    uint4 *const found = reinterpret_cast<uint4 *>(tiles_smem);    // [16][16]
+    uint4 *const found = reinterpret_cast<uint4 *>(tiles_smem);    // [8][16]
 #pragma unroll
     for (int o = 0; o < OUT; ++o) {
         uint4 m = make_uint4(0u, 0u, 0u, 0u);
@@ -461,12 +466,12 @@ __global__ void __launch_bounds__(STRIP_THREADS, Strip<SRC>::CTAS) codes_kernel(
         };
         if (col < cols)
 #pragma unroll 4
-            for (uint32_t i = down; i < in.sets; i += 16) join(in.cols[((uint64_t)i * OUT + o) * pieces + col / E]);
+            for (uint32_t i = down; i < in.sets; i += DOWN) join(in.cols[((uint64_t)i * OUT + o) * pieces + col / E]);
         __syncthreads();
         found[tid] = m;
         __syncthreads();
         if (down == 0) {
-            for (int i = 1; i < 16; ++i) join(found[i * 16 + piece]);
+            for (int i = 1; i < DOWN; ++i) join(found[i * 16 + piece]);
             const uint32_t w[4] = {m.x, m.y, m.z, m.w};
 #pragma unroll
             for (int e = 0; e < E; ++e) {
@@ -480,17 +485,16 @@ __global__ void __launch_bounds__(STRIP_THREADS, Strip<SRC>::CTAS) codes_kernel(
     }
     __syncthreads();
     const bool masked = any_nan != 0u;
-
     // what a thread brings from the tile to memory: chunk `chunk` of columns STEP places apart, which are STEP / 16 columns of its piece p apart
     constexpr int CHUNKS = WORDS / 4, STEP = STRIP_THREADS / CHUNKS;
     const uint32_t chunk = tid % CHUNKS, slot = tid / CHUNKS, p_out = slot % 16, turned = S::turned(p_out), first_col = strip * COLS + p_out * E + slot / 16;
     int8_t *const to_cols = out.codes + (uint64_t)first_col * out.pitch + chunk * 16;
+
     for (uint32_t t = end; t-- > begin;) {
         uint32_t *const tile = tiles_smem + (t & 1u) * S::WORDS_ALL;
         const bool masked_rows = ROWS && nan_rows[t & 1u] == t + 1;
-        // FULL: the tile lies inside the matrix, nothing needs a check
-        auto work = [&](auto full) {
-            constexpr bool FULL = decltype(full)::value;
+        auto work = [&](auto inside_all) {
+            constexpr bool FULL = decltype(inside_all)::value;
 #pragma unroll
             for (int k = 0; k < SWEEPS; ++k) {
                 constexpr int N = Word<T>::N;
@@ -498,37 +502,40 @@ __global__ void __launch_bounds__(STRIP_THREADS, Strip<SRC>::CTAS) codes_kernel(
                 int8_t *to = nullptr;
                 float4 r4 = make_float4(0.f, 0.f, 0.f, 0.f);
                 if constexpr (ROWS) {
-                    to = out_r.codes + (uint64_t)row_of(t, k * 4) * out_r.pitch;
-                    r4 = *reinterpret_cast<const float4 *>(&row_factor[t & 1u][k * 64 + down * 4]);
+                    to = out_r.codes + (uint64_t)row_of(t, k) * out_r.pitch;
+                    r4 = *reinterpret_cast<const float4 *>(&row_factor[t & 1u][k * 32 + down * 4]);
                 }
                 const float rs[4] = {r4.x, r4.y, r4.z, r4.w};
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    const uint32_t row = row_of(t, k * 4 + i);
+                    const uint32_t row = row_of(t, k) + i;
                     if (FULL || (row < rows && col < cols)) {
-                        src.make(row, col, cols, raw[k * 4 + i], w[i]);
+                        src.template make<FULL>(row, col, cols, raw[k % AHEAD][i], w[i]);
                     } else {
 #pragma unroll
                         for (int j = 0; j < OUT * 4; ++j) w[i][j / 4][j % 4] = 0u;
                     }
-                    if constexpr (ROWS) {
-                        if (FULL || row < rows) {
+                }
+                if (k + AHEAD < SWEEPS) fetch(t, k + AHEAD, raw[k % AHEAD]);
+                else if (t > begin) fetch(t - 1, k + AHEAD - SWEEPS, raw[k % AHEAD]);
+                if constexpr (ROWS) {
 #pragma unroll
-                            for (int o = 0; o < OUT; ++o) {
-                                uint32_t c[E / 4];
-                                encode_piece<T>(w[i][o], rs[i], false, c);
-                                if (masked_rows && rs[i] == 0.f)
+                    for (int i = 0; i < 4; ++i, to += out_r.pitch) {
+                        if (!FULL && row_of(t, k) + i >= rows) break;
 #pragma unroll
-                                    for (int j = 0; j < E / 4; ++j) c[j] = 0u;
-                                if (FULL && OUT == 1) store_whole<E>(to + col, c);
-                                else store_row_piece<E, OUT>(to, o, col, cols, out_r.pitch, c);
-                            }
-                            if (OUT > 1 && strip == strips - 1 && piece == 0) pad_row(to, (uint64_t)OUT * cols, out_r.pitch);
+                        for (int o = 0; o < OUT; ++o) {
+                            uint32_t c[E / 4];
+                            encode_piece<T>(w[i][o], rs[i], false, c);
+                            if (masked_rows && rs[i] == 0.f)
+#pragma unroll
+                                for (int j = 0; j < E / 4; ++j) c[j] = 0u;
+                            if (FULL && OUT == 1) store_whole<E>(to + col, c);
+                            else store_row_piece<E, OUT>(to, o, col, cols, out_r.pitch, c);
                         }
-                        to += out_r.pitch;
+                        if (OUT > 1 && strip == strips - 1 && piece == 0) pad_row(to, (uint64_t)OUT * cols, out_r.pitch);
                     }
                 }
-                const uint32_t place = (k * 16 + down) ^ S::turned(piece);
+                const uint32_t place = (k * DOWN + down) ^ S::turned(piece);
 #pragma unroll
                 for (int o = 0; o < OUT; ++o)
 #pragma unroll
@@ -553,12 +560,9 @@ __global__ void __launch_bounds__(STRIP_THREADS, Strip<SRC>::CTAS) codes_kernel(
                     }
             }
         };
-        if (whole_strip && (t + 1) * S::ROWS <= rows) work(std::true_type());
+        if (full(t)) work(std::true_type());
         else work(std::false_type());
-        if (t > begin) {
-            fetch(t - 1);
-            rows_of(t - 1);
-        }
+        if (t > begin) rows_of(t - 1);
         __syncthreads();
         const uint32_t *const from = tile + slot * WORDS + ((chunk ^ (turned >> 2)) * 4);
         int8_t *const at = to_cols + (uint64_t)t * S::ROWS;

@@ -21,18 +21,26 @@ inline bool few_rows(uint64_t M, uint64_t K) { return M <= 4 && (M > 2 ? 4 : M) 
 
 inline uint64_t tiles_of(uint64_t M, uint64_t N, uint32_t rows, uint32_t cols) { return (M + rows - 1) / rows * ((N + cols - 1) / cols); }
 
+// Up to 64 rows: the small kernel with the narrowest tile that holds them, K divided among 4 or 8 CTAs where they are all resident at once, two to an SM, and each
+// keeps two steps (divided in two it gains nothing: joining takes as long as half the steps of a short sum).  More rows: whichever tile takes least time by
+// its number of rounds over the SMs and what a tile of it costs; measured in us, tiles of 256 x 256 on two SMs 0.30 a step and 1.1 a tile, 256 x 128 0.2 and 1.1,
+// 128 x 128 on one 0.2 and 1.0.
 inline Schedule schedule_of(uint64_t M, uint64_t N, uint64_t K, bool gated)
 {
     const uint64_t ksteps = (K + STEP_K - 1) / STEP_K;
     if (const char *e = getenv("I8K")) { const char *f = getenv("I8S"); return {(Kernel)atoi(e), f ? (uint32_t)atoi(f) : 1u}; }
     const uint32_t half = gated ? 2 : 1;
     if (M > 64) {
-        if (M <= 128) return {ONE_128, 1u};
-        return {tiles_of(M, N, 256, 256 / half) * 4 >= LAID_OUT_SMS ? PAIR_256 : PAIR_128, 1u};
+        const uint64_t pairs = LAID_OUT_SMS / 2;
+        const uint64_t r256 = (tiles_of(M, N, 256, 256 / half) + pairs - 1) / pairs, r128 = (tiles_of(M, N, 256, 128 / half) + pairs - 1) / pairs;
+        const uint64_t r1 = (tiles_of(M, N, 128, 128 / half) + LAID_OUT_SMS - 1) / LAID_OUT_SMS;
+        const uint64_t c256 = r256 * (30 * ksteps + 110), c128 = r128 * (20 * ksteps + 110), c1 = r1 * (20 * ksteps + 100);
+        return {c1 <= c128 && c1 <= c256 ? ONE_128 : c128 <= c256 ? PAIR_128 : PAIR_256, 1u};
     }
     Schedule s = {M <= 16 ? SMALL_16 : M <= 32 ? SMALL_32 : SMALL_64, 1u};
     const uint64_t tiles = tiles_of(M, N, M <= 16 ? 16 : M <= 32 ? 32 : 64, 128), resident = gated && s.kernel == SMALL_64 ? LAID_OUT_SMS : 2 * LAID_OUT_SMS;
-    while (s.splits < 8 && tiles * s.splits * 2 <= resident && ksteps >= s.splits * 8) s.splits *= 2;
+    for (uint32_t n = 4; n <= 8; n *= 2)
+        if (tiles * n <= resident && ksteps >= 2 * n) s.splits = n;
     return s;
 }
 

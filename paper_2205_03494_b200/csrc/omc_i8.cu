@@ -100,7 +100,7 @@ int quantise(const void *x, uint64_t ld, uint32_t rows, uint32_t cols, int8_t *c
              void *stream)
 {
     const T *const m = static_cast<const T *>(x);
-    const i8::Matrix<T, WHOLE> src = {m, ld, i8::span_of(m, ld, rows, cols)};
+    const i8::Matrix<T, WHOLE> src = {m, ld, rows};
     return i8::quantise<4>(src, rows, cols, codes, scales, codes_t, scales_t, workspace, stream);
 }
 
