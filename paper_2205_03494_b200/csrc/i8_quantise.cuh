@@ -320,7 +320,7 @@ template <typename SRC, bool ROWS>
 __global__ void __launch_bounds__(32 * MAXIMA_WARPS, SRC::HEAVY ? 2 : 3) maxima_kernel(SRC src, uint32_t rows, uint32_t cols, Place place, Maxima out)
 {
     using T = typename SRC::T;
-    constexpr int E = PIECE<T>, OUT = SRC::OUT, P = WINDOW_PIECES<OUT>, AHEAD = SRC::HEAVY ? 1 : 2;
+    constexpr int E = PIECE<T>, OUT = SRC::OUT, P = WINDOW_PIECES<OUT>, AHEAD = SRC::WHOLE_ROWS ? 2 : 1;
     __shared__ uint4 joined[32 * MAXIMA_WARPS];
     const uint32_t lane = threadIdx.x & 31, warp = threadIdx.x >> 5, window = place.window() * (32 * P * E);
     el::enter_stream_order();
@@ -495,7 +495,7 @@ __global__ void __launch_bounds__(STRIP_THREADS, Strip<SRC>::CTAS) codes_kernel(
         const bool masked_rows = ROWS && nan_rows[t & 1u] == t + 1;
         auto work = [&](auto inside_all) {
             constexpr bool FULL = decltype(inside_all)::value;
-#pragma unroll
+#pragma unroll(AHEAD)
             for (int k = 0; k < SWEEPS; ++k) {
                 constexpr int N = Word<T>::N;
                 uint32_t w[4][OUT][4];

@@ -2,7 +2,6 @@
 // not show in the results.  Plain C++, so that the rule can be checked on the host.
 #pragma once
 #include <stdint.h>
-#include <stdlib.h>
 
 namespace omc {
 namespace i8 {
@@ -21,27 +20,41 @@ inline bool few_rows(uint64_t M, uint64_t K) { return M <= 4 && (M > 2 ? 4 : M) 
 
 inline uint64_t tiles_of(uint64_t M, uint64_t N, uint32_t rows, uint32_t cols) { return (M + rows - 1) / rows * ((N + cols - 1) / cols); }
 
-// Up to 64 rows: the small kernel with the narrowest tile that holds them, K divided among 4 or 8 CTAs where they are all resident at once, two to an SM, and each
-// keeps two steps (divided in two it gains nothing: joining takes as long as half the steps of a short sum).  More rows: whichever tile takes least time by
-// its number of rounds over the SMs and what a tile of it costs; measured in us, tiles of 256 x 256 on two SMs 0.30 a step and 1.1 a tile, 256 x 128 0.2 and 1.1,
-// 128 x 128 on one 0.2 and 1.0.
+// CTAs among which the small kernel divides the K of `tiles` tiles: eight while each has an SM, four while two share one, and each CTA has a step.
+// (In two it gains nothing: joining takes as long as half the steps of a short sum.)
+inline uint32_t splits_of(uint64_t tiles, uint64_t ksteps, uint64_t resident)
+{
+    return tiles * 8 <= LAID_OUT_SMS && ksteps >= 8 ? 8u : tiles * 4 <= resident && ksteps >= 4 ? 4u : 1u;
+}
+
+// Whichever kernel takes least time by what was measured, in 1/100 us: `base` with one tile's results, `step` for each K step of 128, and a further tile of the
+// same SMs as long as its steps or the results of the one before, whichever is longer.
+//   256 x 256 on a pair    480 + 31 a step, 37 while results are stored, 290 for results (gated 550)
+//   256 x 128 on a pair    460 + 25, 175 (290)
+//   128 x 128 on an SM     390 + 24, 175 (290)
+//   small kernel           440 + 28 (two CTAs on an SM: 45), 90 more with divided K
 inline Schedule schedule_of(uint64_t M, uint64_t N, uint64_t K, bool gated)
 {
     const uint64_t ksteps = (K + STEP_K - 1) / STEP_K;
-    if (const char *e = getenv("I8K")) { const char *f = getenv("I8S"); return {(Kernel)atoi(e), f ? (uint32_t)atoi(f) : 1u}; }
-    const uint32_t half = gated ? 2 : 1;
-    if (M > 64) {
-        const uint64_t pairs = LAID_OUT_SMS / 2;
-        const uint64_t r256 = (tiles_of(M, N, 256, 256 / half) + pairs - 1) / pairs, r128 = (tiles_of(M, N, 256, 128 / half) + pairs - 1) / pairs;
-        const uint64_t r1 = (tiles_of(M, N, 128, 128 / half) + LAID_OUT_SMS - 1) / LAID_OUT_SMS;
-        const uint64_t c256 = r256 * (30 * ksteps + 110), c128 = r128 * (20 * ksteps + 110), c1 = r1 * (20 * ksteps + 100);
-        return {c1 <= c128 && c1 <= c256 ? ONE_128 : c128 <= c256 ? PAIR_128 : PAIR_256, 1u};
-    }
-    Schedule s = {M <= 16 ? SMALL_16 : M <= 32 ? SMALL_32 : SMALL_64, 1u};
-    const uint64_t tiles = tiles_of(M, N, M <= 16 ? 16 : M <= 32 ? 32 : 64, 128), resident = gated && s.kernel == SMALL_64 ? LAID_OUT_SMS : 2 * LAID_OUT_SMS;
-    for (uint32_t n = 4; n <= 8; n *= 2)
-        if (tiles * n <= resident && ksteps >= 2 * n) s.splits = n;
-    return s;
+    const uint32_t half = gated ? 2 : 1, rows = M <= 16 ? 16 : M <= 32 ? 32 : 64;
+    const Kernel small = M <= 16 ? SMALL_16 : M <= 32 ? SMALL_32 : SMALL_64;
+    const uint64_t tiles = tiles_of(M, N, rows, 128), resident = gated && small == SMALL_64 ? LAID_OUT_SMS : 2 * LAID_OUT_SMS;
+    const uint32_t splits = splits_of(tiles, ksteps, resident);
+    const uint64_t ctas = tiles * splits, mine = (ksteps + splits - 1) / splits, rounds = (ctas + resident - 1) / resident;
+    Schedule best = {small, splits};
+    uint64_t least = rounds * (440 + mine * (ctas > LAID_OUT_SMS ? 45 : 28)) + (splits > 1 ? 90 : 0);
+    auto consider = [&](Kernel kernel, uint64_t all, uint64_t units, uint64_t base, uint64_t step, uint64_t later_step, uint64_t results) {
+        const uint64_t further = (all + units - 1) / units - 1, later = ksteps * later_step;
+        const uint64_t cost = base + ksteps * step + further * (later > results ? later : results);
+        if (cost < least) {
+            least = cost;
+            best = {kernel, 1u};
+        }
+    };
+    consider(ONE_128, tiles_of(M, N, 128, 128 / half), LAID_OUT_SMS, 390, 24, 24, gated ? 290 : 175);
+    consider(PAIR_128, tiles_of(M, N, 256, 128 / half), LAID_OUT_SMS / 2, 460, 25, 25, gated ? 290 : 175);
+    consider(PAIR_256, tiles_of(M, N, 256, 256 / half), LAID_OUT_SMS / 2, 480, 31, 37, gated ? 550 : 290);
+    return best;
 }
 
 }  // namespace i8

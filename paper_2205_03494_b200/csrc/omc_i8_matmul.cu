@@ -84,6 +84,7 @@ __device__ __forceinline__ uint32_t shared_word(uint32_t addr)
     asm volatile("ld.shared.u32 %0, [%1];" : "=r"(v) : "r"(addr) : "memory");
     return v;
 }
+__device__ __forceinline__ void prefetch_map(const CUtensorMap *map) { asm volatile("prefetch.tensormap [%0];" ::"l"(map) : "memory"); }
 __device__ __forceinline__ void arrive_at(uint32_t cluster_addr) { asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr) : "memory"); }
 __device__ __forceinline__ void store_remote(uint32_t cluster_addr, uint32_t v)
 {
@@ -171,11 +172,10 @@ template <int CG, int BN, bool GATED>
 struct Tile {
     static constexpr int W_ROWS = BN / CG;                           // of a CTA
     static constexpr int STAGE = TILE_BYTES + W_ROWS * BK;
-    static constexpr int THREADS = 320, STORE_WARPS = 8;
+    static constexpr int STORE_WARPS = 8, STORE_THREADS = 32 * STORE_WARPS, THREADS = 64 + STORE_THREADS;
     static constexpr int SCALES = 2 * BN * 4;                        // of W's rows, of two tiles
-    // results on their way from a warp to memory: boxes of 64 bytes of 32 rows, three a warp (or 16 columns of rows off the 16-byte boundaries)
-    static constexpr int BOX = 32 * 64, BOXES = 3, ROOM = STORE_WARPS * BOXES * BOX;
-    static_assert(BOXES * BOX >= 32 * 17 * 4, "");
+    // results on their way from a warp to memory, in boxes of 32 rows (or 16 or 32 columns of rows off the 16-byte boundaries)
+    static constexpr int ROOM_EACH = 6 * 1024, ROOM = STORE_WARPS * ROOM_EACH;
     static constexpr int FIT = (220 * 1024 - SCALES - ROOM - 1024 - 256) / STAGE, NSTAGES = FIT < 8 ? FIT : 8;
     static constexpr int BARRIERS = 2 * NSTAGES + 5;
     static constexpr int SMEM = NSTAGES * STAGE + SCALES + ROOM + 1024 + 256;
@@ -185,16 +185,17 @@ struct Tile {
     static_assert(STAGE % 1024 == 0 && NSTAGES >= 4 && 8 * BARRIERS + 8 <= 256, "");
 };
 
-// Barrier of the 256 threads that store results, and whether all of them say yes: they leave their loop together or not at all.
-__device__ __forceinline__ bool together256(bool ok)
+// Barrier of the threads that store results, and whether all of them say yes: they leave their loop together or not at all.
+template <int THREADS>
+__device__ __forceinline__ bool together(bool ok)
 {
     uint32_t all;
     asm volatile(
         "{\n\t.reg .pred p, q;\n\t"
         "setp.ne.u32 p, %1, 0;\n\t"
-        "barrier.cta.red.and.pred q, 1, 256, p;\n\t"
+        "barrier.cta.red.and.pred q, 1, %2, p;\n\t"
         "selp.u32 %0, 1, 0, q;\n\t}"
-        : "=r"(all) : "r"((uint32_t)ok) : "memory");
+        : "=r"(all) : "r"((uint32_t)ok), "n"(THREADS) : "memory");
     return all != 0u;
 }
 // Tiles in the order in which they are taken: bands of eight tiles of W's rows, so that the tiles in work at a time form a
@@ -207,44 +208,73 @@ __device__ __forceinline__ void tile_of(uint32_t t, uint32_t tiles_n, uint32_t t
     tn = band * 8 + in_band - tm * width;
 }
 
-// Sixteen neighbouring values of each lane's row, from column `col` on, to a matrix of `cols` columns whose rows start anywhere: through shared memory,
-// so that neighbouring lanes store neighbouring values.
-template <typename T>
-__device__ __forceinline__ void store16(const float *f, T *to, uint64_t ld, uint32_t row0, uint32_t rows, uint32_t col, uint32_t cols, int lane, uint32_t *room)
+// COLS neighbouring values of each lane's row, from column `col` on, to a matrix of `cols` columns whose rows start anywhere: through shared memory,
+// so that neighbouring lanes store neighbouring words.  Of 16-bit types a row may start in the upper half of a word: its words are then made with
+// the neighbour lane's, and its first and last values go out alone.
+template <typename T, int COLS>
+__device__ __forceinline__ void store_any(const float *f, T *to, uint64_t ld, uint32_t row0, uint32_t rows, uint32_t col, uint32_t cols, int lane, uint32_t *room)
 {
+    constexpr int N = Word<T>::N, WORDS = COLS / N, PITCH = WORDS + 4, TOGETHER = 32 / WORDS;      // (an odd number of sixteens from row to row: no bank twice)
+    static_assert(WORDS <= 32 && 32 * PITCH * 4 <= 6 * 1024, "");
     __syncwarp();
 #pragma unroll
-    for (int j = 0; j < 16; ++j) {
-        const T v = el::from_float<T>(f[j]);
-        if constexpr (sizeof(T) == 4) room[lane * 17 + j] = *reinterpret_cast<const uint32_t *>(&v);
-        else room[lane * 17 + j] = *reinterpret_cast<const uint16_t *>(&v);
-    }
+    for (int j = 0; j < WORDS; j += 4)
+        *reinterpret_cast<uint4 *>(room + lane * PITCH + j) =
+            make_uint4(Word<T>::pack(f + j * N), Word<T>::pack(f + (j + 1) * N), Word<T>::pack(f + (j + 2) * N), Word<T>::pack(f + (j + 3) * N));
     __syncwarp();
-    const uint32_t c = lane & 15;
-    if (col + c < cols) {
+    const int n = row0 < rows ? (int)min(32u, rows - row0) : 0, j = lane % WORDS, first = lane / WORDS;
+    T *p = to + (uint64_t)(row0 + first) * ld + col;
+    if (col + COLS <= cols) {
 #pragma unroll 4
-        for (int i = 0; i < 16; ++i) {
-            const uint32_t r = 2 * i + (lane >> 4);
-            if (row0 + r < rows) {
-                T *p = to + (uint64_t)(row0 + r) * ld + col + c;
-                if constexpr (sizeof(T) == 4) *reinterpret_cast<uint32_t *>(p) = room[r * 17 + c];
-                else *reinterpret_cast<uint16_t *>(p) = (uint16_t)room[r * 17 + c];
+        for (int r = first; r < 32; r += TOGETHER, p += TOGETHER * ld) {
+            const uint32_t w = room[r * PITCH + j];
+            if constexpr (N == 1) {
+                if (r < n) reinterpret_cast<uint32_t *>(p)[j] = w;
+            } else {
+                const uint32_t before = __shfl_up_sync(0xFFFFFFFFu, w, 1, WORDS);
+                const bool odd = (reinterpret_cast<uintptr_t>(p) & 2) != 0;
+                uint16_t *const h = reinterpret_cast<uint16_t *>(p) + 2 * j;
+                if (r < n) {
+                    if (!odd) *reinterpret_cast<uint32_t *>(h) = w;
+                    else if (j > 0) *reinterpret_cast<uint32_t *>(h - 1) = __byte_perm(before, w, 0x5432);
+                    else h[0] = (uint16_t)w;
+                    if (odd && j == WORDS - 1) h[1] = (uint16_t)(w >> 16);
+                }
+            }
+        }
+    } else {
+        for (int r = first; r < n; r += TOGETHER, p += TOGETHER * ld) {
+            const uint32_t w = room[r * PITCH + j];
+            if constexpr (N == 1) {
+                if (col + j < cols) reinterpret_cast<uint32_t *>(p)[j] = w;
+            } else {
+                uint16_t *const h = reinterpret_cast<uint16_t *>(p) + 2 * j;
+                if (col + 2 * j < cols) h[0] = (uint16_t)w;
+                if (col + 2 * j + 1 < cols) h[1] = (uint16_t)(w >> 16);
             }
         }
     }
 }
 
-// Rows on 16-byte boundaries: a warp's boxes of 32 rows x 64 bytes go out as bulk tensor stores, which write whole sectors and clip at the matrix's ends.
+// Rows on 16-byte boundaries: a warp's boxes of 32 rows go out as bulk tensor stores, which write whole sectors and clip at the matrix's ends.
 // (They clip whole pieces of 16 bytes: a matrix 257 FP32 values wide got 260 written.)
 // (With each lane storing its own row, 32 bytes at a time, the stores took the load/store unit's time: 8192 x 8192 x 256 BF16 46.7 us.)
-// Sixteen values of a lane's row into a box, from its 16-byte piece `piece` on; 64-byte swizzle: piece p of row r sits at piece p ^ (r / 2 mod 4).
-template <typename T>
+// A box is 64 bytes wide, three a warp in turn; in the gated layer of 16-bit types 32 bytes, sixteen columns, so that there are two sets of three (y, a, b).
+// (Sixteen warps instead of eight for the largest tiles: 8192 x 8192 x 256 BF16 37 instead of 40 us, but a stage less, 16384 x 2048 x 8192 174 instead of 165 us.)
+template <typename T, bool GATED>
+struct Box {
+    static constexpr int BYTES = GATED && sizeof(T) == 2 ? 32 : 64, COLS = BYTES / (int)sizeof(T), SIZE = 32 * BYTES;
+};
+// Sixteen values of a lane's row into a box, from its 16-byte piece `piece` on.  64-byte swizzle: piece p of row r sits at piece p ^ (r / 2 mod 4); 32-byte:
+// at p ^ (r / 4 mod 2).  Either way eight lanes' pieces fall into different banks.
+template <typename T, int BYTES>
 __device__ __forceinline__ void box16(uint32_t box, int piece, const float *f, int lane)
 {
     constexpr int N = Word<T>::N;
+    const uint32_t turn = BYTES == 64 ? (lane >> 1) & 3 : (lane >> 2) & 1;
 #pragma unroll
     for (int i = 0; i < 16 / (4 * N); ++i) {
-        const uint32_t at = box + lane * 64 + (((piece + i) ^ ((lane >> 1) & 3)) << 4);
+        const uint32_t at = box + lane * BYTES + (((piece + i) ^ turn) << 4);
         asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(Word<T>::pack(f + (4 * i) * N)), "r"(Word<T>::pack(f + (4 * i + 1) * N)),
                      "r"(Word<T>::pack(f + (4 * i + 2) * N)), "r"(Word<T>::pack(f + (4 * i + 3) * N)) : "memory");
     }
@@ -298,6 +328,11 @@ i8_tile_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant_
         else umma_commit(bar);
     };
 
+    if (tid == 64) {
+        prefetch_map(&map_x);
+        prefetch_map(&map_w);
+        if (whole) prefetch_map(&to.y);
+    }
     if (tid == 0) {
         for (int s = 0; s < NS; ++s) { mbar_init(full(s), 1); mbar_init(empty(s), 1); }
         for (int b = 0; b < 2; ++b) { mbar_init(acc_full(b), 1); mbar_init(acc_empty(b), CG * C::STORE_WARPS); }
@@ -305,6 +340,8 @@ i8_tile_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant_
         shared_word(gave_up, 0u);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
+    // with a tile each the next kernel may take the SMs that are left at once, else when the last tile's sums are there
+    if (ntiles <= units) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     asm volatile("griddepcontrol.wait;" ::: "memory");
     if (warp == 1) {          // with two CTAs the same warp of both takes the pair's tensor memory
         if constexpr (CG == 2) {
@@ -371,11 +408,12 @@ i8_tile_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant_
             if (ok) commit(acc_full(buf));
         }
     } else if (warp >= 2) {
-        const int q = warp & 3, half = (warp - 2) >> 2, mine = tid - 64;
-        constexpr int PER_BOX = 64 / (int)sizeof(T);      // columns: 32 or 16
-        const uint32_t boxes = base + NS * C::STAGE + C::SCALES + (warp - 2) * C::BOXES * C::BOX;
-        uint32_t *const room = reinterpret_cast<uint32_t *>(base_ptr + NS * C::STAGE + C::SCALES + (warp - 2) * C::BOXES * C::BOX);
-        uint32_t lt = 0, box = 0;                          // the next box, of three in turn
+        const int q = warp & 3, part_of_row = (warp - 2) >> 2, mine = tid - 64;
+        using B = Box<T, GATED>;
+        constexpr int PER_BOX = B::COLS, BOXES = C::ROOM_EACH / B::SIZE, SETS = BOXES / 3, SHARE = TN / (C::STORE_WARPS / 4);      // columns of a warp
+        const uint32_t boxes = base + NS * C::STAGE + C::SCALES + (warp - 2) * C::ROOM_EACH;
+        uint32_t *const room = reinterpret_cast<uint32_t *>(base_ptr + NS * C::STAGE + C::SCALES + (warp - 2) * C::ROOM_EACH);
+        uint32_t lt = 0, box = 0;                          // the next box, in turn
         // the store of a box clips at multiples of 16 bytes only: the last columns of other widths go out one by one
         const bool ends_whole = o.N * sizeof(T) % 16 == 0;
         auto boxed = [&](uint32_t col) { return whole && (ends_whole || col + PER_BOX <= o.N); };
@@ -391,7 +429,7 @@ i8_tile_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant_
             const uint32_t row0 = tm * TM + rank * 128 + q * 32;
             const i8::RowScale xs(row0 + lane < o.M ? o.x_scales[row0 + lane] : 0.f);
             const bool any_big = __any_sync(0xFFFFFFFFu, xs.big());
-            ok = together256(mbar_wait_held(acc_full(buf), (lt >> 1) & 1u, waits.results(unit)));
+            ok = together<C::STORE_THREADS>(mbar_wait_held(acc_full(buf), (lt >> 1) & 1u, waits.results(unit)));
             if (t + units >= ntiles) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
             if (!ok) break;
             fence_after();
@@ -399,79 +437,95 @@ i8_tile_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant_
             const float4 *ws = reinterpret_cast<const float4 *>(scales + buf * BN);
             const uint32_t col0 = tn * TN;
             const bool rows_here = row0 < o.M;             // of this warp
+            // sums of the next columns leave tensor memory while those before are worked on
+            const int c_end = min((part_of_row + 1) * SHARE, (int)(o.N - col0));
             if constexpr (GATED) {
-#pragma unroll 1
-                for (int c = half * (TN / 2); c < (half + 1) * (TN / 2) && col0 + c < o.N; c += 16) {
-                    uint32_t v[16], u[16];
+                uint32_t v[16], u[16];
+                int c = part_of_row * SHARE;
+                if (c < c_end) {
                     tmem_load16(acc + c, v);
                     tmem_load16(acc + TN + c, u);
+                }
+#pragma unroll 1
+                for (; c < c_end; c += 16) {
                     tmem_wait();
                     loaded16(v);
                     loaded16(u);
                     float a[16], b[16], y[16];
                     values16(v, xs, any_big, ws + c / 4, a);
                     values16(u, xs, any_big, ws + TN / 4 + c / 4, b);
+                    if (c + 16 < c_end) {
+                        tmem_load16(acc + c + 16, v);
+                        tmem_load16(acc + TN + c + 16, u);
+                    }
                     gate16(o.act, a, b, y);
-                    const int in_box = c % PER_BOX, piece = in_box * (int)sizeof(T) / 16;
-                    if (boxed(col0 + c - in_box)) {
-                        const uint32_t y_box = boxes + box * C::BOX;
-                        if (in_box == 0) {
-                            if (o.pre) boxes_free<0>(lane);
-                            else boxes_free<C::BOXES - 1>(lane);
-                        }
-                        box16<T>(y_box, piece, y, lane);
+                    const uint32_t col = col0 + c;
+                    static_assert(PER_BOX == 16, "");
+                    if (boxed(col)) {
+                        // a set of three boxes with what is kept, else one
                         if (o.pre) {
-                            box16<T>(boxes + C::BOX, piece, a, lane);
-                            box16<T>(boxes + 2 * C::BOX, piece, b, lane);
+                            boxes_free<3 * (SETS - 1)>(lane);
+                        } else {
+                            boxes_free<BOXES - 1>(lane);
                         }
-                        if (in_box + 16 == PER_BOX || c + 16 == (half + 1) * (TN / 2) || col0 + c + 16 >= o.N) {
-                            boxes_written();
-                            if (rows_here) {
-                                const uint32_t col = col0 + c - in_box;
-                                send_box(y_box, &to.y, col, row0, lane);
-                                if (o.pre) {
-                                    send_box(boxes + C::BOX, &to.a, col, row0, lane);
-                                    send_box(boxes + 2 * C::BOX, &to.b, col, row0, lane);
-                                }
+                        const uint32_t here = boxes + box * B::SIZE;
+                        box16<T, B::BYTES>(here, 0, y, lane);
+                        if (o.pre) {
+                            box16<T, B::BYTES>(here + B::SIZE, 0, a, lane);
+                            box16<T, B::BYTES>(here + 2 * B::SIZE, 0, b, lane);
+                        }
+                        boxes_written();
+                        if (rows_here) {
+                            send_box(here, &to.y, col, row0, lane);
+                            if (o.pre) {
+                                send_box(here + B::SIZE, &to.a, col, row0, lane);
+                                send_box(here + 2 * B::SIZE, &to.b, col, row0, lane);
                             }
-                            if (!o.pre) box = box == C::BOXES - 1 ? 0 : box + 1;
                         }
+                        box += o.pre ? 3 : 1;
+                        if (box >= (uint32_t)(o.pre ? 3 * SETS : BOXES)) box = 0;
                     } else {
                         boxes_free<0>(lane);
                         if (o.pre) {
-                            store16<T>(a, o.pre, o.ld_pre, row0, o.M, col0 + c, o.N, lane, room);
-                            store16<T>(b, o.pre + o.N, o.ld_pre, row0, o.M, col0 + c, o.N, lane, room);
+                            store_any<T, 16>(a, o.pre, o.ld_pre, row0, o.M, col, o.N, lane, room);
+                            store_any<T, 16>(b, o.pre + o.N, o.ld_pre, row0, o.M, col, o.N, lane, room);
                         }
-                        store16<T>(y, o.y, o.ldy, row0, o.M, col0 + c, o.N, lane, room);
+                        store_any<T, 16>(y, o.y, o.ldy, row0, o.M, col, o.N, lane, room);
                     }
                 }
             } else {
-#pragma unroll 1
-                for (int c = half * (TN / 2); c < (half + 1) * (TN / 2) && col0 + c < o.N; c += 32) {
-                    uint32_t v[32];
+                uint32_t v[32];
+                int c = part_of_row * SHARE;
+                if (c < c_end) {
                     tmem_load16(acc + c, v);
                     tmem_load16(acc + c + 16, v + 16);
+                }
+#pragma unroll 1
+                for (; c < c_end; c += 32) {
                     tmem_wait();
                     loaded16(v);
                     loaded16(v + 16);
                     float f[32];
                     values16(v, xs, any_big, ws + c / 4, f);
                     values16(v + 16, xs, any_big, ws + c / 4 + 4, f + 16);
+                    if (c + 32 < c_end) {
+                        tmem_load16(acc + c + 32, v);
+                        tmem_load16(acc + c + 48, v + 16);
+                    }
 #pragma unroll
                     for (int part = 0; part < 32 / PER_BOX; ++part) {
-                        const uint32_t col = col0 + c + part * PER_BOX, here = boxes + box * C::BOX;
+                        const uint32_t col = col0 + c + part * PER_BOX, here = boxes + box * B::SIZE;
                         if (col >= o.N) break;
                         if (boxed(col)) {
-                            boxes_free<C::BOXES - 1>(lane);
+                            boxes_free<BOXES - 1>(lane);
 #pragma unroll
-                            for (int i = 0; i < PER_BOX; i += 16) box16<T>(here, i * (int)sizeof(T) / 16, f + part * PER_BOX + i, lane);
+                            for (int i = 0; i < PER_BOX; i += 16) box16<T, B::BYTES>(here, i * (int)sizeof(T) / 16, f + part * PER_BOX + i, lane);
                             boxes_written();
                             if (rows_here) send_box(here, &to.y, col, row0, lane);
-                            box = box == C::BOXES - 1 ? 0 : box + 1;
+                            box = box == BOXES - 1 ? 0 : box + 1;
                         } else {
                             boxes_free<0>(lane);
-#pragma unroll
-                            for (int i = 0; i < PER_BOX; i += 16) store16<T>(f + part * PER_BOX + i, o.y, o.ldy, row0, o.M, col + i, o.N, lane, room);
+                            store_any<T, PER_BOX>(f + part * PER_BOX, o.y, o.ldy, row0, o.M, col, o.N, lane, room);
                         }
                     }
                 }
@@ -511,11 +565,12 @@ struct Small {
     static constexpr int W_TILES = GATED ? 2 : 1, TILE_X = NT * BK;
     static constexpr int STAGE = W_TILES * TILE_BYTES + TILE_X;
     static constexpr int BUDGET = (GATED && NT > 32 ? 212 : 112) * 1024;           // the latter: two CTAs share an SM
-    static constexpr int NSTAGES = (BUDGET - 1024 - 256 - NT * 4) / STAGE;
-    static constexpr int SMEM = NSTAGES * STAGE + NT * 4 + 1024 + 256;
+    static constexpr int PARTS = 128 * NT * 4 * W_TILES;                            // sums of the cluster's CTAs for this one's rows
+    static constexpr int NSTAGES = (BUDGET - 1024 - 256 - NT * 4 - PARTS) / STAGE;
+    static constexpr int SMEM = NSTAGES * STAGE + PARTS + NT * 4 + 1024 + 256;
     static constexpr int COLS = NT < 32 ? 32 : NT, ALL_COLS = W_TILES * COLS;       // of tensor memory
     static constexpr int THREADS = 192;
-    static_assert(NSTAGES >= 3 && STAGE % 1024 == 0 && 8 * (2 * NSTAGES + 2) + 8 <= 256 && 128 * NT * 4 * W_TILES <= NSTAGES * STAGE, "");
+    static_assert(NSTAGES >= 2 && STAGE % 1024 == 0 && 8 * (2 * NSTAGES + 2) + 8 <= 256, "");
 };
 
 template <int NT, typename T, bool GATED, typename WAITS>
@@ -528,8 +583,8 @@ i8_small_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant
     extern __shared__ uint8_t smem_raw[];
     const uint32_t base = (saddr(smem_raw) + 1023u) & ~1023u;
     uint8_t *const base_ptr = smem_raw + (base - saddr(smem_raw));
-    float *const scales = reinterpret_cast<float *>(base_ptr + NS * C::STAGE);     // of the tile's rows of X
-    const uint32_t bars = base + NS * C::STAGE + NT * 4;      // full[NS], empty[NS], done, drained; tmem slot, gave_up
+    float *const scales = reinterpret_cast<float *>(base_ptr + NS * C::STAGE + C::PARTS);      // of the tile's rows of X
+    const uint32_t bars = base + NS * C::STAGE + C::PARTS + NT * 4;      // full[NS], empty[NS], done, drained; tmem slot, gave_up
     auto full = [&](int s) { return bars + 8u * s; };
     auto empty = [&](int s) { return bars + 8u * (NS + s); };
     const uint32_t done = bars + 8u * (2 * NS), drained = done + 8u, tmem_slot = drained + 8u, gave_up = tmem_slot + 4u;
@@ -539,6 +594,10 @@ i8_small_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant
     const uint32_t ksteps = (o.K + BK - 1) / BK;
     const uint32_t k_begin = (uint32_t)((uint64_t)ksteps * rank / splits), k_end = (uint32_t)((uint64_t)ksteps * (rank + 1) / splits);
 
+    if (tid == 64) {
+        prefetch_map(&map_x);
+        prefetch_map(&map_w);
+    }
     if (tid == 0) {
         for (int s = 0; s < NS; ++s) { mbar_init(full(s), 1); mbar_init(empty(s), 1); }
         mbar_init(done, 1);
@@ -547,6 +606,7 @@ i8_small_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     __syncthreads();
+    if (splits > 1) asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");      // this CTA runs: sums may be put into its shared memory
     el::enter_stream_order();
     // tensor memory is taken while the first copies are on their way; warps 2 .. 5 learn where it is at barrier 1
     uint32_t tmem_base = 0;
@@ -595,6 +655,18 @@ i8_small_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant
     __syncwarp();
     const int q = warp & 3;                               // quarter of the lanes a warp may read
     const uint32_t n = tn * 128 + q * 32 + lane, mine = NT / splits;
+    float wa = 0.f, wb = 0.f, was[4], wbs[4];             // scales of W's rows: with divided K this lane's four columns of the rows that its warp adds up
+    if (splits > 1) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const uint32_t col = tn * 128 + i * 32 + lane;
+            was[i] = col < o.N ? o.w_scales[col] : 0.f;
+            wbs[i] = GATED && col < o.N ? o.w_scales[o.N + col] : 0.f;
+        }
+    } else if (warp >= 2 && n < o.N) {
+        wa = o.w_scales[n];
+        if constexpr (GATED) wb = o.w_scales[o.N + n];
+    }
     if (warp >= 2) {
         for (uint32_t i = tid - 64; i < (uint32_t)NT; i += 128) scales[i] = m0 + i < o.M ? o.x_scales[m0 + i] : 0.f;
         asm volatile("bar.sync 1, 160;" ::: "memory");
@@ -603,10 +675,9 @@ i8_small_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant
         ok = __all_sync(0xFFFFFFFFu, ok);
         fence_after();
     }
-    if (splits > 1) cluster_barrier();                     // every CTA of the cluster is through with its stages: sums may be put there
+    if (splits > 1) asm volatile("barrier.cluster.wait.aligned;" ::: "memory");      // every CTA of the cluster runs
     if (warp >= 2) {
         if (ok) {
-            const float wa = n < o.N ? o.w_scales[n] : 0.f, wb = GATED && n < o.N ? o.w_scales[o.N + n] : 0.f;
             const uint32_t at = tmem_base + ((uint32_t)(q * 32) << 16);
 #pragma unroll 1
             for (int c = 0; c < NT && m0 + c < o.M; c += 16) {
@@ -618,7 +689,7 @@ i8_small_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant
                 if constexpr (GATED) loaded16(u);
                 if (splits > 1) {
                     // row r of the tile belongs to CTA r / mine, there place r mod mine of part `rank`: [part][row][half of W][128]
-                    const uint32_t here = base + (rank * mine * C::W_TILES * 128 + q * 32 + lane) * 4, shift = 31 - __clz(mine);
+                    const uint32_t here = base + NS * C::STAGE + (rank * mine * C::W_TILES * 128 + q * 32 + lane) * 4, shift = 31 - __clz(mine);
 #pragma unroll
                     for (int j = 0; j < 16; ++j)
                         if (m0 + c + j < o.M) {
@@ -660,27 +731,33 @@ i8_small_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant
     __syncwarp();
     if (splits > 1) {
         cluster_barrier();                                 // the sums of this CTA's rows have arrived
-        const int32_t *parts = reinterpret_cast<const int32_t *>(base_ptr);
-        for (uint32_t i = warp; i < mine * 4; i += C::THREADS / 32) {
-            const uint32_t r = i >> 2, in_tile = rank * mine + r, m = m0 + in_tile, l = (i & 3) * 32 + lane, col = tn * 128 + l;
-            if (m >= o.M || col >= o.N) continue;
-            int32_t a = 0, b = 0;
-            for (uint32_t p = 0; p < splits; ++p) {
-                const int32_t *part = parts + (p * mine + r) * C::W_TILES * 128 + l;
-                a += part[0];
-                if constexpr (GATED) b += part[128];
-            }
+        const int32_t *parts = reinterpret_cast<const int32_t *>(base_ptr + NS * C::STAGE);
+        for (uint32_t r = warp; r < mine; r += C::THREADS / 32) {
+            const uint32_t in_tile = rank * mine + r, m = m0 + in_tile;
+            if (m >= o.M) break;
             const i8::RowScale xs(scales[in_tile]);
-            const float fa = i8::value_in_two(a, xs, o.w_scales[col]);
-            if constexpr (GATED) {
-                const float fb = i8::value_in_two(b, xs, o.w_scales[o.N + col]);
-                if (o.pre) {
-                    o.pre[m * o.ld_pre + col] = el::from_float<T>(fa);
-                    o.pre[m * o.ld_pre + o.N + col] = el::from_float<T>(fb);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const uint32_t l = i * 32 + lane, col = tn * 128 + l;
+                int32_t a = 0, b = 0;
+                for (uint32_t p = 0; p < splits; ++p) {
+                    const int32_t *part = parts + (p * mine + r) * C::W_TILES * 128 + l;
+                    a += part[0];
+                    if constexpr (GATED) b += part[128];
                 }
-                o.y[m * o.ldy + col] = el::from_float<T>(gate1(o.act, fa, fb));
-            } else {
-                o.y[m * o.ldy + col] = el::from_float<T>(fa);
+                if (col < o.N) {
+                    const float fa = i8::value_in_two(a, xs, was[i]);
+                    if constexpr (GATED) {
+                        const float fb = i8::value_in_two(b, xs, wbs[i]);
+                        if (o.pre) {
+                            o.pre[m * o.ld_pre + col] = el::from_float<T>(fa);
+                            o.pre[m * o.ld_pre + o.N + col] = el::from_float<T>(fb);
+                        }
+                        o.y[m * o.ldy + col] = el::from_float<T>(gate1(o.act, fa, fb));
+                    } else {
+                        o.y[m * o.ldy + col] = el::from_float<T>(fa);
+                    }
+                }
             }
         }
     }
@@ -810,6 +887,9 @@ i8_rows_kernel(SOURCE source, const int8_t *w_codes, const float *w_scales, void
     if (task < tasks) fetch(task, 0);                      // on its way while X is quantised
     bring_rows<MT>(source, M, K, pitch, codes, scales, slots);
     for (; task < tasks; task += step) {
+        const uint32_t n = task * OUTS + lane / MT, m = lane % MT;
+        const bool mine = lane < OUTS * MT && n < N && m < M;
+        const float wa = mine ? w_scales[n] : 0.f, wb = GATED && mine ? w_scales[N + n] : 0.f;
         int32_t acc[W_ROWS][MT];
 #pragma unroll
         for (int i = 0; i < W_ROWS * MT; ++i) acc[i / MT][i % MT] = 0;
@@ -840,12 +920,11 @@ i8_rows_kernel(SOURCE source, const int8_t *w_codes, const float *w_scales, void
             if (i < OUTS * MT) a = lane == (uint32_t)i ? sum : a;
             else b = lane == (uint32_t)(i - OUTS * MT) ? sum : b;
         }
-        const uint32_t n = task * OUTS + lane / MT, m = lane % MT;
-        if (lane < OUTS * MT && n < N && m < M) {
+        if (mine) {
             const i8::RowScale xs(scales[m]);
-            const float fa = i8::value_in_two(a, xs, w_scales[n]);
+            const float fa = i8::value_in_two(a, xs, wa);
             if constexpr (GATED) {
-                const float fb = i8::value_in_two(b, xs, w_scales[N + n]);
+                const float fb = i8::value_in_two(b, xs, wb);
                 if (pre) {
                     put(type, pre, m * ld_pre + n, fa);
                     put(type, pre, m * ld_pre + N + n, fb);
@@ -905,18 +984,19 @@ Result<T> result_of(const Product &p)
     return {p.x_scales, p.w_scales, static_cast<T *>(p.y), static_cast<T *>(p.pre), p.ldy, p.ld_pre, p.M, p.N, p.K, p.act, p.status};
 }
 
-// A result matrix, boxes of 32 rows x 64 bytes, 64-byte swizzle.
-template <typename T>
+// A result matrix in boxes of 32 rows.
+template <typename T, bool GATED>
 bool make_result_map(CUtensorMap *m, T *p, uint64_t rows, uint64_t cols, uint64_t ld)
 {
     EncodeTiledFn fn = encode_fn();
     if (!fn) return false;
     const cuuint64_t dims[2] = {cols, rows};
     const cuuint64_t strides[1] = {ld * sizeof(T)};
-    const cuuint32_t box[2] = {64 / (uint32_t)sizeof(T), 32};
+    const cuuint32_t box[2] = {(cuuint32_t)Box<T, GATED>::COLS, 32};
     const cuuint32_t elem[2] = {1, 1};
     const CUtensorMapDataType type = sizeof(T) == 4 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_UINT16;
-    return fn(m, type, 2, p, dims, strides, box, elem, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_NONE,
+    return fn(m, type, 2, p, dims, strides, box, elem, CU_TENSOR_MAP_INTERLEAVE_NONE,
+              Box<T, GATED>::BYTES == 64 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_32B, CU_TENSOR_MAP_L2_PROMOTION_NONE,
               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 // Whether rows start on 16-byte boundaries, and `second` values on from there.
@@ -939,8 +1019,8 @@ int launch_tiles(const Product &p, WAITS waits)
     Targets to = {};
     // (a tensor map's pitch is below 2^40 bytes)
     const bool whole = whole_rows(r.y, r.ldy, 0) && r.ldy < (1ull << 37) && (!r.pre || (whole_rows(r.pre, r.ld_pre, p.N) && r.ld_pre < (1ull << 37)));
-    if (whole && !make_result_map(&to.y, r.y, p.M, p.N, r.ldy)) return OMC_ERR_CUDA;
-    if (whole && r.pre && (!make_result_map(&to.a, r.pre, p.M, p.N, r.ld_pre) || !make_result_map(&to.b, r.pre + p.N, p.M, p.N, r.ld_pre))) return OMC_ERR_CUDA;
+    if (whole && !make_result_map<T, GATED>(&to.y, r.y, p.M, p.N, r.ldy)) return OMC_ERR_CUDA;
+    if (whole && r.pre && (!make_result_map<T, GATED>(&to.a, r.pre, p.M, p.N, r.ld_pre) || !make_result_map<T, GATED>(&to.b, r.pre + p.N, p.M, p.N, r.ld_pre))) return OMC_ERR_CUDA;
     return note_cuda(el::launch(i8_tile_kernel<CG, BN, T, GATED, WAITS>, dim3(CG * (uint32_t)(tiles < units ? tiles : units)), C::THREADS, C::SMEM, CG, p.stream,
                                 map_x, map_w, to, r, (uint32_t)whole, waits));
 }
