@@ -8,8 +8,8 @@ namespace i8 {
 
 constexpr uint32_t LAID_OUT_SMS = 148, STEP_K = 128;
 
-// Tiles of rows of X x rows of W: 256 x 256 and 256 x 128 on a pair of SMs, 128 x 128 on one; 16, 32 or 64 x 128 of the small kernel.
-enum Kernel { PAIR_256, PAIR_128, ONE_128, SMALL_16, SMALL_32, SMALL_64 };
+// Tiles of rows of X x rows of W: 256 x 256 on a pair of SMs, 128 x 128 on one; 16, 32 or 64 x 128 of the small kernel.
+enum Kernel { PAIR_256, ONE_128, SMALL_16, SMALL_32, SMALL_64 };
 struct Schedule {
     Kernel kernel;
     uint32_t splits;        // CTAs, a cluster, among which a tile's K is divided (small kernel): 1, 2, 4 or 8
@@ -30,8 +30,8 @@ inline uint32_t splits_of(uint64_t tiles, uint64_t ksteps, uint64_t resident)
 // Whichever kernel takes least time by what was measured, in 1/100 us: `base` with one tile's results, `step` for each K step of 128, and a further tile of the
 // same SMs as long as its steps or the results of the one before, whichever is longer.
 //   256 x 256 on a pair    480 + 31 a step, 37 while results are stored, 290 for results (gated 550)
-//   256 x 128 on a pair    460 + 25, 175 (290)
 //   128 x 128 on an SM     390 + 24, 175 (290)
+//   (256 x 128 on a pair is no faster than 128 x 128 on an SM: 8.5 and 7.8 us at 512 x 2048 x 2048 BF16, 17.0 and 18.7 at 3000 x 2002 x 1000 FP32)
 //   small kernel           440 + 28 (two CTAs on an SM: 45), 90 more with divided K
 inline Schedule schedule_of(uint64_t M, uint64_t N, uint64_t K, bool gated)
 {
@@ -52,7 +52,6 @@ inline Schedule schedule_of(uint64_t M, uint64_t N, uint64_t K, bool gated)
         }
     };
     consider(ONE_128, tiles_of(M, N, 128, 128 / half), LAID_OUT_SMS, 390, 24, 24, gated ? 290 : 175);
-    consider(PAIR_128, tiles_of(M, N, 256, 128 / half), LAID_OUT_SMS / 2, 460, 25, 25, gated ? 290 : 175);
     consider(PAIR_256, tiles_of(M, N, 256, 256 / half), LAID_OUT_SMS / 2, 480, 31, 37, gated ? 550 : 290);
     return best;
 }

@@ -1044,7 +1044,6 @@ int launch_any(const Product &p, WAITS waits)
     const i8::Schedule s = i8::schedule_of(p.M, p.N, p.K, GATED);
     switch (s.kernel) {
     case i8::PAIR_256: return launch_tiles<2, 256, T, GATED>(p, waits);
-    case i8::PAIR_128: return launch_tiles<2, 128, T, GATED>(p, waits);
     case i8::ONE_128: return launch_tiles<1, 128, T, GATED>(p, waits);
     case i8::SMALL_16: return launch_small<16, T, GATED>(p, s.splits, waits);
     case i8::SMALL_32: return launch_small<32, T, GATED>(p, s.splits, waits);
