@@ -25,23 +25,26 @@ struct Gradients {
     struct Raw {
         i8::Piece<T, WHOLE> g, a, b;
     };
-    template <bool FULL>
     __device__ __forceinline__ void fetch(uint32_t row, uint32_t col, uint32_t cols, Raw &raw) const
     {
-        const bool in = FULL || i8::inside<T>(row, rows, col, cols);
+        const bool in = i8::inside<T>(row, rows, cols);
         const T *const p = pre + row * ld_pre + col;
         raw.g.load(dy + row * ld_dy + col, in);
         raw.a.load(p, in);
         raw.b.load(p + width, in);
     }
+    template <bool EDGE>
     __device__ __forceinline__ void fetch4(uint32_t row, uint32_t col, Raw *raw) const
     {
-        const T *p = dy + row * ld_dy + col, *q = pre + row * ld_pre + col;
+        const i8::Nearest<WHOLE> near(row, rows);
+        const uint32_t first = EDGE ? near.first() : row;
+        const T *p = dy + first * ld_dy + col, *q = pre + first * ld_pre + col;
 #pragma unroll
-        for (int i = 0; i < 4; ++i, p += ld_dy, q += ld_pre) {
+        for (int i = 0; i < 4; ++i) {
             raw[i].g.load(p, true);
             raw[i].a.load(q, true);
             raw[i].b.load(q + width, true);
+            if (!EDGE || near.on(i)) p += ld_dy, q += ld_pre;
         }
     }
     static __device__ __forceinline__ void make_with(const uint32_t *gs, const uint32_t *as, const uint32_t *bs, uint32_t (*out)[4])
@@ -67,11 +70,10 @@ struct Gradients {
             }
         }
     }
-    template <bool FULL>
     __device__ __forceinline__ void make(uint32_t row, uint32_t col, uint32_t cols, const Raw &raw, uint32_t (*out)[4]) const
     {
         uint32_t g[4], a[4], b[4];
-        const bool in = FULL || i8::inside<T>(row, rows, col, cols);
+        const bool in = WHOLE || i8::inside<T>(row, rows, cols);
         const T *const p = pre + row * ld_pre + col;
         raw.g.words(dy + row * ld_dy + col, cols - col, in, g);
         raw.a.words(p, cols - col, in, a);

@@ -48,6 +48,15 @@ inline uint64_t maxima_bytes(uint64_t rows, uint64_t cols, int out)
     return sets * out * ((cols + 7) / 8 * 8) * 4 + windows * ((rows + 3) / 4 * 4) * 4;
 }
 
+// A piece value by value, `left` of them at most, zeros behind: out of line, since the code of the usual path has to fit the instruction cache.
+template <typename T>
+__device__ __noinline__ uint4 piece_by_value(const T *at, uint32_t left)
+{
+    uint32_t w[4];
+    mx::load<T, false, PIECE<T>>(at, 0, left, w);
+    return make_uint4(w[0], w[1], w[2], w[3]);
+}
+
 // A piece on its way.  WHOLE, rows on 16-byte boundaries and a multiple of 16 bytes wide: its four words.  Else, of a piece that is `inside`, the two aligned
 // sixteens that hold it, which `words` shifts; the others `words` reads value by value.  (Loads are predicated, never one side of a branch: where registers
 // meet after a branch the compiler copies them, which waits for the load.  8192 x 8192 BF16, first kernel, 44 us with a branch, 31 us without.)
@@ -78,17 +87,36 @@ struct Piece {
             for (int i = 0; i < 5; ++i) u[i] = skip & 4 ? v[i + 1] : v[i];
 #pragma unroll
             for (int i = 0; i < 4; ++i) out[i] = sizeof(T) == 4 ? u[i] : __funnelshift_r(u[i], u[i + 1], (skip & 2) * 8);
-            if (!inside) mx::load<T, false, E>(at, 0, left, out);
+            if (!inside) {
+                const uint4 q = piece_by_value<T>(at, left);
+                out[0] = q.x, out[1] = q.y, out[2] = q.z, out[3] = q.w;
+            } else if (left < (uint32_t)E) {              // zeros behind the row's end
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const uint32_t n = left > (uint32_t)(i * E / 4) ? left - i * E / 4 : 0u;
+                    out[i] &= n >= (uint32_t)(E / 4) ? 0xFFFFFFFFu : n ? 0xFFFFu : 0u;
+                }
+            }
         }
     }
 };
-// Whether the two aligned sixteens around a piece lie inside its matrix: a whole piece of any row but the first and the last, of rows of 32 bytes
-// at least (the first begins in the row before it at the earliest, the second ends in the row behind it at the latest).
+// Whether the two aligned sixteens around a piece lie inside its matrix: in any row but the first and the last, of rows of 32 bytes at least (the first
+// begins in the row before it at the earliest, the second ends in the row behind it at the latest).
 template <typename T>
-__device__ __forceinline__ bool inside(uint32_t row, uint32_t rows, uint32_t col, uint32_t cols)
+__device__ __forceinline__ bool inside(uint32_t row, uint32_t rows, uint32_t cols)
 {
-    return row - 1u < rows - 2u && rows > 2u && col + PIECE<T> <= cols && cols >= 2 * PIECE<T>;
+    return row - 1u < rows - 2u && rows > 2u && cols >= 2 * PIECE<T>;
 }
+
+// Four rows from `row` on, each taken to the nearest one whose pieces may be loaded without a check: the first of them, and whether there is another row
+// to go on to behind row i.
+template <bool WHOLE>
+struct Nearest {
+    uint32_t low, high, row;
+    __device__ __forceinline__ Nearest(uint32_t r, uint32_t rows) : low(WHOLE ? 0u : 1u), high(WHOLE ? rows - 1 : rows - 2), row(r) {}
+    __device__ __forceinline__ uint32_t first() const { return min(max(row, low), high); }
+    __device__ __forceinline__ bool on(int i) const { return row + i >= low && row + i < high; }
+};
 
 // A matrix in memory.
 template <typename T_, bool WHOLE>
@@ -102,24 +130,26 @@ struct Matrix {
     struct Raw {
         Piece<T, WHOLE> x;
     };
-    // FULL: the place is known to be inside.
-    template <bool FULL>
     __device__ __forceinline__ void fetch(uint32_t row, uint32_t col, uint32_t cols, Raw &raw) const
     {
-        raw.x.load(x + row * ld + col, FULL || inside<T>(row, rows, col, cols));
+        raw.x.load(x + row * ld + col, inside<T>(row, rows, cols));
     }
-    // Four rows' pieces from one address on, all inside.
+    // Four rows' pieces, all inside, or (EDGE) from the rows nearest to them; not for matrices whose pieces are all read value by value (see inside).
+    template <bool EDGE>
     __device__ __forceinline__ void fetch4(uint32_t row, uint32_t col, Raw *raw) const
     {
-        const T *p = x + row * ld + col;
+        const Nearest<WHOLE> near(row, rows);
+        const T *p = x + (EDGE ? near.first() : row) * ld + col;
 #pragma unroll
-        for (int i = 0; i < 4; ++i, p += ld) raw[i].x.load(p, true);
+        for (int i = 0; i < 4; ++i) {
+            raw[i].x.load(p, true);
+            if (!EDGE || near.on(i)) p += ld;
+        }
     }
     // Of a place that was fetched.
-    template <bool FULL>
     __device__ __forceinline__ void make(uint32_t row, uint32_t col, uint32_t cols, const Raw &raw, uint32_t (*out)[4]) const
     {
-        raw.x.words(x + row * ld + col, cols - col, FULL || inside<T>(row, rows, col, cols), out[0]);
+        raw.x.words(x + row * ld + col, cols - col, WHOLE || inside<T>(row, rows, cols), out[0]);
     }
     __device__ __forceinline__ void emit(uint32_t, uint32_t, uint32_t, const uint32_t (*)[4]) const {}
 };
@@ -250,7 +280,7 @@ __global__ void __launch_bounds__(THREADS, ROWS_CTAS<SRC, P, THREADS>) rows_kern
     auto fetch = [&](uint32_t row, typename SRC::Raw *r) {
 #pragma unroll
         for (int p = 0; p < P; ++p)
-            if (row < rows && column(p) < cols) src.template fetch<false>(row, column(p), cols, r[p]);
+            if (row < rows && column(p) < cols) src.fetch(row, column(p), cols, r[p]);
     };
     const uint32_t step = place.shares * together;
     uint32_t base = place.share() * together, turn = 0;
@@ -265,7 +295,7 @@ __global__ void __launch_bounds__(THREADS, ROWS_CTAS<SRC, P, THREADS>) rows_kern
 #pragma unroll
             for (int p = 0; p < P; ++p) {
                 if (row < rows && column(p) < cols) {
-                    src.template make<false>(row, column(p), cols, raw[a][p], w[p]);
+                    src.make(row, column(p), cols, raw[a][p], w[p]);
                     src.emit(row, column(p), cols, w[p]);
                 } else {
 #pragma unroll
@@ -322,8 +352,8 @@ __global__ void __launch_bounds__(WIDE_THREADS) wide_rows_kernel(SRC src, uint32
         typename SRC::Raw raw;
         uint32_t w[OUT][4], top = 0u;
         for (uint32_t col = threadIdx.x * E; col < cols; col += WIDE_THREADS * E) {
-            src.template fetch<false>(row, col, cols, raw);
-            src.template make<false>(row, col, cols, raw, w);
+            src.fetch(row, col, cols, raw);
+            src.make(row, col, cols, raw, w);
             src.emit(row, col, cols, w);
 #pragma unroll
             for (int i = 0; i < OUT * 4; ++i) top = max_magnitude<T>(top, w[i / 4][i % 4] & MAGNITUDE<T>);
@@ -335,8 +365,8 @@ __global__ void __launch_bounds__(WIDE_THREADS) wide_rows_kernel(SRC src, uint32
         const Scale s = scale_of(top);
         int8_t *to = out.codes + row * out.pitch;
         for (uint32_t col = threadIdx.x * E; col < cols; col += WIDE_THREADS * E) {
-            src.template fetch<false>(row, col, cols, raw);
-            src.template make<false>(row, col, cols, raw, w);
+            src.fetch(row, col, cols, raw);
+            src.make(row, col, cols, raw, w);
 #pragma unroll
             for (int o = 0; o < OUT; ++o) {
                 uint32_t c[E / 4];
@@ -367,7 +397,7 @@ __global__ void __launch_bounds__(32 * MAXIMA_WARPS, SRC::HEAVY ? 2 : 3) maxima_
     auto fetch = [&](uint32_t row, typename SRC::Raw *r) {
 #pragma unroll
         for (int p = 0; p < P; ++p)
-            if (row < rows && column(p) < cols) src.template fetch<false>(row, column(p), cols, r[p]);
+            if (row < rows && column(p) < cols) src.fetch(row, column(p), cols, r[p]);
     };
 #pragma unroll
     for (int i = 0; i < P * OUT * 4; ++i) most[i / (OUT * 4)][i / 4 % OUT][i % 4] = 0u;
@@ -384,7 +414,7 @@ __global__ void __launch_bounds__(32 * MAXIMA_WARPS, SRC::HEAVY ? 2 : 3) maxima_
             for (int p = 0; p < P; ++p) {
                 if (column(p) < cols) {
                     uint32_t w[OUT][4];
-                    src.template make<false>(row, column(p), cols, raw[a][p], w);
+                    src.make(row, column(p), cols, raw[a][p], w);
                     src.emit(row, column(p), cols, w);
 #pragma unroll
                     for (int i = 0; i < OUT * 4; ++i) {
@@ -429,6 +459,15 @@ struct ColsOut {
     uint64_t pitch;
 };
 
+// A truth value that the compiler knows, and one that it does not.
+template <bool V>
+struct Known {
+    static constexpr bool value = V;
+};
+struct Asked {
+    bool value;
+};
+
 // Second kernel: blockIdx.x is a strip of sixteen pieces of columns and a share of the row tiles, the last ones first.  A thread takes four rows of a
 // piece at a time, a CTA a sweep of 32 rows; the loads of the next sweeps are on their way.
 template <typename SRC>
@@ -436,7 +475,7 @@ struct Strip {
     static constexpr int E = PIECE<typename SRC::T>, COLS = 16 * E, SWEEPS = SRC::OUT == 1 ? 4 : 2;     // 128 or 64 columns; sweeps of a tile
     static constexpr int AHEAD = SRC::OUT == 1 && !SRC::HEAVY ? 2 : 1;
     static constexpr int ROWS = 32 * SWEEPS, WORDS = ROWS / 4;                                         // of a tile; of a column of its codes
-    static constexpr int CTAS = SRC::OUT == 1 ? (SRC::HEAVY ? 4 : 5) : SRC::HEAVY == 2 ? 2 : 3;        // on an SM, as the registers allow
+    static constexpr int CTAS = SRC::OUT == 1 ? (SRC::HEAVY ? 4 : 5) : SRC::HEAVY == 2 ? 3 : 3;        // on an SM, as the registers allow
     static constexpr int WORDS_ALL = SRC::OUT * COLS * WORDS;
     // Column e of piece p is column e 16 + p of the tile in shared memory.  Its words are turned by the piece (an even number), so that a warp's
     // stores, sixteen pieces of two words each, fall into different banks.
@@ -462,19 +501,14 @@ __global__ void __launch_bounds__(STRIP_THREADS, Strip<SRC>::CTAS) codes_kernel(
     el::enter_stream_order();
     typename SRC::Raw raw[AHEAD][4];
     auto row_of = [&](uint32_t t, int k) { return t * S::ROWS + k * 32 + down * 4; };      // the first of four, in sweep k of tile t
-    const bool whole_strip = (strip + 1) * COLS <= cols;
-    // a tile that lies inside the matrix, where nothing needs a check (rows that start anywhere: off its first and last row)
-    auto full = [&](uint32_t t) {
-        return whole_strip && (SRC::WHOLE_ROWS ? (t + 1) * S::ROWS <= rows : t > 0 && (t + 1) * S::ROWS < rows && cols >= 2 * E);
-    };
+    const bool here = col < cols;
+    const bool loads = here && (SRC::WHOLE_ROWS || (rows > 2 && cols >= 2 * E));      // (else every piece is read value by value)
+    // whether all of a tile's rows are there and inside
+    auto full = [&](uint32_t t) { return SRC::WHOLE_ROWS ? (t + 1) * S::ROWS <= rows : t > 0 && (t + 1) * S::ROWS < rows; };
     auto fetch = [&](uint32_t t, int k, typename SRC::Raw *r) {
-        if (full(t)) {
-            src.fetch4(row_of(t, k), col, r);
-        } else {
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-                if (row_of(t, k) + i < rows && col < cols) src.template fetch<false>(row_of(t, k) + i, col, cols, r[i]);
-        }
+        if (!loads) return;
+        if (full(t)) src.template fetch4<false>(row_of(t, k), col, r);
+        else src.template fetch4<true>(row_of(t, k), col, r);
     };
     auto rows_of = [&](uint32_t t) {                               // a tile's rows' factors, a row a thread; the first strip stores the scales
         if constexpr (ROWS) {
@@ -494,31 +528,43 @@ __global__ void __launch_bounds__(STRIP_THREADS, Strip<SRC>::CTAS) codes_kernel(
     rows_of(end - 1);
     // the strip's magnitudes: eight threads share the sets of a piece, and join what they found in shared memory
     const uint32_t pieces = (cols + E - 1) / E;
-    uint4 *const found = reinterpret_cast<uint4 *>(tiles_smem);    // [8][16]
+    uint4 *const found = reinterpret_cast<uint4 *>(tiles_smem);    // [OUT][8][16]
+    static_assert(OUT * STRIP_THREADS * 4 <= 2 * S::WORDS_ALL, "");
+    auto join = [](uint4 &m, const uint4 &q) {
+        m.x = max_magnitude<T>(m.x, q.x), m.y = max_magnitude<T>(m.y, q.y);
+        m.z = max_magnitude<T>(m.z, q.z), m.w = max_magnitude<T>(m.w, q.w);
+    };
+    uint4 m[OUT];
 #pragma unroll
-    for (int o = 0; o < OUT; ++o) {
-        uint4 m = make_uint4(0u, 0u, 0u, 0u);
-        auto join = [&](const uint4 &q) {
-            m.x = max_magnitude<T>(m.x, q.x), m.y = max_magnitude<T>(m.y, q.y);
-            m.z = max_magnitude<T>(m.z, q.z), m.w = max_magnitude<T>(m.w, q.w);
-        };
-        if (col < cols)
-#pragma unroll 8
-            for (uint32_t i = down; i < in.sets; i += DOWN) join(in.cols[((uint64_t)i * OUT + o) * pieces + col / E]);
-        __syncthreads();
-        found[tid] = m;
-        __syncthreads();
-        if (down == 0) {
-            for (int i = 1; i < DOWN; ++i) join(found[i * 16 + piece]);
-            const uint32_t w[4] = {m.x, m.y, m.z, m.w};
+    for (int o = 0; o < OUT; ++o) m[o] = make_uint4(0u, 0u, 0u, 0u);
+    if (here) {
+        constexpr int BATCH = 8;                                   // sets on their way
+        const uint4 *from = in.cols + (uint64_t)down * OUT * pieces + col / E;
+        for (uint32_t i = down; i < in.sets; i += DOWN * BATCH) {
+            uint4 q[BATCH][OUT];
 #pragma unroll
-            for (int e = 0; e < E; ++e) {
-                const uint32_t bits = fp32_bits<T>(sizeof(T) == 4 ? w[e % 4] : w[e / 2] >> (16 * (e & 1)) & 0xFFFFu);
-                const Scale s = scale_of(bits);
-                factor[o * COLS + piece * E + e] = s.r;
-                if (s.nan()) any_nan = 1u;
-                if (begin == 0 && col + e < cols) out.scales[(uint64_t)o * cols + col + e] = s.s;
-            }
+            for (int j = 0; j < BATCH; ++j, from += (uint64_t)DOWN * OUT * pieces)
+#pragma unroll
+                for (int o = 0; o < OUT; ++o) q[j][o] = i + j * DOWN < in.sets ? from[(uint64_t)o * pieces] : make_uint4(0u, 0u, 0u, 0u);
+#pragma unroll
+            for (int j = 0; j < BATCH * OUT; ++j) join(m[j % OUT], q[j / OUT][j % OUT]);
+        }
+    }
+#pragma unroll
+    for (int o = 0; o < OUT; ++o) found[o * STRIP_THREADS + tid] = m[o];
+    __syncthreads();
+    if (down < OUT) {                                              // sixteen threads finish a half
+        const uint32_t o = down;
+        uint4 all = found[o * STRIP_THREADS + piece];
+        for (int i = 1; i < DOWN; ++i) join(all, found[o * STRIP_THREADS + i * 16 + piece]);
+        const uint32_t w[4] = {all.x, all.y, all.z, all.w};
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            const uint32_t bits = fp32_bits<T>(sizeof(T) == 4 ? w[e % 4] : w[e / 2] >> (16 * (e & 1)) & 0xFFFFu);
+            const Scale s = scale_of(bits);
+            factor[o * COLS + piece * E + e] = s.r;
+            if (s.nan()) any_nan = 1u;
+            if (begin == 0 && col + e < cols) out.scales[(uint64_t)o * cols + col + e] = s.s;
         }
     }
     __syncthreads();
@@ -530,36 +576,34 @@ __global__ void __launch_bounds__(STRIP_THREADS, Strip<SRC>::CTAS) codes_kernel(
 
     for (uint32_t t = end; t-- > begin;) {
         uint32_t *const tile = tiles_smem + (t & 1u) * S::WORDS_ALL;
-        const bool masked_rows = ROWS && nan_rows[t & 1u] == t + 1;
-        auto work = [&](auto inside_all) {
-            constexpr bool FULL = decltype(inside_all)::value;
-#pragma unroll(AHEAD == 1 ? 1 : SWEEPS)
-            for (int k = 0; k < SWEEPS; ++k) {
+        const bool masked_rows = ROWS && nan_rows[t & 1u] == t + 1, all_there = (strip + 1) * COLS <= cols && (t + 1) * S::ROWS <= rows;
+        auto work = [&](auto all) {
+            const bool all_there = all.value;
+#pragma unroll 1
+            for (int k0 = 0; k0 < SWEEPS; k0 += AHEAD)
+#pragma unroll
+            for (int kk = 0; kk < AHEAD; ++kk) {
                 constexpr int N = Word<T>::N;
+                const int k = k0 + kk;
+                const uint32_t row0 = row_of(t, k);
                 uint32_t w[4][OUT][4];
-                int8_t *to = nullptr;
-                float4 r4 = make_float4(0.f, 0.f, 0.f, 0.f);
-                if constexpr (ROWS) {
-                    to = out_r.codes + (uint64_t)row_of(t, k) * out_r.pitch;
-                    r4 = *reinterpret_cast<const float4 *>(&row_factor[t & 1u][k * 32 + down * 4]);
-                }
-                const float rs[4] = {r4.x, r4.y, r4.z, r4.w};
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    const uint32_t row = row_of(t, k) + i;
-                    if (FULL || (row < rows && col < cols)) {
-                        src.template make<FULL>(row, col, cols, raw[k % AHEAD][i], w[i]);
-                    } else {
+                    const bool there = here && row0 + i < rows;
+                    if (SRC::WHOLE_ROWS || there) src.make(row0 + i, col, cols, raw[kk][i], w[i]);
+                    if (!all_there)
 #pragma unroll
-                        for (int j = 0; j < OUT * 4; ++j) w[i][j / 4][j % 4] = 0u;
-                    }
+                        for (int j = 0; j < OUT * 4; ++j) w[i][j / 4][j % 4] = there ? w[i][j / 4][j % 4] : 0u;
                 }
-                if (k + AHEAD < SWEEPS) fetch(t, k + AHEAD, raw[k % AHEAD]);
-                else if (t > begin) fetch(t - 1, k + AHEAD - SWEEPS, raw[k % AHEAD]);
-                    if constexpr (ROWS) {
+                if (k + AHEAD < SWEEPS) fetch(t, k + AHEAD, raw[kk]);
+                else if (t > begin) fetch(t - 1, k + AHEAD - SWEEPS, raw[kk]);
+                if constexpr (ROWS) {
+                    int8_t *to = out_r.codes + (uint64_t)row0 * out_r.pitch;
+                    const float4 r4 = *reinterpret_cast<const float4 *>(&row_factor[t & 1u][k * 32 + down * 4]);
+                    const float rs[4] = {r4.x, r4.y, r4.z, r4.w};
 #pragma unroll
                     for (int i = 0; i < 4; ++i, to += out_r.pitch) {
-                        if (!FULL && row_of(t, k) + i >= rows) break;
+                        if (!all_there && row0 + i >= rows) break;
 #pragma unroll
                         for (int o = 0; o < OUT; ++o) {
                             uint32_t c[E / 4];
@@ -567,8 +611,7 @@ __global__ void __launch_bounds__(STRIP_THREADS, Strip<SRC>::CTAS) codes_kernel(
                             if (masked_rows && rs[i] == 0.f)
 #pragma unroll
                                 for (int j = 0; j < E / 4; ++j) c[j] = 0u;
-                            if (FULL && OUT == 1) store_whole<E>(to + col, c);
-                            else store_row_piece<E, OUT>(to, o, col, cols, out_r.pitch, c);
+                            store_row_piece<E, OUT>(to, o, col, cols, out_r.pitch, c);
                         }
                         if (OUT > 1 && strip == strips - 1 && piece == 0) pad_row(to, (uint64_t)OUT * cols, out_r.pitch);
                     }
@@ -598,8 +641,13 @@ __global__ void __launch_bounds__(STRIP_THREADS, Strip<SRC>::CTAS) codes_kernel(
                     }
             }
         };
-        if (full(t)) work(std::true_type());
-        else work(std::false_type());
+        // compiled with and without the checks where that is faster (gated layer, 8192 x 8192 BF16: 141 and 154 us; else the code is better short)
+        if constexpr (OUT > 1 && SRC::WHOLE_ROWS) {
+            if (all_there) work(Known<true>());
+            else work(Known<false>());
+        } else {
+            work(Asked{all_there});
+        }
         if (t > begin) rows_of(t - 1);
         __syncthreads();
         const uint32_t *const from = tile + slot * WORDS + ((chunk ^ (turned >> 2)) * 4);
