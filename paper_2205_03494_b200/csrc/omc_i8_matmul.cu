@@ -1006,6 +1006,14 @@ bool whole_rows(const T *p, uint64_t ld, uint64_t second)
     return ((uint64_t)reinterpret_cast<uintptr_t>(p) | ld * sizeof(T) | second * sizeof(T)) % 16 == 0;
 }
 
+// Whether every row of the results can go out in boxes (a tensor map's pitch is below 2^40 bytes).
+template <typename T>
+bool whole_results(const Product &p)
+{
+    return whole_rows(static_cast<const T *>(p.y), p.ldy, 0) && p.ldy < (1ull << 37) &&
+           (!p.pre || (whole_rows(static_cast<const T *>(p.pre), p.ld_pre, p.N) && p.ld_pre < (1ull << 37)));
+}
+
 template <int CG, int BN, typename T, bool GATED, typename WAITS>
 int launch_tiles(const Product &p, WAITS waits)
 {
@@ -1017,8 +1025,7 @@ int launch_tiles(const Product &p, WAITS waits)
     if (tiles >= (1ull << 31)) return OMC_ERR_INVALID_ARG;
     const Result<T> r = result_of<T>(p);
     Targets to = {};
-    // (a tensor map's pitch is below 2^40 bytes)
-    const bool whole = whole_rows(r.y, r.ldy, 0) && r.ldy < (1ull << 37) && (!r.pre || (whole_rows(r.pre, r.ld_pre, p.N) && r.ld_pre < (1ull << 37)));
+    const bool whole = whole_results<T>(p);
     if (whole && !make_result_map<T, GATED>(&to.y, r.y, p.M, p.N, r.ldy)) return OMC_ERR_CUDA;
     if (whole && r.pre && (!make_result_map<T, GATED>(&to.a, r.pre, p.M, p.N, r.ld_pre) || !make_result_map<T, GATED>(&to.b, r.pre + p.N, p.M, p.N, r.ld_pre))) return OMC_ERR_CUDA;
     return note_cuda(el::launch(i8_tile_kernel<CG, BN, T, GATED, WAITS>, dim3(CG * (uint32_t)(tiles < units ? tiles : units)), C::THREADS, C::SMEM, CG, p.stream,
@@ -1041,7 +1048,7 @@ int launch_small(const Product &p, uint32_t splits, WAITS waits)
 template <typename T, bool GATED, typename WAITS>
 int launch_any(const Product &p, WAITS waits)
 {
-    const i8::Schedule s = i8::schedule_of(p.M, p.N, p.K, GATED);
+    const i8::Schedule s = i8::schedule_of(p.M, p.N, p.K, GATED, whole_results<T>(p));
     switch (s.kernel) {
     case i8::PAIR_256: return launch_tiles<2, 256, T, GATED>(p, waits);
     case i8::ONE_128: return launch_tiles<1, 128, T, GATED>(p, waits);

@@ -26,12 +26,13 @@ int main()
     }
     const uint64_t lengths[] = {1, 31, 128, 129, 512, 1000, 1024, 1025, 2048, 4096, 8192, 100000, (1ull << 17) - 1};
     bool chosen[2][5] = {};
-    for (int gated = 0; gated < 2; ++gated)
+    for (int form = 0; form < 4; ++form)
         for (uint64_t M : sizes)
             for (uint64_t N : sizes)
                 for (uint64_t K : lengths) {
+                    const int gated = form % 2;
                     if (M > 128ull * 65535 || (gated && N >= (1ull << 30))) continue;
-                    const Schedule s = schedule_of(M, N, K, gated != 0);
+                    const Schedule s = schedule_of(M, N, K, gated != 0, form >= 2);
                     const uint64_t steps = (K + STEP_K - 1) / STEP_K;
                     chosen[gated][s.kernel] = true;
                     if (s.kernel < SMALL_16) {

@@ -36,7 +36,7 @@ def values(codes, scales):
 
 def product(xc, xs, wc, ws):
     """FP32 values of the product: (sum * sx) * sw, each step rounded; the first one as if FP32 had no largest value."""
-    total = xc.astype(np.int64) @ wc.astype(np.int64).T
+    total = (xc.astype(np.float64) @ wc.astype(np.float64).T).astype(np.int64)       # whole numbers below 2^53: exact
     assert np.abs(total).max() < 2 ** 31
     with np.errstate(over="ignore", invalid="ignore"):
         sx = xs.astype(np.float64)
