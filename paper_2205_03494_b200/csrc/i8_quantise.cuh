@@ -9,7 +9,13 @@
 // from one more read: four rows of a piece a thread; along the rows they go out as they are, along the columns the codes of four rows make a word that
 // goes to shared memory, and from there 64 or 128 bytes of a column at a time to memory.  It starts with the rows that the first kernel read last,
 // which the L2 cache still holds.
+// Whole rows along both axes: the first kernel is the one of the rows alone, which has each row's codes on the way, and leaves the columns' maxima.
 // Magnitudes are compared as bit patterns, two 16-bit values in one instruction: their order is that of the values, Inf and NaN on top.
+//
+// Along the rows memory bounds it: 16384 x 8192 BF16 61.5 us, 6.55 TB/s of values and codes, the rate of a copy.  Along both axes (8192 x 8192 BF16 70.7 us,
+// 8192 x 2048 FP32 29.8) the values' second read takes what the first did as far as L2 does not hold them, and codes_kernel the more, whose
+// stores of 64 or 128 bytes of a column do not fill its SMs' memory pipes; made in codes_kernel too, the rows' codes cost 83 us instead of 71.  Rows off
+// the 16-byte boundaries: 8192 x 8191 BF16 48.6 us along the rows, 130 along both axes (two aligned loads for a piece, which are shifted together).
 #pragma once
 #include <type_traits>
 
@@ -475,7 +481,7 @@ struct Strip {
     static constexpr int E = PIECE<typename SRC::T>, COLS = 16 * E, SWEEPS = SRC::OUT == 1 ? 4 : 2;     // 128 or 64 columns; sweeps of a tile
     static constexpr int AHEAD = SRC::OUT == 1 && !SRC::HEAVY ? 2 : 1;
     static constexpr int ROWS = 32 * SWEEPS, WORDS = ROWS / 4;                                         // of a tile; of a column of its codes
-    static constexpr int CTAS = SRC::OUT == 1 ? (SRC::HEAVY ? 4 : 5) : SRC::HEAVY == 2 ? 3 : 3;        // on an SM, as the registers allow
+    static constexpr int CTAS = SRC::OUT == 1 ? (SRC::HEAVY ? 4 : 5) : 3;        // on an SM, as the registers allow
     static constexpr int WORDS_ALL = SRC::OUT * COLS * WORDS;
     // Column e of piece p is column e 16 + p of the tile in shared memory.  Its words are turned by the piece (an even number), so that a warp's
     // stores, sixteen pieces of two words each, fall into different banks.

@@ -161,13 +161,17 @@ __device__ __forceinline__ void values16(const uint32_t *v, const i8::RowScale &
 
 // ---- tiles of 128 or 256 rows of X ---------------------------------------------------------------------
 // CG CTAs, a cluster, share a tile of 128 CG rows of X by BN rows of W (gated: BN / 2 of either half).  With two, each holds 128 rows of X and
-// BN / 2 rows of W for a K step (32 KB for the largest tile, six steps on their way), the leader issues products of 256 x BN x 32 whose upper half
+// BN / 2 rows of W for a K step (32 KB for the largest tile, five steps on their way), the leader issues products of 256 x BN x 32 whose upper half
 // accumulates in its own tensor memory and whose lower half in its peer's, and each CTA stores its 128 rows.  In the gated layer the accumulator's
 // first BN / 2 columns are a, the others b: with two CTAs the leader holds the gate's rows and its peer the same rows of the other half.
 // Barriers as their waiters need them: full (in the leader, the bytes of both CTAs' copies), empty and acc_full (in each CTA, a commit
 // reaches both), acc_empty (in the leader, an arrival of each of the warps that store results).
 // Every wait is bounded, and a role whose wait ran out leaves its loop, so that both CTAs reach the closing barrier on every path.
 // Tensor memory is taken after the kernel before on the stream has finished and let go after the products.
+// The tensor cores bound long sums: 16384 x 2048 x 8192 BF16 162 us in bursts, 3.4 POP/s (twice the rate measured of BF16 products is 3.2), 8192 x 2048 x 8192 92 us;
+// for seconds the board's power does (about 1 kW).  Short sums are bound by results: 8192 x 8192 x 256 BF16 40 us, of which 128 MB of results take
+// 20 at the copy rate and the sums 11; gated 8192 x 8192 x 2048 BF16 with what is kept 209 us (188 without), products alone 171.
+// A tile's results leave tensor memory while the next tile's products are made: two accumulators, 512 columns for the largest tile.
 template <int CG, int BN, bool GATED>
 struct Tile {
     static constexpr int W_ROWS = BN / CG;                           // of a CTA
@@ -617,6 +621,9 @@ i8_tile_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant_
 // A CTA has one tile of 128 rows of W (gated: of either half of W, with an accumulator each) by NT rows of X, or a range of its K steps.
 // With a divided K each CTA of the cluster owns a share of the tile's rows of X and gets the others' sums of these (stores to distributed
 // shared memory).  Lanes of tensor memory run along Y's contiguous dimension: a warp's store is 32 neighbouring values.
+// Bound by latency: without steps a CTA takes 2.5 us (gated 3.5), a step 0.25 (0.39), as copies, products and results follow one another.  16 x 8192 x 2048 BF16 5.9 us (W's 16.8 MB take 2.6 at the copy
+// rate), 64 x 2048 x 8192 8.0 us, 77 x 777 x 1000 5.3 us (8-fold divided K).  (With all of an SM's shared memory for one gated CTA of 16 or 32 rows
+// 16 x 8192 x 2048 takes 11.4 us, with two CTAs an SM 7.2.)
 template <int NT, bool GATED>
 struct Small {
     static constexpr int W_TILES = GATED ? 2 : 1, TILE_X = NT * BK;
@@ -823,6 +830,9 @@ i8_small_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant
 }
 
 // ---- up to four rows of X --------------------------------------------------------------------------------
+// W is read once, sixteen bytes a lane, and multiplied with dp4a against X's codes in shared memory; a warp adds up its lanes' sums at the end of its four rows.  Bound by
+// W's bytes: 1 x 8192 x 2048 with quantisation 3.6 us (4.7 TB/s; 2.6 at the copy rate), four rows 5.9 us (dp4a and reading X from shared memory), gated
+// 1 x 2048 x 512 2.5 us.
 constexpr int ROWS_THREADS = 256, ROWS_WARPS = 8, W_ROWS = 4, CHUNKS = 4;      // W rows of a warp at a time; 512-byte chunks on their way
 
 // Rows of X in memory, quantised already or not.
