@@ -13,9 +13,9 @@
 // Magnitudes are compared as bit patterns, two 16-bit values in one instruction: their order is that of the values, Inf and NaN on top.
 //
 // Along the rows memory bounds it: 16384 x 8192 BF16 61.5 us, 6.55 TB/s of values and codes, the rate of a copy.  Along both axes (8192 x 8192 BF16 70.7 us,
-// 8192 x 2048 FP32 29.8) the values' second read takes what the first did as far as L2 does not hold them, and codes_kernel the more, whose
-// stores of 64 or 128 bytes of a column do not fill its SMs' memory pipes; made in codes_kernel too, the rows' codes cost 83 us instead of 71.  Rows off
-// the 16-byte boundaries: 8192 x 8191 BF16 48.6 us along the rows, 130 along both axes (two aligned loads for a piece, which are shifted together).
+// 8192 x 2048 FP32 29.8) the values are read twice and each kernel falls short of the memory's rate, 36 us each: the first issues 60 % of what it could, the second
+// waits for loads, its two tiles in shared memory leaving five CTAs of four warps an SM.  (With the rows' codes made in the second: 83 us instead of 71.)  Rows off
+// the 16-byte boundaries: 8192 x 8191 BF16 48.6 us along the rows, 130 along both axes (two aligned loads for a piece, shifted together; 109 and 124 registers).
 #pragma once
 #include <type_traits>
 

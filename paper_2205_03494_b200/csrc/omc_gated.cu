@@ -4,8 +4,8 @@
 // layer's backward pass take: (da | db) is made again in the second kernel instead of being written and read (16 bytes a value
 // of dy for 16-bit types instead of 22).
 // The matrix alone is bound by memory: 8192 x 8192 BF16 105 us, 6.4 TB/s.  With the codes along both axes 8192 x 8192 BF16 takes 223 us, 4.8 TB/s of what both
-// kernels read and write (maxima 77, codes 141): the exponential, reciprocal and two roundings of each value are computed twice, at three CTAs an SM
-// the registers allow.  Rows off the 16-byte boundaries: 491 us at 8192 x 8191.
+// kernels read and write (maxima 77, codes 141): the second kernel waits for the latencies of its arithmetic, 168 registers leaving three CTAs of four warps an SM (with
+// four and fewer registers 228 us).  Rows off the 16-byte boundaries: 491 us at 8192 x 8191.
 #include <cuda_runtime.h>
 
 #include "element.cuh"

@@ -831,7 +831,7 @@ i8_small_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant
 
 // ---- up to four rows of X --------------------------------------------------------------------------------
 // W is read once, sixteen bytes a lane, and multiplied with dp4a against X's codes in shared memory; a warp adds up its lanes' sums at the end of its four rows.  Bound by
-// W's bytes: 1 x 8192 x 2048 with quantisation 3.6 us (4.7 TB/s; 2.6 at the copy rate), four rows 5.9 us (dp4a and reading X from shared memory), gated
+// W's bytes: 1 x 8192 x 2048 with quantisation 3.6 us (4.7 TB/s; 2.6 at the copy rate), four rows 5.9 us, gated
 // 1 x 2048 x 512 2.5 us.
 constexpr int ROWS_THREADS = 256, ROWS_WARPS = 8, W_ROWS = 4, CHUNKS = 4;      // W rows of a warp at a time; 512-byte chunks on their way
 
