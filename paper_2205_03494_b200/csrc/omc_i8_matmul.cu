@@ -830,9 +830,10 @@ i8_small_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant
 }
 
 // ---- up to four rows of X --------------------------------------------------------------------------------
-// W is read once, sixteen bytes a lane, and multiplied with dp4a against X's codes in shared memory; a warp adds up its lanes' sums at the end of its four rows.  Bound by
-// W's bytes: 1 x 8192 x 2048 with quantisation 3.6 us (4.7 TB/s; 2.6 at the copy rate), four rows 5.9 us, gated
-// 1 x 2048 x 512 2.5 us.
+// W is read once, sixteen bytes a lane, and multiplied with dp4a against X's codes in shared memory; a chunk's registers take the next one as soon as they are free, and
+// a warp adds up its lanes' sums at the end of its four rows.  Bound by W's bytes: 1 x 8192 x 2048 with quantisation 3.4 us (4.9 TB/s; 2.6 at the copy rate),
+// 1 x 32768 x 4096 23.3 us (5.8 TB/s), four rows against 8192 x 2048 5.7 us, gated 1 x 2048 x 512 2.3 us.  (Neighbouring rows of W in the warps of a CTA, so that
+// some SMs have twice the others': 1 x 2048 x 8192 6.3 us, now 5.7.)
 constexpr int ROWS_THREADS = 256, ROWS_WARPS = 8, W_ROWS = 4, CHUNKS = 4;      // W rows of a warp at a time; 512-byte chunks on their way
 
 // Rows of X in memory, quantised already or not.
@@ -934,7 +935,7 @@ i8_rows_kernel(SOURCE source, const int8_t *w_codes, const float *w_scales, void
     __shared__ uint32_t slots[MT * ROWS_WARPS];
     const uint32_t pitch = (uint32_t)i8::row_bytes(K), lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const uint32_t tasks = (N + OUTS - 1) / OUTS, step = gridDim.x * ROWS_WARPS;
-    uint32_t task = blockIdx.x * ROWS_WARPS + warp;
+    uint32_t task = blockIdx.x + warp * gridDim.x;        // every SM the same number of them, within one a CTA
     el::enter_stream_order();
     uint4 w[CHUNKS][W_ROWS];
     // row r of W of a task: gated, the gate's rows first; rows that do not exist are the last one again
@@ -942,16 +943,17 @@ i8_rows_kernel(SOURCE source, const int8_t *w_codes, const float *w_scales, void
         const uint32_t n = min(t * OUTS + r % OUTS, N - 1) + (GATED && r >= OUTS ? N : 0u);
         return w_codes + (uint64_t)n * pitch;
     };
-    auto fetch = [&](uint32_t t, uint32_t k0) {
+    auto fetch = [&](uint32_t t, uint32_t k0, int c) {
 #pragma unroll
-        for (int c = 0; c < CHUNKS; ++c)
-#pragma unroll
-            for (int r = 0; r < W_ROWS; ++r) {
-                const uint32_t k = k0 + c * 512 + lane * 16;
-                w[c][r] = k < pitch ? *reinterpret_cast<const uint4 *>(row_of(t, r) + k) : make_uint4(0u, 0u, 0u, 0u);
-            }
+        for (int r = 0; r < W_ROWS; ++r) {
+            const uint32_t k = k0 + c * 512 + lane * 16;
+            w[c][r] = k < pitch ? *reinterpret_cast<const uint4 *>(row_of(t, r) + k) : make_uint4(0u, 0u, 0u, 0u);
+        }
     };
-    if (task < tasks) fetch(task, 0);                      // on its way while X is quantised
+    if (task < tasks) {                                    // on its way while X is quantised
+#pragma unroll
+        for (int c = 0; c < CHUNKS; ++c) fetch(task, 0, c);
+    }
     bring_rows<MT>(source, M, K, pitch, codes, scales, slots);
     for (; task < tasks; task += step) {
         const uint32_t n = task * OUTS + lane / MT, m = lane % MT;
@@ -961,6 +963,7 @@ i8_rows_kernel(SOURCE source, const int8_t *w_codes, const float *w_scales, void
 #pragma unroll
         for (int i = 0; i < W_ROWS * MT; ++i) acc[i / MT][i % MT] = 0;
         for (uint32_t k0 = 0; k0 < pitch; k0 += CHUNKS * 512) {
+            const bool more = k0 + CHUNKS * 512 < pitch;   // of these rows of W
 #pragma unroll
             for (int c = 0; c < CHUNKS; ++c) {
                 const uint32_t k = k0 + c * 512 + lane * 16;
@@ -976,9 +979,8 @@ i8_rows_kernel(SOURCE source, const int8_t *w_codes, const float *w_scales, void
                             acc[r][m] = __dp4a((int)w[c][r].w, (int)x.w, acc[r][m]);
                         }
                     }
+                if (more || task + step < tasks) fetch(more ? task : task + step, more ? k0 + CHUNKS * 512 : 0u, c);
             }
-            if (k0 + CHUNKS * 512 < pitch) fetch(task, k0 + CHUNKS * 512);
-            else if (task + step < tasks) fetch(task + step, 0);
         }
         int32_t a = 0, b = 0;                              // lane i < OUTS MT has the sums of column i / MT, row i mod MT
 #pragma unroll
@@ -1130,8 +1132,8 @@ int launch_rows(const Product &p, const SOURCE &source)
 {
     const uint32_t smem = MT * (uint32_t)i8::row_bytes(p.K);
     if (const int rc = el::allow_smem<i8_rows_kernel<MT, GATED, SOURCE>>(smem)) return rc;
-    const uint32_t outs = GATED ? W_ROWS / 2 : W_ROWS, tasks = (p.N + outs - 1) / outs, ctas = (tasks + ROWS_WARPS - 1) / ROWS_WARPS, most = 2 * DEFAULT_SMS;
-    return note_cuda(el::launch(i8_rows_kernel<MT, GATED, SOURCE>, dim3(ctas < most ? ctas : most), ROWS_THREADS, smem, 1, p.stream, source, p.w_codes,
+    const uint32_t outs = GATED ? W_ROWS / 2 : W_ROWS, tasks = (p.N + outs - 1) / outs, most = 2 * DEFAULT_SMS;
+    return note_cuda(el::launch(i8_rows_kernel<MT, GATED, SOURCE>, dim3(tasks < most ? tasks : most), ROWS_THREADS, smem, 1, p.stream, source, p.w_codes,
                                 p.w_scales, p.y, p.type, p.ldy, p.pre, p.ld_pre, p.M, p.N, p.K, p.act));
 }
 template <bool GATED, typename SOURCE>
