@@ -130,7 +130,10 @@ template <int ACT>
 __device__ __forceinline__ void gate16(const float *a, const float *b, float *y)
 {
 #pragma unroll
-    for (int j = 0; j < 16; ++j) y[j] = gate::act<ACT>(a[j]) * b[j];
+    for (int j = 0; j < 16; j += 2) {
+        const float2 v = el::mul2(gate::act2<ACT>(make_float2(a[j], a[j + 1])), make_float2(b[j], b[j + 1]));
+        y[j] = v.x, y[j + 1] = v.y;
+    }
 }
 __device__ __forceinline__ void gate16(int act, const float *a, const float *b, float *y)
 {
@@ -140,7 +143,8 @@ __device__ __forceinline__ void gate16(int act, const float *a, const float *b, 
 }
 __device__ __forceinline__ float gate1(int act, float a, float b)
 {
-    return (act == OMC_GATE_SILU ? gate::act<OMC_GATE_SILU>(a) : act == OMC_GATE_SIGMOID ? gate::act<OMC_GATE_SIGMOID>(a) : gate::act<OMC_GATE_GELU>(a)) * b;
+    const float2 aa = el::twice(a);
+    return (act == OMC_GATE_SILU ? gate::act2<OMC_GATE_SILU>(aa) : act == OMC_GATE_SIGMOID ? gate::act2<OMC_GATE_SIGMOID>(aa) : gate::act2<OMC_GATE_GELU>(aa)).x * b;
 }
 // Sixteen sums of a row as values; ws: the columns' scales, in shared memory.
 __device__ __forceinline__ void values16(const uint32_t *v, const i8::RowScale &x, bool any_big, const float4 *ws, float *f)
