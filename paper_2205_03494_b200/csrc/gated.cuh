@@ -60,7 +60,7 @@ struct Gradients {
                 Word<T>::unpack(bs[i + j], b + j);
             }
             float2 v, d;
-            gate::act_slope2<ACT>(make_float2(a[0], a[1]), v, d);
+            gate::act_slope2<ACT, sizeof(T) == 4>(make_float2(a[0], a[1]), v, d);
             const float2 g2 = make_float2(g[0], g[1]), da = el::mul2(el::mul2(g2, make_float2(b[0], b[1])), d), db = el::mul2(g2, v);
             const float x[2] = {da.x, da.y}, y[2] = {db.x, db.y};
 #pragma unroll

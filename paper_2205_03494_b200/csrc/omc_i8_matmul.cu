@@ -126,25 +126,29 @@ struct Result {
     uint32_t *status;
 };
 
-template <int ACT>
+template <int ACT, bool FINE>
 __device__ __forceinline__ void gate16(const float *a, const float *b, float *y)
 {
 #pragma unroll
     for (int j = 0; j < 16; j += 2) {
-        const float2 v = el::mul2(gate::act2<ACT>(make_float2(a[j], a[j + 1])), make_float2(b[j], b[j + 1]));
+        const float2 v = el::mul2(gate::act2<ACT, FINE>(make_float2(a[j], a[j + 1])), make_float2(b[j], b[j + 1]));
         y[j] = v.x, y[j + 1] = v.y;
     }
 }
+// FINE: results are FP32 numbers.
+template <bool FINE>
 __device__ __forceinline__ void gate16(int act, const float *a, const float *b, float *y)
 {
-    if (act == OMC_GATE_SILU) gate16<OMC_GATE_SILU>(a, b, y);
-    else if (act == OMC_GATE_SIGMOID) gate16<OMC_GATE_SIGMOID>(a, b, y);
-    else gate16<OMC_GATE_GELU>(a, b, y);
+    if (act == OMC_GATE_SILU) gate16<OMC_GATE_SILU, FINE>(a, b, y);
+    else if (act == OMC_GATE_SIGMOID) gate16<OMC_GATE_SIGMOID, FINE>(a, b, y);
+    else gate16<OMC_GATE_GELU, FINE>(a, b, y);
 }
+template <bool FINE>
 __device__ __forceinline__ float gate1(int act, float a, float b)
 {
     const float2 aa = el::twice(a);
-    return (act == OMC_GATE_SILU ? gate::act2<OMC_GATE_SILU>(aa) : act == OMC_GATE_SIGMOID ? gate::act2<OMC_GATE_SIGMOID>(aa) : gate::act2<OMC_GATE_GELU>(aa)).x * b;
+    return (act == OMC_GATE_SILU ? gate::act2<OMC_GATE_SILU, FINE>(aa)
+            : act == OMC_GATE_SIGMOID ? gate::act2<OMC_GATE_SIGMOID, FINE>(aa) : gate::act2<OMC_GATE_GELU, FINE>(aa)).x * b;
 }
 // Sixteen sums of a row as values; ws: the columns' scales, in shared memory.
 __device__ __forceinline__ void values16(const uint32_t *v, const i8::RowScale &x, bool any_big, const float4 *ws, float *f)
@@ -517,7 +521,7 @@ i8_tile_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant_
                         tmem_load16(acc + c + 16, v);
                         tmem_load16(acc + TN + c + 16, u);
                     }
-                    gate16(o.act, a, b, y);
+                    gate16<sizeof(T) == 4>(o.act, a, b, y);
                     const uint32_t col = col0 + c;
                     static_assert(PER_BOX == 16, "");
                     if (boxed(col)) {
@@ -778,7 +782,7 @@ i8_small_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant
                                     o.pre[m * o.ld_pre + n] = el::from_float<T>(a);
                                     o.pre[m * o.ld_pre + o.N + n] = el::from_float<T>(b);
                                 }
-                                o.y[m * o.ldy + n] = el::from_float<T>(gate1(o.act, a, b));
+                                o.y[m * o.ldy + n] = el::from_float<T>(gate1<sizeof(T) == 4>(o.act, a, b));
                             } else {
                                 o.y[m * o.ldy + n] = el::from_float<T>(a);
                             }
@@ -821,7 +825,7 @@ i8_small_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant
                             o.pre[m * o.ld_pre + col] = el::from_float<T>(fa);
                             o.pre[m * o.ld_pre + o.N + col] = el::from_float<T>(fb);
                         }
-                        o.y[m * o.ldy + col] = el::from_float<T>(gate1(o.act, fa, fb));
+                        o.y[m * o.ldy + col] = el::from_float<T>(gate1<sizeof(T) == 4>(o.act, fa, fb));
                     } else {
                         o.y[m * o.ldy + col] = el::from_float<T>(fa);
                     }
@@ -1002,7 +1006,7 @@ i8_rows_kernel(SOURCE source, const int8_t *w_codes, const float *w_scales, void
                     put(type, pre, m * ld_pre + n, fa);
                     put(type, pre, m * ld_pre + N + n, fb);
                 }
-                put(type, y, m * ldy + n, gate1(act, fa, fb));
+                put(type, y, m * ldy + n, type == OMC_TYPE_F32 ? gate1<true>(act, fa, fb) : gate1<false>(act, fa, fb));
             } else {
                 put(type, y, m * ldy + n, fa);
             }

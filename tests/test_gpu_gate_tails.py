@@ -1,10 +1,14 @@
 """The gated layer where its activations are small: results relative to themselves, far into the tails, against the formulas in 64 bits.
 
 Errors in units u = 2^-23, relative; the hardware's exponential of 2 is off by 2 of its last places and its reciprocal by 1 (at most u each).
-  e = e^(-a^2 / 2): 2 and a last sum's half, the exponent being held in two numbers.
-  P: the tail Q e has a polynomial Q off by 0.6 where it is exact, and by 4.4 with its roundings and those of t; e's 2.5 and a product's half: 7.5.  Above 0
-      P = 1 - tail, the tail being the smaller one, and half a unit more: 8.
-  y = a P b: two products, half a unit each."""
+  e = e^-|a| or e^(-a^2 / 2), as the square of its root: 2 twice, the square's half, and half for what the exponent's rounding left out: 5.  Where the result has 16
+      bits that is not done: the exponent's half and its constant's 0.11 make |a| 0.61 instead, a^2 / 2 those and the square's half, a^2 0.56.
+  P: the tail Q e has a polynomial Q off by 0.6 where it is exact, and by 4.4 with its roundings and those of t; e's and a product's half.  Above 0
+      P = 1 - tail, the tail being the smaller one, and half a unit more: e's + 5.4.
+  r = 1 / (1 + e): e's error enters with e / (1 + e) <= 1 / (1 + e); the sum's half and the reciprocal's 1: e's + 1.5.
+  The larger one of s and 1 - s is r; the smaller one e r: e's error with 1 / (1 + e), the other two, and a product's half: e's + 2.
+  y = act(a) b, act = a P or a s: two products, half a unit each (of the sigmoid one).
+Absolute: where e^-|a| is no normal number it is off by a subnormal step of FP32 or two, and s with it; where the result has 16 bits it is then 0."""
 import numpy as np
 import pytest
 import torch
@@ -20,9 +24,20 @@ LEAST = {"f32": 2.0 ** -149, "f16": 2.0 ** -24, "bf16": 2.0 ** -133}      # the 
 ACTS = {"sigmoid": omc.GATE_SIGMOID, "silu": omc.GATE_SILU, "gelu": omc.GATE_GELU}
 
 
-def act_units(name, a):
+def e_units(name, a, ty):
+    if ty == "f32":
+        return 5.0
+    return 4.5 + (0.56 * a * a if name == "gelu" else 0.61 * np.abs(a))
+
+
+def least_of(ty):
+    """Absolute error of s and 1 - s."""
+    return 3 * LEAST["f32"] if ty == "f32" else 2.0 ** -126
+
+
+def act_units(name, a, ty):
     """Relative error of act(a), in u."""
-    return 8 + 0.5 + 0 * a
+    return e_units(name, a, ty) + {"gelu": 5.4 + 0.5, "sigmoid": 2.0, "silu": 2.0 + 0.5}[name]
 
 
 def gated(M, low, high, name, ty, value=1.0):
@@ -44,10 +59,12 @@ def gated(M, low, high, name, ty, value=1.0):
 
 
 def check_relative(got, want, units, ty, least):
-    """Relative: `units` u and half a step of the type; absolute: `least`, and a subnormal step of the type."""
+    """Relative: `units` u and half a step of the type; absolute: `least`, and a subnormal step of the type.  What rounds past the type's largest value is infinite."""
+    past = float(torch.finfo(TYPES[ty][1]).max) * (1 + UNIT[ty])
+    got, want = np.where(np.isinf(got), np.copysign(past, got), got), np.clip(want, -past, past)
     bound = np.abs(want) * (1.01 * units * U + 1.01 * UNIT[ty]) + least + LEAST[ty]
     err = np.abs(got - want)
-    assert np.isfinite(got).all()
+    assert not np.isnan(got).any()
     assert (err <= bound).all(), float((err / bound).max())
 
 
@@ -57,7 +74,16 @@ def test_gelu_tails_forward(M, ty):
     for low, high in ((-8.0, 4.0), (-1.0, 1.0)):
         y, a, b = gated(M, low, high, "gelu", ty, 1024.0)
         assert a.min() < low + 0.1 and (np.abs(b) > 500).all()
-        check_relative(y, i8.act("gelu", a) * b, act_units("gelu", a) + 0.5, ty, 0.0)
+        check_relative(y, i8.act("gelu", a) * b, act_units("gelu", a, ty) + 0.5, ty, 0.0)
+
+
+@pytest.mark.parametrize("ty", list(TYPES))
+@pytest.mark.parametrize("name", ["sigmoid", "silu"])
+@pytest.mark.parametrize("M", [3, 40, 2000])
+def test_sigmoid_tails_forward(M, name, ty):
+    for low, high in ((-100.0, 10.0), (-16.0, 16.0)):
+        y, a, b = gated(M, low, high, name, ty, 1024.0 if ty == "f16" else 2.0 ** 70)
+        check_relative(y, i8.act(name, a) * b, act_units(name, a, ty) + 0.5, ty, least_of(ty) * np.maximum(np.abs(a), 1) * np.abs(b))
 
 
 def backward(dy, pre, name, ty):
@@ -80,11 +106,40 @@ def problem(F, low, high, scale):
 @pytest.mark.parametrize("ty", list(TYPES))
 @pytest.mark.parametrize("F", [512, 333])
 def test_gelu_tails_backward(F, ty):
-    """dy act(a) as the forward pass; dy b act'(a) with act' = P + a phi: P's 8 of P; of a phi e's 2.5, the constant's half and a product's; half of the sum;
+    """dy act(a) as the forward pass; dy b act'(a) with act' = P + a phi: P's units of P; of a phi e's, the constant's half and a product's; half of the sum;
     and two products' halves."""
     got, dy, a, b = backward(*problem(F, -8.0, 4.0, 1024.0), "gelu", ty)
-    check_relative(got[:, F:], dy * i8.act("gelu", a), act_units("gelu", a) + 0.5, ty, 0.0)
+    check_relative(got[:, F:], dy * i8.act("gelu", a), act_units("gelu", a, ty) + 0.5, ty, 0.0)
     tail = np.abs(a) * np.exp(-0.5 * a * a) / np.sqrt(2 * np.pi)
     slope = i8.slope("gelu", a)
-    own = i8.cdf(a) * 8 + tail * 3.5 + np.abs(slope) * 1.5
+    units = e_units("gelu", a, ty)
+    own = i8.cdf(a) * (units + 5.4) + tail * (units + 1) + np.abs(slope) * 1.5
     check_relative(got[:, :F], dy * b * slope, 0.0, ty, np.abs(dy * b) * own * 1.01 * U)
+
+
+@pytest.mark.parametrize("ty", list(TYPES))
+@pytest.mark.parametrize("F", [512, 333])
+def test_sigmoid_tails_backward(F, ty):
+    """act' = s t, t = 1 - s: e's units and 2 of one, 1.5 of the other (into which e's enter with e / (1 + e), into the first with 1 / (1 + e)), the product's half, and two
+    products more."""
+    for low, high in ((-100.0, 100.0), (-6.0, 18.0)):
+        got, dy, a, b = backward(*problem(F, low, high, 1024.0 if ty == "f16" else 2.0 ** 40), "sigmoid", ty)
+        least = least_of(ty) * np.abs(dy) * np.maximum(np.abs(b), 1)
+        check_relative(got[:, :F], dy * b * i8.slope("sigmoid", a), e_units("sigmoid", a, ty) + 3.5 + 1.5, ty, least)
+        check_relative(got[:, F:], dy * i8.act("sigmoid", a), act_units("sigmoid", a, ty) + 0.5, ty, least)
+
+
+@pytest.mark.parametrize("ty", list(TYPES))
+@pytest.mark.parametrize("F", [512, 333])
+def test_silu_tails_backward(F, ty):
+    """act' = s (1 + a t): t's units (e's and 2) of s |a| t; of the whole s's, the sum's half, the product's half, and two products more.  Where the result has 16 bits as
+    (a s) t + s: of s |a| t both factors' units, of s its own; of the whole the sum's half, and two products."""
+    for low, high in ((-100.0, 100.0), (-16.0, 30.0)):
+        got, dy, a, b = backward(*problem(F, low, high, 1024.0 if ty == "f16" else 2.0 ** 40), "silu", ty)
+        least = least_of(ty) * np.abs(dy) * np.maximum(np.abs(b), 1) * np.maximum(np.abs(a), 1)
+        want = dy * b * i8.slope("silu", a)
+        units = e_units("silu", a, ty) + 2
+        s, t = i8.sigmoid(a), i8.sigmoid(-a)
+        own = s * np.abs(a) * t * units if ty == "f32" else s * np.abs(a) * t * (2 * units + 0.5) + s * units
+        check_relative(got[:, :F], want, units + 2 if ty == "f32" else 1.5, ty, least + np.abs(dy * b) * own * 1.01 * U)
+        check_relative(got[:, F:], dy * i8.act("silu", a), act_units("silu", a, ty) + 0.5, ty, least)
