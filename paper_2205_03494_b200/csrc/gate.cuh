@@ -113,6 +113,12 @@ __device__ __forceinline__ void act_slope2(float2 a, float2 &v, float2 &d)
     } else {
         float2 s, t;
         sigmoid2<FINE>(a, s, t);
+        // SiLU of 16-bit values: a product of these by a slope or an s next to 1 often lies next to a tie of the result, so that these are to be off by their last
+        // rounding alone (1 - t is; the reciprocal by as much as three times that).
+        if constexpr (ACT == OMC_GATE_SILU && !FINE) {
+            const float2 high = el::fma2(t, el::twice(-1.f), el::twice(1.f));
+            s = make_float2(a.x < 0.f ? s.x : high.x, a.y < 0.f ? s.y : high.y);
+        }
         v = ACT == OMC_GATE_SILU ? el::mul2(a, s) : s;
         // (SiLU: where FINE = false in the shorter form, whose parts are larger than d where they cancel, around a = -1.28)
         d = ACT == OMC_GATE_SIGMOID ? el::mul2(s, t) : FINE ? el::mul2(s, el::fma2(a, t, el::twice(1.f))) : el::fma2(v, t, s);

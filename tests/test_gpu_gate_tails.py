@@ -143,3 +143,27 @@ def test_silu_tails_backward(F, ty):
         own = s * np.abs(a) * t * units if ty == "f32" else s * np.abs(a) * t * (2 * units + 0.5) + s * units
         check_relative(got[:, :F], want, units + 2 if ty == "f32" else 1.5, ty, least + np.abs(dy * b) * own * 1.01 * U)
         check_relative(got[:, F:], dy * i8.act("silu", a), act_units("silu", a, ty) + 0.5, ty, least)
+
+
+def half_step(x, dtype):
+    """Half the distance of the neighbours of FP64 values in a 16-bit type, normal numbers."""
+    _, e = np.frexp(x)
+    return np.ldexp(float(torch.finfo(dtype).eps) / 4, e)
+
+
+@pytest.mark.parametrize("ty", ["f16", "bf16"])
+@pytest.mark.parametrize("name", ["silu", "gelu"])
+def test_open_gates_next_to_ties(name, ty):
+    """Where act(a) / a and act'(a) are next to 1 the gradients are g a and g b times almost 1, which lie on ties of the result for many 16-bit g, a and b, and next to them
+    a little further down.  The result is the nearer one wherever the formula's value is further from the middle than: of a 1 - t and of the slope the last rounding, a quarter
+    of a u and half of one, of a P or a s another half, of the last product another; and next to nothing of the tails (2.7e-3 of themselves below, off by 8 u + 0.7 a u, or
+    GELU's at a = 4, 2.1e-3, 22 u)."""
+    _, dtype = TYPES[ty]
+    low, high = (8.0, 24.0) if name == "silu" else (4.0, 7.0)
+    a = np.unique(torch.linspace(low, high, 600).to(dtype).double().numpy())
+    g = np.unique(torch.linspace(1.0, 2.0, 300).to(dtype).double().numpy())[:-1]
+    for b in (1.0, 1.0078125, 1.2578125, 1.5234375, 1.9921875):
+        pre = np.concatenate([np.broadcast_to(a, (len(g), len(a))), np.full((len(g), len(a)), b)], 1)
+        got, dy, av, bv = backward(np.broadcast_to(g[:, None], (len(g), len(a))).copy(), pre, name, ty)
+        for part, want in ((got[:, :len(a)], dy * bv * i8.slope(name, av)), (got[:, len(a):], dy * i8.act(name, av))):
+            assert (np.abs(part - want) <= half_step(want, dtype) + np.abs(want) * (1.25 + 0.1) * U).all(), float(((np.abs(part - want) - half_step(want, dtype)) / np.abs(want)).max() / U)
