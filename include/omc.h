@@ -558,7 +558,8 @@ int omc_byte_inject_wait_timeout(uint32_t polls, int what);
  * in any of three forms (at least one): dpre of `type`; its 8-bit form along its rows (codes, scales: rows x 2F) and along its columns (codes_t,
  * scales_t: 2F x rows), exactly omc_byte_quantise of dpre, which need not be stored.  With them the gradients of a gated layer are two products:
  * dX = codes * (W quantised along 2F)^T and dW = codes_t * (X quantised along the rows of the batch)^T.
- *   dpre       device, written, overlaps neither dy nor pre (else OMC_ERR_INVALID_ARG); NULL if it is not wanted.
+ *   dpre       device, written, overlaps neither dy nor pre (else OMC_ERR_INVALID_ARG); NULL if it is not wanted.  Columns of one buffer, of its pitch, may lie beside
+ *              one another; matrices of different pitch overlap if the ranges from their first to their last byte do.
  *   workspace  device, 16-byte aligned, omc_gated_backward_workspace(rows, F) bytes, undefined afterwards; may be NULL if codes_t is.
  */
 int omc_gated_backward_workspace(uint64_t rows, uint64_t F, uint64_t *bytes);

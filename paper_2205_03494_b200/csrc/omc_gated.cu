@@ -23,12 +23,19 @@ using namespace omc;
 
 bool aligned4(const void *p) { return reinterpret_cast<uintptr_t>(p) % 4 == 0; }
 
-// Whether rows x cols matrices of pitch ld have a byte in common, taken from their first to their last.
+// Whether matrices of `rows` rows share a byte: of one pitch exactly (column ranges of one buffer do not), else by the ranges from their first to their last byte.
 bool overlap(const void *a, uint64_t ld_a, uint64_t cols_a, const void *b, uint64_t ld_b, uint64_t cols_b, uint64_t rows, uint64_t size)
 {
-    const uintptr_t p = reinterpret_cast<uintptr_t>(a), q = reinterpret_cast<uintptr_t>(b);
-    const uint64_t na = ((rows - 1) * ld_a + cols_a) * size, nb = ((rows - 1) * ld_b + cols_b) * size;
-    return p < q + nb && q < p + na;
+    using Wide = __int128;
+    const Wide pitch = (Wide)ld_a * size, other = (Wide)ld_b * size, na = (Wide)cols_a * size, nb = (Wide)cols_b * size, last = rows - 1;
+    const Wide d = (Wide)reinterpret_cast<uintptr_t>(b) - (Wide)reinterpret_cast<uintptr_t>(a);          // where b starts, counted from a
+    if (d >= last * pitch + na || d + last * other + nb <= 0) return false;
+    if (pitch != other) return true;
+    // row j of b and row j - k of a: d + k pitch into it, which lies within one row's width for two values of k at most
+    const Wide k = d >= 0 ? -(d / pitch) : (-d) / pitch;
+    for (Wide i = k - 1; i <= k + 1; ++i)
+        if (i >= -last && i <= last && d + i * pitch < na && d + i * pitch + nb > 0) return true;
+    return false;
 }
 
 }  // namespace
