@@ -167,3 +167,37 @@ def test_open_gates_next_to_ties(name, ty):
         got, dy, av, bv = backward(np.broadcast_to(g[:, None], (len(g), len(a))).copy(), pre, name, ty)
         for part, want in ((got[:, :len(a)], dy * bv * i8.slope(name, av)), (got[:, len(a):], dy * i8.act(name, av))):
             assert (np.abs(part - want) <= half_step(want, dtype) + np.abs(want) * (1.25 + 0.1) * U).all(), float(((np.abs(part - want) - half_step(want, dtype)) / np.abs(want)).max() / U)
+
+
+@pytest.mark.parametrize("ty", list(TYPES))
+@pytest.mark.parametrize("name", list(ACTS))
+def test_gates_far_out_and_infinite(name, ty):
+    """Gates from 200 up to the type's largest, of both signs: the activation and its slope are their limits.  An infinite gate or value makes its own two gradients what
+    the formula gives for it (Inf or NaN, or a limit), and nothing else."""
+    code, dtype = TYPES[ty]
+    rows, F = 24, 48
+    rng = np.random.default_rng(3)
+    top = float(torch.finfo(dtype).max)
+    far = np.concatenate([[200.0, 1000.0, 30000.0, top], np.geomspace(200.0, top, F - 4)])
+    a = np.where(np.arange(rows)[:, None] % 2, -far, far)
+    dy, b = (rng.choice([0.5, 0.25, -0.5], (rows, F)) for _ in range(2))
+    got, g, av, bv = backward(dy, np.concatenate([a, b], 1), name, ty)
+    near = lambda got, want: (np.abs(got - want) <= np.abs(want) * 1.01 * UNIT[ty]).all()
+    if name == "sigmoid":
+        assert (got[:, :F] == 0).all() and near(got[:, F:], np.where(av > 0, g, 0.0))
+    else:
+        assert near(got[:, :F], np.where(av > 0, g * bv, 0.0)) and near(got[:, F:], np.where(av > 0, g * av, 0.0))
+    pre = np.concatenate([rng.standard_normal((rows, F)), b], 1)
+    want, *_ = backward(dy, pre, name, ty)
+    pre[3, 7], pre[4, 8], pre[10, F + 5], pre[11, F + 6] = np.inf, -np.inf, np.inf, -np.inf
+    got, g, av, bv = backward(dy, pre, name, ty)
+    own = np.zeros((rows, 2 * F), bool)
+    for r, c in ((3, 7), (4, 8), (10, 5), (11, 6)):
+        own[r, [c, c + F]] = True
+    assert np.array_equal(got[~own], want[~own])
+    # (value: da is infinite, db as it was.  Gate: the sigmoid's limits; a or a P times 0 is NaN, or its limit)
+    assert np.isinf(got[[10, 11], [5, 6]]).all() and np.array_equal(got[[10, 11], [F + 5, F + 6]], want[[10, 11], [F + 5, F + 6]])
+    if name == "sigmoid":
+        assert (got[[3, 4], [7, 8]] == 0).all() and got[3, F + 7] == dy[3, 7] and got[4, F + 8] == 0
+    else:
+        assert np.isinf(got[3, F + 7]) and all(np.isnan(v) or v == 0 for v in (got[4, 8], got[4, F + 8])) and (np.isnan(got[3, 7]) or got[3, 7] == g[3, 7] * bv[3, 7])
