@@ -96,11 +96,11 @@ __device__ __forceinline__ void give_up(uint32_t *status, uint32_t gave_up)
     atomicExch(status, 1u);
     shared_word(gave_up, 1u);
 }
-// Before a CTA ends, also after a wait that ran out: the copies of the last `stages` of `issued` steps have landed.
+// Before a CTA ends, also after a wait that ran out: the copies of the last `stages` of `issued` steps have landed, by the barriers that tell.
 template <typename F>
-__device__ __forceinline__ void copies_landed(uint32_t issued, uint32_t stages, uint32_t limit, F full)
+__device__ __forceinline__ void copies_landed(uint32_t issued, uint32_t stages, uint32_t limit, F barrier)
 {
-    for (uint32_t it = issued > stages ? issued - stages : 0u; it < issued; ++it) mbar_wait_held(full(it % stages), (it / stages) & 1u, limit);
+    for (uint32_t it = issued > stages ? issued - stages : 0u; it < issued; ++it) mbar_wait_held(barrier(it % stages), (it / stages) & 1u, limit);
 }
 // The waits' limits: constants; for omc_byte_inject_wait_timeout, in kernels of their own, the given number of polls, and in the first CTA (or
 // pair) copies that are announced without being issued, or results that are given up at once with the products on their way.
@@ -446,7 +446,10 @@ i8_tile_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant_
                 }
             }
         }
+        // (the peer's copies tell the leader; the products that read them tell both: without this a peer that had issued its last copies could end before they
+        // landed, if the leader gave up meanwhile)
         if (rank == 0) copies_landed(it, NS, waits.held, full);
+        else copies_landed(it, NS, waits.held, empty);
     } else if (tid == 32 && rank == 0) {
         uint32_t it = 0, lt = 0;
         for (uint32_t t = unit; t < ntiles && ok; t += units, ++lt) {
