@@ -12,7 +12,7 @@ constexpr uint32_t LAID_OUT_SMS = 148, STEP_K = 128;
 enum Kernel { PAIR_256, ONE_128, SMALL_16, SMALL_32, SMALL_64 };
 struct Schedule {
     Kernel kernel;
-    uint32_t splits;        // CTAs, a cluster, among which a tile's K is divided (small kernel): 1, 2, 4 or 8
+    uint32_t splits;        // CTAs, a cluster, among which a tile's K is divided (small kernel): 1, 4 or 8
 };
 
 // Up to four rows are multiplied without the tensor cores, if their codes fit in shared memory with two CTAs on an SM.

@@ -1,11 +1,11 @@
 // omc_gated_backward: from the gradient of y = act(a) b and the (a | b) that the forward pass left,
 //     da = dy b act'(a),   db = dy act(a)
 // as a matrix of the activations' type, and / or as 8-bit integers along its rows and its columns (i8_quantise.cuh), which the two products of the
-// layer's backward pass take: (da | db) is made again in the second kernel instead of being written and read (16 bytes a value
-// of dy for 16-bit types instead of 22).
-// The matrix alone is bound by memory: 8192 x 8192 BF16 105 us, 6.4 TB/s.  With the codes along both axes 8192 x 8192 BF16 takes 223 us, 4.8 TB/s of what both
-// kernels read and write (maxima 77, codes 141): the second kernel waits for the latencies of its arithmetic, 168 registers leaving three CTAs of four warps an SM (with
-// four and fewer registers 228 us).  Rows off the 16-byte boundaries: 491 us at 8192 x 8191.
+// layer's backward pass take: (da | db) is made again in the second kernel instead of being written by the first and read by the second (16 bytes a value
+// of dy for 16-bit types instead of 18; the other way, with a second kernel of fewer registers, has not been tried).
+// The matrix alone is bound by memory: 8192 x 8192 BF16 107 us, 6.3 TB/s.  With the codes along both axes 8192 x 8192 BF16 takes 232 us (SiLU; sigmoid 228, GELU 253),
+// 4.6 TB/s of what both kernels read and write (more than half of it the second's): the second kernel waits for the latencies of its arithmetic, 168 registers leaving three CTAs of four
+// warps an SM.  Rows off the 16-byte boundaries: 506 us at 8192 x 8191.
 #include <cuda_runtime.h>
 
 #include "element.cuh"
